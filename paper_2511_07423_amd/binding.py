@@ -118,6 +118,42 @@ _lib.synera_debug_gemm_epilogue.restype = C.c_int32
 _lib.synera_debug_gemm_epilogue.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp]
 
 
+class _RopeDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("original", C.c_double), ("magnitude", C.c_double), ("h_inv_freq", C.POINTER(C.c_double))]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("d_in", _vp), ("d_out", _vp), ("d_gain", _vp), ("n_heads", C.c_int32), ("in_token", C.c_int64),
+                ("in_head", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64)]
+
+
+_headsp = C.POINTER(_Heads)
+_lib.synera_rope_create.restype = C.c_int32
+_lib.synera_rope_create.argtypes = [C.POINTER(_vp), C.POINTER(_RopeDesc)]
+_lib.synera_rope_destroy.restype = C.c_int32
+_lib.synera_rope_destroy.argtypes = [_vp]
+_lib.synera_rope_apply.restype = C.c_int32
+_lib.synera_rope_apply.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _headsp, _headsp, _vp]
+_lib.synera_qk_norm_rope.restype = C.c_int32
+_lib.synera_qk_norm_rope.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _headsp, _headsp, C.c_float, _vp]
+_lib.synera_batch_create.restype = C.c_int32
+_lib.synera_batch_create.argtypes = [C.POINTER(_vp)] + [C.c_int32] * 6
+_lib.synera_batch_destroy.restype = C.c_int32
+_lib.synera_batch_destroy.argtypes = [_vp]
+_lib.synera_validate_shared.restype = C.c_int32
+_lib.synera_validate_shared.argtypes = [C.c_int32, _i32p, _i32p, _i32p, C.c_int32, C.c_int32, C.c_int32, C.c_int64]
+_lib.synera_batch_plan.restype = C.c_int32
+_lib.synera_batch_plan.argtypes = [_vp, C.c_int32, _i32p, _i32p, _i32p, C.c_int32, C.c_int32, _vp]
+_lib.synera_append_rope.restype = C.c_int32
+_lib.synera_append_rope.argtypes = [_vp, _vp, C.c_int32, _headsp, _headsp, _headsp, C.c_float, _vp, _vp, _vp]
+_lib.synera_shared_attention.restype = C.c_int32
+_lib.synera_shared_attention.argtypes = [_vp, _headsp, _vp, _vp, C.c_float, _vp, _vp]
+_lib.synera_debug_shared_plan.restype = C.c_int32
+_lib.synera_debug_shared_plan.argtypes = [C.c_int32] * 5 + [_i32p] * 3 + [C.c_int32] * 2 + [_i32p, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
+
+
 class SyneraError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -538,6 +574,222 @@ class Verifier:
                                    _dev(v, torch.bfloat16), bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool,
                                    _dev(k_pool, torch.bfloat16), _dev(v_pool, torch.bfloat16), _stream())
         _check(st, "synera_kv_append")
+
+
+# ---------------------------------------------------------------------------------- rotary positions, batches that share pages
+_HEAD_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+
+
+def _heads(x, out, gain, device, name):
+    """The synera_heads of x and out, [tokens][heads][head_dim] with the values of a head side by side."""
+    for t in (x, out):
+        if t is not None and (t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1) or t.device != device):
+            raise ValueError(f"{name}: expected [tokens, heads, head_dim] on {device}, the values of a head side by side")
+    if out is not None and out.shape != x.shape:
+        raise ValueError(f"{name}: the output's shape is {tuple(out.shape)}, the input's {tuple(x.shape)}")
+    if gain is not None and (gain.dtype != torch.bfloat16 or gain.shape != x.shape[2:] or not gain.is_contiguous() or gain.device != device):
+        raise ValueError(f"{name}: gains are bf16 [head_dim] on {device}")
+    o = x if out is None else out
+    return _Heads(x.data_ptr(), None if out is None else out.data_ptr(), None if gain is None else gain.data_ptr(), x.shape[1],
+                  x.stride(0), x.stride(1), o.stride(0), o.stride(1))
+
+
+def _on(device, *tensors):
+    """Refuses tensors that are elsewhere than the handle, and a handle that is elsewhere than the current device."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the handle belongs to {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"expected tensors on {device}, got one on {t.device}")
+
+
+class Rope:
+    """Rotary positions of heads of head_dim values, of which the first rot_dim turn (all by default): pairs (2i, 2i+1)
+    with layout "interleaved", (i, i + rot_dim/2) with "half".  scaling: None, ("linear", factor) or ("bands", factor, low, high,
+    original context); inv_freq: rot_dim/2 numbers in place of base and scaling; magnitude multiplies cosines and sines.
+    Belongs to the device that is current when it is made."""
+
+    def __init__(self, head_dim, rot_dim=None, layout="interleaved", base=10000.0, scaling=None, inv_freq=None, magnitude=1.0):
+        self._h = _vp()
+        kind, args = (0, ()) if scaling is None else ({"linear": 1, "bands": 2}[scaling[0]], tuple(scaling[1:]))
+        if len(args) != (0, 1, 4)[kind]:
+            raise ValueError('scaling is None, ("linear", factor) or ("bands", factor, low, high, original)')
+        factor, low, high, original = (args + (0.0,) * 4)[:4]
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        table = None
+        if inv_freq is not None:
+            table = np.ascontiguousarray(inv_freq, dtype=np.float64)
+            if table.shape != (rot_dim // 2,):
+                raise ValueError(f"inv_freq has {table.shape}, rot_dim / 2 is {rot_dim // 2}")
+        desc = _RopeDesc(head_dim, rot_dim, ROPE_LAYOUTS[layout], kind, base, factor, low, high, original, magnitude,
+                         None if table is None else table.ctypes.data_as(C.POINTER(C.c_double)))
+        _check(_lib.synera_rope_create(C.byref(self._h), C.byref(desc)), "synera_rope_create")
+        self.head_dim, self.rot_dim = head_dim, rot_dim
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def close(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.synera_rope_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _turn(self, pos, q, k, gains, eps, out_q, out_k):
+        _on(self.device, pos, q, k)
+        if pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous():
+            raise ValueError("positions are a contiguous int32 vector")
+        both = [(q, out_q, "q")] + ([] if k is None else [(k, out_k, "k")])
+        heads, outs = [], []
+        for (x, out, name), gain in zip(both, gains):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+            if x.dtype not in _HEAD_TYPES or x.dtype != q.dtype or out.dtype != x.dtype:
+                raise ValueError(f"{name}: f32, bf16 or f16, one type for all: got {x.dtype} -> {out.dtype}")
+            if x.dim() != 3 or x.shape[0] != pos.numel() or x.shape[2] != self.head_dim:
+                raise ValueError(f"{name}: expected [{pos.numel()}, heads, {self.head_dim}], got {tuple(x.shape)}")
+            heads.append(_heads(x, out, gain, self.device, name))
+            outs.append(out)
+        args = (self._h, _HEAD_TYPES[q.dtype], pos.numel(), pos.data_ptr(), C.byref(heads[0]), C.byref(heads[1]) if k is not None else None)
+        if eps is None:
+            _check(_lib.synera_rope_apply(*args, _stream()), "synera_rope_apply")
+        else:
+            _check(_lib.synera_qk_norm_rope(*args, float(eps), _stream()), "synera_qk_norm_rope")
+        return outs[0], (outs[1] if k is not None else None)
+
+    def apply(self, pos, q, k=None, out_q=None, out_k=None):
+        """q [T, Hq, head_dim] and k [T, Hk, head_dim] (or None) turned by their positions (int32 [T]) -> (q, k), new tensors
+        unless out_q / out_k are given (q and k themselves for in place)."""
+        return self._turn(pos, q, k, (None, None), None, out_q, out_k)
+
+    def norm_apply(self, pos, q, k, q_gain, k_gain, eps, out_q=None, out_k=None):
+        """The same behind an RMS norm of each head with bf16 gains [head_dim]."""
+        if q_gain is None or (k is not None and k_gain is None):
+            raise ValueError("norm_apply needs the gains")
+        return self._turn(pos, q, k, (q_gain, k_gain), eps, out_q, out_k)
+
+
+def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max_tokens):
+    """Host-only check of a batch whose requests may share pages; returns the status code (no GPU needed)."""
+    bt = np.ascontiguousarray(block_table, dtype=np.int32)
+    (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
+    if bt.ndim != 2 or len(ctx) != len(new) or len(bt) != len(ctx):
+        raise ValueError("ctx_len, n_new and the rows of block_table belong together")
+    return _lib.synera_validate_shared(len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool, max_batch, max_tokens)
+
+
+class SharedBatch:
+    """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
+    attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too.
+    Belongs to the device that is current when it is made."""
+
+    def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):
+        self._h = _vp()
+        _check(_lib.synera_batch_create(C.byref(self._h), n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages),
+               "synera_batch_create")
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.n_tokens = self.n_pages = 0
+
+    def close(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.synera_batch_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def plan(self, ctx_len, n_new, block_table, n_pages_in_pool):
+        """Host: cached and new tokens of each request, block_table [B, columns]; shared pages first in their rows."""
+        bt = np.ascontiguousarray(block_table, dtype=np.int32)
+        (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
+        if bt.ndim != 2 or len(ctx) != len(new) or len(bt) != len(ctx):
+            raise ValueError("ctx_len, n_new and the rows of block_table belong together")
+        _on(self.device)
+        _check(_lib.synera_batch_plan(self._h, len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool, _stream()),
+               "synera_batch_plan")
+        self.n_tokens, self.n_pages = int(new.sum()), n_pages_in_pool
+
+    def _pools(self, k_pool, v_pool):
+        shape = (self.n_kv_heads, PAGE_SIZE, self.head_dim)
+        for t, want in ((k_pool, shape), (v_pool, (shape[0], shape[2], shape[1]))):
+            if t.dtype != torch.bfloat16 or t.device != self.device or not t.is_contiguous() or t.dim() != 4 or \
+                    tuple(t.shape[1:]) != want or t.shape[0] < self.n_pages:
+                raise ValueError(f"expected one layer's pool, bf16 [>= {self.n_pages}, {want[0]}, {want[1]}, {want[2]}] on {self.device}, contiguous")
+        return k_pool.data_ptr(), v_pool.data_ptr()
+
+    def _rows(self, x, heads, name):
+        if x.dim() != 3 or x.shape[0] < self.n_tokens or x.shape[1:] != (heads, self.head_dim):
+            raise ValueError(f"{name}: expected [>= {self.n_tokens}, {heads}, {self.head_dim}], got {tuple(x.shape)}")
+
+    def append_rope(self, rope, q, k, v, k_pool, v_pool, q_gain=None, k_gain=None, eps=1e-5, out_q=None):
+        """One layer's new tokens (rows of q, k, v in the batch's order; f32, bf16 or f16): keys turned (and normed, with k_gain)
+        into their pages, values into theirs, queries turned into out_q (bf16, new if None) -> out_q; q may be None."""
+        _on(self.device, q, k, v)
+        if rope.device != self.device:
+            raise ValueError(f"the rope belongs to {rope.device}")
+        if k.dtype not in _HEAD_TYPES or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+            raise ValueError("f32, bf16 or f16, one type for q, k and v")
+        self._rows(k, self.n_kv_heads, "k")
+        self._rows(v, self.n_kv_heads, "v")
+        hq = None
+        if q is not None:
+            self._rows(q, self.n_q_heads, "q")
+            out_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out_q is None else out_q
+            if out_q.dtype != torch.bfloat16:
+                raise ValueError("out_q is bf16")
+            hq = _heads(q, out_q, q_gain, self.device, "q")
+        hk, hv = _heads(k, None, k_gain, self.device, "k"), _heads(v, None, None, self.device, "v")
+        _check(_lib.synera_append_rope(self._h, rope._h, _HEAD_TYPES[k.dtype], C.byref(hq) if hq is not None else None, C.byref(hk),
+                                       C.byref(hv), float(eps), *self._pools(k_pool, v_pool), _stream()), "synera_append_rope")
+        return out_q
+
+    def attention(self, q, k_pool, v_pool, scale=None, out=None, want_lse=False):
+        """softmax(scale q K^T) V of one layer over the planned batch: q bf16 [T, Hq, head_dim], turned; scale None: 1/sqrt(head_dim)
+        -> o bf16 (out, new if None), or (o, lse f32 [T, Hq])."""
+        _on(self.device, q, out)
+        self._rows(q, self.n_q_heads, "q")
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out is None else out
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+            raise ValueError("q and out are bf16")
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+        if scale is not None and not scale > 0:
+            raise ValueError("scale is positive")
+        h = _heads(q, out, None, self.device, "q")
+        _check(_lib.synera_shared_attention(self._h, C.byref(h), *self._pools(k_pool, v_pool), 0.0 if scale is None else float(scale),
+                                            None if lse is None else lse.data_ptr(), _stream()), "synera_shared_attention")
+        return (out, lse) if want_lse else out
+
+
+_SHARED_REGIONS = {"head": (0, 16), "pos": (1, 1), "slot": (2, 1), "windows": (3, 4), "items": (4, 16), "list": (5, 1), "pages": (6, 1),
+                   "joined": (7, 2), "first_entry": (8, 1), "req_tok": (9, 1), "entries": (10, 8)}
+
+
+def debug_shared_plan(n_q_heads, n_kv_heads, slots, ctx_len, n_new, block_table, max_tokens=None):
+    """Test hook (host only): what SharedBatch.plan uploads for one batch -> dict of int32 arrays, and "limits" (room for items, list,
+    entries, pages, windows, partial rows, rows of shared nodes)."""
+    (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
+    bt = np.ascontiguousarray(block_table, dtype=np.int32)
+    limits = (C.c_int64 * 7)()
+    out = {}
+    for name, (which, width) in _SHARED_REGIONS.items():
+        n = C.c_int64(0)
+        args = (n_q_heads, n_kv_heads, slots, int(new.sum()) if max_tokens is None else max_tokens, len(ctx), p_ctx, p_new,
+                bt.ctypes.data_as(_i32p), bt.shape[1], which)
+        st = _lib.synera_debug_shared_plan(*args, None, 0, C.byref(n), limits)
+        if st != ENOSPC:
+            _check(st, "synera_debug_shared_plan")
+        words = np.zeros(n.value, np.int32)
+        _check(_lib.synera_debug_shared_plan(*args, words.ctypes.data_as(_i32p), n.value, C.byref(n), limits), "synera_debug_shared_plan")
+        out[name] = words.reshape(-1, width) if width > 1 else words
+    out["limits"] = list(limits)
+    return out
 
 
 # ---------------------------------------------------------------------------------- scheduler (host only)

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsynera.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["gemm_nf4_high.hip", "gemm_nf4_low.hip", "gemm_nf2.hip", "gemm_k64.hip", "gemm_k64_whole.hip", "gemm_k64_once.hip", "stream.hip", "api.hip", "elementwise.hip", "confidence.hip", "attention.hip",
-           "importance.hip", "gemm.hip", "gemm_static.hip", "ceilings.hip", "scheduler.cpp"]
+           "importance.hip", "gemm.hip", "gemm_static.hip", "ceilings.hip", "scheduler.cpp",
+           "rope.hip", "shared.hip", "shared_plan.cpp"]
 # sources whose kernels issue MFMAs from inline assembly: their device assembly is kept and checked
 ASM_CHECKED = {"gemm_nf4_high.hip": "proj_kernel", "gemm_nf4_low.hip": "proj_kernel", "gemm_nf2.hip": "proj_kernel", "gemm_k64.hip": "proj_kernel",
                "gemm_k64_once.hip": "proj_kernel",
@@ -21,7 +22,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # The attention kernel's builtin MFMAs take their accumulators in VGPRs: in AGPRs (the compiler's default choice)
 # all 36 of them were read out at the top of every tile iteration and written back at its end.
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("attention.hip", "shared.hip")}
 
 
 def _quiet(stderr):

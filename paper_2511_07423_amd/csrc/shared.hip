@@ -1,0 +1,903 @@
+// Batches over a paged cache whose pages requests may share: the handle behind synera_batch, the append with the rotation on
+// the way, and the attention that reads a shared prefix once for all its requests.  shared_plan.cpp finds the prefixes and
+// cuts the work; everything a kernel needs of a plan lies on the device, at addresses that never change, its sizes
+// included: a captured launch serves any later plan.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <type_traits>
+
+#include "../../include/synera_debug.h"
+#include "rope.h"
+#include "shared.h"
+
+#define SH_STAGES 4            // plans that may run ahead of their uploads
+#define SH_CONST_AS __attribute__((address_space(4)))
+
+// ------------------------------------------------------------------------------------ the handle
+enum { R_HEAD, R_POS, R_SLOT, R_WIN, R_ITEM, R_LIST, R_PAGE, R_JOINED, R_FIRST, R_REQ, R_ENTRY, N_REGIONS };
+
+struct synera_batch {
+  ShLimits lim;
+  int device;
+  ShPlan plan;                 // sizes of the current plan
+  bool planned;
+  int32_t n_pages;
+  char* dev;                   // regions of a plan, then the partial results
+  size_t at[N_REGIONS], room[N_REGIONS];
+  float* part_o;               // [part_rows][hd]
+  float2* part_ml;             // [part_rows]: softmax reference (exponent-2 domain) and sum
+  char* host[SH_STAGES];       // pinned: a plan's regions on their way
+  size_t host_bytes;
+  hipEvent_t done[SH_STAGES];
+  bool pending[SH_STAGES];
+  uint64_t plans;
+  template <typename T> const T* region(int r) const { return reinterpret_cast<const T*>(dev + at[r]); }
+};
+
+static size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+extern "C" int32_t synera_batch_destroy(synera_batch* b) {
+  if (!b) return SYNERA_OK;
+  (void)hipDeviceSynchronize();
+  for (int s = 0; s < SH_STAGES; ++s) {
+    if (b->done[s]) (void)hipEventDestroy(b->done[s]);
+    if (b->host[s]) (void)hipHostFree(b->host[s]);
+  }
+  if (b->dev) (void)hipFree(b->dev);
+  delete b;
+  return SYNERA_OK;
+}
+
+extern "C" int32_t synera_batch_create(synera_batch** out, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                       int32_t max_batch, int32_t max_tokens, int32_t max_pages) {
+  if (!out) return SYNERA_EINVAL;
+  *out = nullptr;
+  if (n_q_heads < 1 || n_kv_heads < 1 || max_batch < 1 || max_tokens < 1 || max_pages < 1) return SYNERA_EINVAL;
+  if ((head_dim != 64 && head_dim != 128) || n_q_heads % n_kv_heads || n_q_heads > 1024) return SYNERA_EUNSUP;
+  if ((int64_t)max_tokens * n_q_heads >= (int64_t)1 << 30 || (int64_t)max_batch * max_pages >= (int64_t)1 << 30) return SYNERA_EUNSUP;
+  int dev = 0;
+  hipDeviceProp_t prop;
+  if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return SYNERA_EHIP;
+  }
+  synera_batch* b = new (std::nothrow) synera_batch();
+  if (!b) return SYNERA_ENOMEM;
+  b->device = dev;
+  b->planned = false;
+  b->plans = 0;
+  ShLimits& l = b->lim;
+  l.Hq = n_q_heads;
+  l.Hkv = n_kv_heads;
+  l.hd = head_dim;
+  l.max_batch = max_batch;
+  l.max_tokens = max_tokens;
+  l.max_pages = max_pages;
+  l.slots = 2 * std::max(1, prop.multiProcessorCount);
+  sh_limits(l);
+  const size_t T = (size_t)max_tokens, B = (size_t)max_batch;
+  b->room[R_HEAD] = sizeof(ShHeader);
+  b->room[R_POS] = b->room[R_SLOT] = T * 4;
+  b->room[R_WIN] = (size_t)l.windows * sizeof(ShWindow);
+  b->room[R_ITEM] = (size_t)l.items * sizeof(ShItem);
+  b->room[R_LIST] = (size_t)l.list * 4;
+  b->room[R_PAGE] = (size_t)l.pages * 4;
+  b->room[R_JOINED] = T * 8;
+  b->room[R_FIRST] = (B + 1) * 4;
+  b->room[R_REQ] = B * 4;
+  b->room[R_ENTRY] = (size_t)l.entries * sizeof(ShEntry);
+  size_t off = 0;
+  for (int r = 0; r < N_REGIONS; ++r) {
+    b->at[r] = off;
+    off += up(b->room[r]);
+  }
+  b->host_bytes = off;
+  const size_t o_po = off, o_ml = o_po + up((size_t)l.part_rows * l.hd * 4), all = o_ml + up((size_t)l.part_rows * 8);
+  if (hipMalloc(reinterpret_cast<void**>(&b->dev), all) != hipSuccess) {
+    (void)hipGetLastError();
+    b->dev = nullptr;
+    (void)synera_batch_destroy(b);
+    return SYNERA_ENOMEM;
+  }
+  b->part_o = reinterpret_cast<float*>(b->dev + o_po);
+  b->part_ml = reinterpret_cast<float2*>(b->dev + o_ml);
+  for (int s = 0; s < SH_STAGES; ++s)
+    if (hipHostMalloc(reinterpret_cast<void**>(&b->host[s]), b->host_bytes, hipHostMallocDefault) != hipSuccess ||
+        hipEventCreateWithFlags(&b->done[s], hipEventDisableTiming) != hipSuccess) {
+      (void)hipGetLastError();
+      (void)synera_batch_destroy(b);
+      return SYNERA_ENOMEM;
+    }
+  *out = b;
+  return SYNERA_OK;
+}
+
+// ------------------------------------------------------------------------------------ planning
+// The regions of a plan go from pinned host memory to their places in one launch (a copy command for each took longer than
+// all of them together).  Sizes in 16-byte pieces; regions are padded to 256 bytes on both sides.
+struct ShUpload {
+  const u32x4* from[N_REGIONS];
+  u32x4* to[N_REGIONS];
+  uint32_t end[N_REGIONS];     // pieces up to here, regions end to end
+};
+__global__ __launch_bounds__(256) void plan_upload_kernel(ShUpload u) {
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < u.end[N_REGIONS - 1]; i += gridDim.x * 256) {
+    uint32_t before = 0;
+#pragma unroll
+    for (int r = 0; r < N_REGIONS; ++r) {
+      if (i >= before && i < u.end[r]) u.to[r][i - before] = u.from[r][i - before];
+      before = u.end[r];
+    }
+  }
+}
+
+static bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return true;               // the legacy stream while another one is captured: nothing may be launched there
+  }
+  return st != hipStreamCaptureStatusNone;
+}
+
+extern "C" int32_t synera_batch_plan(synera_batch* b, int32_t B, const int32_t* h_ctx_len, const int32_t* h_n_new,
+                                     const int32_t* h_block_table, int32_t max_pages, int32_t n_pages_in_pool, void* stream) {
+  if (!b) return SYNERA_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const ShLimits& l = b->lim;
+  int32_t st = synera_validate_shared(B, h_ctx_len, h_n_new, h_block_table, max_pages, n_pages_in_pool, l.max_batch, l.max_tokens);
+  if (st != SYNERA_OK) return st;
+  if (max_pages > l.max_pages) return SYNERA_ENOSPC;
+  if (!rope_device_ok(b->device) || capturing(s)) return SYNERA_EINVAL;
+  ShPlan p;
+  try {
+    sh_plan(l, B, h_ctx_len, h_n_new, h_block_table, max_pages, p);
+  } catch (const std::bad_alloc&) {
+    return SYNERA_ENOMEM;
+  }
+  const void* from[N_REGIONS] = {&p.head, p.tok_pos.data(), p.tok_slot.data(), p.windows.data(), p.items.data(), p.list.data(),
+                                 p.pages.data(), p.joined.data(), p.first_entry.data(), p.req_tok.data(), p.entries.data()};
+  const size_t bytes[N_REGIONS] = {sizeof(ShHeader), p.tok_pos.size() * 4, p.tok_slot.size() * 4, p.windows.size() * sizeof(ShWindow),
+                                   p.items.size() * sizeof(ShItem), p.list.size() * 4, p.pages.size() * 4, p.joined.size() * 4,
+                                   p.first_entry.size() * 4, p.req_tok.size() * 4, p.entries.size() * sizeof(ShEntry)};
+  int64_t part_rows = 0;
+  for (const ShItem& it : p.items)
+    if (it.part >= 0) part_rows = std::max<int64_t>(part_rows, (int64_t)it.part + it.n_rows);
+  bool room = part_rows <= l.part_rows;
+  for (int r = 0; r < N_REGIONS; ++r) room = room && bytes[r] <= b->room[r];
+  if (!room) return SYNERA_ENOMEM;                  // (the capacities cover every plan: sh_limits)
+  const int slot = (int)(b->plans % SH_STAGES);
+  if (b->pending[slot]) {
+    if (hipEventSynchronize(b->done[slot]) != hipSuccess) {
+      (void)hipGetLastError();
+      return SYNERA_EHIP;
+    }
+    b->pending[slot] = false;
+  }
+  ShUpload u;
+  uint32_t end = 0;
+  size_t off = 0;
+  for (int r = 0; r < N_REGIONS; ++r) {
+    if (bytes[r]) std::memcpy(b->host[slot] + off, from[r], bytes[r]);
+    u.from[r] = reinterpret_cast<const u32x4*>(b->host[slot] + off);
+    u.to[r] = reinterpret_cast<u32x4*>(b->dev + b->at[r]);
+    off += up(bytes[r]);
+    u.end[r] = end += (uint32_t)((bytes[r] + 15) / 16);
+  }
+  plan_upload_kernel<<<std::min<uint32_t>((end + 255) / 256, 1024), 256, 0, s>>>(u);
+  bool ok = hipGetLastError() == hipSuccess;
+  ok = hipEventRecord(b->done[slot], s) == hipSuccess && ok;
+  b->pending[slot] = true;
+  ++b->plans;
+  if (!ok) {
+    (void)hipGetLastError();
+    b->planned = false;
+    return SYNERA_EHIP;
+  }
+  b->plan = std::move(p);
+  b->planned = true;
+  b->n_pages = n_pages_in_pool;
+  return SYNERA_OK;
+}
+
+// ------------------------------------------------------------------------------------ append
+// Wavefronts take queries' and keys' head groups (rope.h), or the values of one page window: 128 of a token's Hkv hd values for up
+// to 16 consecutive tokens, turned in LDS from token-major to the page's [dim][slot] order so that a whole page leaves in
+// 16-byte pieces.  In a page that other tokens share only the appended slots are written.
+struct AppendArgs {
+  TurnArgs turn;
+  const ShHeader* head;
+  const ShWindow* windows;
+  const void* v;
+  int64_t v_ts, v_hs;
+  bf16_t* v_layer;
+  int32_t n, hd;               // n = Hkv hd
+  int32_t v_pairs;             // whether two values of v can be loaded together
+  int32_t v_blocks;            // the first blocks take values, the others heads
+};
+
+template <typename TI>
+__device__ __forceinline__ uint32_t value_pair(const TI* v, bool pairs) {    // two neighbouring values as bf16
+  TurnChunk<TI, 2> c;
+  float f[2];
+  if (pairs) {
+    c.load(v);
+    c.widen(f);
+  } else {
+    TurnChunk<TI, 1> c0, c1;
+    c0.load(v);
+    c1.load(v + 1);
+    c0.widen(f);
+    c1.widen(f + 1);
+  }
+  return pack_bf2(f[0], f[1]);
+}
+
+template <typename TI>
+__device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindow w, const int e0, uint32_t* turn) {
+  const int lane = threadIdx.x & 63, e = e0 + 2 * lane;
+  const bool on = e < a.n;
+  const int head = on ? e / a.hd : 0, dim = on ? e % a.hd : 0;
+  const TI* v = static_cast<const TI*>(a.v) + (int64_t)head * a.v_hs + dim;
+  bf16_t* dst = a.v_layer + (size_t)w.page * a.n * SY_PAGE + (size_t)e0 * SY_PAGE;
+  if (w.s1 - w.s0 == 1) {                       // one token: the shortest way
+    const uint32_t x = value_pair(v + (int64_t)w.row * a.v_ts, a.v_pairs);
+    if (on) {
+      dst[2 * lane * SY_PAGE + w.s0] = (bf16_t)(x & 0xFFFF);
+      dst[(2 * lane + 1) * SY_PAGE + w.s0] = (bf16_t)(x >> 16);
+    }
+    return;
+  }
+  uint32_t vr[SY_PAGE];
+  // (slots that are not covered load a covered one's row: without branches all loads are on their way together)
+#pragma unroll
+  for (int j = 0; j < SY_PAGE; ++j) vr[j] = value_pair(v + (int64_t)(w.row - w.s0 + min(max(j, w.s0), w.s1 - 1)) * a.v_ts, a.v_pairs);
+  // lane's two rows of 16 slots = 16 words; the pieces of 4 words rotate with the lane so that the 16-byte LDS accesses of
+  // neighbouring lanes fall on different banks
+  uint32_t* mine = turn + lane * 16;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {                 // piece q: slots (q & 1) * 8 .. + 7 of dim q >> 1
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t l = vr[(q & 1) * 8 + 2 * i], h = vr[(q & 1) * 8 + 2 * i + 1];
+      x[i] = (q >> 1) ? (l >> 16) | (h & 0xFFFF0000u) : (l & 0xFFFFu) | (h << 16);
+    }
+    *reinterpret_cast<u32x4*>(mine + ((q + (lane >> 1)) & 3) * 4) = x;
+  }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int piece = j * 64 + lane, from = piece >> 2;
+    if (e0 + 2 * from >= a.n) continue;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(turn + from * 16 + (((piece & 3) + (from >> 1)) & 3) * 4);
+    const int slot0 = (piece & 1) * 8;          // the piece's first slot
+    bf16_t* to = dst + piece * 8;
+    if (slot0 >= w.s0 && slot0 + 8 <= w.s1) {
+      *reinterpret_cast<u32x4*>(to) = x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool l = slot0 + 2 * i >= w.s0 && slot0 + 2 * i < w.s1, h = slot0 + 2 * i + 1 >= w.s0 && slot0 + 2 * i + 1 < w.s1;
+        if (l && h) *reinterpret_cast<uint32_t*>(to + 2 * i) = x[i];
+        else if (l) to[2 * i] = (bf16_t)(x[i] & 0xFFFF);
+        else if (h) to[2 * i + 1] = (bf16_t)(x[i] >> 16);
+      }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();              // the next window's values come into the same words
+}
+
+template <typename TI, int VEC>
+__global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint32_t turn[4][64 * 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int)blockIdx.x < a.v_blocks) {
+    const uint32_t slabs = (uint32_t)(a.n + 127) / 128, items = (uint32_t)a.head->n_windows * slabs;
+    for (uint32_t i = blockIdx.x * 4 + wave; i < items; i += (uint32_t)a.v_blocks * 4)
+      append_values<TI>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
+  } else {
+    const uint32_t items = (uint32_t)a.head->n_tokens * (uint32_t)a.turn.n_item_cols;
+    for (uint32_t i = (blockIdx.x - a.v_blocks) * 4 + wave; i < items; i += (gridDim.x - a.v_blocks) * 4)
+      turn_item<TI, bf16_t, VEC, true>(a.turn, i);
+  }
+}
+
+template <typename TI>
+static hipError_t launch_append(const AppendArgs& a, int vec, uint32_t blocks, hipStream_t s) {
+  switch (vec) {
+    case 8: append_rope_kernel<TI, 8><<<blocks, 256, 0, s>>>(a); break;
+    case 4: append_rope_kernel<TI, 4><<<blocks, 256, 0, s>>>(a); break;
+    case 2: append_rope_kernel<TI, 2><<<blocks, 256, 0, s>>>(a); break;
+    default: append_rope_kernel<TI, 1><<<blocks, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, int32_t dtype, const synera_heads* q,
+                                      const synera_heads* k, const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer,
+                                      void* stream) {
+  if (!b || !rope || !k || !v || !d_k_layer || !d_v_layer || dtype < 0 || dtype > 2) return SYNERA_EINVAL;
+  if (!b->planned || !(eps >= 0.f) || !std::isfinite(eps)) return SYNERA_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool graph = capturing(s);
+  if (b->plan.head.n_tokens == 0 && !graph) return SYNERA_OK;          // (an empty tensor has no address)
+  if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16) return SYNERA_EINVAL;
+  const ShLimits& l = b->lim;
+  const int bytes = dtype == 0 ? 4 : 2, hd = l.hd;
+  if (rope->desc.head_dim != hd || k->n_heads != l.Hkv || v->n_heads != l.Hkv || (q && q->n_heads != l.Hq)) return SYNERA_EINVAL;
+  const int64_t T = b->plan.head.n_tokens, n1 = std::max<int64_t>(T, 1);
+  int32_t st = turn_check(*k, n1, hd, bytes, 2, false);
+  if (st == SYNERA_OK) st = turn_check(*v, n1, hd, bytes, 2, false);
+  if (st == SYNERA_OK && q) st = turn_check(*q, n1, hd, bytes, 2, true);
+  if (st != SYNERA_OK || v->d_gain) return SYNERA_EINVAL;
+  // whole pools as ranges, so that no output lies on an input or on another output
+  const int64_t layer = (int64_t)b->n_pages * l.Hkv * SY_PAGE * hd;
+  const void* pools[2] = {d_k_layer, d_v_layer};
+  const synera_heads* ins[3] = {k, v, q};
+  const uintptr_t kp = reinterpret_cast<uintptr_t>(d_k_layer), vp = reinterpret_cast<uintptr_t>(d_v_layer);
+  if (kp < vp + 2 * layer && vp < kp + 2 * layer) return SYNERA_EINVAL;
+  for (const synera_heads* i : ins) {
+    if (!i) continue;
+    const int64_t span = ((n1 - 1) * i->in_token + (int64_t)(i->n_heads - 1) * i->in_head + hd) * bytes;
+    const uintptr_t ip = reinterpret_cast<uintptr_t>(i->d_in);
+    for (const void* pool : pools) {
+      const uintptr_t pp = reinterpret_cast<uintptr_t>(pool);
+      if (ip < pp + 2 * layer && pp < ip + span) return SYNERA_EINVAL;
+    }
+    if (!q) continue;
+    if (i == q && dtype == 1 && q->d_in == q->d_out && (n1 == 1 || q->in_token == q->out_token) && (q->n_heads == 1 || q->in_head == q->out_head)) continue;
+    if (turn_overlap(q->d_out, q->out_token, q->out_head, q->n_heads, 2, i->d_in, i->in_token, i->in_head, i->n_heads, bytes, n1, hd))
+      return SYNERA_EINVAL;
+  }
+  if (q) {
+    const uintptr_t op = reinterpret_cast<uintptr_t>(q->d_out);
+    const int64_t span = ((n1 - 1) * q->out_token + (int64_t)(q->n_heads - 1) * q->out_head + hd) * 2;
+    for (const void* pool : pools) {
+      const uintptr_t pp = reinterpret_cast<uintptr_t>(pool);
+      if (op < pp + 2 * layer && pp < op + span) return SYNERA_EINVAL;
+    }
+  }
+  if (!rope_device_ok(b->device) || rope->device != b->device) return SYNERA_EINVAL;
+  AppendArgs a = {};
+  const int vec = turn_setup(a.turn, rope, n1, q, k, bytes, 2, true, eps);
+  a.turn.pos = b->region<int32_t>(R_POS);
+  a.turn.slot = b->region<int32_t>(R_SLOT);
+  a.turn.k_layer = static_cast<bf16_t*>(d_k_layer);
+  a.turn.q.tail = a.turn.k.tail = 1;
+  if (dtype == 1 && q && q->d_in == q->d_out && !q->d_gain) a.turn.q.tail = 0;
+  a.head = b->region<ShHeader>(R_HEAD);
+  a.windows = b->region<ShWindow>(R_WIN);
+  a.v = v->d_in;
+  a.v_ts = v->in_token;
+  a.v_hs = v->in_head;
+  a.v_layer = static_cast<bf16_t*>(d_v_layer);
+  a.n = l.Hkv * hd;
+  a.hd = hd;
+  const uint64_t va = reinterpret_cast<uintptr_t>(v->d_in) | (uint64_t)(v->in_token * bytes) | (uint64_t)(v->in_head * bytes);
+  a.v_pairs = va % (2 * bytes) == 0;
+  const int64_t v_items = std::max<int64_t>(1, (int64_t)b->plan.head.n_windows * ((a.n + 127) / 128));
+  a.v_blocks = (int32_t)std::min<int64_t>((v_items + 3) / 4, 1 << 16);
+  const int64_t t_blocks = std::min<int64_t>((n1 * a.turn.n_item_cols + 3) / 4, 1 << 20);
+  const uint32_t blocks = (uint32_t)(a.v_blocks + t_blocks);
+  const hipError_t e = dtype == 0   ? launch_append<float>(a, vec, blocks, s)
+                       : dtype == 1 ? launch_append<bf16_t>(a, vec, blocks, s)
+                                    : launch_append<_Float16>(a, vec, blocks, s);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return SYNERA_EHIP;
+  }
+  return SYNERA_OK;
+}
+
+// ------------------------------------------------------------------------------------ attention
+//   o = softmax(scale q K^T) V over the keys each row sees, online: running maximum m and sum l of a row, o rescaled where m moves.
+// A block takes one item: up to 128 rows (tokens x G heads of one KV head) against a range of a node's keys, in tiles of 32.
+//   * Up to 32 rows, the four wavefronts take every fourth tile each; up to 64, two take the rows' halves and every second tile;
+//     above, each takes 32 rows and all tiles.  Wavefronts that split the keys merge through LDS at the end.
+//   * Scores are computed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16): a lane then holds 16 keys of one row, so that the
+//     statistics are the lane's own but for one exchange with the other half, and, with the rows of the K operand dealt out in
+//     the order 0-3, 8-11, 4-7, 12-15 of each page's slots, its probabilities are already the B operand of O^T = V^T P^T.
+//   * Pages come by asynchronous copies (no registers, 1 KB an instruction) into rings of five slots, one ring for each group of
+//     wavefronts that share keys; a slot holds a page for each wavefront of the group.  80 KB in all: two blocks a compute
+//     unit, whose matrix and softmax work overlap.  K chunks are swizzled by slot, V halves by dim on the way in, for
+//     LDS reads without bank conflicts.
+//   * The probabilities are rounded to bf16 (to nearest): 2^-9 of each, which a sum over keys averages out to less than the rounding of the
+//     bf16 output.  The sum l takes them as they were.
+struct SharedAttnArgs {
+  const bf16_t* q;
+  bf16_t* o;
+  int64_t q_ts, q_hs, o_ts, o_hs;
+  const bf16_t* k_layer;
+  const bf16_t* v_layer;
+  const ShHeader* head;
+  const ShItem* items;
+  const int32_t* list;
+  const int32_t* pages;
+  const int32_t* joined;
+  const int32_t* first_entry;
+  const int32_t* req_tok;
+  const ShEntry* entries;
+  float* part_o;
+  float2* part_ml;
+  float* lse;
+  float c;                     // scale x log2 e
+  int32_t Hq, Hkv, G;
+};
+
+typedef __attribute__((ext_vector_type(8))) int sh_i32x8v;
+typedef SH_CONST_AS sh_i32x8v sh_i32x8;                      // read with scalar loads
+
+__device__ __forceinline__ float sh_ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float other_half(float v) {      // of lane l ^ 32
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? a[0] : a[1]);
+}
+
+// copy_to_lds (common.h) from a base in scalar registers and each lane's own offset in bytes
+__device__ __forceinline__ void copy_page_piece(const bf16_t* base, uint32_t off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(base) : "memory", "m0");
+}
+
+// At most `n` positions of IPP copies may still be on their way, and this wavefront's LDS reads are done.
+template <int IPP>
+__device__ __forceinline__ void wait_positions(int n) {
+  if (n >= 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * IPP) : "memory");
+  else if (n == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPP) : "memory");
+  else if (n == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IPP) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+}
+
+template <int HD>
+__device__ __forceinline__ int sh_swz(int slot) { return HD == 128 ? slot : slot >> 1; }
+
+template <int HD, int WR>      // WR wavefronts share keys and split the rows, 4 / WR groups of them split the keys
+__device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it, unsigned char* lds) {
+  constexpr int WK = 4 / WR, NT = 5, PPT = 4 / WR;            // key groups; slots of a ring; positions of a tile (K a, K b, V a, V b)
+  constexpr int PAGE_B = SY_PAGE * HD * 2, SLOT_B = WR * PAGE_B, RING_B = NT * SLOT_B, IPP = PAGE_B / 1024;
+  constexpr int KS = HD / 16, DB = HD / 32;
+  const int lane = threadIdx.x & 63, n32 = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave % WR, kp = wave / WR;
+  const bool leaf = (it.flags & SY_SH_LEAF) != 0;
+  unsigned char* ring = lds + kp * RING_B;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)ring;
+
+  // ---- keys
+  const int n_tiles = (it.key_end - it.key_begin + 31) / 32;
+  const int my_tiles = (n_tiles - kp + WK - 1) / WK, n_iter = (n_tiles + WK - 1) / WK;
+  const int n_pos = my_tiles * PPT;
+  const SH_CONST_AS int32_t* pages = reinterpret_cast<const SH_CONST_AS int32_t*>((uintptr_t)(a.pages + it.page));
+  const int page0 = it.key_begin / SY_PAGE;
+  const size_t page_elems = (size_t)a.Hkv * SY_PAGE * HD, head_at = (size_t)it.kv_head * SY_PAGE * HD;
+  uint32_t k_off[IPP], v_off[IPP];                            // bytes
+#pragma unroll
+  for (int j = 0; j < IPP; ++j) {
+    const int slot = j * (16 / IPP) + lane / (HD / 8);
+    k_off[j] = slot * HD * 2 + ((lane % (HD / 8)) ^ sh_swz<HD>(slot)) * 16;
+    const int at = j * 64 + lane, dim = at >> 1;
+    v_off[j] = (dim * 2 + ((at & 1) ^ ((dim >> 3) & 1))) * 16;
+  }
+  // position p of the ring: pages p WR .. p WR + WR - 1 of the sequence K a, K b, V a, V b of tile 0, of tile 1, ...; this wavefront
+  // copies one of them
+  auto page_of = [&](int p) {
+    const int s = min(p, n_pos - 1) * WR + wr;
+    return pages[min(page0 + 2 * ((s >> 2) * WK + kp) + (s & 1), it.n_pages - 1)];
+  };
+  auto issue = [&](int p, int32_t page) {
+    const uint32_t to = ring_at + (uint32_t)(p % NT) * SLOT_B + wr * PAGE_B;
+    if (((p * WR + wr) & 2) == 0) {
+      const bf16_t* from = a.k_layer + (size_t)page * page_elems + head_at;
+#pragma unroll
+      for (int j = 0; j < IPP; ++j) copy_page_piece(from, k_off[j], to + j * 1024);
+    } else {
+      const bf16_t* from = a.v_layer + (size_t)page * page_elems + head_at;
+#pragma unroll
+      for (int j = 0; j < IPP; ++j) copy_page_piece(from, v_off[j], to + j * 1024);
+    }
+  };
+  constexpr int AHEAD = WR == 1 ? NT : NT - PPT;              // positions on their way when the loop begins
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p)
+    if (p < n_pos) issue(p, page_of(p));
+
+  // ---- rows
+  const int row = wr * 32 + n32;
+  const int in_node = it.row0 + min(row, it.n_rows - 1);
+  const int j_tok = in_node / a.G, head = it.kv_head * a.G + in_node % a.G;
+  const int tok = leaf ? it.tok + j_tok : a.list[it.tok + j_tok];
+  const int lim = leaf ? it.lim0 + j_tok : 0x7FFFFFFF;        // last key that the row sees
+  const int free_end = leaf ? min(it.key_end, it.lim0 + it.row0 / a.G + 1) : it.key_end;   // keys below need no mask
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(a.q + (int64_t)tok * a.q_ts + (int64_t)head * a.q_hs + 16 * s + 8 * h);
+
+  const float c = a.c;
+  float m = c > 1.f ? -3e38f / c : -3e38f, l = 0.f;           // m in units of the raw scores; m c stays finite
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+
+  // where this lane reads its K rows and V rows inside a page
+  const int kslot = (n32 & 3) | ((n32 >> 2) & 1) << 3 | ((n32 >> 3) & 1) << 2;
+  const int v_at = n32 * 32 + (h ^ ((n32 >> 3) & 1)) * 16;
+  bf16x8 kf[KS], vf[DB][2];
+  // page `part` of tile i (of this group) in the ring
+  auto page_at = [&](int i, int part) { const int s = 4 * i + part; return ring + (s / WR % NT) * SLOT_B + (s % WR) * PAGE_B; };
+  auto read_k = [&](int i) {
+    const unsigned char* at = ((n32 >> 4) ? page_at(i, 1) : page_at(i, 0)) + kslot * (HD * 2);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(at + (((2 * s + h) ^ sh_swz<HD>(kslot)) << 4));
+  };
+  auto read_v = [&](int i) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vf[db][b] = *reinterpret_cast<const bf16x8*>(page_at(i, 2 + b) + db * 1024 + v_at);
+  };
+  f32x16 sc;
+  auto scores = [&]() {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
+  };
+  bf16x8 pf[2];
+  auto softmax = [&](int kb, auto masked) {                   // register r holds key kb + 16 (r / 8) + 8 h + r % 8
+    if constexpr (masked) {
+      const int seen = min(it.key_end - 1, lim) - kb - 8 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = 16 * (r >> 3) + (r & 7) <= seen ? sc[r] : -INFINITY;
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    mx = fmaxf(mx, other_half(mx));
+    // The reference only has to keep 2^(c (s - m)) in range: it moves when a score exceeds it by more than 2^8.
+    const float m_new = (mx - m) * c > 8.0f ? mx : m;
+    const float alpha = sh_ex2((m - m_new) * c), mc = m_new * c;
+    m = m_new;
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = sh_ex2(fmaf(sc[r], c, -mc));
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+    }
+    float t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      t0 += p[r];
+      t1 += p[r + 1];
+    }
+    l += t0 + t1;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      pf[b] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf2(p[8 * b], p[8 * b + 1]), pack_bf2(p[8 * b + 2], p[8 * b + 3]),
+                                                    pack_bf2(p[8 * b + 4], p[8 * b + 5]), pack_bf2(p[8 * b + 6], p[8 * b + 7])));
+  };
+  auto values = [&](int kb, auto masked) {
+    if constexpr (masked) {
+      // Keys past the end may hold junk, and 0 x NaN is NaN: they are blanked.  So may keys that only some rows see.
+      bool odd = false;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int n = it.key_end - kb - 16 * b - 8 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          u32x4 w = __builtin_bit_cast(u32x4, vf[db][b]);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            w[d] &= (2 * d < n ? 0x0000FFFFu : 0u) | (2 * d + 1 < n ? 0xFFFF0000u : 0u);
+            odd |= (w[d] & 0x7F80u) == 0x7F80u || (w[d] & 0x7F800000u) == 0x7F800000u;
+          }
+          vf[db][b] = __builtin_bit_cast(bf16x8, w);
+        }
+      }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {            // infinities or NaN among them: key by key, each to the rows that see it
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll 1
+          for (int k = 0; k < 16; ++k) {
+            const bool seen = kb + 16 * b + k <= lim;
+            const uint32_t keep = (k >> 3) == h ? ((k & 1) ? 0xFFFF0000u : 0x0000FFFFu) : 0u;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              u32x4 w = __builtin_bit_cast(u32x4, vf[db][b]);
+#pragma unroll
+              for (int d = 0; d < 4; ++d) w[d] &= d == ((k & 7) >> 1) ? keep : 0u;
+              f32x16 t;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) t[r] = 0.f;
+              t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[b], t, 0, 0, 0);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[db][r] += seen ? t[r] : 0.f;
+            }
+          }
+        return;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db][b], pf[b], acc[db], 0, 0, 0);
+  };
+
+  // The tiles that need no mask, then (masked) the last few: the code for hidden keys stays out of the first loop's registers.
+  const int free_tiles = max(0, free_end - it.key_begin) / 32;              // of all groups
+  const int my_free = min(my_tiles, max(0, (free_tiles - kp + WK - 1) / WK));
+  if constexpr (WR == 1) {
+    // No other wavefront touches this ring: K slots are filled again as soon as the scores' operands are in registers.
+    int32_t n0 = n_pos > 0 ? page_of(5) : 0, n1 = n_pos > 0 ? page_of(6) : 0;
+    auto tile = [&](int i, auto masked) {
+      const int kb = it.key_begin + 32 * (i * WK + kp);
+      const int32_t n2 = page_of(4 * i + 7), n3 = page_of(4 * i + 8);
+      wait_positions<IPP>(min(n_pos, 4 * i + 5) - (4 * i + 2));
+      read_k(i);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (4 * i + 5 < n_pos) issue(4 * i + 5, n0);
+      if (4 * i + 6 < n_pos) issue(4 * i + 6, n1);
+      scores();
+      softmax(kb, masked);
+      n0 = page_of(4 * i + 9);
+      n1 = page_of(4 * i + 10);
+      wait_positions<IPP>(min(n_pos, 4 * i + 7) - (4 * i + 4));
+      read_v(i);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (4 * i + 7 < n_pos) issue(4 * i + 7, n2);
+      if (4 * i + 8 < n_pos) issue(4 * i + 8, n3);
+      values(kb, masked);
+    };
+    for (int i = 0; i < my_free; ++i) tile(i, std::false_type());
+    for (int i = my_free; i < my_tiles; ++i) tile(i, std::true_type());
+  } else {
+    int32_t next[PPT];
+#pragma unroll
+    for (int q = 0; q < PPT; ++q) next[q] = n_pos > 0 ? page_of(AHEAD + q) : 0;
+    auto tile = [&](int i, auto masked) {
+      // Own copies of tile i have landed and own reads of tile i - 1 are done; the barrier extends both to the block, so the
+      // slots of tile i - 1 may be filled again.
+      wait_positions<IPP>(min(n_pos, i * PPT + AHEAD) - (i + 1) * PPT);
+      asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+      for (int q = 0; q < PPT; ++q)
+        if (i * PPT + AHEAD + q < n_pos) issue(i * PPT + AHEAD + q, next[q]);
+      const int kb = it.key_begin + 32 * (i * WK + kp);
+#pragma unroll
+      for (int q = 0; q < PPT; ++q) next[q] = page_of((i + 1) * PPT + AHEAD + q);
+      read_k(i);
+      scores();
+      read_v(i);
+      softmax(kb, masked);
+      values(kb, masked);
+    };
+    for (int i = 0; i < my_free; ++i) tile(i, std::false_type());
+    for (int i = my_free; i < my_tiles; ++i) tile(i, std::true_type());
+    if (my_tiles < n_iter) {                                  // the other key group has one tile more: its barrier
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      asm volatile("s_barrier" ::: "memory");
+    }
+  }
+
+  // ---- wavefronts that split the keys: the first group takes the others' results
+  if constexpr (WK > 1) {
+    constexpr int WORDS = (DB * 16 + 2) * 64;
+    __syncthreads();                                          // every copy has been waited for and every tile read
+    float* park = reinterpret_cast<float*>(lds);
+    if (kp > 0) {
+      float* to = park + ((kp - 1) * WR + wr) * WORDS + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(db * 16 + r) * 64] = acc[db][r];
+      to[DB * 16 * 64] = m;
+      to[(DB * 16 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (kp > 0) return;
+#pragma unroll
+    for (int g = 1; g < WK; ++g) {
+      const float* from = park + ((g - 1) * WR + wr) * WORDS + lane;
+      const float m1 = from[DB * 16 * 64], l1 = from[(DB * 16 + 1) * 64];
+      const float top = fmaxf(m, m1), f0 = sh_ex2((m - top) * c), f1 = sh_ex2((m1 - top) * c);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = acc[db][r] * f0 + from[(db * 16 + r) * 64] * f1;
+      l = l * f0 + l1 * f1;
+      m = top;
+    }
+  }
+  l += other_half(l);
+  if (row >= it.n_rows) return;
+  if (it.part < 0) {
+    const float inv = 1.0f / l;
+    bf16_t* to = a.o + (int64_t)tok * a.o_ts + (int64_t)head * a.o_hs + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<uint2*>(to + db * 32 + 2 * r) = make_uint2(pack_bf2(acc[db][r] * inv, acc[db][r + 1] * inv),
+                                                                     pack_bf2(acc[db][r + 2] * inv, acc[db][r + 3] * inv));
+    if (a.lse && h == 0) a.lse[(size_t)tok * a.Hq + head] = (m * c + __log2f(l)) * 0.69314718055994531f;
+  } else {
+    float* to = a.part_o + (size_t)(it.part + row) * HD + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(to + db * 32 + 2 * r) = make_float4(acc[db][r], acc[db][r + 1], acc[db][r + 2], acc[db][r + 3]);
+    if (h == 0) a.part_ml[it.part + row] = make_float2(m * c, l);
+  }
+}
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedAttnArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int n = a.head->n_items;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const sh_i32x8* at = reinterpret_cast<const sh_i32x8*>((uintptr_t)(a.items + i));
+    const sh_i32x8v w0 = at[0], w1 = at[1];
+    const ShItem it = {w0[0], w0[1], w0[2], w0[3], w0[4], w0[5], w0[6], w0[7], w1[0], w1[1], w1[2], {0, 0, 0, 0, 0}};
+    if (it.n_rows <= 32) attend<HD, 1>(a, it, lds);
+    else if (it.n_rows <= 64) attend<HD, 2>(a, it, lds);
+    else attend<HD, 4>(a, it, lds);
+    __syncthreads();                                          // the next item's copies come into the same LDS
+  }
+}
+
+// Joins the partial results of rows that several items worked on: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A thread takes four
+// values of one row; four partials are asked for together.
+#define JOIN_FLY 4
+template <int HD>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a) {
+  const int n = a.head->n_joined;
+  const int piece = blockIdx.y * 256 + threadIdx.x;
+  if (piece >= a.Hq * (HD / 4)) return;
+  const int head = piece / (HD / 4), d4 = piece % (HD / 4) * 4, kh = head / a.G, g = head % a.G;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int tok = a.joined[2 * i], req = a.joined[2 * i + 1];
+    const int r = (tok - a.req_tok[req]) * a.G + g;
+    float M = -3e38f, l = 0.f;
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int e = a.first_entry[req]; e < a.first_entry[req + 1]; ++e) {
+      const ShEntry en = a.entries[e];
+      int keys = en.keys;
+      if (en.lim0 >= 0) {                                     // causal: splits beyond the last key that the row's tile sees were left out
+        const int last = min((en.row0 + r) / SY_SH_TILE_ROWS * SY_SH_TILE_ROWS + SY_SH_TILE_ROWS, en.rows) - 1;
+        keys = min(keys, en.lim0 + last / a.G + 1);
+      }
+      const int splits = (keys + en.chunk - 1) / en.chunk;
+      const size_t row = (size_t)en.base + (size_t)kh * en.rows + r, step = (size_t)en.rows * a.Hkv;
+      for (int s0 = 0; s0 < splits; s0 += JOIN_FLY) {
+        float2 ml[JOIN_FLY];
+        float4 v[JOIN_FLY];
+#pragma unroll
+        for (int s = 0; s < JOIN_FLY; ++s) {
+          const size_t at = row + (size_t)min(s0 + s, splits - 1) * step;
+          ml[s] = a.part_ml[at];
+          v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
+        }
+#pragma unroll
+        for (int s = 0; s < JOIN_FLY; ++s)
+          if (s0 + s < splits) {
+            const float top = fmaxf(M, ml[s].x), f0 = sh_ex2(M - top), f1 = sh_ex2(ml[s].x - top);
+            M = top;
+            l = l * f0 + ml[s].y * f1;
+            sum.x = sum.x * f0 + v[s].x * f1;
+            sum.y = sum.y * f0 + v[s].y * f1;
+            sum.z = sum.z * f0 + v[s].z * f1;
+            sum.w = sum.w * f0 + v[s].w * f1;
+          }
+      }
+    }
+    const float inv = 1.0f / l;
+    *reinterpret_cast<uint2*>(a.o + (int64_t)tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
+        make_uint2(pack_bf2(sum.x * inv, sum.y * inv), pack_bf2(sum.z * inv, sum.w * inv));
+    if (a.lse && d4 == 0) a.lse[(size_t)tok * a.Hq + head] = (M + __log2f(l)) * 0.69314718055994531f;
+  }
+}
+
+template <int HD>
+static hipError_t launch_shared(const SharedAttnArgs& a, int items, int joined, hipStream_t s) {
+  const size_t lds = (size_t)20 * SY_PAGE * HD * 2;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_attn_kernel<HD>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  if (items > 0) shared_attn_kernel<HD><<<items, 256, lds, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (joined > 0) shared_join_kernel<HD><<<dim3(joined, (a.Hq * (HD / 4) + 255) / 256), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* q, const void* d_k_layer, const void* d_v_layer,
+                                           float scale, float* d_lse, void* stream) {
+  if (!b || !q || !d_k_layer || !d_v_layer || !b->planned) return SYNERA_EINVAL;
+  if (!std::isfinite(scale) || scale < 0.f) return SYNERA_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool graph = capturing(s);
+  if (b->plan.head.n_tokens == 0 && !graph) return SYNERA_OK;
+  if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16 || reinterpret_cast<uintptr_t>(d_lse) % 4) return SYNERA_EINVAL;
+  const ShLimits& l = b->lim;
+  if (q->n_heads != l.Hq) return SYNERA_EINVAL;
+  const int64_t T = b->plan.head.n_tokens, n1 = std::max<int64_t>(T, 1);
+  if (turn_check(*q, n1, l.hd, 2, 2, true) != SYNERA_OK) return SYNERA_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(q->d_in) | (uint64_t)(2 * q->in_token) | (uint64_t)(2 * q->in_head)) % 16) return SYNERA_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(q->d_out) | (uint64_t)(2 * q->out_token) | (uint64_t)(2 * q->out_head)) % 8) return SYNERA_EINVAL;
+  if (turn_overlap(q->d_out, q->out_token, q->out_head, l.Hq, 2, q->d_in, q->in_token, q->in_head, l.Hq, 2, n1, l.hd)) return SYNERA_EINVAL;
+  if (!rope_device_ok(b->device)) return SYNERA_EINVAL;
+  SharedAttnArgs a = {};
+  a.q = static_cast<const bf16_t*>(q->d_in);
+  a.o = static_cast<bf16_t*>(q->d_out);
+  a.q_ts = q->in_token;
+  a.q_hs = q->in_head;
+  a.o_ts = q->out_token;
+  a.o_hs = q->out_head;
+  a.k_layer = static_cast<const bf16_t*>(d_k_layer);
+  a.v_layer = static_cast<const bf16_t*>(d_v_layer);
+  a.head = b->region<ShHeader>(R_HEAD);
+  a.items = b->region<ShItem>(R_ITEM);
+  a.list = b->region<int32_t>(R_LIST);
+  a.pages = b->region<int32_t>(R_PAGE);
+  a.joined = b->region<int32_t>(R_JOINED);
+  a.first_entry = b->region<int32_t>(R_FIRST);
+  a.req_tok = b->region<int32_t>(R_REQ);
+  a.entries = b->region<ShEntry>(R_ENTRY);
+  a.part_o = b->part_o;
+  a.part_ml = b->part_ml;
+  a.lse = d_lse;
+  a.c = (scale > 0.f ? scale : 1.0f / sqrtf((float)l.hd)) * 1.4426950408889634f;
+  a.Hq = l.Hq;
+  a.Hkv = l.Hkv;
+  a.G = l.Hq / l.Hkv;
+  // A captured call serves plans of any size: both launches are made, for as much as may come; the kernels loop.
+  const int items = graph ? std::max(b->plan.head.n_items, l.slots) : b->plan.head.n_items;
+  const int joined = graph ? std::min(l.max_tokens, std::max(b->plan.head.n_joined, l.slots)) : b->plan.head.n_joined;
+  const hipError_t e = l.hd == 128 ? launch_shared<128>(a, items, joined, s) : launch_shared<64>(a, items, joined, s);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return SYNERA_EHIP;
+  }
+  return SYNERA_OK;
+}
+
+// ------------------------------------------------------------------------------------ test hook
+extern "C" int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t slots, int32_t max_tokens, int32_t B,
+                                            const int32_t* h_ctx_len, const int32_t* h_n_new, const int32_t* h_block_table, int32_t max_pages,
+                                            int32_t which, int32_t* h_out, int64_t cap, int64_t* n_words, int64_t* limits) {
+  if (!h_ctx_len || !h_n_new || !h_block_table || !n_words || (cap > 0 && !h_out) || B < 1 || slots < 1 || n_kv_heads < 1) return SYNERA_EINVAL;
+  try {
+    ShLimits l = {};
+    l.Hq = n_q_heads;
+    l.Hkv = n_kv_heads;
+    l.hd = 128;
+    l.max_batch = B;
+    l.max_tokens = max_tokens;
+    l.max_pages = max_pages;
+    l.slots = slots;
+    sh_limits(l);
+    if (limits) {
+      const int64_t v[7] = {l.items, l.list, l.entries, l.pages, l.windows, l.part_rows, l.shared_rows};
+      std::memcpy(limits, v, sizeof v);
+    }
+    ShPlan p;
+    sh_plan(l, B, h_ctx_len, h_n_new, h_block_table, max_pages, p);
+    const void* from[N_REGIONS] = {&p.head, p.tok_pos.data(), p.tok_slot.data(), p.windows.data(), p.items.data(), p.list.data(),
+                                   p.pages.data(), p.joined.data(), p.first_entry.data(), p.req_tok.data(), p.entries.data()};
+    const size_t words[N_REGIONS] = {sizeof(ShHeader) / 4, p.tok_pos.size(), p.tok_slot.size(), p.windows.size() * 4, p.items.size() * 16,
+                                     p.list.size(), p.pages.size(), p.joined.size(), p.first_entry.size(), p.req_tok.size(), p.entries.size() * 8};
+    if (which < 0 || which >= N_REGIONS) return SYNERA_EINVAL;
+    *n_words = (int64_t)words[which];
+    if ((int64_t)words[which] > cap) return SYNERA_ENOSPC;
+    if (words[which]) std::memcpy(h_out, from[which], words[which] * 4);
+    return SYNERA_OK;
+  } catch (const std::bad_alloc&) {
+    return SYNERA_ENOMEM;
+  }
+}

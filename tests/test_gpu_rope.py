@@ -1,0 +1,186 @@
+"""GPU parity of rotary positions and head norms (Rope.apply, Rope.norm_apply) with float64, and their refusals."""
+import numpy as np
+import pytest
+import torch
+
+import shared_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def synera():
+    import paper_2511_07423_amd as s
+    return s
+
+
+def draw(shape, dtype, seed, scale=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def positions(n, seed, far=5000):
+    return torch.randint(-far, far, (n,), generator=torch.Generator(device=DEV).manual_seed(seed + 99), device=DEV).to(torch.int32)
+
+
+def check(got, x, pos, freq, layout, name, magnitude=1.0, gain=None, eps=0.0):
+    want, err = ref.turn(ref.to64(x), pos.cpu().numpy(), freq, layout, magnitude, None if gain is None else ref.to64(gain), eps)
+    step = ref.half_step(got.dtype)
+    tiny = torch.finfo(got.dtype).smallest_normal * torch.finfo(got.dtype).eps
+    ref.close(ref.to64(got), want, np.abs(want) * step + err * (1 + step) + tiny, name)
+
+
+# (head_dim, rot_dim): chunks of 8, 4, 2 and 1 values in both layouts, heads of one pair and of 256 values, rests that are odd in chunks
+SHAPES = [(128, 128), (64, 64), (128, 64), (128, 32), (80, 20), (96, 24), (72, 36), (80, 48), (256, 256), (256, 2), (2, 2), (6, 4), (250, 250), (48, 22), (160, 16)]
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("hd,rot", SHAPES)
+def test_rope_and_norm(hd, rot, dtype, layout):
+    s = synera()
+    rope = s.Rope(hd, rot, layout=layout)
+    freq = ref.frequencies(rot)
+    for T, hq, hk in ((1, 5, 1), (37, 3, 2)):
+        fused = draw((T, hq + 2 * hk, hd), TYPES[dtype], hd * 1000 + rot + T, 2.0)
+        q, k = fused[:, :hq], fused[:, hq: hq + hk]
+        pos = positions(T, rot)
+        oq, ok = rope.apply(pos, q, k)
+        check(oq, q, pos, freq, layout, "q")
+        check(ok, k, pos, freq, layout, "k")
+        assert torch.equal(oq[..., rot:], q[..., rot:]) and torch.equal(ok[..., rot:], k[..., rot:])   # the rest passes as it is
+        gq, gk = draw((hd,), torch.bfloat16, 5) + 1, draw((hd,), torch.bfloat16, 6) + 1
+        nq, nk = rope.norm_apply(pos, q, k, gq, gk, 1e-5)
+        check(nq, q, pos, freq, layout, "normed q", gain=gq, eps=1e-5)
+        check(nk, k, pos, freq, layout, "normed k", gain=gk, eps=1e-5)
+        # in place, in slices of one array; the values' heads stay
+        want_q, want_k, rest = oq.clone(), ok.clone(), fused[:, hq + hk:].clone()
+        rope.apply(pos, q, k, out_q=q, out_k=k)
+        assert torch.equal(q, want_q) and torch.equal(k, want_k) and torch.equal(fused[:, hq + hk:], rest)
+
+
+@pytest.mark.parametrize("scaling", [None, ("linear", 8.0), ("bands", 8.0, 1.0, 4.0, 8192.0), ("bands", 4.0, 0.0, 32.0, 4096.0)])
+@pytest.mark.parametrize("base", [10000.0, 500000.0])
+def test_far_positions(scaling, base):
+    s = synera()
+    pos = torch.tensor([0, 1, -1, 131071, 1 << 24, (1 << 24) + 1, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV)
+    q = draw((8, 2, 128), torch.float32, 3)
+    for layout in ("interleaved", "half"):
+        got, _ = s.Rope(128, layout=layout, base=base, scaling=scaling).apply(pos, q)
+        check(got, q, pos, ref.frequencies(128, base, scaling), layout, layout)
+
+
+def test_own_table_and_magnitude():
+    s = synera()
+    freq = np.linspace(-2.0, 3.0, 16)
+    q, pos = draw((9, 3, 64), torch.float32, 4), positions(9, 1)
+    got, k = s.Rope(64, 32, layout="half", inv_freq=freq, magnitude=-1.25).apply(pos, q)
+    assert k is None
+    check(got, q, pos, freq, "half", "q", magnitude=-1.25)
+
+
+@pytest.mark.parametrize("T,heads", [(5000, (32, 8)), (3001, (7, 1))])
+def test_many_tokens(T, heads):
+    s = synera()
+    rope = s.Rope(128, layout="half")
+    q, k, pos = draw((T, heads[0], 128), torch.bfloat16, 1), draw((T, heads[1], 128), torch.bfloat16, 2), positions(T, 3, 100000)
+    oq, ok = rope.apply(pos, q, k)
+    check(oq, q, pos, ref.frequencies(128), "half", "q")
+    check(ok, k, pos, ref.frequencies(128), "half", "k")
+
+
+def test_strides_and_alignment():
+    """Rows that start on any element, tokens inside heads, heads that are one head repeated, outputs with gaps that stay."""
+    s = synera()
+    rope, freq = s.Rope(64, layout="half"), ref.frequencies(64)
+    pos = positions(11, 2)
+    for shift in (1, 2, 4, 8):
+        flat = draw((11 * 3 * 64 + 16,), torch.bfloat16, shift)
+        q = flat[shift: shift + 11 * 3 * 64].view(11, 3, 64)
+        for out_shift in (0, 1):
+            room = torch.full((11 * 3 * 72 + 16,), 7.0, dtype=torch.bfloat16, device=DEV)
+            out = room[out_shift: out_shift + 11 * 3 * 72].view(11, 3, 72)[..., :64]
+            rope.apply(pos, q, out_q=out)
+            check(out, q, pos, freq, "half", f"shift {shift}, {out_shift}")
+            gaps = room[out_shift: out_shift + 11 * 3 * 72].view(11, 3, 72)[..., 64:]
+            assert (gaps == 7).all() and (room[:out_shift] == 7).all() and (room[out_shift + 11 * 3 * 72:] == 7).all()
+    by_head = draw((3, 11, 64), torch.float16, 8).transpose(0, 1)
+    out = torch.empty((3, 11, 64), dtype=torch.float16, device=DEV).transpose(0, 1)
+    rope.apply(pos, by_head, out_q=out)
+    check(out, by_head, pos, freq, "half", "tokens inside heads")
+    one = draw((11, 1, 64), torch.float32, 9).expand(11, 6, 64)
+    check(rope.apply(pos, one)[0], one, pos, freq, "half", "one head for all")
+
+
+def test_rows_stay_their_own():
+    """Infinities, NaN and zeros of one head reach no other; a head of zeros is normed to zeros by eps."""
+    s = synera()
+    rope, pos = s.Rope(64, layout="interleaved"), positions(4, 2)
+    q = draw((4, 4, 64), torch.float32, 7)
+    q[0, 1, 5], q[1, 2, 63], q[2, 3] = float("nan"), float("inf"), 0.0
+    gain = draw((64,), torch.bfloat16, 1) + 1
+    freq = ref.frequencies(64)
+    for got, g in ((rope.apply(pos, q)[0], None), (rope.norm_apply(pos, q, None, gain, None, 1e-6)[0], gain)):
+        bad = torch.zeros((4, 4), dtype=torch.bool)
+        bad[0, 1] = bad[1, 2] = True
+        assert torch.isfinite(got.cpu()[~bad]).all() and not torch.isfinite(got.cpu()[bad]).all()
+        keep = ~bad
+        want, err = ref.turn(ref.to64(q), pos.cpu().numpy(), freq, "interleaved", 1.0, None if g is None else ref.to64(g), 1e-6)
+        ref.close(ref.to64(got)[keep.numpy()], want[keep.numpy()], (np.abs(want) * ref.U + err)[keep.numpy()] + 1e-38, "others")
+    assert (rope.norm_apply(pos, q, None, gain, None, 1e-6)[0][2, 3] == 0).all()
+
+
+def test_empty_streams_and_graph():
+    s = synera()
+    rope = s.Rope(128)
+    q = draw((0, 4, 128), torch.bfloat16, 1)
+    assert rope.apply(torch.empty(0, dtype=torch.int32, device=DEV), q)[0].shape == (0, 4, 128)
+    q, pos = draw((65, 4, 128), torch.bfloat16, 2), positions(65, 1)
+    want, _ = rope.apply(pos, q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got, _ = rope.apply(pos, q)
+    side.synchronize()
+    assert torch.equal(got, want)
+    out, graph = torch.empty_like(q), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rope.apply(pos, q, out_q=out)
+    for i in range(4):
+        q.copy_(draw((65, 4, 128), torch.bfloat16, 10 + i))
+        pos.copy_(positions(65, 20 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, rope.apply(pos, q)[0])
+
+
+def test_refusals():
+    s = synera()
+    rope = s.Rope(64, 32)
+    q, pos = draw((6, 4, 64), torch.bfloat16, 1), positions(6, 1)
+    gain = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    for bad in (dict(pos=pos.long()), dict(pos=pos[:5]), dict(pos=pos.cpu()), dict(q=q.cpu()), dict(q=q.double()), dict(q=q[..., :32]),
+                dict(q=q.transpose(1, 2)), dict(k=draw((5, 4, 64), torch.bfloat16, 1)), dict(k=q.float()), dict(out_q=q.float()),
+                dict(out_q=torch.empty((6, 3, 64), dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises(ValueError):
+            rope.apply(**{**dict(pos=pos, q=q), **bad})
+    for bad in (dict(q_gain=None), dict(q_gain=gain.float()), dict(q_gain=gain[:32]), dict(k=q, k_gain=None)):
+        with pytest.raises(ValueError):
+            rope.norm_apply(**{**dict(pos=pos, q=q, k=None, q_gain=gain, k_gain=None, eps=1e-5), **bad})
+
+    def status(call):
+        with pytest.raises(s.SyneraError) as e:
+            call()
+        return e.value.status
+    assert status(lambda: rope.norm_apply(pos, q, None, gain, None, -1.0)) == s.EINVAL
+    assert status(lambda: rope.norm_apply(pos, q, None, gain, None, float("nan"))) == s.EINVAL
+    wide = draw((6, 9, 64), torch.bfloat16, 2)
+    assert status(lambda: rope.apply(pos, wide[:, :4], out_q=wide[:, 1:5])) == s.EINVAL          # out on another head's input
+    assert status(lambda: rope.apply(pos, wide[:, :4], wide[:, 4:8], out_q=wide[:, 4:8], out_k=wide[:, :4])) == s.EINVAL
+    same = torch.empty((6, 4, 64), dtype=torch.bfloat16, device=DEV)
+    assert status(lambda: rope.apply(pos, q, q, out_q=same, out_k=same)) == s.EINVAL             # two outputs on one another
+    one = torch.empty((6, 1, 64), dtype=torch.bfloat16, device=DEV)
+    assert status(lambda: rope.apply(pos, q, out_q=one.expand(6, 4, 64))) == s.EINVAL            # an output on itself
+    rope.apply(pos, wide[:, :4], out_q=wide[:, 5:])                                              # slices side by side are fine
+    torch.cuda.synchronize()

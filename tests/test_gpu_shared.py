@@ -1,0 +1,373 @@
+"""GPU parity of appends with the rotation and of attention over shared prefixes with float64: element by element, over random trees of
+shared pages whose unwritten slots hold NaN."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import shared_reference as ref
+from test_shared_plan_cpu import make_batch
+
+pytestmark = pytest.mark.gpu
+DEV, P = "cuda:0", 16
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def synera():
+    import paper_2511_07423_amd as s
+    return s
+
+
+def draw(shape, seed, dtype=torch.bfloat16, scale=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def bits(shape, value):
+    return torch.full(shape, value, dtype=torch.int16, device=DEV).view(torch.bfloat16)
+
+
+def filled_pools(ctx, new, table, n_pages, hkv, hd, seed, junk=0x7FC0, spare=2):
+    """Pools in which every position that a request holds or appends has values and everything else is junk (NaN)."""
+    k, v = bits((n_pages + spare, hkv, P, hd), junk), bits((n_pages + spare, hkv, hd, P), junk)
+    live = torch.zeros((n_pages + spare, P), dtype=torch.bool)
+    for c, n, row in zip(ctx, new, table):
+        at = np.arange(c + n)
+        live[row[at // P], at % P] = True
+    live = live.to(DEV)
+    k = torch.where(live[:, None, :, None], draw(k.shape, seed), k)
+    v = torch.where(live[:, None, None, :], draw(v.shape, seed + 1), v)
+    return k.contiguous(), v.contiguous()
+
+
+def planned(hq, hkv, hd, ctx, new, table, n_pages, more=0):
+    b = synera().SharedBatch(hq, hkv, hd, len(ctx) + more, max(1, int(new.sum())) + more, table.shape[1] + more)
+    b.plan(ctx, new, table, n_pages)
+    return b
+
+
+def check_attention(hq, hkv, hd, ctx, new, table, n_pages, seed, scale=None, std=1.5):
+    b = planned(hq, hkv, hd, ctx, new, table, n_pages)
+    k, v = filled_pools(ctx, new, table, n_pages, hkv, hd, seed)
+    T = int(new.sum())
+    q = draw((T + 3, hq, hd), seed + 2, scale=std)
+    out = bits((T + 3, hq, hd), 0x1234)
+    got, lse = b.attention(q, k, v, scale=scale, out=out, want_lse=True)
+    want, want_lse, eo, el = ref.attention(ref.to64(q)[:T], ref.to64(k), ref.to64(v), ctx, new, table, hd ** -0.5 if scale is None else scale)
+    ref.close(ref.to64(got)[:T], want, eo, "o")
+    ref.close(ref.to64(lse)[:T], want_lse, el, "lse")
+    assert torch.equal(got[T:].view(torch.int16), bits((3, hq, hd), 0x1234).view(torch.int16))     # rows behind the batch stay
+    return b, q, k, v
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_attention_trees(seed):
+    rng = random.Random(seed)
+    B = rng.choice((1, 2, 5, 20))
+    hkv = rng.choice((1, 2, 3))
+    hq, hd = hkv * rng.choice((1, 3, 4, 7, 16)), rng.choice((64, 128))
+    ctx, new, table, n_pages = make_batch(rng, B, max_new=rng.choice((1, 4, 33)), max_own=rng.choice((0, 30, 500)))
+    check_attention(hq, hkv, hd, ctx, new, table, n_pages, seed * 10)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ctx,new", [(0, 1), (0, 2), (15, 1), (16, 1), (31, 1), (32, 1), (127, 1), (128, 2), (255, 3), (256, 1), (257, 9), (1000, 40),
+                                     (5000, 1), (0, 300), (77, 150)])
+def test_attention_one_request(ctx, new, hd):
+    """Lengths around pages, tiles and cuts; one token and long chunks; every class of rows."""
+    n = -(-(ctx + new) // P)
+    table = np.random.RandomState(ctx).permutation(n).astype(np.int32)[None]
+    for hq, hkv in ((1, 1), (8, 2)):
+        check_attention(hq, hkv, hd, np.array([ctx], np.int32), np.array([new], np.int32), table, n, ctx + new)
+
+
+def shared_batch(B, shared, own, new, seed=0):
+    """B requests behind `shared` common pages, with own[i] more cached tokens and new[i] new ones."""
+    own, new = np.broadcast_to(own, B), np.broadcast_to(new, B).astype(np.int32)
+    ctx = (shared * P + own).astype(np.int32)
+    need = -(-(ctx + new) // P)
+    table = np.full((B, int(need.max())), -1, np.int32)
+    at = shared
+    perm = np.random.RandomState(seed).permutation(shared + int((need - shared).sum())).astype(np.int32)
+    for i in range(B):
+        table[i, : need[i]] = perm[np.concatenate([np.arange(shared), at + np.arange(need[i] - shared)])]
+        at += need[i] - shared
+    return ctx, new, table, len(perm)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B,shared,own,new", [(2, 8, 0, 1), (40, 33, 5, 1), (70, 9, 40, 2), (9, 40, 0, 20), (3, 65, 17, 64)])
+def test_attention_shared(B, shared, own, new, hd):
+    rs = np.random.RandomState(B)
+    ctx, new, table, n = shared_batch(B, shared, rs.randint(0, own + 1, B), rs.randint(1, new + 1, B), B)
+    check_attention(8, 2, hd, ctx, new, table, n, B)
+
+
+def test_attention_repeats_bit_for_bit():
+    ctx, new, table, n = shared_batch(30, 20, 7, 3)
+    b, q, k, v = check_attention(8, 2, 128, ctx, new, table, n, 1)
+    T = int(new.sum())                                         # (a new output's rows behind the batch are whatever they were)
+    first = b.attention(q, k, v)[:T]
+    for _ in range(3):
+        assert torch.equal(b.attention(q, k, v)[:T], first)
+
+
+def test_attention_scales_and_large_scores():
+    ctx, new, table, n = shared_batch(5, 10, 3, 2)
+    for scale, std in ((1e-4, 1.0), (1.0, 1.5), (7.0, 3.0)):
+        check_attention(4, 2, 64, ctx, new, table, n, 3, scale=scale, std=std)
+
+
+def test_attention_strides():
+    """Queries inside a fused array, outputs with tokens inside heads."""
+    s, hq, hkv, hd = synera(), 6, 2, 64
+    ctx, new, table, n = shared_batch(6, 9, 4, 5)
+    b = planned(hq, hkv, hd, ctx, new, table, n, more=3)
+    k, v = filled_pools(ctx, new, table, n, hkv, hd, 5)
+    T = int(new.sum())
+    q = draw((T, hq + 2 * hkv, hd), 6)[:, :hq]
+    plain = b.attention(q.contiguous(), k, v)
+    assert torch.equal(b.attention(q, k, v), plain)
+    out = torch.zeros((hq, T, hd), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    assert b.attention(q, k, v, out=out) is out and torch.equal(out, plain)
+
+
+def test_attention_hidden_values():
+    """Infinities and NaN: of a key or value, they reach the rows that see it and no other; of a query, its own row."""
+    hq, hkv, hd = 4, 2, 128
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        ctx, new, table, n = shared_batch(3, 8, np.array([0, 21, 40]), np.array([1, 12, 40]))
+        b = planned(hq, hkv, hd, ctx, new, table, n)
+        k, v = filled_pools(ctx, new, table, n, hkv, hd, 5)
+        pos = ctx[1] + 7                                       # seen by rows 7 .. 11 of request 1 alone
+        v[table[1, pos // P], 1, 5, pos % P] = bad
+        pos = ctx[2] + 33
+        k[table[2, pos // P], 0, pos % P, 9] = float("nan")    # rows 33 .. 39 of request 2
+        q = draw((int(new.sum()), hq, hd), 6)
+        q[0, 3, 0] = float("nan")
+        got, lse = b.attention(q, k, v, want_lse=True)
+        want, wl, eo, el = ref.attention(ref.to64(q), ref.to64(k), ref.to64(v), ctx, new, table, hd ** -0.5)
+        ref.close(ref.to64(got), want, eo, f"o with {bad}")
+        ref.close(ref.to64(lse), wl, el, f"lse with {bad}")
+
+
+def check_append(hq, hkv, hd, rot, layout, dtype, ctx, new, table, n_pages, seed, norm=False, shift=0, with_q=True, scaling=None):
+    s = synera()
+    rope = s.Rope(hd, rot, layout=layout, scaling=scaling)
+    b = planned(hq, hkv, hd, ctx, new, table, n_pages)
+    T = int(new.sum())
+    width = (hq + 2 * hkv) * hd
+    flat = draw((T * width + 16,), seed, TYPES[dtype], 2.0)
+    x = flat[shift: shift + T * width].view(T, hq + 2 * hkv, hd)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    gq, gk = (draw((hd,), 5) + 1, draw((hd,), 6) + 1) if norm else (None, None)
+    kp, vp = bits((n_pages + 1, hkv, P, hd), 0x1234), bits((n_pages + 1, hkv, hd, P), 0x4321)
+    oq = b.append_rope(rope, q if with_q else None, k, v, kp, vp, q_gain=gq, k_gain=gk, eps=1e-5)
+    pos = np.concatenate([c + np.arange(m) for c, m in zip(ctx, new)]).astype(np.int64)
+    req = np.repeat(np.arange(len(ctx)), new)
+    freq = ref.frequencies(rot, scaling=scaling)
+    step = 2.0 ** -8
+    if with_q:
+        want, err = ref.turn(ref.to64(q), pos, freq, layout, 1.0, None if gq is None else ref.to64(gq), 1e-5)
+        ref.close(ref.to64(oq), want, np.abs(want) * step + err * (1 + step) + 1e-38, "q")
+    else:
+        assert oq is None
+    want, err = ref.turn(ref.to64(k), pos, freq, layout, 1.0, None if gk is None else ref.to64(gk), 1e-5)
+    page, slot = torch.from_numpy(table[req, pos // P].astype(np.int64)).to(DEV), torch.from_numpy(pos % P).to(DEV)
+    ref.close(ref.to64(kp[page, :, slot]), want, np.abs(want) * step + err * (1 + step) + 1e-38, "k")
+    assert torch.equal(vp[page, :, :, slot], v.to(torch.bfloat16))
+    kp[page, :, slot] = bits((), 0x1234)                       # everything else is as it was
+    vp[page, :, :, slot] = bits((), 0x4321)
+    assert (kp.view(torch.int16) == 0x1234).all() and (vp.view(torch.int16) == 0x4321).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("hd,rot,hq,hkv", [(128, 128, 8, 2), (64, 64, 3, 3), (64, 20, 4, 1), (128, 64, 2, 1), (128, 6, 5, 5)])
+def test_append(hd, rot, hq, hkv, layout, dtype):
+    for seed, (B, new, own) in enumerate(((1, 1, 0), (7, 1, 40), (6, 20, 40), (2, 90, 7))):
+        ctx, n, table, pages = make_batch(random.Random(seed + hd), B, max_new=new, max_own=own, zero=0.2 if B > 2 else 0.0)
+        if n.sum() == 0:
+            n[0] = 1
+            continue
+        check_append(hq, hkv, hd, rot, layout, dtype, ctx, n, table, pages, seed, norm=seed % 2 == 0, shift=(0, 8, 1, 2)[seed], with_q=seed != 1,
+                     scaling=(None, ("linear", 4.0), ("bands", 8.0, 1.0, 4.0, 64.0), None)[seed])
+
+
+def test_append_writes_what_rope_and_kv_append_write():
+    """The keys an append turns are those that Rope.apply turns, and its pages those of Verifier.kv_append, bit for bit."""
+    import workloads as wl
+    from helpers import drawn_model, small_shape
+    s = synera()
+    shape = small_shape(d_model=256, n_q_heads=4, n_kv_heads=4, head_dim=64, d_ffn=128, vocab=128, n_layers=1)
+    head, layers = drawn_model(shape, 1, DEV)
+    ver = s.Verifier(shape, head, layers, 4, 200, 8)
+    ctx, new = np.array([0, 9, 40], np.int32), np.array([50, 3, 1], np.int32)
+    table = np.arange(24, dtype=np.int32).reshape(3, 8)
+    x = draw((54, 12, 64), 3)
+    rope = s.Rope(64, layout="half")
+    pos = torch.from_numpy(np.concatenate([c + np.arange(n) for c, n in zip(ctx, new)]).astype(np.int32)).to(DEV)
+    q1, k1 = rope.apply(pos, x[:, :4], x[:, 4:8])
+    pools = [bits((24, 4, 16, 64), 0), bits((24, 4, 64, 16), 0), bits((1, 24, 4, 16, 64), 0), bits((1, 24, 4, 64, 16), 0)]
+    ver.kv_append(0, ctx, new, k1, x[:, 8:].contiguous(), table, 24, pools[2], pools[3])
+    b = planned(4, 4, 64, ctx, new, table, 24)
+    assert torch.equal(b.append_rope(rope, x[:, :4], x[:, 4:8], x[:, 8:], pools[0], pools[1]), q1)
+    assert torch.equal(pools[0], pools[2][0]) and torch.equal(pools[1], pools[3][0])
+    ver.close()
+
+
+def test_steps_of_a_decoder_layer():
+    """As a server runs them: norms, rotation, append and attention over three steps of a batch that shares a prompt; one token each, then
+    drafts, then a request that joins and one that waits.  Every step against float64 over what the cache then holds."""
+    s, hq, hkv, hd = synera(), 8, 2, 128
+    rope = s.Rope(hd, 64, layout="half", base=500000.0, scaling=("bands", 8.0, 1.0, 4.0, 8192.0))
+    freq = ref.frequencies(64, 500000.0, ("bands", 8.0, 1.0, 4.0, 8192.0))
+    gains = draw((hd,), 1) + 1, draw((hd,), 2) + 1
+    B, shared, cols = 6, 12, 16
+    table = np.concatenate([np.tile(np.arange(shared), (B, 1)), shared + np.arange(B * (cols - shared)).reshape(B, -1)], 1).astype(np.int32)
+    n_pages = int(table.max()) + 1
+    b = s.SharedBatch(hq, hkv, hd, B, 64, cols)
+    kp, vp = bits((n_pages, hkv, P, hd), 0x7FC0), bits((n_pages, hkv, hd, P), 0x7FC0)
+    kp[:shared], vp[:shared] = draw((shared, hkv, P, hd), 3), draw((shared, hkv, hd, P), 4)
+    ctx = np.full(B, shared * P, np.int32)
+    for step, new in enumerate(([1] * B, [4, 1, 9, 2, 1, 0], [1, 0, 30, 3, 5, 2])):
+        new = np.array(new, np.int32)
+        b.plan(ctx, new, table, n_pages)
+        T = int(new.sum())
+        x = draw((T, hq + 2 * hkv, hd), 50 + step, torch.float32)
+        q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+        turned = b.append_rope(rope, q, k, v, kp, vp, q_gain=gains[0], k_gain=gains[1], eps=1e-6)
+        o = b.attention(turned, kp, vp)
+        pos = np.concatenate([c + np.arange(n) for c, n in zip(ctx, new)]).astype(np.int64)
+        req = np.repeat(np.arange(B), new)
+        want_q, err = ref.turn(ref.to64(q), pos, freq, "half", 1.0, ref.to64(gains[0]), 1e-6)
+        ref.close(ref.to64(turned), want_q, np.abs(want_q) * 2.0 ** -8 + 2 * err, "q")
+        want_k, err = ref.turn(ref.to64(k), pos, freq, "half", 1.0, ref.to64(gains[1]), 1e-6)
+        got_k = ref.to64(kp)[table[req, pos // P], :, pos % P]
+        ref.close(got_k, want_k, np.abs(want_k) * 2.0 ** -8 + 2 * err, "k")
+        want, _, eo, _ = ref.attention(ref.to64(turned), ref.to64(kp), ref.to64(vp), ctx, new, table, hd ** -0.5)
+        ref.close(ref.to64(o), want, eo, f"o of step {step}")
+        ctx = ctx + new
+
+
+def test_captured_calls_serve_later_plans():
+    """A graph of append and attention, captured for one small plan, replayed for others: smaller, larger, cut and uncut, empty."""
+    s, hq, hkv, hd = synera(), 8, 2, 64
+    rope = s.Rope(hd, layout="half")
+    B, cols, room = 12, 140, 96
+    b = s.SharedBatch(hq, hkv, hd, B, room, cols)
+    n_pages = 1100
+    kp, vp = draw((n_pages, hkv, P, hd), 1), draw((n_pages, hkv, hd, P), 2)
+    x = draw((room, hq + 2 * hkv, hd), 3)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    out_q, out = torch.zeros((room, hq, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((room, hq, hd), dtype=torch.bfloat16, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        b.plan(np.array([3], np.int32), np.array([1], np.int32), np.zeros((1, 1), np.int32), n_pages)
+        with torch.cuda.graph(graph, stream=side):
+            b.append_rope(rope, q, k, v, kp, vp, out_q=out_q)
+            b.attention(out_q, kp, vp, out=out)
+            with pytest.raises(s.SyneraError):                 # a plan cannot be captured
+                b.plan(np.array([3], np.int32), np.array([1], np.int32), np.zeros((1, 1), np.int32), n_pages)
+        plans = [shared_batch(12, 60, np.arange(12) * 5, 1 + np.arange(12) % 8), shared_batch(1, 0, 0, 96), shared_batch(12, 130, 3, 1),
+                 (np.array([5], np.int32), np.zeros(1, np.int32), np.zeros((1, 1), np.int32), 1), shared_batch(2, 1, 1, 1)]
+        for round_, (ctx, new, table, _) in enumerate(plans + plans[::-1]):
+            x.copy_(draw(x.shape, 100 + round_))
+            kp.copy_(draw(kp.shape, 200 + round_))
+            vp.copy_(draw(vp.shape, 300 + round_))
+            out.fill_(7.0)
+            b.plan(ctx, new, table, n_pages)
+            graph.replay()
+            T = int(new.sum())
+            got, got_q = out.clone(), out_q.clone()
+            kp2, vp2 = kp.clone(), vp.clone()
+            want_q = b.append_rope(rope, q, k, v, kp2, vp2)
+            want = b.attention(want_q, kp2, vp2)
+            side.synchronize()
+            assert torch.equal(kp, kp2) and torch.equal(vp, vp2)
+            assert torch.equal(got_q[:T], want_q[:T]) and torch.equal(got[:T], want[:T]), round_
+            assert (got[T:] == 7).all()
+
+
+def test_two_batches_on_two_streams():
+    s = synera()
+    runs = []
+    for i in range(2):
+        ctx, new, table, n = shared_batch(20 + i, 30 + i, 9, 2, i)
+        k, v = filled_pools(ctx, new, table, n, 2, 64, i)
+        q = draw((int(new.sum()), 8, 64), 10 + i)
+        b = planned(8, 2, 64, ctx, new, table, n)
+        runs.append((b, q, k, v, b.attention(q, k, v), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(5):
+        for i, (b, q, k, v, _, st) in enumerate(runs):
+            with torch.cuda.stream(st):
+                outs[i].append(b.attention(q, k, v))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, runs[i][4]) for o in outs[i])
+
+
+def test_plans_ahead_of_their_uploads():
+    """More plans in a row than there are staging slots: the last one counts, each call sees its own."""
+    s = synera()
+    b = s.SharedBatch(4, 4, 64, 8, 64, 40)
+    k, v, q = draw((400, 4, P, 64), 1), draw((400, 4, 64, P), 2), draw((64, 4, 64), 3)
+    plans = [shared_batch(1 + i % 8, 3 + i, 2 * i, 1 + i % 7, i) for i in range(11)]
+    got = []
+    for ctx, new, table, _ in plans:
+        b.plan(ctx, new, table, 400)
+        got.append(b.attention(q, k, v)[: int(new.sum())].clone())
+    for (ctx, new, table, _), o in zip(plans, got):
+        want, _, eo, _ = ref.attention(ref.to64(q)[: int(new.sum())], ref.to64(k), ref.to64(v), ctx, new, table, 0.125)
+        ref.close(ref.to64(o), want, eo, "o")
+
+
+def test_refusals():
+    s, hq, hkv, hd = synera(), 4, 2, 64
+    ctx, new, table, n = shared_batch(3, 2, 4, 2)
+    T = int(new.sum())
+    kp, vp = draw((n, hkv, P, hd), 1), draw((n, hkv, hd, P), 2)
+    x = draw((T, hq + 2 * hkv, hd), 3)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    rope = s.Rope(hd)
+    b = s.SharedBatch(hq, hkv, hd, 3, T, table.shape[1])
+
+    def status(call):
+        with pytest.raises(s.SyneraError) as e:
+            call()
+        return e.value.status
+    assert status(lambda: b.attention(q, kp, vp)) == s.EINVAL                       # no plan yet
+    assert status(lambda: b.append_rope(rope, q, k, v, kp, vp)) == s.EINVAL
+    b.plan(ctx, new, table, n)
+    good = b.append_rope(rope, q, k, v, kp, vp)
+    o = b.attention(good, kp, vp)
+    wide = np.concatenate([table, table[:, :1] * 0 - 1], 1)
+    assert status(lambda: b.plan(ctx, new, wide, n)) == s.ENOSPC                    # more columns than the batch has room for
+    assert status(lambda: b.plan(ctx, new + 1, table, n)) == s.ENOSPC
+    assert status(lambda: b.plan(ctx, new, table, 3)) == s.ERANGE
+    assert torch.equal(b.attention(good, kp, vp), o)                                # a refused plan leaves the one before
+    for bad in (dict(q=q[:, :2]), dict(k=k[: T - 1]), dict(k=k.float()), dict(q=q.double(), k=k.double(), v=v.double()), dict(k_pool=kp[:-1]),
+                dict(k_pool=vp), dict(v_pool=vp.float()), dict(k_pool=kp.transpose(0, 1)), dict(v=v.cpu()), dict(out_q=q.float()),
+                dict(k_gain=torch.ones(32, dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises(ValueError):
+            b.append_rope(**{**dict(rope=rope, q=q, k=k, v=v, k_pool=kp, v_pool=vp), **bad})
+    for bad in (dict(q=q.float()), dict(q=q[:1]), dict(scale=0.0), dict(scale=-1.0), dict(out=q.float()), dict(k_pool=kp[:, :1])):
+        with pytest.raises(ValueError):
+            b.attention(**{**dict(q=good, k_pool=kp, v_pool=vp), **bad})
+    assert status(lambda: b.append_rope(s.Rope(128), q, k, v, kp, vp)) == s.EINVAL  # another head width
+    assert status(lambda: b.append_rope(rope, q, k, v, kp, vp, eps=-1.0)) == s.EINVAL
+    assert status(lambda: b.append_rope(rope, q, k, v, kp, vp, out_q=x[:, 2:6])) == s.EINVAL      # out on the keys
+    assert status(lambda: b.append_rope(rope, q, kp.view(-1, 2, 64)[:T], v, kp, vp)) == s.EINVAL  # keys inside the pool
+    both = draw((2 * n, hkv, P * hd), 1)
+    assert status(lambda: b.append_rope(rope, q, k, v, both[:n].view(n, hkv, P, hd), both[1: n + 1].view(n, hkv, hd, P))) == s.EINVAL
+    assert status(lambda: b.attention(good, kp, vp, out=good)) == s.EINVAL          # not in place
+    assert status(lambda: b.attention(good, kp, vp, scale=float("inf"))) == s.EINVAL
+    odd = torch.empty(T * hq * hd + 8, dtype=torch.bfloat16, device=DEV)
+    assert status(lambda: b.attention(odd[1: 1 + T * hq * hd].view(T, hq, hd), kp, vp)) == s.EINVAL
+    assert status(lambda: b.attention(good, kp, vp, out=odd[2: 2 + T * hq * hd].view(T, hq, hd))) == s.EINVAL
+    assert torch.equal(b.attention(good, kp, vp), o)
