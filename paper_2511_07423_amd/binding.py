@@ -1,6 +1,7 @@
 """ctypes binding with the same entry points as include/synera.h (marshalling only)."""
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -124,20 +125,17 @@ class _RopeDesc(C.Structure):
                 ("original", C.c_double), ("magnitude", C.c_double), ("h_inv_freq", C.POINTER(C.c_double))]
 
 
-class _Heads(C.Structure):
-    _fields_ = [("d_in", _vp), ("d_out", _vp), ("d_gain", _vp), ("n_heads", C.c_int32), ("in_token", C.c_int64),
-                ("in_head", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64)]
-
-
-_headsp = C.POINTER(_Heads)
+# synera_heads as bytes: d_in, d_out, d_gain, n_heads, strides in and out of tokens and heads.  (Filling a ctypes structure field
+# by field, and asking torch for the stream object, took longer than the kernels of a decoding step.)
+_pack_heads = struct.Struct("@PPPi4xqqqq").pack
 _lib.synera_rope_create.restype = C.c_int32
 _lib.synera_rope_create.argtypes = [C.POINTER(_vp), C.POINTER(_RopeDesc)]
 _lib.synera_rope_destroy.restype = C.c_int32
 _lib.synera_rope_destroy.argtypes = [_vp]
 _lib.synera_rope_apply.restype = C.c_int32
-_lib.synera_rope_apply.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _headsp, _headsp, _vp]
+_lib.synera_rope_apply.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _vp, _vp, _vp]
 _lib.synera_qk_norm_rope.restype = C.c_int32
-_lib.synera_qk_norm_rope.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _headsp, _headsp, C.c_float, _vp]
+_lib.synera_qk_norm_rope.argtypes = [_vp, C.c_int32, C.c_int64, _vp, _vp, _vp, C.c_float, _vp]
 _lib.synera_batch_create.restype = C.c_int32
 _lib.synera_batch_create.argtypes = [C.POINTER(_vp)] + [C.c_int32] * 6
 _lib.synera_batch_destroy.restype = C.c_int32
@@ -147,9 +145,9 @@ _lib.synera_validate_shared.argtypes = [C.c_int32, _i32p, _i32p, _i32p, C.c_int3
 _lib.synera_batch_plan.restype = C.c_int32
 _lib.synera_batch_plan.argtypes = [_vp, C.c_int32, _i32p, _i32p, _i32p, C.c_int32, C.c_int32, _vp]
 _lib.synera_append_rope.restype = C.c_int32
-_lib.synera_append_rope.argtypes = [_vp, _vp, C.c_int32, _headsp, _headsp, _headsp, C.c_float, _vp, _vp, _vp]
+_lib.synera_append_rope.argtypes = [_vp, _vp, C.c_int32, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
 _lib.synera_shared_attention.restype = C.c_int32
-_lib.synera_shared_attention.argtypes = [_vp, _headsp, _vp, _vp, C.c_float, _vp, _vp]
+_lib.synera_shared_attention.argtypes = [_vp, _vp, _vp, _vp, C.c_float, _vp, _vp]
 _lib.synera_debug_shared_plan.restype = C.c_int32
 _lib.synera_debug_shared_plan.argtypes = [C.c_int32] * 5 + [_i32p] * 3 + [C.c_int32] * 2 + [_i32p, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
 
@@ -581,27 +579,28 @@ _HEAD_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 
 
-def _heads(x, out, gain, device, name):
-    """The synera_heads of x and out, [tokens][heads][head_dim] with the values of a head side by side."""
-    for t in (x, out):
-        if t is not None and (t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1) or t.device != device):
-            raise ValueError(f"{name}: expected [tokens, heads, head_dim] on {device}, the values of a head side by side")
-    if out is not None and out.shape != x.shape:
-        raise ValueError(f"{name}: the output's shape is {tuple(out.shape)}, the input's {tuple(x.shape)}")
-    if gain is not None and (gain.dtype != torch.bfloat16 or gain.shape != x.shape[2:] or not gain.is_contiguous() or gain.device != device):
-        raise ValueError(f"{name}: gains are bf16 [head_dim] on {device}")
-    o = x if out is None else out
-    return _Heads(x.data_ptr(), None if out is None else out.data_ptr(), None if gain is None else gain.data_ptr(), x.shape[1],
-                  x.stride(0), x.stride(1), o.stride(0), o.stride(1))
+def _raw_stream(index):
+    """The current stream of a device, as _stream() without the object around it."""
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _on(device, *tensors):
-    """Refuses tensors that are elsewhere than the handle, and a handle that is elsewhere than the current device."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the handle belongs to {device}, the current device is cuda:{torch.cuda.current_device()}")
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"expected tensors on {device}, got one on {t.device}")
+def _heads(x, out, gain, index, name):
+    """The synera_heads of x and out (or None), [tokens][heads][head_dim] with the values of a head side by side."""
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or (strides[2] != 1 and shape[2] > 1) or x.get_device() != index:
+        raise ValueError(f"{name}: expected [tokens, heads, head_dim] on cuda:{index}, the values of a head side by side")
+    at_out, out_strides = 0, strides
+    if out is not None:
+        out_strides = out.stride()
+        if out.shape != shape or (out_strides[2] != 1 and shape[2] > 1) or out.get_device() != index:
+            raise ValueError(f"{name}: the output is a tensor on cuda:{index} of the input's shape {tuple(shape)}, the values of a head side by side")
+        at_out = out.data_ptr()
+    at_gain = 0
+    if gain is not None:
+        if gain.dtype != torch.bfloat16 or gain.shape != shape[2:] or not gain.is_contiguous() or gain.get_device() != index:
+            raise ValueError(f"{name}: gains are bf16 [head_dim] on cuda:{index}")
+        at_gain = gain.data_ptr()
+    return _pack_heads(x.data_ptr(), at_out, at_gain, shape[1], strides[0], strides[1], out_strides[0], out_strides[1])
 
 
 class Rope:
@@ -627,6 +626,7 @@ class Rope:
         _check(_lib.synera_rope_create(C.byref(self._h), C.byref(desc)), "synera_rope_create")
         self.head_dim, self.rot_dim = head_dim, rot_dim
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
@@ -639,37 +639,43 @@ class Rope:
         except Exception:
             pass
 
-    def _turn(self, pos, q, k, gains, eps, out_q, out_k):
-        _on(self.device, pos, q, k)
-        if pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous():
-            raise ValueError("positions are a contiguous int32 vector")
-        both = [(q, out_q, "q")] + ([] if k is None else [(k, out_k, "k")])
-        heads, outs = [], []
-        for (x, out, name), gain in zip(both, gains):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-            if x.dtype not in _HEAD_TYPES or x.dtype != q.dtype or out.dtype != x.dtype:
-                raise ValueError(f"{name}: f32, bf16 or f16, one type for all: got {x.dtype} -> {out.dtype}")
-            if x.dim() != 3 or x.shape[0] != pos.numel() or x.shape[2] != self.head_dim:
-                raise ValueError(f"{name}: expected [{pos.numel()}, heads, {self.head_dim}], got {tuple(x.shape)}")
-            heads.append(_heads(x, out, gain, self.device, name))
-            outs.append(out)
-        args = (self._h, _HEAD_TYPES[q.dtype], pos.numel(), pos.data_ptr(), C.byref(heads[0]), C.byref(heads[1]) if k is not None else None)
+    def _one(self, x, out, gain, dtype, n, name):
+        if x.dtype != dtype or x.dim() != 3 or x.shape[0] != n or x.shape[2] != self.head_dim:
+            raise ValueError(f"{name}: expected {dtype} [{n}, heads, {self.head_dim}], got {x.dtype} {tuple(x.shape)}")
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        elif out.dtype != dtype:
+            raise ValueError(f"{name}: the output's type is the input's, {dtype}: got {out.dtype}")
+        return _heads(x, out, gain, self._index, name), out
+
+    def _turn(self, pos, q, k, q_gain, k_gain, eps, out_q, out_k):
+        if pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous() or pos.get_device() != self._index:
+            raise ValueError(f"positions are a contiguous int32 vector on {self.device}")
+        dtype, n = q.dtype, pos.numel()
+        if dtype not in _HEAD_TYPES:
+            raise ValueError(f"f32, bf16 or f16: got {dtype}")
+        hq, out_q = self._one(q, out_q, q_gain, dtype, n, "q")
+        hk = None
+        if k is not None:
+            hk, out_k = self._one(k, out_k, k_gain, dtype, n, "k")
         if eps is None:
-            _check(_lib.synera_rope_apply(*args, _stream()), "synera_rope_apply")
+            st = _lib.synera_rope_apply(self._h, _HEAD_TYPES[dtype], n, pos.data_ptr(), hq, hk, _raw_stream(self._index))
+            _check(st, "synera_rope_apply")
         else:
-            _check(_lib.synera_qk_norm_rope(*args, float(eps), _stream()), "synera_qk_norm_rope")
-        return outs[0], (outs[1] if k is not None else None)
+            st = _lib.synera_qk_norm_rope(self._h, _HEAD_TYPES[dtype], n, pos.data_ptr(), hq, hk, eps, _raw_stream(self._index))
+            _check(st, "synera_qk_norm_rope")
+        return out_q, out_k if k is not None else None
 
     def apply(self, pos, q, k=None, out_q=None, out_k=None):
         """q [T, Hq, head_dim] and k [T, Hk, head_dim] (or None) turned by their positions (int32 [T]) -> (q, k), new tensors
         unless out_q / out_k are given (q and k themselves for in place)."""
-        return self._turn(pos, q, k, (None, None), None, out_q, out_k)
+        return self._turn(pos, q, k, None, None, None, out_q, out_k)
 
     def norm_apply(self, pos, q, k, q_gain, k_gain, eps, out_q=None, out_k=None):
         """The same behind an RMS norm of each head with bf16 gains [head_dim]."""
         if q_gain is None or (k is not None and k_gain is None):
             raise ValueError("norm_apply needs the gains")
-        return self._turn(pos, q, k, (q_gain, k_gain), eps, out_q, out_k)
+        return self._turn(pos, q, k, q_gain, k_gain, eps, out_q, out_k)
 
 
 def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max_tokens):
@@ -692,7 +698,9 @@ class SharedBatch:
                "synera_batch_create")
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.n_tokens = self.n_pages = 0
+        self._tiles = (n_kv_heads, PAGE_SIZE, head_dim), (n_kv_heads, head_dim, PAGE_SIZE)
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
@@ -711,59 +719,61 @@ class SharedBatch:
         (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
         if bt.ndim != 2 or len(ctx) != len(new) or len(bt) != len(ctx):
             raise ValueError("ctx_len, n_new and the rows of block_table belong together")
-        _on(self.device)
-        _check(_lib.synera_batch_plan(self._h, len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool, _stream()),
-               "synera_batch_plan")
+        _check(_lib.synera_batch_plan(self._h, len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool,
+                                      _raw_stream(self._index)), "synera_batch_plan")
         self.n_tokens, self.n_pages = int(new.sum()), n_pages_in_pool
 
-    def _pools(self, k_pool, v_pool):
-        shape = (self.n_kv_heads, PAGE_SIZE, self.head_dim)
-        for t, want in ((k_pool, shape), (v_pool, (shape[0], shape[2], shape[1]))):
-            if t.dtype != torch.bfloat16 or t.device != self.device or not t.is_contiguous() or t.dim() != 4 or \
-                    tuple(t.shape[1:]) != want or t.shape[0] < self.n_pages:
-                raise ValueError(f"expected one layer's pool, bf16 [>= {self.n_pages}, {want[0]}, {want[1]}, {want[2]}] on {self.device}, contiguous")
-        return k_pool.data_ptr(), v_pool.data_ptr()
+    def _pool(self, pool, tile):
+        shape = pool.shape
+        if pool.dtype != torch.bfloat16 or len(shape) != 4 or shape[1:] != tile or shape[0] < self.n_pages or not pool.is_contiguous() or \
+                pool.get_device() != self._index:
+            raise ValueError(f"expected one layer's pool, bf16 [>= {self.n_pages}, {tile[0]}, {tile[1]}, {tile[2]}] on {self.device}, contiguous")
+        return pool.data_ptr()
 
-    def _rows(self, x, heads, name):
-        if x.dim() != 3 or x.shape[0] < self.n_tokens or x.shape[1:] != (heads, self.head_dim):
-            raise ValueError(f"{name}: expected [>= {self.n_tokens}, {heads}, {self.head_dim}], got {tuple(x.shape)}")
+    def _rows(self, x, dtype, heads, name):
+        shape = x.shape
+        if x.dtype != dtype or len(shape) != 3 or shape[0] < self.n_tokens or shape[1] != heads or shape[2] != self.head_dim:
+            raise ValueError(f"{name}: expected {dtype} [>= {self.n_tokens}, {heads}, {self.head_dim}], got {x.dtype} {tuple(shape)}")
 
     def append_rope(self, rope, q, k, v, k_pool, v_pool, q_gain=None, k_gain=None, eps=1e-5, out_q=None):
         """One layer's new tokens (rows of q, k, v in the batch's order; f32, bf16 or f16): keys turned (and normed, with k_gain)
         into their pages, values into theirs, queries turned into out_q (bf16, new if None) -> out_q; q may be None."""
-        _on(self.device, q, k, v)
-        if rope.device != self.device:
-            raise ValueError(f"the rope belongs to {rope.device}")
-        if k.dtype not in _HEAD_TYPES or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
-            raise ValueError("f32, bf16 or f16, one type for q, k and v")
-        self._rows(k, self.n_kv_heads, "k")
-        self._rows(v, self.n_kv_heads, "v")
+        dtype = k.dtype
+        if dtype not in _HEAD_TYPES:
+            raise ValueError(f"f32, bf16 or f16: got {dtype}")
+        self._rows(k, dtype, self.n_kv_heads, "k")
+        self._rows(v, dtype, self.n_kv_heads, "v")
         hq = None
         if q is not None:
-            self._rows(q, self.n_q_heads, "q")
-            out_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out_q is None else out_q
-            if out_q.dtype != torch.bfloat16:
+            self._rows(q, dtype, self.n_q_heads, "q")
+            if out_q is None:
+                out_q = torch.empty_like(q, dtype=torch.bfloat16, memory_format=torch.contiguous_format)
+            elif out_q.dtype != torch.bfloat16:
                 raise ValueError("out_q is bf16")
-            hq = _heads(q, out_q, q_gain, self.device, "q")
-        hk, hv = _heads(k, None, k_gain, self.device, "k"), _heads(v, None, None, self.device, "v")
-        _check(_lib.synera_append_rope(self._h, rope._h, _HEAD_TYPES[k.dtype], C.byref(hq) if hq is not None else None, C.byref(hk),
-                                       C.byref(hv), float(eps), *self._pools(k_pool, v_pool), _stream()), "synera_append_rope")
+            hq = _heads(q, out_q, q_gain, self._index, "q")
+        st = _lib.synera_append_rope(self._h, rope._h, _HEAD_TYPES[dtype], hq, _heads(k, None, k_gain, self._index, "k"),
+                                     _heads(v, None, None, self._index, "v"), eps, self._pool(k_pool, self._tiles[0]),
+                                     self._pool(v_pool, self._tiles[1]), _raw_stream(self._index))
+        _check(st, "synera_append_rope")
         return out_q
 
     def attention(self, q, k_pool, v_pool, scale=None, out=None, want_lse=False):
         """softmax(scale q K^T) V of one layer over the planned batch: q bf16 [T, Hq, head_dim], turned; scale None: 1/sqrt(head_dim)
         -> o bf16 (out, new if None), or (o, lse f32 [T, Hq])."""
-        _on(self.device, q, out)
-        self._rows(q, self.n_q_heads, "q")
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out is None else out
-        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
-            raise ValueError("q and out are bf16")
+        self._rows(q, torch.bfloat16, self.n_q_heads, "q")
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        elif out.dtype != torch.bfloat16:
+            raise ValueError("out is bf16")
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
-        if scale is not None and not scale > 0:
+        if scale is None:
+            scale = 0.0
+        elif not scale > 0:
             raise ValueError("scale is positive")
-        h = _heads(q, out, None, self.device, "q")
-        _check(_lib.synera_shared_attention(self._h, C.byref(h), *self._pools(k_pool, v_pool), 0.0 if scale is None else float(scale),
-                                            None if lse is None else lse.data_ptr(), _stream()), "synera_shared_attention")
+        st = _lib.synera_shared_attention(self._h, _heads(q, out, None, self._index, "q"), self._pool(k_pool, self._tiles[0]),
+                                          self._pool(v_pool, self._tiles[1]), scale, lse.data_ptr() if want_lse else None,
+                                          _raw_stream(self._index))
+        _check(st, "synera_shared_attention")
         return (out, lse) if want_lse else out
 
 

@@ -51,7 +51,7 @@ def test_batch_limits(args, status):
 
 
 def test_null_handles():
-    lib, one = b._lib, C.byref(b._Heads(16, 16, None, 1, 64, 64, 64, 64))
+    lib, one = b._lib, b._pack_heads(16, 16, 0, 1, 64, 64, 64, 64)
     table, n = np.zeros((1, 1), np.int32), np.ones(1, np.int32)
     p = lambda a: a.ctypes.data_as(C.POINTER(C.c_int32))                                   # noqa: E731
     assert lib.synera_rope_apply(None, 0, 1, 16, one, None, None) == s.EINVAL
