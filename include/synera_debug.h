@@ -136,18 +136,22 @@ int32_t synera_debug_attention_plan(const synera_model_desc* desc, int32_t attn_
 
 /*
  * Test hook, host only: what synera_batch_plan would upload for one batch (not validated here) on a chip that runs `slots`
- * blocks at once.  `which` picks a region: 0 header (tokens, page windows, attention items, tokens with several partial results,
- * 0 ..), 1 positions, 2 page x 16 + slot, 3 windows [n][4] = page, first token, slots from, to, 4 items [n][16] = flags (1 = one
- * request's rows), KV head, rows, first row in the node, first token or entry of the token list, first page entry, pages, first
- * key, end of keys, last key the first token sees, partial row or -1, 0 .., 5 token list, 6 page list, 7 tokens to be joined with
- * their requests, 8 first entry of each request, 9 first token of each request, 10 entries [n][8] = partial row, row in the node,
- * rows of the node, keys, keys of a split, last key the first token sees or -1, 0, 0.
+ * blocks at once.  `which` picks a region: 0 header (tokens, page windows, tokens with several partial results, groups of 8 items that a
+ * block takes each, groups of 32 that a wavefront takes each, 0 ..), 1 positions, 2 page x 16 + slot, 3 windows [n][4] = page, first
+ * token, slots from, to, 4 items [n][32] = flags (1 = one request's rows), KV head, rows, first row in the node, first token or entry
+ * of the token list, first page entry, pages, first key, end of keys, last key the first token sees, partial row or -1, 0 .., the 16
+ * pages from the first key on, 5 token list, 6 page list, 7 tokens with several partial results [n][4] = token, first entry of the list,
+ * entries, 0, 8 that list [n][2] = partial row of head 0, step to the next KV head's.
  * n_words: size of the region, in 32-bit words; h_out: the region (ENOSPC where cap words are too few); limits (or NULL) [7]: room
- * for items, list, entries, pages, windows, partial rows, rows of shared nodes.  Errors: EINVAL, ENOSPC, ENOMEM.
+ * for items, list, partial results, pages, windows, partial rows, rows of shared nodes.  Errors: EINVAL, ENOSPC, ENOMEM.
  */
 int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t slots, int32_t max_tokens, int32_t B,
                                  const int32_t* h_ctx_len, const int32_t* h_n_new, const int32_t* h_block_table, int32_t max_pages,
                                  int32_t which, int32_t* h_out, int64_t cap, int64_t* n_words, int64_t* limits);
+
+/* Test hook, host only: the item (of a plan with that many groups, `run` groups of a kind in a row) that block `block` of the launch takes,
+ * or the first of its wavefronts' four.  Errors: EINVAL. */
+int32_t synera_debug_shared_block(int32_t block_groups, int32_t wave_groups, int32_t run, int32_t block, int32_t* item);
 
 /*
  * Tuning hook: the constants of the attention share planner of one context, for sweeps.  attn_blocks:

@@ -148,6 +148,8 @@ _lib.synera_append_rope.restype = C.c_int32
 _lib.synera_append_rope.argtypes = [_vp, _vp, C.c_int32, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
 _lib.synera_shared_attention.restype = C.c_int32
 _lib.synera_shared_attention.argtypes = [_vp, _vp, _vp, _vp, C.c_float, _vp, _vp]
+_lib.synera_debug_shared_block.restype = C.c_int32
+_lib.synera_debug_shared_block.argtypes = [C.c_int32] * 4 + [_i32p]
 _lib.synera_debug_shared_plan.restype = C.c_int32
 _lib.synera_debug_shared_plan.argtypes = [C.c_int32] * 5 + [_i32p] * 3 + [C.c_int32] * 2 + [_i32p, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
 
@@ -777,13 +779,13 @@ class SharedBatch:
         return (out, lse) if want_lse else out
 
 
-_SHARED_REGIONS = {"head": (0, 16), "pos": (1, 1), "slot": (2, 1), "windows": (3, 4), "items": (4, 16), "list": (5, 1), "pages": (6, 1),
-                   "joined": (7, 2), "first_entry": (8, 1), "req_tok": (9, 1), "entries": (10, 8)}
+_SHARED_REGIONS = {"head": (0, 16), "pos": (1, 1), "slot": (2, 1), "windows": (3, 4), "items": (4, 32), "list": (5, 1), "pages": (6, 1),
+                   "joined": (7, 4), "parts": (8, 2)}
 
 
 def debug_shared_plan(n_q_heads, n_kv_heads, slots, ctx_len, n_new, block_table, max_tokens=None):
     """Test hook (host only): what SharedBatch.plan uploads for one batch -> dict of int32 arrays, and "limits" (room for items, list,
-    entries, pages, windows, partial rows, rows of shared nodes)."""
+    partial results, pages, windows, partial rows, rows of shared nodes)."""
     (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
     bt = np.ascontiguousarray(block_table, dtype=np.int32)
     limits = (C.c_int64 * 7)()
@@ -800,6 +802,13 @@ def debug_shared_plan(n_q_heads, n_kv_heads, slots, ctx_len, n_new, block_table,
         out[name] = words.reshape(-1, width) if width > 1 else words
     out["limits"] = list(limits)
     return out
+
+
+def debug_shared_block(block_groups, wave_groups, run, block):
+    """Test hook (host only): (item that a block of the attention's launch takes, whether the whole block takes it)."""
+    at = C.c_int32(0)
+    _check(_lib.synera_debug_shared_block(block_groups, wave_groups, run, block, C.byref(at)), "synera_debug_shared_block")
+    return at.value, at.value < 8 * block_groups
 
 
 # ---------------------------------------------------------------------------------- scheduler (host only)

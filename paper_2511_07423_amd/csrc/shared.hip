@@ -16,7 +16,7 @@
 #define SH_CONST_AS __attribute__((address_space(4)))
 
 // ------------------------------------------------------------------------------------ the handle
-enum { R_HEAD, R_POS, R_SLOT, R_WIN, R_ITEM, R_LIST, R_PAGE, R_JOINED, R_FIRST, R_REQ, R_ENTRY, N_REGIONS };
+enum { R_HEAD, R_POS, R_SLOT, R_WIN, R_ITEM, R_LIST, R_PAGE, R_JOINED, R_PARTS, N_REGIONS };
 
 struct synera_batch {
   ShLimits lim;
@@ -77,17 +77,15 @@ extern "C" int32_t synera_batch_create(synera_batch** out, int32_t n_q_heads, in
   l.max_pages = max_pages;
   l.slots = 2 * std::max(1, prop.multiProcessorCount);
   sh_limits(l);
-  const size_t T = (size_t)max_tokens, B = (size_t)max_batch;
+  const size_t T = (size_t)max_tokens;
   b->room[R_HEAD] = sizeof(ShHeader);
   b->room[R_POS] = b->room[R_SLOT] = T * 4;
   b->room[R_WIN] = (size_t)l.windows * sizeof(ShWindow);
   b->room[R_ITEM] = (size_t)l.items * sizeof(ShItem);
   b->room[R_LIST] = (size_t)l.list * 4;
   b->room[R_PAGE] = (size_t)l.pages * 4;
-  b->room[R_JOINED] = T * 8;
-  b->room[R_FIRST] = (B + 1) * 4;
-  b->room[R_REQ] = B * 4;
-  b->room[R_ENTRY] = (size_t)l.entries * sizeof(ShEntry);
+  b->room[R_JOINED] = T * sizeof(ShJoin);
+  b->room[R_PARTS] = (size_t)l.parts * sizeof(ShPart);
   size_t off = 0;
   for (int r = 0; r < N_REGIONS; ++r) {
     b->at[r] = off;
@@ -158,14 +156,11 @@ extern "C" int32_t synera_batch_plan(synera_batch* b, int32_t B, const int32_t* 
     return SYNERA_ENOMEM;
   }
   const void* from[N_REGIONS] = {&p.head, p.tok_pos.data(), p.tok_slot.data(), p.windows.data(), p.items.data(), p.list.data(),
-                                 p.pages.data(), p.joined.data(), p.first_entry.data(), p.req_tok.data(), p.entries.data()};
+                                 p.pages.data(), p.joined.data(), p.parts.data()};
   const size_t bytes[N_REGIONS] = {sizeof(ShHeader), p.tok_pos.size() * 4, p.tok_slot.size() * 4, p.windows.size() * sizeof(ShWindow),
-                                   p.items.size() * sizeof(ShItem), p.list.size() * 4, p.pages.size() * 4, p.joined.size() * 4,
-                                   p.first_entry.size() * 4, p.req_tok.size() * 4, p.entries.size() * sizeof(ShEntry)};
-  int64_t part_rows = 0;
-  for (const ShItem& it : p.items)
-    if (it.part >= 0) part_rows = std::max<int64_t>(part_rows, (int64_t)it.part + it.n_rows);
-  bool room = part_rows <= l.part_rows;
+                                   p.items.size() * sizeof(ShItem), p.list.size() * 4, p.pages.size() * 4, p.joined.size() * sizeof(ShJoin),
+                                   p.parts.size() * sizeof(ShPart)};
+  bool room = p.part_rows <= l.part_rows;
   for (int r = 0; r < N_REGIONS; ++r) room = room && bytes[r] <= b->room[r];
   if (!room) return SYNERA_ENOMEM;                  // (the capacities cover every plan: sh_limits)
   const int slot = (int)(b->plans % SH_STAGES);
@@ -416,15 +411,15 @@ struct SharedAttnArgs {
   const ShItem* items;
   const int32_t* list;
   const int32_t* pages;
-  const int32_t* joined;
-  const int32_t* first_entry;
-  const int32_t* req_tok;
-  const ShEntry* entries;
+  const ShJoin* joined;
+  const ShPart* parts;
   float* part_o;
   float2* part_ml;
   float* lse;
   float c;                     // scale x log2 e
   int32_t Hq, Hkv, G;
+  int32_t run;                 // groups of blocks of a kind in a row (sh_block)
+  int32_t block_groups, wave_groups;   // the plan's, or -1: read on the device (graphs, which serve other plans too)
 };
 
 typedef __attribute__((ext_vector_type(8))) int sh_i32x8v;
@@ -436,10 +431,22 @@ __device__ __forceinline__ float other_half(float v) {      // of lane l ^ 32
   return __uint_as_float((threadIdx.x & 32) ? a[0] : a[1]);
 }
 
-// copy_to_lds (common.h) from a base in scalar registers and each lane's own offset in bytes
-__device__ __forceinline__ void copy_page_piece(const bf16_t* base, uint32_t off, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(base) : "memory", "m0");
+// Asynchronous copies of N kilobytes, global -> LDS (16 bytes a lane; lane i of kilobyte j lands at lds_addr + 1024 j + 16 i), from a
+// base in scalar registers and each lane's own offsets.  An instruction's offset counts on both sides.
+template <int N>
+__device__ __forceinline__ void copy_page(const bf16_t* base, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3, uint32_t lds_addr) {
+  if constexpr (N == 4)
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds_addr),
+        "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base)
+        : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds_addr),
+                 "v"(o0), "v"(o1), "s"(base)
+                 : "memory", "m0");
 }
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
 // At most `n` positions of IPP copies may still be on their way, and this wavefront's LDS reads are done.
 template <int IPP>
@@ -453,17 +460,19 @@ __device__ __forceinline__ void wait_positions(int n) {
 template <int HD>
 __device__ __forceinline__ int sh_swz(int slot) { return HD == 128 ? slot : slot >> 1; }
 
-template <int HD, int WR>      // WR wavefronts share keys and split the rows, 4 / WR groups of them split the keys
-__device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it, unsigned char* lds) {
-  constexpr int WK = 4 / WR, NT = 5, PPT = 4 / WR;            // key groups; slots of a ring; positions of a tile (K a, K b, V a, V b)
+// WR wavefronts share keys and split the rows, WK groups of them split the keys; WR WK == 1: the wavefront has an item of its own.
+template <int HD, int WR, int WK>
+__device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it, const int32_t* first_pages, unsigned char* lds) {
+  constexpr int NT = 5, PPT = 4 / WR;                         // slots of a ring; positions of a tile (K a, K b, V a, V b)
   constexpr int PAGE_B = SY_PAGE * HD * 2, SLOT_B = WR * PAGE_B, RING_B = NT * SLOT_B, IPP = PAGE_B / 1024;
   constexpr int KS = HD / 16, DB = HD / 32;
-  const int lane = threadIdx.x & 63, n32 = lane & 31, h = lane >> 5;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));                              // (what follows from it is formed for each item, not kept for all of them)
+  const int n32 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave % WR, kp = wave / WR;
+  const int wr = wave % WR, kp = WK == 1 ? 0 : wave / WR;
   const bool leaf = (it.flags & SY_SH_LEAF) != 0;
-  unsigned char* ring = lds + kp * RING_B;
-  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)ring;
+  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds + wave / WR * RING_B;
 
   // ---- keys
   const int n_tiles = (it.key_end - it.key_begin + 31) / 32;
@@ -472,36 +481,37 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   const SH_CONST_AS int32_t* pages = reinterpret_cast<const SH_CONST_AS int32_t*>((uintptr_t)(a.pages + it.page));
   const int page0 = it.key_begin / SY_PAGE;
   const size_t page_elems = (size_t)a.Hkv * SY_PAGE * HD, head_at = (size_t)it.kv_head * SY_PAGE * HD;
-  uint32_t k_off[IPP], v_off[IPP];                            // bytes
-#pragma unroll
-  for (int j = 0; j < IPP; ++j) {
-    const int slot = j * (16 / IPP) + lane / (HD / 8);
-    k_off[j] = slot * HD * 2 + ((lane % (HD / 8)) ^ sh_swz<HD>(slot)) * 16;
-    const int at = j * 64 + lane, dim = at >> 1;
-    v_off[j] = (dim * 2 + ((at & 1) ^ ((dim >> 3) & 1))) * 16;
-  }
+  // K: 16-byte chunks swizzled by slot (kilobyte j holds 16 / IPP slots on, whose number changes bits 6 and 7 of the offset); V: the
+  // 16-byte halves of every second group of 8 dims swapped.  (What follows from one register is formed again in each iteration:
+  // kept, it was spilled.)
+  const int c_slot = lane / (HD / 8);
+  uint32_t k_off = c_slot * HD * 2 + ((lane % (HD / 8)) ^ sh_swz<HD>(c_slot)) * 16;
+  const uint32_t v_off = ((lane >> 1) * 2 + ((lane & 1) ^ ((lane >> 4) & 1))) * 16;
   // position p of the ring: pages p WR .. p WR + WR - 1 of the sequence K a, K b, V a, V b of tile 0, of tile 1, ...; this wavefront
   // copies one of them
   auto page_of = [&](int p) {
     const int s = min(p, n_pos - 1) * WR + wr;
     return pages[min(page0 + 2 * ((s >> 2) * WK + kp) + (s & 1), it.n_pages - 1)];
   };
+  const SH_CONST_AS int32_t* near = reinterpret_cast<const SH_CONST_AS int32_t*>((uintptr_t)first_pages);
+  auto first_page_of = [&](int p) {                           // of the prologue's positions: at most page 15 from key_begin on
+    const int s = p * WR + wr;
+    return near[2 * ((s >> 2) * WK + kp) + (s & 1)];
+  };
   auto issue = [&](int p, int32_t page) {
-    const uint32_t to = ring_at + (uint32_t)(p % NT) * SLOT_B + wr * PAGE_B;
+    const uint32_t to = ring + (uint32_t)(p % NT) * SLOT_B + wr * PAGE_B;
+    const size_t at = (size_t)page * page_elems + head_at;
     if (((p * WR + wr) & 2) == 0) {
-      const bf16_t* from = a.k_layer + (size_t)page * page_elems + head_at;
-#pragma unroll
-      for (int j = 0; j < IPP; ++j) copy_page_piece(from, k_off[j], to + j * 1024);
+      asm volatile("" : "+v"(k_off));
+      copy_page<IPP>(a.k_layer + at, k_off, k_off ^ 64, k_off ^ 128, k_off ^ 192, to);
     } else {
-      const bf16_t* from = a.v_layer + (size_t)page * page_elems + head_at;
-#pragma unroll
-      for (int j = 0; j < IPP; ++j) copy_page_piece(from, v_off[j], to + j * 1024);
+      copy_page<IPP>(a.v_layer + at, v_off, v_off, v_off, v_off, to);
     }
   };
   constexpr int AHEAD = WR == 1 ? NT : NT - PPT;              // positions on their way when the loop begins
 #pragma unroll
   for (int p = 0; p < AHEAD; ++p)
-    if (p < n_pos) issue(p, page_of(p));
+    if (p < n_pos) issue(p, first_page_of(p));
 
   // ---- rows
   const int row = wr * 32 + n32;
@@ -514,6 +524,10 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
 #pragma unroll
   for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(a.q + (int64_t)tok * a.q_ts + (int64_t)head * a.q_hs + 16 * s + 8 * h);
 
+  // All of that has arrived before the loop begins: a load that the compiler has not seen waited for there it would wait for inside,
+  // each time, and for the copies with it.
+  __builtin_amdgcn_s_waitcnt(0x0F70);                         // vmcnt(0)
+
   const float c = a.c;
   float m = c > 1.f ? -3e38f / c : -3e38f, l = 0.f;           // m in units of the raw scores; m c stays finite
   f32x16 acc[DB];
@@ -522,22 +536,26 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
 
-  // where this lane reads its K rows and V rows inside a page
+  // where this lane reads its K rows (of two pages, behind each other but in the rings of single pages) and V rows
   const int kslot = (n32 & 3) | ((n32 >> 2) & 1) << 3 | ((n32 >> 3) & 1) << 2;
-  const int v_at = n32 * 32 + (h ^ ((n32 >> 3) & 1)) * 16;
+  uint32_t k_at = (WR == 1 ? 0 : (n32 >> 4) * PAGE_B) + kslot * HD * 2 + ((h ^ sh_swz<HD>(kslot)) << 4);
+  const uint32_t v_at = n32 * 32 + (h ^ ((n32 >> 3) & 1)) * 16;
   bf16x8 kf[KS], vf[DB][2];
   // page `part` of tile i (of this group) in the ring
-  auto page_at = [&](int i, int part) { const int s = 4 * i + part; return ring + (s / WR % NT) * SLOT_B + (s % WR) * PAGE_B; };
+  auto page_at = [&](int i, int part) { const int s = 4 * i + part; return ring + (uint32_t)((s / WR % NT) * SLOT_B + (s % WR) * PAGE_B); };
   auto read_k = [&](int i) {
-    const unsigned char* at = ((n32 >> 4) ? page_at(i, 1) : page_at(i, 0)) + kslot * (HD * 2);
+    asm volatile("" : "+v"(k_at));
+    const uint32_t at = k_at + (WR == 1 ? ((n32 >> 4) ? page_at(i, 1) : page_at(i, 0)) : page_at(i, 0));
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(at + (((2 * s + h) ^ sh_swz<HD>(kslot)) << 4));
+    for (int s = 0; s < KS; ++s) kf[s] = *(lds_bf16x8*)(uintptr_t)(at ^ (s << 5));      // chunk (2 s + h) ^ swizzle
   };
   auto read_v = [&](int i) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b) {
+      const uint32_t at = page_at(i, 2 + b) + v_at;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) vf[db][b] = *reinterpret_cast<const bf16x8*>(page_at(i, 2 + b) + db * 1024 + v_at);
+      for (int db = 0; db < DB; ++db) vf[db][b] = *(lds_bf16x8*)(uintptr_t)(at + db * 1024);
+    }
   };
   f32x16 sc;
   auto scores = [&]() {
@@ -619,6 +637,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
               t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[b], t, 0, 0, 0);
 #pragma unroll
               for (int r = 0; r < 16; ++r) acc[db][r] += seen ? t[r] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);              // one t at a time
             }
           }
         return;
@@ -738,81 +757,88 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   }
 }
 
+__device__ __forceinline__ ShItem item_of(const ShItem* p) {
+  const sh_i32x8* at = reinterpret_cast<const sh_i32x8*>((uintptr_t)p);
+  const sh_i32x8v w0 = at[0], w1 = at[1];
+  return ShItem{w0[0], w0[1], w0[2], w0[3], w0[4], w0[5], w0[6], w0[7], w1[0], w1[1], w1[2]};   // (its pages are looked up where they are)
+}
+
 template <int HD>
 __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int n = a.head->n_items;
+  const int block_groups = a.block_groups >= 0 ? a.block_groups : a.head->block_groups;
+  const int wave_groups = a.wave_groups >= 0 ? a.wave_groups : a.head->wave_groups;
+  const int n = (block_groups + wave_groups) * SY_SH_DEAL;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const sh_i32x8* at = reinterpret_cast<const sh_i32x8*>((uintptr_t)(a.items + i));
-    const sh_i32x8v w0 = at[0], w1 = at[1];
-    const ShItem it = {w0[0], w0[1], w0[2], w0[3], w0[4], w0[5], w0[6], w0[7], w1[0], w1[1], w1[2], {0, 0, 0, 0, 0}};
-    if (it.n_rows <= 32) attend<HD, 1>(a, it, lds);
-    else if (it.n_rows <= 64) attend<HD, 2>(a, it, lds);
-    else attend<HD, 4>(a, it, lds);
+    bool whole;
+    const ShItem* at = a.items + sh_block(block_groups, wave_groups, a.run, i, whole);
+    if (!whole) at += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const ShItem it = item_of(at);
+    if (it.n_rows > 0) {
+      if (!whole) attend<HD, 1, 1>(a, it, at->pages, lds);
+      else if (it.n_rows <= 32) attend<HD, 1, 4>(a, it, at->pages, lds);
+      else if (it.n_rows <= 64) attend<HD, 2, 2>(a, it, at->pages, lds);
+      else attend<HD, 4, 1>(a, it, at->pages, lds);
+    }
     __syncthreads();                                          // the next item's copies come into the same LDS
   }
 }
 
 // Joins the partial results of rows that several items worked on: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A thread takes four
-// values of one row; four partials are asked for together.
-#define JOIN_FLY 4
+// values of one row; JOIN_FLY partials are asked for together, behind two dependent loads.
+#define JOIN_FLY 8
 template <int HD>
-__global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a) {
-  const int n = a.head->n_joined;
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a, int n_joined) {
+  const int n = n_joined >= 0 ? n_joined : a.head->n_joined;
   const int piece = blockIdx.y * 256 + threadIdx.x;
   if (piece >= a.Hq * (HD / 4)) return;
   const int head = piece / (HD / 4), d4 = piece % (HD / 4) * 4, kh = head / a.G, g = head % a.G;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const int tok = a.joined[2 * i], req = a.joined[2 * i + 1];
-    const int r = (tok - a.req_tok[req]) * a.G + g;
+    const ShJoin jn = a.joined[i];
     float M = -3e38f, l = 0.f;
     float4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int e = a.first_entry[req]; e < a.first_entry[req + 1]; ++e) {
-      const ShEntry en = a.entries[e];
-      int keys = en.keys;
-      if (en.lim0 >= 0) {                                     // causal: splits beyond the last key that the row's tile sees were left out
-        const int last = min((en.row0 + r) / SY_SH_TILE_ROWS * SY_SH_TILE_ROWS + SY_SH_TILE_ROWS, en.rows) - 1;
-        keys = min(keys, en.lim0 + last / a.G + 1);
-      }
-      const int splits = (keys + en.chunk - 1) / en.chunk;
-      const size_t row = (size_t)en.base + (size_t)kh * en.rows + r, step = (size_t)en.rows * a.Hkv;
-      for (int s0 = 0; s0 < splits; s0 += JOIN_FLY) {
-        float2 ml[JOIN_FLY];
-        float4 v[JOIN_FLY];
+    for (int s0 = 0; s0 < jn.count; s0 += JOIN_FLY) {
+      float2 ml[JOIN_FLY];
+      float4 v[JOIN_FLY];
+      ShPart part[JOIN_FLY];
 #pragma unroll
-        for (int s = 0; s < JOIN_FLY; ++s) {
-          const size_t at = row + (size_t)min(s0 + s, splits - 1) * step;
-          ml[s] = a.part_ml[at];
-          v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
+      for (int s = 0; s < JOIN_FLY; ++s) part[s] = a.parts[jn.first + min(s0 + s, jn.count - 1)];
+#pragma unroll
+      for (int s = 0; s < JOIN_FLY; ++s) {
+        const size_t at = (size_t)part[s].row + (size_t)kh * part[s].step + g;
+        ml[s] = a.part_ml[at];
+        v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
+      }
+      float top = M;
+#pragma unroll
+      for (int s = 0; s < JOIN_FLY; ++s) top = fmaxf(top, ml[s].x);
+      const float f = sh_ex2(M - top);
+      M = top;
+      l *= f;
+      sum.x *= f; sum.y *= f; sum.z *= f; sum.w *= f;
+#pragma unroll
+      for (int s = 0; s < JOIN_FLY; ++s)
+        if (s0 + s < jn.count) {
+          const float w = sh_ex2(ml[s].x - M);
+          l += ml[s].y * w;
+          sum.x += v[s].x * w; sum.y += v[s].y * w; sum.z += v[s].z * w; sum.w += v[s].w * w;
         }
-#pragma unroll
-        for (int s = 0; s < JOIN_FLY; ++s)
-          if (s0 + s < splits) {
-            const float top = fmaxf(M, ml[s].x), f0 = sh_ex2(M - top), f1 = sh_ex2(ml[s].x - top);
-            M = top;
-            l = l * f0 + ml[s].y * f1;
-            sum.x = sum.x * f0 + v[s].x * f1;
-            sum.y = sum.y * f0 + v[s].y * f1;
-            sum.z = sum.z * f0 + v[s].z * f1;
-            sum.w = sum.w * f0 + v[s].w * f1;
-          }
-      }
     }
     const float inv = 1.0f / l;
-    *reinterpret_cast<uint2*>(a.o + (int64_t)tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
+    *reinterpret_cast<uint2*>(a.o + (int64_t)jn.tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
         make_uint2(pack_bf2(sum.x * inv, sum.y * inv), pack_bf2(sum.z * inv, sum.w * inv));
-    if (a.lse && d4 == 0) a.lse[(size_t)tok * a.Hq + head] = (M + __log2f(l)) * 0.69314718055994531f;
+    if (a.lse && d4 == 0) a.lse[(size_t)jn.tok * a.Hq + head] = (M + __log2f(l)) * 0.69314718055994531f;
   }
 }
 
 template <int HD>
-static hipError_t launch_shared(const SharedAttnArgs& a, int items, int joined, hipStream_t s) {
+static hipError_t launch_shared(const SharedAttnArgs& a, int blocks, int joined, hipStream_t s) {
   const size_t lds = (size_t)20 * SY_PAGE * HD * 2;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_attn_kernel<HD>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  if (items > 0) shared_attn_kernel<HD><<<items, 256, lds, s>>>(a);
+  if (blocks > 0) shared_attn_kernel<HD><<<blocks, 256, lds, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (joined > 0) shared_join_kernel<HD><<<dim3(joined, (a.Hq * (HD / 4) + 255) / 256), 256, 0, s>>>(a);
+  if (joined > 0) shared_join_kernel<HD><<<dim3(joined, (a.Hq * (HD / 4) + 255) / 256), 256, 0, s>>>(a, a.block_groups < 0 ? -1 : joined);
   return hipGetLastError();
 }
 
@@ -845,10 +871,8 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   a.items = b->region<ShItem>(R_ITEM);
   a.list = b->region<int32_t>(R_LIST);
   a.pages = b->region<int32_t>(R_PAGE);
-  a.joined = b->region<int32_t>(R_JOINED);
-  a.first_entry = b->region<int32_t>(R_FIRST);
-  a.req_tok = b->region<int32_t>(R_REQ);
-  a.entries = b->region<ShEntry>(R_ENTRY);
+  a.joined = b->region<ShJoin>(R_JOINED);
+  a.parts = b->region<ShPart>(R_PARTS);
   a.part_o = b->part_o;
   a.part_ml = b->part_ml;
   a.lse = d_lse;
@@ -857,9 +881,14 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   a.Hkv = l.Hkv;
   a.G = l.Hq / l.Hkv;
   // A captured call serves plans of any size: both launches are made, for as much as may come; the kernels loop.
-  const int items = graph ? std::max(b->plan.head.n_items, l.slots) : b->plan.head.n_items;
-  const int joined = graph ? std::min(l.max_tokens, std::max(b->plan.head.n_joined, l.slots)) : b->plan.head.n_joined;
-  const hipError_t e = l.hd == 128 ? launch_shared<128>(a, items, joined, s) : launch_shared<64>(a, items, joined, s);
+  const ShHeader& head = b->plan.head;
+  a.run = std::max(1, l.slots / 2 / SY_SH_DEAL);
+  a.block_groups = graph ? -1 : head.block_groups;
+  a.wave_groups = graph ? -1 : head.wave_groups;
+  int blocks = (head.block_groups + head.wave_groups) * SY_SH_DEAL;
+  if (graph) blocks = std::max(blocks, l.slots);
+  const int joined = graph ? std::min(l.max_tokens, std::max(head.n_joined, l.slots)) : head.n_joined;
+  const hipError_t e = l.hd == 128 ? launch_shared<128>(a, blocks, joined, s) : launch_shared<64>(a, blocks, joined, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
@@ -883,15 +912,15 @@ extern "C" int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_head
     l.slots = slots;
     sh_limits(l);
     if (limits) {
-      const int64_t v[7] = {l.items, l.list, l.entries, l.pages, l.windows, l.part_rows, l.shared_rows};
+      const int64_t v[7] = {l.items, l.list, l.parts, l.pages, l.windows, l.part_rows, l.shared_rows};
       std::memcpy(limits, v, sizeof v);
     }
     ShPlan p;
     sh_plan(l, B, h_ctx_len, h_n_new, h_block_table, max_pages, p);
     const void* from[N_REGIONS] = {&p.head, p.tok_pos.data(), p.tok_slot.data(), p.windows.data(), p.items.data(), p.list.data(),
-                                   p.pages.data(), p.joined.data(), p.first_entry.data(), p.req_tok.data(), p.entries.data()};
-    const size_t words[N_REGIONS] = {sizeof(ShHeader) / 4, p.tok_pos.size(), p.tok_slot.size(), p.windows.size() * 4, p.items.size() * 16,
-                                     p.list.size(), p.pages.size(), p.joined.size(), p.first_entry.size(), p.req_tok.size(), p.entries.size() * 8};
+                                   p.pages.data(), p.joined.data(), p.parts.data()};
+    const size_t words[N_REGIONS] = {sizeof(ShHeader) / 4, p.tok_pos.size(), p.tok_slot.size(), p.windows.size() * 4, p.items.size() * 32,
+                                     p.list.size(), p.pages.size(), p.joined.size() * 4, p.parts.size() * 2};
     if (which < 0 || which >= N_REGIONS) return SYNERA_EINVAL;
     *n_words = (int64_t)words[which];
     if ((int64_t)words[which] > cap) return SYNERA_ENOSPC;
@@ -900,4 +929,11 @@ extern "C" int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_head
   } catch (const std::bad_alloc&) {
     return SYNERA_ENOMEM;
   }
+}
+
+extern "C" int32_t synera_debug_shared_block(int32_t block_groups, int32_t wave_groups, int32_t run, int32_t block, int32_t* item) {
+  if (!item || block_groups < 0 || wave_groups < 0 || run < 1 || block < 0 || block / SY_SH_DEAL >= block_groups + wave_groups) return SYNERA_EINVAL;
+  bool whole;
+  *item = sh_block(block_groups, wave_groups, run, block, whole);
+  return SYNERA_OK;
 }

@@ -63,8 +63,14 @@ extern "C" int32_t synera_validate_shared(int32_t B, const int32_t* h_ctx_len, c
 }
 
 // ------------------------------------------------------------------------------------ capacities
-// Blocks to cut the work for: a few times what runs at once, so that no block's last item holds up the launch.
+// What the work is cut for, in blocks.  Items of many rows: two for each place on the chip, so that no block's last one holds up
+// the launch; of up to 32 rows, whose keys are the work: one for each place, or four wavefronts'.
 static int64_t item_target(const ShLimits& l) { return 2 * (int64_t)l.slots; }
+#ifndef SH_MIN_BLOCK
+#define SH_MIN_BLOCK 256
+#define SH_MIN_WAVE 256
+#define SH_WAVES_MOST 4
+#endif
 
 void sh_limits(ShLimits& l) {
   const int64_t G = l.Hq / l.Hkv, rows = (int64_t)l.max_tokens * G;        // per KV head
@@ -72,13 +78,14 @@ void sh_limits(ShLimits& l) {
   // rows that shared nodes may hold beyond each request's own: what their partials are kept for
   l.shared_rows = std::min<int64_t>(2 * rows, ((int64_t)1 << 18) / l.Hkv);
   l.list = l.shared_rows / G;
-  l.entries = l.max_batch + l.list;
   l.pages = (int64_t)l.max_batch * l.max_pages;
-  // A node is cut into at most keys x cost / share + 1 ranges (shares are rounded down to whole keys, by less than 1/256): so
-  // many items and, twice (the first range of a node that is cut needs partials too), their rows.
+  // A node is cut into at most keys x cost / share + 1 ranges (shares are rounded down to whole keys, by less than 1/128): for all
+  // nodes as many more as the target has blocks of SY_SH_TILE_ROWS rows, or twice as many wavefronts' of a quarter of the rows.  Twice
+  // their rows in partial results: the first range of a node that is cut needs them too.
   const int64_t extra = item_target(l) + item_target(l) / 64 + 64;
-  l.items = (2 * (int64_t)l.max_batch + (rows + l.shared_rows) / SY_SH_TILE_ROWS + 2) * l.Hkv + extra;
+  l.items = (2 * (int64_t)l.max_batch + (rows + l.shared_rows) / SY_SH_TILE_ROWS + 2) * l.Hkv + 2 * extra + 5 * SY_SH_DEAL;
   l.part_rows = (l.shared_rows + std::min<int64_t>(rows, l.shared_rows)) * l.Hkv + 2 * extra * SY_SH_TILE_ROWS;
+  l.parts = l.part_rows / l.Hkv;
 }
 
 // ------------------------------------------------------------------------------------ shared prefixes
@@ -108,11 +115,11 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
   p = ShPlan();
   p.head = ShHeader{};
   // ---- the new tokens: positions, slots, and the pages they fall on
-  p.req_tok.resize(B);
+  std::vector<int32_t> req_tok(B);               // flattened index of each request's first new token
   int32_t T = 0;
   std::vector<int32_t> all;
   for (int i = 0; i < B; ++i) {
-    p.req_tok[i] = T;
+    req_tok[i] = T;
     const int32_t* row = row_of(i);
     for (int j = 0; j < n_new[i]; ++j) {
       const int64_t pos = (int64_t)ctx[i] + j;
@@ -187,131 +194,147 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
   }
 
   // ---- how the keys are cut: equal shares of the modelled cost
+  const size_t N = nodes.size();
+  struct Cut { int64_t keys, rows, tiles, chunk, splits; double w; bool wave; int64_t page, list, base; };
+  std::vector<Cut> cut(N);
   double total = 0;
-  for (const Node& n : nodes) {
-    const int64_t tiles = (n.tokens * G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
-    const double w = key_cost(n.tokens * G) / (double)tiles;
-    total += w * (double)tiles * (double)((n.last - n.first) * P) * l.Hkv;
+  for (size_t k = 0; k < N; ++k) {
+    const Node& n = nodes[k];
+    Cut& c = cut[k];
+    const int i0 = n.who[0];
+    c.keys = n.leaf ? (int64_t)ctx[i0] + n_new[i0] - n.first * P : (n.last - n.first) * P;
+    c.rows = n.tokens * G;
+    c.tiles = (c.rows + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
+    c.w = key_cost(c.rows) / (double)c.tiles;
+    total += key_cost(c.rows) * (double)c.keys * l.Hkv;
   }
   const double share = total / (double)item_target(l);
+  std::vector<int64_t> n_parts(B, 0);            // ranges of keys that are read for a request's rows
+  for (size_t k = 0; k < N; ++k) {
+    Cut& c = cut[k];
+    int64_t chunk;
+    c.wave = false;
+    if (c.rows <= SY_SH_WAVE_ROWS) {
+      const int64_t wave_chunk = std::max<int64_t>(SH_MIN_WAVE, (int64_t)(share / 2));
+      c.wave = c.keys <= SH_WAVES_MOST * wave_chunk;
+      chunk = c.wave ? wave_chunk : std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(2 * share));
+    } else {
+      chunk = std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(share / c.w));
+    }
+    c.splits = (c.keys + chunk - 1) / chunk;
+    c.chunk = (c.keys + c.splits - 1) / c.splits;                         // even shares
+    c.chunk = (c.chunk + SY_SH_STEP - 1) / SY_SH_STEP * SY_SH_STEP;
+    c.splits = (c.keys + c.chunk - 1) / c.chunk;
+    for (int i : nodes[k].who) n_parts[i] += c.splits;
+  }
 
-  // ---- items
-  struct Draft { int32_t node; int64_t chunk, base; };
-  std::vector<Draft> draft(nodes.size());
-  std::vector<int32_t> n_parts(B, 0);            // nodes x splits that read keys for a request's rows
-  std::vector<std::vector<int32_t>> of(B);       // nodes of each request
-  for (size_t k = 0; k < nodes.size(); ++k) {
+  // ---- page and token lists, partial results
+  p.part_rows = 0;
+  for (size_t k = 0; k < N; ++k) {
     const Node& n = nodes[k];
-    const int i0 = n.who[0];
-    const int64_t keys = n.leaf ? (int64_t)ctx[i0] + n_new[i0] - n.first * P : (n.last - n.first) * P;
-    const int64_t rows = n.tokens * G, tiles = (rows + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
-    const double w = key_cost(rows) / (double)tiles;
-    int64_t chunk = (int64_t)(share / w);
-    chunk = std::max<int64_t>(chunk, 256);
-    int64_t splits = (keys + chunk - 1) / chunk;
-    chunk = (keys + splits - 1) / splits;                                   // even shares
-    chunk = (chunk + SY_SH_STEP - 1) / SY_SH_STEP * SY_SH_STEP;
-    splits = (keys + chunk - 1) / chunk;
-    draft[k] = Draft{(int32_t)k, chunk, 0};
-    for (int i : n.who) {
-      n_parts[i] += (int32_t)splits;
-      of[i].push_back((int32_t)k);
+    Cut& c = cut[k];
+    c.page = (int64_t)p.pages.size();
+    p.pages.insert(p.pages.end(), row_of(n.who[0]) + n.first, row_of(n.who[0]) + n.last);
+    c.list = (int64_t)p.list.size();
+    if (!n.leaf)
+      for (int i : n.who)
+        for (int j = 0; j < n_new[i]; ++j) p.list.push_back(req_tok[i] + j);
+    const bool direct = n.leaf && n_parts[n.who[0]] == 1;
+    c.base = direct ? -1 : p.part_rows;
+    if (!direct) p.part_rows += c.rows * l.Hkv * c.splits;
+  }
+  // the last key (exclusive) that some row of tile `t` of node k sees
+  auto seen_by = [&](size_t k, int64_t t) {
+    const Node& n = nodes[k];
+    if (!n.leaf) return cut[k].keys;
+    const int64_t last = std::min((t + 1) * SY_SH_TILE_ROWS, cut[k].rows) - 1;
+    return (int64_t)ctx[n.who[0]] - n.first * P + last / G + 1;
+  };
+  std::vector<std::vector<std::pair<int32_t, int64_t>>> where(B);          // nodes of a request, its first row there
+  for (size_t k = 0; k < N; ++k) {
+    int64_t row = 0;
+    for (int i : nodes[k].who) {
+      if (n_parts[i] > 1) where[i].emplace_back((int32_t)k, row);
+      row += n_new[i] * G;
     }
   }
-  std::vector<int64_t> page_at(nodes.size()), list_at(nodes.size());
-  std::vector<std::vector<int32_t>> row_at(nodes.size());                   // first row of each request of a shared node
-  int64_t part_rows = 0;
-  for (size_t k = 0; k < nodes.size(); ++k) {
-    const Node& n = nodes[k];
-    const int i0 = n.who[0];
-    page_at[k] = (int64_t)p.pages.size();
-    p.pages.insert(p.pages.end(), row_of(i0) + n.first, row_of(i0) + n.last);
-    list_at[k] = (int64_t)p.list.size();
-    int64_t rows = 0;
-    for (int i : n.who) {
-      row_at[k].push_back((int32_t)rows);
-      rows += n_new[i] * G;
-      if (!n.leaf)
-        for (int j = 0; j < n_new[i]; ++j) p.list.push_back(p.req_tok[i] + j);
+  for (int i = 0; i < B; ++i) {
+    if (n_parts[i] <= 1) continue;
+    for (int j = 0; j < n_new[i]; ++j) {
+      const int32_t first = (int32_t)p.parts.size();
+      for (const auto& [k, row] : where[i]) {
+        const Cut& c = cut[k];
+        const int64_t r = row + j * G;           // (a token's G rows may lie in two tiles: each of them has these ranges at least)
+        const int64_t keys = seen_by(k, r / SY_SH_TILE_ROWS);
+        for (int64_t s = 0; s * c.chunk < keys; ++s)
+          p.parts.push_back(ShPart{(int32_t)(c.base + s * l.Hkv * c.rows + r), (int32_t)c.rows});
+      }
+      p.joined.push_back(ShJoin{req_tok[i] + j, first, (int32_t)p.parts.size() - first, 0});
     }
-    const bool direct = n.leaf && n_parts[i0] == 1;
-    const int64_t keys = n.leaf ? (int64_t)ctx[i0] + n_new[i0] - n.first * P : (n.last - n.first) * P;
-    const int64_t splits = (keys + draft[k].chunk - 1) / draft[k].chunk;
-    draft[k].base = direct ? -1 : part_rows;
-    if (!direct) part_rows += rows * l.Hkv * splits;
   }
-  // Items that read the same keys go to one XCD (blocks are dealt to the eight in turn), next to each other in time: eight
-  // queues, the least loaded takes the next range of keys.  Long items first.
+  p.head.n_joined = (int32_t)p.joined.size();
+
+  // ---- items.  Ranges of keys, the costliest first, go to the least loaded of eight queues, with all the tiles of rows that read
+  // them: blocks are dealt to the eight XCDs in turn, so these meet in one L2.
   struct Range { double cost; int32_t node, head; int64_t split; };
-  std::vector<Range> ranges;
-  for (size_t k = 0; k < nodes.size(); ++k) {
-    const Node& n = nodes[k];
-    const int i0 = n.who[0];
-    const int64_t keys = n.leaf ? (int64_t)ctx[i0] + n_new[i0] - n.first * P : (n.last - n.first) * P;
-    const int64_t splits = (keys + draft[k].chunk - 1) / draft[k].chunk;
+  std::vector<Range> ranges, waves;
+  for (size_t k = 0; k < N; ++k) {
+    const Cut& c = cut[k];
     for (int h = 0; h < l.Hkv; ++h)
-      for (int64_t s = 0; s < splits; ++s)
-        ranges.push_back(Range{key_cost(n.tokens * G) * (double)std::min(draft[k].chunk, keys - s * draft[k].chunk), (int32_t)k, h, s});
+      for (int64_t s = 0; s < c.splits; ++s)
+        (c.wave ? waves : ranges).push_back(Range{key_cost(c.rows) * (double)std::min(c.chunk, c.keys - s * c.chunk), (int32_t)k, h, s});
   }
-  std::stable_sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.cost > b.cost; });
-  const int X = 8;
+  auto by_cost = [](const Range& a, const Range& b) { return a.cost > b.cost; };
+  std::stable_sort(ranges.begin(), ranges.end(), by_cost);
+  std::stable_sort(waves.begin(), waves.end(), by_cost);
+  auto put = [&](const Range& r, int64_t t, std::vector<ShItem>& to) {
+    const Node& n = nodes[r.node];
+    const Cut& c = cut[r.node];
+    const int i0 = n.who[0];
+    ShItem it = {};
+    it.flags = n.leaf ? SY_SH_LEAF : 0;
+    it.kv_head = r.head;
+    it.row0 = (int32_t)(t * SY_SH_TILE_ROWS);
+    it.n_rows = (int32_t)std::min<int64_t>(SY_SH_TILE_ROWS, c.rows - it.row0);
+    it.tok = n.leaf ? req_tok[i0] : (int32_t)c.list;
+    it.page = (int32_t)c.page;
+    it.n_pages = (int32_t)(n.last - n.first);
+    it.key_begin = (int32_t)(r.split * c.chunk);
+    const int64_t seen = seen_by(r.node, t);
+    if (it.key_begin >= seen) return;
+    it.key_end = (int32_t)std::min(seen, (r.split + 1) * c.chunk);
+    it.lim0 = n.leaf ? (int32_t)(ctx[i0] - n.first * P) : -1;
+    it.part = c.base < 0 ? -1 : (int32_t)(c.base + (r.split * l.Hkv + r.head) * c.rows + it.row0);
+    for (int q = 0; q < 16; ++q) it.pages[q] = p.pages[c.page + std::min<int64_t>(it.key_begin / P + q, it.n_pages - 1)];
+    to.push_back(it);
+  };
+  const int X = SY_SH_DEAL;
   std::vector<ShItem> queue[X];
   double load[X] = {};
   for (const Range& r : ranges) {
-    int x = 0;
-    for (int y = 1; y < X; ++y)
-      if (load[y] < load[x]) x = y;
+    const int x = (int)(std::min_element(load, load + X) - load);
     load[x] += r.cost;
-    const Node& n = nodes[r.node];
-    const int i0 = n.who[0];
-    const int64_t rows = n.tokens * G, chunk = draft[r.node].chunk;
-    const int64_t keys = n.leaf ? (int64_t)ctx[i0] + n_new[i0] - n.first * P : (n.last - n.first) * P;
-    const int64_t lim0 = n.leaf ? (int64_t)ctx[i0] - n.first * P : -1;
-    for (int64_t r0 = 0; r0 < rows; r0 += SY_SH_TILE_ROWS) {
-      ShItem it = {};
-      it.flags = n.leaf ? SY_SH_LEAF : 0;
-      it.kv_head = r.head;
-      it.n_rows = (int32_t)std::min<int64_t>(SY_SH_TILE_ROWS, rows - r0);
-      it.row0 = (int32_t)r0;
-      it.tok = n.leaf ? p.req_tok[i0] : (int32_t)list_at[r.node];
-      it.page = (int32_t)page_at[r.node];
-      it.n_pages = (int32_t)(n.last - n.first);
-      it.key_begin = (int32_t)(r.split * chunk);
-      const int64_t seen = n.leaf ? lim0 + (r0 + it.n_rows - 1) / G + 1 : keys;   // keys that the tile's last row sees
-      if (it.key_begin >= seen) continue;
-      it.key_end = (int32_t)std::min(seen, (r.split + 1) * chunk);
-      it.lim0 = (int32_t)lim0;
-      it.part = draft[r.node].base < 0 ? -1 : (int32_t)(draft[r.node].base + (r.split * l.Hkv + r.head) * rows + r0);
-      queue[x].push_back(it);
-    }
+    for (int64_t t = 0; t < cut[r.node].tiles; ++t) put(r, t, queue[x]);
   }
-  for (size_t n = 0, left = 1; left; ++n) {
-    left = 0;
-    for (int x = 0; x < X; ++x)
-      if (n < queue[x].size()) {
-        p.items.push_back(queue[x][n]);
-        left = 1;
+  size_t next[X] = {}, left = 0;
+  for (const auto& q : queue) left += q.size();
+  while (left) {
+    for (int x = 0; x < X; ++x) {
+      int y = x;
+      if (next[x] == queue[x].size())            // this queue is done: from the longest one, so that the others keep their turn
+        for (int z = 0; z < X; ++z)
+          if (queue[z].size() - next[z] > queue[y].size() - next[y]) y = z;
+      if (next[y] < queue[y].size()) {
+        p.items.push_back(queue[y][next[y]++]);
+        --left;
+      } else {
+        p.items.push_back(ShItem{});
       }
-  }
-  p.head.n_items = (int32_t)p.items.size();
-
-  // ---- what is joined
-  p.first_entry.resize(B + 1);
-  for (int i = 0; i < B; ++i) {
-    p.first_entry[i] = (int32_t)p.entries.size();
-    if (n_parts[i] <= 1) continue;
-    for (int32_t k : of[i]) {
-      const Node& n = nodes[k];
-      const size_t at = std::find(n.who.begin(), n.who.end(), i) - n.who.begin();
-      const int64_t keys = n.leaf ? (int64_t)ctx[i] + n_new[i] - n.first * P : (n.last - n.first) * P;
-      p.entries.push_back(ShEntry{(int32_t)(draft[k].base + row_at[k][at]), row_at[k][at], (int32_t)(n.tokens * G), (int32_t)keys,
-                                  (int32_t)draft[k].chunk, n.leaf ? (int32_t)(ctx[i] - n.first * P) : -1, {0, 0}});
-    }
-    for (int j = 0; j < n_new[i]; ++j) {
-      p.joined.push_back(p.req_tok[i] + j);
-      p.joined.push_back(i);
     }
   }
-  p.first_entry[B] = (int32_t)p.entries.size();
-  p.head.n_joined = (int32_t)(p.joined.size() / 2);
+  p.head.block_groups = (int32_t)(p.items.size() / X);
+  const size_t begin = p.items.size();
+  for (const Range& r : waves) put(r, 0, p.items);
+  while ((p.items.size() - begin) % (4 * X)) p.items.push_back(ShItem{});
+  p.head.wave_groups = (int32_t)((p.items.size() - begin) / (4 * X));
 }

@@ -41,8 +41,9 @@ def check_plan(hq, hkv, slots, ctx, new, table, max_tokens=None):
     pl = synera.debug_shared_plan(hq, hkv, slots, ctx, new, table, max_tokens)
     G, B, T = hq // hkv, len(ctx), int(new.sum())
     head = pl["head"][0]
-    assert head[0] == T and head[1] == len(pl["windows"]) and head[2] == len(pl["items"]) and head[3] == len(pl["joined"])
-    for name, room in zip(("items", "list", "entries", "pages", "windows"), pl["limits"]):
+    assert head[0] == T and head[1] == len(pl["windows"]) and head[2] == len(pl["joined"])
+    assert len(pl["items"]) == 8 * head[3] + 32 * head[4]
+    for name, room in zip(("items", "list", "parts", "pages", "windows"), pl["limits"]):
         assert len(pl[name]) <= room, name
     tok0 = np.concatenate([[0], np.cumsum(new)])
     req_of = np.repeat(np.arange(B), new)
@@ -59,7 +60,12 @@ def check_plan(hq, hkv, slots, ctx, new, table, max_tokens=None):
 
     seen = {}                    # (token, head, kv head) -> list of (first page column, key from, key to, partial row)
     parts = np.zeros(max(1, pl["limits"][5]), np.int32)
-    for flags, kh, n_rows, row0, tok, page, n_pages, k0, k1, lim0, part in pl["items"][:, :11]:
+    for at_item, item in enumerate(pl["items"]):
+        flags, kh, n_rows, row0, tok, page, n_pages, k0, k1, lim0, part = item[:11]
+        if n_rows == 0:
+            continue
+        assert n_rows <= (TILE if at_item < 8 * head[3] else 32)
+        assert list(item[16:]) == [pl["pages"][page + min(k0 // P + q, n_pages - 1)] for q in range(16)]
         assert 1 <= n_rows <= TILE and row0 % TILE == 0 and k0 % 128 == 0 and 0 <= k0 < k1 <= n_pages * P and 0 <= kh < hkv
         ids = pl["pages"][page: page + n_pages]
         assert len(ids) == n_pages
@@ -79,30 +85,25 @@ def check_plan(hq, hkv, slots, ctx, new, table, max_tokens=None):
                 end = min(end, lim0 + j + 1)                   # what the kernel's mask leaves
             seen.setdefault((t, g, kh), []).append((col * P + k0, col * P + end, part + r if part >= 0 else -1))
     assert parts.max(initial=0) <= 1                           # no partial row is written twice
-    joined = {int(t): int(i) for t, i in pl["joined"]}
+    joined = {int(t): (int(first), int(n)) for t, first, n, _ in pl["joined"]}
+    assert len(joined) == len(pl["joined"])
     for t in range(T):
         i = req_of[t]
         for kh in range(hkv):
             for g in range(G):
-                ranges = sorted(seen[(t, g, kh)])
+                # a tile's other rows may see keys that this one does not: such ranges hold nothing for it
+                ranges = sorted(r for r in seen[(t, g, kh)] if r[1] > r[0])
                 at = 0
                 for a, b, _ in ranges:
-                    if b > a:                                  # a tile's later rows may see keys that this one does not
-                        assert a == at
-                        at = b
+                    assert a == at
+                    at = b
                 assert at == pos[t] + 1
                 if t not in joined:
-                    assert len(ranges) == 1 and ranges[0][2] == -1
+                    assert len(seen[(t, g, kh)]) == 1 and ranges[0][2] == -1
                     continue
-                assert joined[t] == i
-                want = []
-                r = (t - tok0[i]) * G + g
-                for base, row_in, rows, keys, chunk, lim0 in pl["entries"][pl["first_entry"][i]: pl["first_entry"][i + 1], :6]:
-                    if lim0 >= 0:
-                        last = min((row_in + r) // TILE * TILE + TILE, rows) - 1
-                        keys = min(keys, lim0 + last // G + 1)
-                    want += [base + (s * hkv + kh) * rows + r for s in range(-(-keys // chunk))]
-                assert sorted(want) == sorted(p for _, _, p in ranges)
+                first, n = joined[t]
+                mine = {row + kh * step + g for row, step in pl["parts"][first: first + n]}
+                assert len(mine) == n and {p for _, _, p in ranges} <= mine <= {p for _, _, p in seen[(t, g, kh)]}
     return pl
 
 
@@ -124,7 +125,7 @@ def test_plan_shares_where_it_is_shorter():
     ctx = np.full(B, shared * P + 5, np.int32)
     table = np.concatenate([np.tile(np.arange(shared), (B, 1)), shared + np.arange(B)[:, None]], 1).astype(np.int32)
     pl = check_plan(32, 8, 512, ctx, np.ones(B, np.int32), table)
-    shared_items = pl["items"][(pl["items"][:, 0] & 1) == 0]
+    shared_items = pl["items"][((pl["items"][:, 0] & 1) == 0) & (pl["items"][:, 2] > 0)]
     assert len(pl["pages"]) == shared + B and len(pl["list"]) == B
     assert {int(r) for r in shared_items[:, 2]} == {128}       # 64 x 4 rows are two full tiles
     # two levels: halves of the batch share more
@@ -141,14 +142,27 @@ def test_plan_of_long_chunks_reads_for_itself():
     ctx, new = np.array([160, 160], np.int32), np.array([512, 512], np.int32)
     table = np.concatenate([np.tile(np.arange(10), (2, 1)), 10 + np.arange(64).reshape(2, 32)], 1).astype(np.int32)
     pl = check_plan(8, 1, 512, ctx, new, table)
-    assert (pl["items"][:, 0] & 1).all()
+    assert (pl["items"][pl["items"][:, 2] > 0, 0] & 1).all()
+
+
+@pytest.mark.parametrize("block_groups,wave_groups", [(0, 0), (1, 0), (0, 3), (5, 2), (2, 5), (70, 33), (200, 31), (64, 64), (3, 400)])
+@pytest.mark.parametrize("run", [1, 2, 32])
+def test_blocks_take_every_item_once(block_groups, wave_groups, run):
+    """The order in which blocks take the two lists (as the kernel's sh_block has it)."""
+    taken, whole_before = [], 0
+    for b in range(8 * (block_groups + wave_groups)):
+        at, whole = synera.debug_shared_block(block_groups, wave_groups, run, b)
+        assert whole == (at < 8 * block_groups)
+        assert at % 8 == b % 8 or not whole                    # the XCD that the item was queued for
+        taken += [at] if whole else range(at, at + 4)
+    assert sorted(taken) == list(range(8 * block_groups + 32 * wave_groups))
 
 
 def test_plan_without_rows():
     ctx, new, table, n = np.array([20, 0], np.int32), np.zeros(2, np.int32), np.array([[0, 1], [5, 5]], np.int32), 2
     assert synera.validate_shared(ctx, new, table, n, 2, 1) == synera.OK
     pl = check_plan(4, 4, 64, ctx, new, table, max_tokens=1)
-    assert not pl["head"][0, :4].any()
+    assert not pl["head"].any()
 
 
 def test_validation_codes():
