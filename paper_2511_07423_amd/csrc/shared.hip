@@ -426,9 +426,14 @@ typedef __attribute__((ext_vector_type(8))) int sh_i32x8v;
 typedef SH_CONST_AS sh_i32x8v sh_i32x8;                      // read with scalar loads
 
 __device__ __forceinline__ float sh_ex2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float other_half(float v) {      // of lane l ^ 32
+// Of lanes l and l ^ 32: swapping the halves of two copies leaves the lower lane's value in one and the upper lane's in the other.
+__device__ __forceinline__ float both_max(float v) {
   auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float((threadIdx.x & 32) ? a[0] : a[1]);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
 // Asynchronous copies of N kilobytes, global -> LDS (16 bytes a lane; lane i of kilobyte j lands at lds_addr + 1024 j + 16 i), from a
@@ -448,12 +453,12 @@ __device__ __forceinline__ void copy_page(const bf16_t* base, uint32_t o0, uint3
 }
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
-// At most `n` positions of IPP copies may still be on their way, and this wavefront's LDS reads are done.
-template <int IPP>
+// At most `n` positions of IPP copies may still be on their way, and this wavefront's LDS reads are done.  USUAL: what n mostly is.
+template <int IPP, int USUAL>
 __device__ __forceinline__ void wait_positions(int n) {
-  if (n >= 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * IPP) : "memory");
-  else if (n == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPP) : "memory");
-  else if (n == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IPP) : "memory");
+  if (n >= USUAL) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(USUAL * IPP) : "memory");
+  else if (USUAL > 2 && n == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * IPP) : "memory");
+  else if (USUAL > 1 && n == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IPP) : "memory");
   else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 }
 
@@ -494,24 +499,28 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
     return pages[min(page0 + 2 * ((s >> 2) * WK + kp) + (s & 1), it.n_pages - 1)];
   };
   const SH_CONST_AS int32_t* near = reinterpret_cast<const SH_CONST_AS int32_t*>((uintptr_t)first_pages);
-  auto first_page_of = [&](int p) {                           // of the prologue's positions: at most page 15 from key_begin on
+  auto first_page_of = [&](int p) {                           // of the first NT positions: at most page 15 from key_begin on
     const int s = p * WR + wr;
     return near[2 * ((s >> 2) * WK + kp) + (s & 1)];
   };
-  auto issue = [&](int p, int32_t page) {
-    const uint32_t to = ring + (uint32_t)(p % NT) * SLOT_B + wr * PAGE_B;
-    const size_t at = (size_t)page * page_elems + head_at;
-    if (((p * WR + wr) & 2) == 0) {
+  auto wrap = [&](uint32_t at) { return at >= RING_B ? at - RING_B : at; };
+  int issued = 0;                                             // positions on their way or landed
+  uint32_t fill = 0;                                          // where the next one goes in the ring
+  auto issue = [&](int32_t page) {
+    const uint32_t to = ring + fill + wr * PAGE_B;
+    const size_t at = (size_t)(uint32_t)page * page_elems + head_at;
+    if (((issued * WR + wr) & 2) == 0) {
       asm volatile("" : "+v"(k_off));
       copy_page<IPP>(a.k_layer + at, k_off, k_off ^ 64, k_off ^ 128, k_off ^ 192, to);
     } else {
       copy_page<IPP>(a.v_layer + at, v_off, v_off, v_off, v_off, to);
     }
+    fill = wrap(fill + SLOT_B);
+    ++issued;
   };
-  constexpr int AHEAD = WR == 1 ? NT : NT - PPT;              // positions on their way when the loop begins
 #pragma unroll
-  for (int p = 0; p < AHEAD; ++p)
-    if (p < n_pos) issue(p, first_page_of(p));
+  for (int p = 0; p < NT; ++p)
+    if (p < n_pos) issue(first_page_of(p));
 
   // ---- rows
   const int row = wr * 32 + n32;
@@ -541,47 +550,51 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   uint32_t k_at = (WR == 1 ? 0 : (n32 >> 4) * PAGE_B) + kslot * HD * 2 + ((h ^ sh_swz<HD>(kslot)) << 4);
   const uint32_t v_at = n32 * 32 + (h ^ ((n32 >> 3) & 1)) * 16;
   bf16x8 kf[KS], vf[DB][2];
-  // page `part` of tile i (of this group) in the ring
-  auto page_at = [&](int i, int part) { const int s = 4 * i + part; return ring + (uint32_t)((s / WR % NT) * SLOT_B + (s % WR) * PAGE_B); };
-  auto read_k = [&](int i) {
+  uint32_t take = 0;                                          // where the tile at hand begins in the ring
+  auto page_at = [&](uint32_t tile, int part) {               // its page `part`
+    if constexpr (WR == 4) return ring + tile + part * PAGE_B;
+    else if constexpr (WR == 2) return ring + wrap(tile + (part >> 1) * SLOT_B) + (part & 1) * PAGE_B;
+    else return ring + wrap(tile + part * SLOT_B);
+  };
+  auto read_k = [&](uint32_t tile) {
     asm volatile("" : "+v"(k_at));
-    const uint32_t at = k_at + (WR == 1 ? ((n32 >> 4) ? page_at(i, 1) : page_at(i, 0)) : page_at(i, 0));
+    const uint32_t at = k_at + (WR == 1 ? ((n32 >> 4) ? page_at(tile, 1) : page_at(tile, 0)) : page_at(tile, 0));
 #pragma unroll
     for (int s = 0; s < KS; ++s) kf[s] = *(lds_bf16x8*)(uintptr_t)(at ^ (s << 5));      // chunk (2 s + h) ^ swizzle
   };
-  auto read_v = [&](int i) {
+  auto read_v = [&](uint32_t tile) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const uint32_t at = page_at(i, 2 + b) + v_at;
+      const uint32_t at = page_at(tile, 2 + b) + v_at;
 #pragma unroll
       for (int db = 0; db < DB; ++db) vf[db][b] = *(lds_bf16x8*)(uintptr_t)(at + db * 1024);
     }
   };
-  f32x16 sc;
-  auto scores = [&]() {
+  auto scores = [&](f32x16& sc) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
   };
-  bf16x8 pf[2];
-  auto softmax = [&](int kb, auto masked) {                   // register r holds key kb + 16 (r / 8) + 8 h + r % 8
+  // N tiles' scores (register r of a tile: key kb + 16 (r / 8) + 8 h + r % 8) to probabilities, statistics and accumulators brought up
+  auto softmax = [&](auto& sc, auto& pf, int kb, auto masked) {
+    constexpr int N = sizeof(sc) / sizeof(f32x16);
     if constexpr (masked) {
+      static_assert(N == 1, "masked tiles come one at a time");
       const int seen = min(it.key_end - 1, lim) - kb - 8 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 16 * (r >> 3) + (r & 7) <= seen ? sc[r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) sc[0][r] = 16 * (r >> 3) + (r & 7) <= seen ? sc[0][r] : -INFINITY;
     }
-    float mx = sc[0];
+    float mx = sc[0][0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    mx = fmaxf(mx, other_half(mx));
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[n][r]);
+    mx = both_max(mx);
     // The reference only has to keep 2^(c (s - m)) in range: it moves when a score exceeds it by more than 2^8.
     const float m_new = (mx - m) * c > 8.0f ? mx : m;
     const float alpha = sh_ex2((m - m_new) * c), mc = m_new * c;
     m = m_new;
-    float p[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) p[r] = sh_ex2(fmaf(sc[r], c, -mc));
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
       l *= alpha;
 #pragma unroll
@@ -591,17 +604,23 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
     }
     float t0 = 0.f, t1 = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      t0 += p[r];
-      t1 += p[r + 1];
+    for (int n = 0; n < N; ++n) {
+      float p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = sh_ex2(fmaf(sc[n][r], c, -mc));
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        t0 += p[r];
+        t1 += p[r + 1];
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        pf[n][b] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf2(p[8 * b], p[8 * b + 1]), pack_bf2(p[8 * b + 2], p[8 * b + 3]),
+                                                         pack_bf2(p[8 * b + 4], p[8 * b + 5]), pack_bf2(p[8 * b + 6], p[8 * b + 7])));
     }
     l += t0 + t1;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      pf[b] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf2(p[8 * b], p[8 * b + 1]), pack_bf2(p[8 * b + 2], p[8 * b + 3]),
-                                                    pack_bf2(p[8 * b + 4], p[8 * b + 5]), pack_bf2(p[8 * b + 6], p[8 * b + 7])));
   };
-  auto values = [&](int kb, auto masked) {
+  auto values = [&](const bf16x8* pf, int kb, auto masked) {
     if constexpr (masked) {
       // Keys past the end may hold junk, and 0 x NaN is NaN: they are blanked.  So may keys that only some rows see.
       bool odd = false;
@@ -652,53 +671,84 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   // The tiles that need no mask, then (masked) the last few: the code for hidden keys stays out of the first loop's registers.
   const int free_tiles = max(0, free_end - it.key_begin) / 32;              // of all groups
   const int my_free = min(my_tiles, max(0, (free_tiles - kp + WK - 1) / WK));
+  int32_t next[PPT > 1 ? PPT : 2];                            // pages of the positions to be issued next
+  if (n_pos > 0) {
+#pragma unroll
+    for (int q = 0; q < (PPT > 1 ? PPT : 2); ++q) next[q] = page_of(NT + q);
+  }
   if constexpr (WR == 1) {
     // No other wavefront touches this ring: K slots are filled again as soon as the scores' operands are in registers.
-    int32_t n0 = n_pos > 0 ? page_of(5) : 0, n1 = n_pos > 0 ? page_of(6) : 0;
     auto tile = [&](int i, auto masked) {
       const int kb = it.key_begin + 32 * (i * WK + kp);
-      const int32_t n2 = page_of(4 * i + 7), n3 = page_of(4 * i + 8);
-      wait_positions<IPP>(min(n_pos, 4 * i + 5) - (4 * i + 2));
-      read_k(i);
+      f32x16 sc[1];
+      bf16x8 pf[1][2];
+      wait_positions<IPP, 3>(issued - (4 * i + 2));
+      read_k(take);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (4 * i + 5 < n_pos) issue(4 * i + 5, n0);
-      if (4 * i + 6 < n_pos) issue(4 * i + 6, n1);
-      scores();
-      softmax(kb, masked);
-      n0 = page_of(4 * i + 9);
-      n1 = page_of(4 * i + 10);
-      wait_positions<IPP>(min(n_pos, 4 * i + 7) - (4 * i + 4));
-      read_v(i);
+      if (issued < n_pos) issue(next[0]);
+      if (issued < n_pos) issue(next[1]);
+      scores(sc[0]);
+      softmax(sc, pf, kb, masked);
+      next[0] = page_of(4 * i + 9);
+      next[1] = page_of(4 * i + 10);
+      wait_positions<IPP, 3>(issued - (4 * i + 4));
+      read_v(take);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (4 * i + 7 < n_pos) issue(4 * i + 7, n2);
-      if (4 * i + 8 < n_pos) issue(4 * i + 8, n3);
-      values(kb, masked);
+      if (issued < n_pos) issue(next[2]);
+      if (issued < n_pos) issue(next[3]);
+      next[2] = page_of(4 * i + 11);
+      next[3] = page_of(4 * i + 12);
+      values(pf[0], kb, masked);
+      take = wrap(take + 4 * SLOT_B);
     };
     for (int i = 0; i < my_free; ++i) tile(i, std::false_type());
     for (int i = my_free; i < my_tiles; ++i) tile(i, std::true_type());
   } else {
-    int32_t next[PPT];
-#pragma unroll
-    for (int q = 0; q < PPT; ++q) next[q] = n_pos > 0 ? page_of(AHEAD + q) : 0;
-    auto tile = [&](int i, auto masked) {
-      // Own copies of tile i have landed and own reads of tile i - 1 are done; the barrier extends both to the block, so the
-      // slots of tile i - 1 may be filled again.
-      wait_positions<IPP>(min(n_pos, i * PPT + AHEAD) - (i + 1) * PPT);
+    // Own copies of the coming N tiles have landed and own reads of the ones before are done; the barrier extends both to the block,
+    // so the slots of the ones before may be filled again.
+    auto begin = [&](int i, auto n) {
+      wait_positions<IPP, 1>(issued - (i + n) * PPT);
       asm volatile("s_barrier" ::: "memory");
 #pragma unroll
-      for (int q = 0; q < PPT; ++q)
-        if (i * PPT + AHEAD + q < n_pos) issue(i * PPT + AHEAD + q, next[q]);
-      const int kb = it.key_begin + 32 * (i * WK + kp);
+      for (int q = 0; q < 2; ++q)
+        if (issued < min(n_pos, i * PPT + NT)) issue(next[q]);
 #pragma unroll
-      for (int q = 0; q < PPT; ++q) next[q] = page_of((i + 1) * PPT + AHEAD + q);
-      read_k(i);
-      scores();
-      read_v(i);
-      softmax(kb, masked);
-      values(kb, masked);
+      for (int q = 0; q < 2; ++q) next[q] = page_of(issued + q);
     };
-    for (int i = 0; i < my_free; ++i) tile(i, std::false_type());
-    for (int i = my_free; i < my_tiles; ++i) tile(i, std::true_type());
+    auto tile = [&](int i, auto masked) {
+      begin(i, std::integral_constant<int, 1>());
+      const int kb = it.key_begin + 32 * (i * WK + kp);
+      f32x16 sc[1];
+      bf16x8 pf[1][2];
+      read_k(take);
+      scores(sc[0]);
+      read_v(take);
+      softmax(sc, pf, kb, masked);
+      values(pf[0], kb, masked);
+      take = wrap(take + PPT * SLOT_B);
+    };
+    int i = 0;
+    if constexpr (WR == 4)
+      // two tiles at a time: half the barriers, waits and exchanges, and two chains of products to interleave
+      for (; i + 2 <= my_free; i += 2) {
+        begin(i, std::integral_constant<int, 2>());
+        const uint32_t second = wrap(take + SLOT_B);
+        f32x16 sc[2];
+        bf16x8 pf[2][2];
+        read_k(take);
+        scores(sc[0]);
+        read_k(second);
+        scores(sc[1]);
+        read_v(take);
+        softmax(sc, pf, 0, std::false_type());
+        values(pf[0], 0, std::false_type());
+        read_v(second);
+        values(pf[1], 0, std::false_type());
+        take = wrap(second + SLOT_B);
+      }
+    else
+      for (; i < my_free; ++i) tile(i, std::false_type());
+    for (; i < my_tiles; ++i) tile(i, std::true_type());
     if (my_tiles < n_iter) {                                  // the other key group has one tile more: its barrier
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       asm volatile("s_barrier" ::: "memory");
@@ -734,7 +784,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
       m = top;
     }
   }
-  l += other_half(l);
+  l = both_sum(l);
   if (row >= it.n_rows) return;
   if (it.part < 0) {
     const float inv = 1.0f / l;
