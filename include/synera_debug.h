@@ -138,7 +138,7 @@ int32_t synera_debug_attention_plan(const synera_model_desc* desc, int32_t attn_
  * Test hook, host only: what synera_batch_plan would upload for one batch (not validated here) on a chip that runs `slots`
  * blocks at once.  `which` picks a region: 0 header (tokens, page windows, tokens with several partial results, groups of 8 items that a
  * block takes each, groups of 32 that a wavefront takes each, 0 ..), 1 positions, 2 page x 16 + slot, 3 windows [n][4] = page, first
- * token, slots from, to, 4 items [n][32] = flags (1 = one request's rows), KV head, rows, first row in the node, first token or entry
+ * token, slots from, to, 4 items [n][32] = flags (1 = one request's rows, 2 = keys not wanted again), KV head, rows, first row in the node, first token or entry
  * of the token list, first page entry, pages, first key, end of keys, last key the first token sees, partial row or -1, 0 .., the 16
  * pages from the first key on, 5 token list, 6 page list, 7 tokens with several partial results [n][4] = token, first entry of the list,
  * entries, 0, 8 that list [n][2] = partial row of head 0, step to the next KV head's.

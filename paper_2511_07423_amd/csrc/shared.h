@@ -14,7 +14,10 @@
 #define SY_SH_STEP 128           // keys that all wavefronts of a block take together at most: key ranges are cut at multiples of it
 #define SY_SH_WAVE_ROWS 32       // rows of a tile that one wavefront can take alone
 #define SY_SH_DEAL 8             // XCDs that blocks are dealt to in turn
-enum { SY_SH_LEAF = 1 };         // the item's rows are one request's, in order: causal, rows without a list
+enum {
+  SY_SH_LEAF = 1,                // the item's rows are one request's, in order: causal, rows without a list
+  SY_SH_ONCE = 2                 // its keys and values are marked as not wanted again
+};
 
 // A tile of rows against a range of the keys of one node (a run of pages with the requests that all read it).  Keys count from the
 // node's first page on.  128 bytes, read with scalar loads.

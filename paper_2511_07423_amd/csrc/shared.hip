@@ -417,6 +417,7 @@ struct SharedAttnArgs {
   float2* part_ml;
   float* lse;
   float c;                     // scale x log2 e
+  float m0;                    // below all scores, and m0 c is finite
   int32_t Hq, Hkv, G;
   int32_t run;                 // groups of blocks of a kind in a row (sh_block)
   int32_t block_groups, wave_groups;   // the plan's, or -1: read on the device (graphs, which serve other plans too)
@@ -439,17 +440,24 @@ __device__ __forceinline__ float both_sum(float v) {
 // Asynchronous copies of N kilobytes, global -> LDS (16 bytes a lane; lane i of kilobyte j lands at lds_addr + 1024 j + 16 i), from a
 // base in scalar registers and each lane's own offsets.  An instruction's offset counts on both sides.
 template <int N>
-__device__ __forceinline__ void copy_page(const bf16_t* base, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3, uint32_t lds_addr) {
-  if constexpr (N == 4)
-    asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds_addr),
-        "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base)
-        : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds_addr),
-                 "v"(o0), "v"(o1), "s"(base)
-                 : "memory", "m0");
+__device__ __forceinline__ void copy_page(const bf16_t* base, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3, uint32_t lds_addr, bool once) {
+#define SH_COPY_4(MARK)                                                                                                            \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5" MARK                                               \
+               "\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024" MARK "\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048" MARK          \
+               "\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base) \
+               : "memory", "m0")
+#define SH_COPY_2(MARK)                                                                                                            \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" MARK                                               \
+               "\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "s"(base) : "memory", "m0")
+  if constexpr (N == 4) {
+    if (once) SH_COPY_4(" nt");
+    else SH_COPY_4("");
+  } else {
+    if (once) SH_COPY_2(" nt");
+    else SH_COPY_2("");
+  }
+#undef SH_COPY_4
+#undef SH_COPY_2
 }
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
@@ -477,6 +485,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave % WR, kp = WK == 1 ? 0 : wave / WR;
   const bool leaf = (it.flags & SY_SH_LEAF) != 0;
+  const bool once = WR < 4 && (it.flags & SY_SH_ONCE) != 0;   // (four wavefronts' rows are seldom a whole request's)
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds + wave / WR * RING_B;
 
   // ---- keys
@@ -511,9 +520,9 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
     const size_t at = (size_t)(uint32_t)page * page_elems + head_at;
     if (((issued * WR + wr) & 2) == 0) {
       asm volatile("" : "+v"(k_off));
-      copy_page<IPP>(a.k_layer + at, k_off, k_off ^ 64, k_off ^ 128, k_off ^ 192, to);
+      copy_page<IPP>(a.k_layer + at, k_off, k_off ^ 64, k_off ^ 128, k_off ^ 192, to, once);
     } else {
-      copy_page<IPP>(a.v_layer + at, v_off, v_off, v_off, v_off, to);
+      copy_page<IPP>(a.v_layer + at, v_off, v_off, v_off, v_off, to, once);
     }
     fill = wrap(fill + SLOT_B);
     ++issued;
@@ -538,7 +547,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
   __builtin_amdgcn_s_waitcnt(0x0F70);                         // vmcnt(0)
 
   const float c = a.c;
-  float m = c > 1.f ? -3e38f / c : -3e38f, l = 0.f;           // m in units of the raw scores; m c stays finite
+  float m = a.m0, l = 0.f;                                    // m in units of the raw scores
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -576,49 +585,49 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
 #pragma unroll
     for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sc, 0, 0, 0);
   };
-  // N tiles' scores (register r of a tile: key kb + 16 (r / 8) + 8 h + r % 8) to probabilities, statistics and accumulators brought up
-  auto softmax = [&](auto& sc, auto& pf, int kb, auto masked) {
-    constexpr int N = sizeof(sc) / sizeof(f32x16);
+  // A tile's scores (register r: key kb + 16 (r / 8) + 8 h + r % 8) to probabilities; statistics and accumulators brought up.
+  auto softmax = [&](f32x16& sc, bf16x8* pf, int kb, auto masked) {
     if constexpr (masked) {
-      static_assert(N == 1, "masked tiles come one at a time");
       const int seen = min(it.key_end - 1, lim) - kb - 8 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[0][r] = 16 * (r >> 3) + (r & 7) <= seen ? sc[0][r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) sc[r] = 16 * (r >> 3) + (r & 7) <= seen ? sc[r] : -INFINITY;
     }
-    float mx = sc[0][0];
+    // The reference m only has to keep 2^(c (s - m)) in range.  So no maximum is sought: the probabilities are formed with the m
+    // there is, and their sum, which is wanted anyway, tells whether some score is far above it (the first tile, then hardly ever).
+    float p[16], t;
+    auto form = [&]() {
+      const float mc = m * c;
+      float t0 = 0.f, t1 = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[n][r]);
-    mx = both_max(mx);
-    // The reference only has to keep 2^(c (s - m)) in range: it moves when a score exceeds it by more than 2^8.
-    const float m_new = (mx - m) * c > 8.0f ? mx : m;
-    const float alpha = sh_ex2((m - m_new) * c), mc = m_new * c;
-    m = m_new;
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
-    }
-    float t0 = 0.f, t1 = 0.f;
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      float p[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = sh_ex2(fmaf(sc[n][r], c, -mc));
+      for (int r = 0; r < 16; ++r) p[r] = sh_ex2(fmaf(sc[r], c, -mc));
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         t0 += p[r];
         t1 += p[r + 1];
       }
+      t = t0 + t1;
+    };
+    form();
+    if (__builtin_amdgcn_ballot_w64(!(t < 4096.0f)) != 0) {
+      float mx = sc[0];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-        pf[n][b] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf2(p[8 * b], p[8 * b + 1]), pack_bf2(p[8 * b + 2], p[8 * b + 3]),
-                                                         pack_bf2(p[8 * b + 4], p[8 * b + 5]), pack_bf2(p[8 * b + 6], p[8 * b + 7])));
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      mx = both_max(mx);
+      const float m_new = (mx - m) * c > 8.0f ? mx : m;
+      const float alpha = sh_ex2((m - m_new) * c);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+      form();
     }
-    l += t0 + t1;
+    l += t;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      pf[b] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf2(p[8 * b], p[8 * b + 1]), pack_bf2(p[8 * b + 2], p[8 * b + 3]),
+                                                    pack_bf2(p[8 * b + 4], p[8 * b + 5]), pack_bf2(p[8 * b + 6], p[8 * b + 7])));
   };
   auto values = [&](const bf16x8* pf, int kb, auto masked) {
     if constexpr (masked) {
@@ -680,14 +689,14 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
     // No other wavefront touches this ring: K slots are filled again as soon as the scores' operands are in registers.
     auto tile = [&](int i, auto masked) {
       const int kb = it.key_begin + 32 * (i * WK + kp);
-      f32x16 sc[1];
-      bf16x8 pf[1][2];
+      f32x16 sc;
+      bf16x8 pf[2];
       wait_positions<IPP, 3>(issued - (4 * i + 2));
       read_k(take);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (issued < n_pos) issue(next[0]);
       if (issued < n_pos) issue(next[1]);
-      scores(sc[0]);
+      scores(sc);
       softmax(sc, pf, kb, masked);
       next[0] = page_of(4 * i + 9);
       next[1] = page_of(4 * i + 10);
@@ -698,7 +707,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
       if (issued < n_pos) issue(next[3]);
       next[2] = page_of(4 * i + 11);
       next[3] = page_of(4 * i + 12);
-      values(pf[0], kb, masked);
+      values(pf, kb, masked);
       take = wrap(take + 4 * SLOT_B);
     };
     for (int i = 0; i < my_free; ++i) tile(i, std::false_type());
@@ -718,13 +727,13 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
     auto tile = [&](int i, auto masked) {
       begin(i, std::integral_constant<int, 1>());
       const int kb = it.key_begin + 32 * (i * WK + kp);
-      f32x16 sc[1];
-      bf16x8 pf[1][2];
+      f32x16 sc;
+      bf16x8 pf[2];
       read_k(take);
-      scores(sc[0]);
+      scores(sc);
       read_v(take);
       softmax(sc, pf, kb, masked);
-      values(pf[0], kb, masked);
+      values(pf, kb, masked);
       take = wrap(take + PPT * SLOT_B);
     };
     int i = 0;
@@ -734,16 +743,17 @@ __device__ __forceinline__ void attend(const SharedAttnArgs& a, const ShItem& it
         begin(i, std::integral_constant<int, 2>());
         const uint32_t second = wrap(take + SLOT_B);
         f32x16 sc[2];
-        bf16x8 pf[2][2];
+        bf16x8 pf[2];
         read_k(take);
         scores(sc[0]);
         read_k(second);
         scores(sc[1]);
         read_v(take);
-        softmax(sc, pf, 0, std::false_type());
-        values(pf[0], 0, std::false_type());
+        softmax(sc[0], pf, 0, std::false_type());
+        values(pf, 0, std::false_type());
         read_v(second);
-        values(pf[1], 0, std::false_type());
+        softmax(sc[1], pf, 0, std::false_type());
+        values(pf, 0, std::false_type());
         take = wrap(second + SLOT_B);
       }
     else
@@ -927,6 +937,7 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   a.part_ml = b->part_ml;
   a.lse = d_lse;
   a.c = (scale > 0.f ? scale : 1.0f / sqrtf((float)l.hd)) * 1.4426950408889634f;
+  a.m0 = a.c > 1.f ? -3e38f / a.c : -3e38f;
   a.Hq = l.Hq;
   a.Hkv = l.Hkv;
   a.G = l.Hq / l.Hkv;

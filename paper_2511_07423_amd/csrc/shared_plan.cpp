@@ -63,14 +63,13 @@ extern "C" int32_t synera_validate_shared(int32_t B, const int32_t* h_ctx_len, c
 }
 
 // ------------------------------------------------------------------------------------ capacities
-// What the work is cut for, in blocks.  Items of many rows: two for each place on the chip, so that no block's last one holds up
-// the launch; of up to 32 rows, whose keys are the work: one for each place, or four wavefronts'.
-static int64_t item_target(const ShLimits& l) { return 2 * (int64_t)l.slots; }
-#ifndef SH_MIN_BLOCK
-#define SH_MIN_BLOCK 256
-#define SH_MIN_WAVE 256
-#define SH_WAVES_MOST 4
-#endif
+// Ranges that one launch may be cut into beyond one for each node, tile of rows and KV head: enough for every rule of sh_plan.
+static int64_t most_cuts(const ShLimits& l) { return 4 * (int64_t)l.slots; }
+#define SH_MIN_BLOCK 256         // keys that a block's range has at least: the rings are barely filled below
+#define SH_MIN_WAVE 128          // a wavefront's: one request of 900 tokens 14 us, with at least 256 18 us
+#define SH_WAVES_MOST 4          // ranges that a node is cut into for wavefronts alone
+#define SH_KEYS_A_ROW 16         // keys a range has for each row whose partial result it leaves
+#define SH_KEYS_A_CUT 400        // what one more range costs blocks of many rows, in keys: their beginning and their partial results
 
 void sh_limits(ShLimits& l) {
   const int64_t G = l.Hq / l.Hkv, rows = (int64_t)l.max_tokens * G;        // per KV head
@@ -79,12 +78,10 @@ void sh_limits(ShLimits& l) {
   l.shared_rows = std::min<int64_t>(2 * rows, ((int64_t)1 << 18) / l.Hkv);
   l.list = l.shared_rows / G;
   l.pages = (int64_t)l.max_batch * l.max_pages;
-  // A node is cut into at most keys x cost / share + 1 ranges (shares are rounded down to whole keys, by less than 1/128): for all
-  // nodes as many more as the target has blocks of SY_SH_TILE_ROWS rows, or twice as many wavefronts' of a quarter of the rows.  Twice
-  // their rows in partial results: the first range of a node that is cut needs them too.
-  const int64_t extra = item_target(l) + item_target(l) / 64 + 64;
-  l.items = (2 * (int64_t)l.max_batch + (rows + l.shared_rows) / SY_SH_TILE_ROWS + 2) * l.Hkv + 2 * extra + 5 * SY_SH_DEAL;
-  l.part_rows = (l.shared_rows + std::min<int64_t>(rows, l.shared_rows)) * l.Hkv + 2 * extra * SY_SH_TILE_ROWS;
+  // Partial results: of shared nodes and of the rows behind them, and twice those of the ranges that nodes are cut into (the first range of
+  // a node that is cut needs them too).
+  l.items = (2 * (int64_t)l.max_batch + (rows + l.shared_rows) / SY_SH_TILE_ROWS + 2) * l.Hkv + most_cuts(l) + 5 * SY_SH_DEAL;
+  l.part_rows = (l.shared_rows + std::min<int64_t>(rows, l.shared_rows)) * l.Hkv + 2 * most_cuts(l) * SY_SH_TILE_ROWS;
   l.parts = l.part_rows / l.Hkv;
 }
 
@@ -208,23 +205,46 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
     c.w = key_cost(c.rows) / (double)c.tiles;
     total += key_cost(c.rows) * (double)c.keys * l.Hkv;
   }
-  const double share = total / (double)item_target(l);
+  // An equal share for each block that runs at once.  (Two each, so that no block's last one holds up the launch: twice the partial
+  // results; 256 requests behind 8192 shared tokens 97 -> 105 us, 64 chunks of 16 behind 1000 of their own 55 -> 79.)
+  const double share = total / (double)l.slots;
   std::vector<int64_t> n_parts(B, 0);            // ranges of keys that are read for a request's rows
+  int64_t cuts = 0;
   for (size_t k = 0; k < N; ++k) {
     Cut& c = cut[k];
-    int64_t chunk;
+    int64_t splits;
     c.wave = false;
     if (c.rows <= SY_SH_WAVE_ROWS) {
-      const int64_t wave_chunk = std::max<int64_t>(SH_MIN_WAVE, (int64_t)(share / 2));
+      // Keys are the work.  A wavefront alone, four to a block, where that makes a few ranges; else a block's four together.
+      // (64 requests of 32 rows behind 1000 tokens: 67 -> 61 us; where there is little work the rings of all units count more)
+      const int64_t least = std::min<int64_t>(SH_KEYS_A_ROW * c.rows, (int64_t)(share / 2));
+      const int64_t wave_chunk = std::max<int64_t>({SH_MIN_WAVE, least, (int64_t)(share / 4)});
       c.wave = c.keys <= SH_WAVES_MOST * wave_chunk;
-      chunk = c.wave ? wave_chunk : std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(2 * share));
+      const int64_t chunk = c.wave ? wave_chunk : std::max<int64_t>({SH_MIN_BLOCK, least, (int64_t)(2 * share)});
+      splits = (c.keys + chunk - 1) / chunk;
     } else {
-      chunk = std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(share / c.w));
+      const int64_t chunk = std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(share / c.w));
+      splits = (c.keys + chunk - 1) / chunk;
+      if (2 * key_cost(c.rows) * (double)c.keys * l.Hkv > total) {
+        // Most of the launch are equal blocks of this node: as many ranges as leave the last round of blocks fullest, each at
+        // its price.  (8 prompts of 64 heads behind 16384 tokens, 103 tiles: 3 ranges 915 us, 2 930, 5 930, 1 995.)
+        double best = 1e300;
+        for (int64_t s = 1; s <= c.keys / SH_MIN_BLOCK && s <= 16 && (s == 1 || s * c.tiles * l.Hkv <= 8 * (int64_t)l.slots); ++s) {
+          const int64_t rounds = (s * c.tiles * l.Hkv + l.slots - 1) / l.slots;
+          const double t = (double)rounds * ((double)c.keys / (double)s + SH_KEYS_A_CUT);
+          if (t < best) {
+            best = t;
+            splits = s;
+          }
+        }
+      }
     }
-    c.splits = (c.keys + chunk - 1) / chunk;
-    c.chunk = (c.keys + c.splits - 1) / c.splits;                         // even shares
+    // (capacity: the rules above stay within it but for shares of very many tiny nodes)
+    splits = std::max<int64_t>(1, std::min(splits, 1 + (most_cuts(l) - cuts) / (c.tiles * l.Hkv)));
+    c.chunk = (c.keys + splits - 1) / splits;                             // even shares
     c.chunk = (c.chunk + SY_SH_STEP - 1) / SY_SH_STEP * SY_SH_STEP;
     c.splits = (c.keys + c.chunk - 1) / c.chunk;
+    cuts += (c.splits - 1) * c.tiles * l.Hkv;
     for (int i : nodes[k].who) n_parts[i] += c.splits;
   }
 
@@ -274,6 +294,13 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
   }
   p.head.n_joined = (int32_t)p.joined.size();
 
+  // Keys and values that one item alone reads, and that no cache will hold until the next call, are read as such: 256 requests of 64 .. 1024
+  // tokens (373 MB) 80 -> 72 us.  Where the last-level cache held them between the calls it costs: 16 requests (80 MB) 22.2 -> 24.2 us.
+  int64_t alone = 0;
+  for (size_t k = 0; k < N; ++k)
+    if (nodes[k].leaf && cut[k].tiles == 1) alone += cut[k].keys * l.Hkv * l.hd * 4;
+  const bool once = alone > ((int64_t)96 << 20);
+
   // ---- items.  Ranges of keys, the costliest first, go to the least loaded of eight queues, with all the tiles of rows that read
   // them: blocks are dealt to the eight XCDs in turn, so these meet in one L2.
   struct Range { double cost; int32_t node, head; int64_t split; };
@@ -292,7 +319,7 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
     const Cut& c = cut[r.node];
     const int i0 = n.who[0];
     ShItem it = {};
-    it.flags = n.leaf ? SY_SH_LEAF : 0;
+    it.flags = (n.leaf ? SY_SH_LEAF : 0) | (n.leaf && c.tiles == 1 && once ? SY_SH_ONCE : 0);
     it.kv_head = r.head;
     it.row0 = (int32_t)(t * SY_SH_TILE_ROWS);
     it.n_rows = (int32_t)std::min<int64_t>(SY_SH_TILE_ROWS, c.rows - it.row0);
