@@ -845,49 +845,57 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedAttnArgs a) {
 }
 
 // Joins the partial results of rows that several items worked on: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A thread takes four
-// values of one row; JOIN_FLY partials are asked for together, behind two dependent loads.
-#define JOIN_FLY 8
+// values of one row; FLY partials (no more than the token has, but for the last round) are asked for together, behind two
+// dependent loads.
+template <int HD, int FLY>
+__device__ __forceinline__ void join_token(const SharedAttnArgs& a, const ShJoin& jn, const int head, const int d4) {
+  const int kh = head / a.G, g = head % a.G;
+  float M = -3e38f, l = 0.f;
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < jn.count; s0 += FLY) {
+    float2 ml[FLY];
+    float4 v[FLY];
+    ShPart part[FLY];
+#pragma unroll
+    for (int s = 0; s < FLY; ++s) part[s] = a.parts[jn.first + min(s0 + s, jn.count - 1)];
+#pragma unroll
+    for (int s = 0; s < FLY; ++s) {
+      const size_t at = (size_t)part[s].row + (size_t)kh * part[s].step + g;
+      ml[s] = a.part_ml[at];
+      v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
+    }
+    float top = M;
+#pragma unroll
+    for (int s = 0; s < FLY; ++s) top = fmaxf(top, ml[s].x);
+    const float f = sh_ex2(M - top);
+    M = top;
+    l *= f;
+    sum.x *= f; sum.y *= f; sum.z *= f; sum.w *= f;
+#pragma unroll
+    for (int s = 0; s < FLY; ++s)
+      if (s0 + s < jn.count) {
+        const float w = sh_ex2(ml[s].x - M);
+        l += ml[s].y * w;
+        sum.x += v[s].x * w; sum.y += v[s].y * w; sum.z += v[s].z * w; sum.w += v[s].w * w;
+      }
+  }
+  const float inv = 1.0f / l;
+  *reinterpret_cast<uint2*>(a.o + (int64_t)jn.tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
+      make_uint2(pack_bf2(sum.x * inv, sum.y * inv), pack_bf2(sum.z * inv, sum.w * inv));
+  if (a.lse && d4 == 0) a.lse[(size_t)jn.tok * a.Hq + head] = (M + __log2f(l)) * 0.69314718055994531f;
+}
+
 template <int HD>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a, int n_joined) {
   const int n = n_joined >= 0 ? n_joined : a.head->n_joined;
   const int piece = blockIdx.y * 256 + threadIdx.x;
   if (piece >= a.Hq * (HD / 4)) return;
-  const int head = piece / (HD / 4), d4 = piece % (HD / 4) * 4, kh = head / a.G, g = head % a.G;
+  const int head = piece / (HD / 4), d4 = piece % (HD / 4) * 4;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const ShJoin jn = a.joined[i];
-    float M = -3e38f, l = 0.f;
-    float4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < jn.count; s0 += JOIN_FLY) {
-      float2 ml[JOIN_FLY];
-      float4 v[JOIN_FLY];
-      ShPart part[JOIN_FLY];
-#pragma unroll
-      for (int s = 0; s < JOIN_FLY; ++s) part[s] = a.parts[jn.first + min(s0 + s, jn.count - 1)];
-#pragma unroll
-      for (int s = 0; s < JOIN_FLY; ++s) {
-        const size_t at = (size_t)part[s].row + (size_t)kh * part[s].step + g;
-        ml[s] = a.part_ml[at];
-        v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
-      }
-      float top = M;
-#pragma unroll
-      for (int s = 0; s < JOIN_FLY; ++s) top = fmaxf(top, ml[s].x);
-      const float f = sh_ex2(M - top);
-      M = top;
-      l *= f;
-      sum.x *= f; sum.y *= f; sum.z *= f; sum.w *= f;
-#pragma unroll
-      for (int s = 0; s < JOIN_FLY; ++s)
-        if (s0 + s < jn.count) {
-          const float w = sh_ex2(ml[s].x - M);
-          l += ml[s].y * w;
-          sum.x += v[s].x * w; sum.y += v[s].y * w; sum.z += v[s].z * w; sum.w += v[s].w * w;
-        }
-    }
-    const float inv = 1.0f / l;
-    *reinterpret_cast<uint2*>(a.o + (int64_t)jn.tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
-        make_uint2(pack_bf2(sum.x * inv, sum.y * inv), pack_bf2(sum.z * inv, sum.w * inv));
-    if (a.lse && d4 == 0) a.lse[(size_t)jn.tok * a.Hq + head] = (M + __log2f(l)) * 0.69314718055994531f;
+    if (jn.count <= 2) join_token<HD, 2>(a, jn, head, d4);
+    else if (jn.count <= 4) join_token<HD, 4>(a, jn, head, d4);
+    else join_token<HD, 8>(a, jn, head, d4);
   }
 }
 

@@ -2,7 +2,9 @@
 // work into items.  No HIP call, no arithmetic of the method.
 #include <algorithm>
 #include <cstring>
+#include <functional>
 #include <new>
+#include <queue>
 
 #include "shared.h"
 
@@ -69,7 +71,10 @@ static int64_t most_cuts(const ShLimits& l) { return 4 * (int64_t)l.slots; }
 #define SH_MIN_WAVE 128          // a wavefront's: one request of 900 tokens 14 us, with at least 256 18 us
 #define SH_WAVES_MOST 4          // ranges that a node is cut into for wavefronts alone
 #define SH_KEYS_A_ROW 16         // keys a range has for each row whose partial result it leaves
-#define SH_KEYS_A_CUT 400        // what one more range costs blocks of many rows, in keys: their beginning and their partial results
+#define SH_JOIN_BYTES 16e6
+#define SH_UNCUT_KEYS 512        // up to here no range is worth the launch that joins the parts: 8 requests of 300 tokens 12.5 -> 10.2 us
+#define SH_KEYS_AN_ITEM 100      // what it takes to begin an item of many rows, in keys
+#define SH_KEYS_A_CUT 400        // that, and its partial results
 
 void sh_limits(ShLimits& l) {
   const int64_t G = l.Hq / l.Hkv, rows = (int64_t)l.max_tokens * G;        // per KV head
@@ -176,10 +181,10 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
       apart += key_cost(t * G);
       parts.push_back(std::move(part));
     }
-    // One pass for all leaves a partial of each row (4 hd + 8 bytes: what a key and its value take), which is read again.
-    const double keys = (double)(at - s.first) * P;
-    const bool split = at > s.first && (apart - key_cost(tokens * G)) * keys > 2.0 * (double)(tokens * G) + 128.0 &&
-                       shared_rows + tokens * G <= l.shared_rows;
+    // One pass for all leaves a partial of each row (4 hd + 8 bytes: what a key and its value take), which is read again, in a
+    // launch of its own: 3 us at least, or SH_JOIN_BYTES of keys and values.
+    const double keys = (double)(at - s.first) * P, saved = (apart - key_cost(tokens * G)) * keys - 2.0 * (double)(tokens * G);
+    const bool split = at > s.first && saved * l.Hkv * l.hd * 4 > SH_JOIN_BYTES && shared_rows + tokens * G <= l.shared_rows;
     for (Open& part : parts) {
       if (split) part.first = at;
       open.push_back(std::move(part));
@@ -208,37 +213,69 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
   // An equal share for each block that runs at once.  (Two each, so that no block's last one holds up the launch: twice the partial
   // results; 256 requests behind 8192 shared tokens 97 -> 105 us, 64 chunks of 16 behind 1000 of their own 55 -> 79.)
   const double share = total / (double)l.slots;
+  // Nothing is cut where nothing is shared and no request is much longer than the share: each block takes one.  (64 requests of 32 rows
+  // behind 1000 tokens 56 -> 49 us.)
+  bool uncut = (int64_t)N * l.Hkv <= l.slots;
+  for (size_t k = 0; k < N; ++k)
+    uncut = uncut && nodes[k].leaf && cut[k].rows <= SY_SH_WAVE_ROWS && (double)cut[k].keys <= std::max((double)SH_UNCUT_KEYS, 1.15 * share);
+  // Where tiles of many rows fill the chip several times over, how full the last time is counts: a few lengths are tried, the costliest
+  // items handed out first.  (8 prompts of 64 heads behind 16384 tokens, 848 tiles: 3 ranges 880 us, 1 950 us.)
+  double wide = 0;
+  int64_t wide_tiles = 0, longest = 0;
+  for (const Cut& c : cut)
+    if (c.rows > SY_SH_WAVE_ROWS) {
+      wide += key_cost(c.rows) * (double)c.keys * l.Hkv;
+      wide_tiles += c.tiles * l.Hkv;
+      longest = std::max(longest, c.keys);
+    }
+  int64_t wide_chunk = 0;
+  if (2 * wide > total && wide_tiles >= l.slots && wide_tiles <= 8 * (int64_t)l.slots) {
+    double best = 1e300;
+    for (int64_t s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32, 48, 64}) {
+      const int64_t chunk = (longest + s - 1) / s;
+      if (s > 1 && (chunk < SH_MIN_BLOCK || (s - 1) * wide_tiles > most_cuts(l))) break;
+      std::vector<std::pair<double, int64_t>> sizes;
+      for (const Cut& c : cut)
+        if (c.rows > SY_SH_WAVE_ROWS) {
+          const int64_t n = (c.keys + chunk - 1) / chunk;
+          sizes.emplace_back(c.w * ((double)c.keys / (double)n + (n > 1 ? SH_KEYS_A_CUT : SH_KEYS_AN_ITEM)), n * c.tiles * l.Hkv);
+        }
+      std::sort(sizes.rbegin(), sizes.rend());
+      std::priority_queue<double, std::vector<double>, std::greater<double>> place;
+      for (int64_t i = 0; i < l.slots; ++i) place.push(0);
+      double end = 0;
+      for (const auto& [size, n] : sizes)
+        for (int64_t i = 0; i < n; ++i) {
+          const double t = place.top() + size;
+          place.pop();
+          place.push(t);
+          end = std::max(end, t);
+        }
+      if (end < best) {
+        best = end;
+        wide_chunk = chunk;
+      }
+    }
+  }
   std::vector<int64_t> n_parts(B, 0);            // ranges of keys that are read for a request's rows
   int64_t cuts = 0;
   for (size_t k = 0; k < N; ++k) {
     Cut& c = cut[k];
-    int64_t splits;
     c.wave = false;
-    if (c.rows <= SY_SH_WAVE_ROWS) {
+    int64_t chunk;
+    if (uncut) {
+      chunk = c.keys;
+    } else if (c.rows <= SY_SH_WAVE_ROWS) {
       // Keys are the work.  A wavefront alone, four to a block, where that makes a few ranges; else a block's four together.
       // (64 requests of 32 rows behind 1000 tokens: 67 -> 61 us; where there is little work the rings of all units count more)
       const int64_t least = std::min<int64_t>(SH_KEYS_A_ROW * c.rows, (int64_t)(share / 2));
       const int64_t wave_chunk = std::max<int64_t>({SH_MIN_WAVE, least, (int64_t)(share / 4)});
       c.wave = c.keys <= SH_WAVES_MOST * wave_chunk;
-      const int64_t chunk = c.wave ? wave_chunk : std::max<int64_t>({SH_MIN_BLOCK, least, (int64_t)(2 * share)});
-      splits = (c.keys + chunk - 1) / chunk;
+      chunk = c.wave ? wave_chunk : std::max<int64_t>({SH_MIN_BLOCK, least, (int64_t)(2 * share)});
     } else {
-      const int64_t chunk = std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(share / c.w));
-      splits = (c.keys + chunk - 1) / chunk;
-      if (2 * key_cost(c.rows) * (double)c.keys * l.Hkv > total) {
-        // Most of the launch are equal blocks of this node: as many ranges as leave the last round of blocks fullest, each at
-        // its price.  (8 prompts of 64 heads behind 16384 tokens, 103 tiles: 3 ranges 915 us, 2 930, 5 930, 1 995.)
-        double best = 1e300;
-        for (int64_t s = 1; s <= c.keys / SH_MIN_BLOCK && s <= 16 && (s == 1 || s * c.tiles * l.Hkv <= 8 * (int64_t)l.slots); ++s) {
-          const int64_t rounds = (s * c.tiles * l.Hkv + l.slots - 1) / l.slots;
-          const double t = (double)rounds * ((double)c.keys / (double)s + SH_KEYS_A_CUT);
-          if (t < best) {
-            best = t;
-            splits = s;
-          }
-        }
-      }
+      chunk = wide_chunk ? wide_chunk : std::max<int64_t>(SH_MIN_BLOCK, (int64_t)(share / c.w));
     }
+    int64_t splits = (c.keys + chunk - 1) / chunk;
     // (capacity: the rules above stay within it but for shares of very many tiny nodes)
     splits = std::max<int64_t>(1, std::min(splits, 1 + (most_cuts(l) - cuts) / (c.tiles * l.Hkv)));
     c.chunk = (c.keys + splits - 1) / splits;                             // even shares

@@ -128,9 +128,10 @@ def test_plan_shares_where_it_is_shorter():
     shared_items = pl["items"][((pl["items"][:, 0] & 1) == 0) & (pl["items"][:, 2] > 0)]
     assert len(pl["pages"]) == shared + B and len(pl["list"]) == B
     assert {int(r) for r in shared_items[:, 2]} == {128}       # 64 x 4 rows are two full tiles
-    # two levels: halves of the batch share more
-    table2 = table.copy()
-    ctx2 = ctx + 64 * P
+    # two levels: behind 9600 common tokens, halves of the batch share more
+    shared = 600
+    table = np.concatenate([np.tile(np.arange(shared), (B, 1)), 3000 + np.arange(B)[:, None]], 1).astype(np.int32)
+    ctx2 = np.full(B, (shared + 64) * P + 5, np.int32)
     more = np.concatenate([np.tile(1000 + np.arange(64), (B // 2, 1)), np.tile(2000 + np.arange(64), (B // 2, 1))])
     table2 = np.concatenate([table[:, :shared], more, table[:, shared:]], 1).astype(np.int32)
     pl = check_plan(32, 8, 512, ctx2, np.ones(B, np.int32), table2)
