@@ -581,28 +581,40 @@ _HEAD_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 
 
+def _head_type(dtype):
+    if dtype not in _HEAD_TYPES:
+        raise ValueError(f"f32, bf16 or f16: got {dtype}")
+    return _HEAD_TYPES[dtype]
+
+
 def _raw_stream(index):
     """The current stream of a device, as _stream() without the object around it."""
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _heads(x, out, gain, index, name):
-    """The synera_heads of x and out (or None), [tokens][heads][head_dim] with the values of a head side by side."""
+def _heads(x, out, gain, dtype, n, n_heads, hd, index, name, out_dtype=None, exact=True):
+    """(synera_heads of x and out, out): x [n or, with exact unset, more][n_heads or, if None, any][hd] of `dtype` with the values of a
+    head side by side.  out: a tensor of x's shape, None for a new one of out_dtype, False for none."""
     shape, strides = x.shape, x.stride()
-    if len(shape) != 3 or (strides[2] != 1 and shape[2] > 1) or x.get_device() != index:
-        raise ValueError(f"{name}: expected [tokens, heads, head_dim] on cuda:{index}, the values of a head side by side")
-    at_out, out_strides = 0, strides
-    if out is not None:
-        out_strides = out.stride()
-        if out.shape != shape or (out_strides[2] != 1 and shape[2] > 1) or out.get_device() != index:
-            raise ValueError(f"{name}: the output is a tensor on cuda:{index} of the input's shape {tuple(shape)}, the values of a head side by side")
-        at_out = out.data_ptr()
+    if x.dtype != dtype or len(shape) != 3 or shape[2] != hd or (shape[0] != n if exact else shape[0] < n) or \
+            (n_heads is not None and shape[1] != n_heads) or (strides[2] != 1 and hd > 1) or x.get_device() != index:
+        raise ValueError(f"{name}: expected {dtype} [{'' if exact else '>= '}{n}, {n_heads or 'heads'}, {hd}] on cuda:{index}, the values of a "
+                         f"head side by side; got {x.dtype} {tuple(shape)}, strides {strides}, on {x.device}")
     at_gain = 0
     if gain is not None:
         if gain.dtype != torch.bfloat16 or gain.shape != shape[2:] or not gain.is_contiguous() or gain.get_device() != index:
-            raise ValueError(f"{name}: gains are bf16 [head_dim] on cuda:{index}")
+            raise ValueError(f"{name}: gains are bf16 [{hd}] on cuda:{index}")
         at_gain = gain.data_ptr()
-    return _pack_heads(x.data_ptr(), at_out, at_gain, shape[1], strides[0], strides[1], out_strides[0], out_strides[1])
+    if out is False:
+        return _pack_heads(x.data_ptr(), 0, at_gain, shape[1], strides[0], strides[1], 0, 0), None
+    if out is None:
+        out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
+        return _pack_heads(x.data_ptr(), out.data_ptr(), at_gain, shape[1], strides[0], strides[1], shape[1] * hd, hd), out
+    out_strides = out.stride()
+    if out.shape != shape or out.dtype != (out_dtype or dtype) or (out_strides[2] != 1 and hd > 1) or out.get_device() != index:
+        raise ValueError(f"{name}: the output is {out_dtype or dtype} {tuple(shape)} on cuda:{index}, the values of a head side by side; "
+                         f"got {out.dtype} {tuple(out.shape)}, strides {out_strides}, on {out.device}")
+    return _pack_heads(x.data_ptr(), out.data_ptr(), at_gain, shape[1], strides[0], strides[1], out_strides[0], out_strides[1]), out
 
 
 class Rope:
@@ -641,43 +653,33 @@ class Rope:
         except Exception:
             pass
 
-    def _one(self, x, out, gain, dtype, n, name):
-        if x.dtype != dtype or x.dim() != 3 or x.shape[0] != n or x.shape[2] != self.head_dim:
-            raise ValueError(f"{name}: expected {dtype} [{n}, heads, {self.head_dim}], got {x.dtype} {tuple(x.shape)}")
-        if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        elif out.dtype != dtype:
-            raise ValueError(f"{name}: the output's type is the input's, {dtype}: got {out.dtype}")
-        return _heads(x, out, gain, self._index, name), out
-
-    def _turn(self, pos, q, k, q_gain, k_gain, eps, out_q, out_k):
+    def _positions(self, pos):
         if pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous() or pos.get_device() != self._index:
             raise ValueError(f"positions are a contiguous int32 vector on {self.device}")
-        dtype, n = q.dtype, pos.numel()
-        if dtype not in _HEAD_TYPES:
-            raise ValueError(f"f32, bf16 or f16: got {dtype}")
-        hq, out_q = self._one(q, out_q, q_gain, dtype, n, "q")
-        hk = None
-        if k is not None:
-            hk, out_k = self._one(k, out_k, k_gain, dtype, n, "k")
-        if eps is None:
-            st = _lib.synera_rope_apply(self._h, _HEAD_TYPES[dtype], n, pos.data_ptr(), hq, hk, _raw_stream(self._index))
-            _check(st, "synera_rope_apply")
-        else:
-            st = _lib.synera_qk_norm_rope(self._h, _HEAD_TYPES[dtype], n, pos.data_ptr(), hq, hk, eps, _raw_stream(self._index))
-            _check(st, "synera_qk_norm_rope")
-        return out_q, out_k if k is not None else None
+        return pos.numel()
 
     def apply(self, pos, q, k=None, out_q=None, out_k=None):
         """q [T, Hq, head_dim] and k [T, Hk, head_dim] (or None) turned by their positions (int32 [T]) -> (q, k), new tensors
         unless out_q / out_k are given (q and k themselves for in place)."""
-        return self._turn(pos, q, k, None, None, None, out_q, out_k)
+        n, dtype, hd, index = self._positions(pos), q.dtype, self.head_dim, self._index
+        hk, out_k = (None, None) if k is None else _heads(k, out_k, None, dtype, n, None, hd, index, "k")
+        hq, out_q = _heads(q, out_q, None, dtype, n, None, hd, index, "q")
+        st = _lib.synera_rope_apply(self._h, _head_type(dtype), n, pos.data_ptr(), hq, hk, _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_rope_apply")
+        return out_q, out_k
 
     def norm_apply(self, pos, q, k, q_gain, k_gain, eps, out_q=None, out_k=None):
         """The same behind an RMS norm of each head with bf16 gains [head_dim]."""
         if q_gain is None or (k is not None and k_gain is None):
             raise ValueError("norm_apply needs the gains")
-        return self._turn(pos, q, k, q_gain, k_gain, eps, out_q, out_k)
+        n, dtype, hd, index = self._positions(pos), q.dtype, self.head_dim, self._index
+        hk, out_k = (None, None) if k is None else _heads(k, out_k, k_gain, dtype, n, None, hd, index, "k")
+        hq, out_q = _heads(q, out_q, q_gain, dtype, n, None, hd, index, "q")
+        st = _lib.synera_qk_norm_rope(self._h, _head_type(dtype), n, pos.data_ptr(), hq, hk, eps, _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_qk_norm_rope")
+        return out_q, out_k
 
 
 def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max_tokens):
@@ -732,50 +734,35 @@ class SharedBatch:
             raise ValueError(f"expected one layer's pool, bf16 [>= {self.n_pages}, {tile[0]}, {tile[1]}, {tile[2]}] on {self.device}, contiguous")
         return pool.data_ptr()
 
-    def _rows(self, x, dtype, heads, name):
-        shape = x.shape
-        if x.dtype != dtype or len(shape) != 3 or shape[0] < self.n_tokens or shape[1] != heads or shape[2] != self.head_dim:
-            raise ValueError(f"{name}: expected {dtype} [>= {self.n_tokens}, {heads}, {self.head_dim}], got {x.dtype} {tuple(shape)}")
-
     def append_rope(self, rope, q, k, v, k_pool, v_pool, q_gain=None, k_gain=None, eps=1e-5, out_q=None):
         """One layer's new tokens (rows of q, k, v in the batch's order; f32, bf16 or f16): keys turned (and normed, with k_gain)
         into their pages, values into theirs, queries turned into out_q (bf16, new if None) -> out_q; q may be None."""
-        dtype = k.dtype
-        if dtype not in _HEAD_TYPES:
-            raise ValueError(f"f32, bf16 or f16: got {dtype}")
-        self._rows(k, dtype, self.n_kv_heads, "k")
-        self._rows(v, dtype, self.n_kv_heads, "v")
+        dtype, n, hd, index, hkv = k.dtype, self.n_tokens, self.head_dim, self._index, self.n_kv_heads
+        hk, _ = _heads(k, False, k_gain, dtype, n, hkv, hd, index, "k", None, False)
+        hv, _ = _heads(v, False, None, dtype, n, hkv, hd, index, "v", None, False)
         hq = None
         if q is not None:
-            self._rows(q, dtype, self.n_q_heads, "q")
-            if out_q is None:
-                out_q = torch.empty_like(q, dtype=torch.bfloat16, memory_format=torch.contiguous_format)
-            elif out_q.dtype != torch.bfloat16:
-                raise ValueError("out_q is bf16")
-            hq = _heads(q, out_q, q_gain, self._index, "q")
-        st = _lib.synera_append_rope(self._h, rope._h, _HEAD_TYPES[dtype], hq, _heads(k, None, k_gain, self._index, "k"),
-                                     _heads(v, None, None, self._index, "v"), eps, self._pool(k_pool, self._tiles[0]),
-                                     self._pool(v_pool, self._tiles[1]), _raw_stream(self._index))
-        _check(st, "synera_append_rope")
+            hq, out_q = _heads(q, out_q, q_gain, dtype, n, self.n_q_heads, hd, index, "q", torch.bfloat16, False)
+        st = _lib.synera_append_rope(self._h, rope._h, _head_type(dtype), hq, hk, hv, eps, self._pool(k_pool, self._tiles[0]),
+                                     self._pool(v_pool, self._tiles[1]), _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_append_rope")
         return out_q
 
     def attention(self, q, k_pool, v_pool, scale=None, out=None, want_lse=False):
         """softmax(scale q K^T) V of one layer over the planned batch: q bf16 [T, Hq, head_dim], turned; scale None: 1/sqrt(head_dim)
         -> o bf16 (out, new if None), or (o, lse f32 [T, Hq])."""
-        self._rows(q, torch.bfloat16, self.n_q_heads, "q")
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        elif out.dtype != torch.bfloat16:
-            raise ValueError("out is bf16")
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
         if scale is None:
             scale = 0.0
         elif not scale > 0:
             raise ValueError("scale is positive")
-        st = _lib.synera_shared_attention(self._h, _heads(q, out, None, self._index, "q"), self._pool(k_pool, self._tiles[0]),
-                                          self._pool(v_pool, self._tiles[1]), scale, lse.data_ptr() if want_lse else None,
-                                          _raw_stream(self._index))
-        _check(st, "synera_shared_attention")
+        index = self._index
+        h, out = _heads(q, out, None, torch.bfloat16, self.n_tokens, self.n_q_heads, self.head_dim, index, "q", None, False)
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
+        st = _lib.synera_shared_attention(self._h, h, self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1]), scale,
+                                          lse.data_ptr() if want_lse else None, _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_shared_attention")
         return (out, lse) if want_lse else out
 
 

@@ -50,6 +50,8 @@ extern "C" int32_t synera_batch_destroy(synera_batch* b) {
   return SYNERA_OK;
 }
 
+static hipError_t prepare_attention(int hd);   // once for each device
+
 extern "C" int32_t synera_batch_create(synera_batch** out, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                        int32_t max_batch, int32_t max_tokens, int32_t max_pages) {
   if (!out) return SYNERA_EINVAL;
@@ -60,6 +62,10 @@ extern "C" int32_t synera_batch_create(synera_batch** out, int32_t n_q_heads, in
   int dev = 0;
   hipDeviceProp_t prop;
   if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return SYNERA_EHIP;
+  }
+  if (prepare_attention(head_dim) != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
   }
@@ -900,14 +906,20 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a, int 
 }
 
 template <int HD>
+static constexpr size_t shared_lds() { return (size_t)20 * SY_PAGE * HD * 2; }
+template <int HD>
 static hipError_t launch_shared(const SharedAttnArgs& a, int blocks, int joined, hipStream_t s) {
-  const size_t lds = (size_t)20 * SY_PAGE * HD * 2;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_attn_kernel<HD>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
+  const size_t lds = shared_lds<HD>();
+  hipError_t e = hipSuccess;
   if (blocks > 0) shared_attn_kernel<HD><<<blocks, 256, lds, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (joined > 0) shared_join_kernel<HD><<<dim3(joined, (a.Hq * (HD / 4) + 255) / 256), 256, 0, s>>>(a, a.block_groups < 0 ? -1 : joined);
   return hipGetLastError();
+}
+
+static hipError_t prepare_attention(int hd) {
+  const void* kernel = hd == 128 ? reinterpret_cast<const void*>(&shared_attn_kernel<128>) : reinterpret_cast<const void*>(&shared_attn_kernel<64>);
+  return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(hd == 128 ? shared_lds<128>() : shared_lds<64>()));
 }
 
 extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* q, const void* d_k_layer, const void* d_v_layer,
