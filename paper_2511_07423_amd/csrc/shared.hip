@@ -430,6 +430,8 @@ struct SharedAttnArgs {
 };
 
 typedef __attribute__((ext_vector_type(8))) int sh_i32x8v;
+typedef __attribute__((ext_vector_type(4))) int sh_i32x4v;
+typedef __attribute__((ext_vector_type(2))) int sh_i32x2v;
 typedef SH_CONST_AS sh_i32x8v sh_i32x8;                      // read with scalar loads
 
 __device__ __forceinline__ float sh_ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -852,21 +854,22 @@ __global__ __launch_bounds__(256, 2) void shared_attn_kernel(SharedAttnArgs a) {
 
 // Joins the partial results of rows that several items worked on: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A thread takes four
 // values of one row; FLY partials (no more than the token has, but for the last round) are asked for together, behind two
-// dependent loads.
+// dependent scalar loads.
 template <int HD, int FLY>
 __device__ __forceinline__ void join_token(const SharedAttnArgs& a, const ShJoin& jn, const int head, const int d4) {
+  const SH_CONST_AS sh_i32x2v* list = reinterpret_cast<const SH_CONST_AS sh_i32x2v*>((uintptr_t)(a.parts + jn.first));
   const int kh = head / a.G, g = head % a.G;
   float M = -3e38f, l = 0.f;
   float4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < jn.count; s0 += FLY) {
     float2 ml[FLY];
     float4 v[FLY];
-    ShPart part[FLY];
+    sh_i32x2v part[FLY];                                      // ShPart: row, step
 #pragma unroll
-    for (int s = 0; s < FLY; ++s) part[s] = a.parts[jn.first + min(s0 + s, jn.count - 1)];
+    for (int s = 0; s < FLY; ++s) part[s] = list[min(s0 + s, jn.count - 1)];
 #pragma unroll
     for (int s = 0; s < FLY; ++s) {
-      const size_t at = (size_t)part[s].row + (size_t)kh * part[s].step + g;
+      const size_t at = (size_t)part[s][0] + (size_t)kh * part[s][1] + g;
       ml[s] = a.part_ml[at];
       v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
     }
@@ -898,7 +901,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a, int 
   if (piece >= a.Hq * (HD / 4)) return;
   const int head = piece / (HD / 4), d4 = piece % (HD / 4) * 4;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const ShJoin jn = a.joined[i];
+    const sh_i32x4v w = *reinterpret_cast<const SH_CONST_AS sh_i32x4v*>((uintptr_t)(a.joined + i));
+    const ShJoin jn = {w[0], w[1], w[2], 0};
     if (jn.count <= 2) join_token<HD, 2>(a, jn, head, d4);
     else if (jn.count <= 4) join_token<HD, 4>(a, jn, head, d4);
     else join_token<HD, 8>(a, jn, head, d4);
