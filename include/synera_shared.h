@@ -7,7 +7,7 @@
  * Element types: 0 = f32, 1 = bf16, 2 = f16.  The cache is bf16, gains are bf16.
  * Arithmetic is 32-bit throughout, angles are 64-bit; each output is rounded once, to nearest even.
  * The handles belong to the HIP device that was current when they were made: a call with another device current is
- * refused (EINVAL), so is one without a device.  Nothing here waits for the GPU except the creates and destroys, and
+ * refused (EINVAL).  They must outlive the graphs that captured calls with them.  Nothing here waits for the GPU except the creates and destroys, and
  * synera_batch_plan if it runs more than four plans ahead of its uploads.
  */
 #ifndef SYNERA_SHARED_H
@@ -123,6 +123,7 @@ int32_t synera_batch_plan(synera_batch* batch, int32_t B, const int32_t* h_ctx_l
  * theirs.  Inputs of type `dtype`, T = sum n_new tokens, request after request; heads are normed first where they come
  * with gains (not v).  k->d_out, v->d_out and their strides are not looked at.  d_k_layer, d_v_layer: one layer of the pools,
  * 16-byte aligned, of at least the planned n_pages_in_pool pages.  Slots that are not appended to stay as they were.
+ * Outputs must not lie on inputs (but for q in place, bf16) nor on the pools.
  * Errors: EINVAL (also: no plan, head counts or head_dim other than the batch's), EHIP.
  */
 int32_t synera_append_rope(synera_batch* batch, const synera_rope* rope, int32_t dtype, const synera_heads* q,
@@ -137,8 +138,8 @@ int32_t synera_append_rope(synera_batch* batch, const synera_rope* rope, int32_t
  *                       strides on 16 bytes, d_out and its strides on 8
  *   scale               finite, > 0 (0 takes 1 / sqrt(head_dim))
  *   d_lse               f32 [T][n_q_heads], ln sum exp(scale q k), or NULL
- * Softmax statistics and sums are 32-bit; the probabilities meet the bf16 values as bf16.  Keys and values in pages that a
- * row does not see may hold anything, infinities and NaN too.  Calls with one batch must be ordered (they share its scratch), in
+ * Softmax statistics and sums are 32-bit; the probabilities meet the bf16 values as bf16.  Keys and values that a
+ * row does not see may hold anything, infinities and NaN too.  Outputs must not lie on inputs.  Calls with one batch must be ordered (they share its scratch), in
  * graphs as well.  Errors: EINVAL, EHIP.
  */
 int32_t synera_shared_attention(synera_batch* batch, const synera_heads* q, const void* d_k_layer, const void* d_v_layer,

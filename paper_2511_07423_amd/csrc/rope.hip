@@ -1,8 +1,8 @@
 // Rotary positions and norms of query and key heads over whole tensors: the entry points of include/synera_shared.h and
 // their kernel (rope.h has the arithmetic and the layout of the work).
+#include <algorithm>
 #include <cmath>
 #include <new>
-#include <vector>
 
 #include "../../include/synera.h"
 #include "rope.h"
@@ -114,8 +114,8 @@ bool turn_overlap(const void* a, int64_t a_ts, int64_t a_hs, int a_heads, int a_
   return true;
 }
 
-// The widest chunk that divides the head as the layout needs and whose vectors everything is aligned for.  (16-byte loads
-// against 2-byte ones, 6000 tokens of 40 x 128 bf16: see the figures at the kernel.)
+// The widest chunk that divides the head as the layout needs and whose vectors everything is aligned for.  6000 tokens of 40 x 128 bf16 in
+// chunks of 8, 4, 2, 1 values: 24.7, 21.7, 32.7, 43.8 us; normed on the way into their pages (16 K tokens) 8 beats 4, 95 against 106 us.
 static bool fits(int vec, const synera_rope* rope, const synera_heads* s, int in_bytes, int out_bytes, bool out) {
   if (rope->desc.head_dim % vec || rope->desc.rot_dim % (2 * vec)) return false;
   if (!s) return true;
@@ -170,14 +170,14 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
 // ------------------------------------------------------------------------------------ whole tensors
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void rope_kernel(TurnArgs a) {
-  const uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (item >= (uint32_t)a.T * (uint32_t)a.n_item_cols) return;
-  turn_item<T, T, VEC, false>(a, item);
+  const uint32_t items = (uint32_t)a.T * (uint32_t)a.n_item_cols;
+  for (uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += gridDim.x * 4)
+    turn_item<T, T, VEC, false>(a, item);
 }
 
 template <typename T>
 static hipError_t launch_rope(const TurnArgs& a, int vec, hipStream_t s) {
-  const uint32_t blocks = ((uint32_t)a.T * (uint32_t)a.n_item_cols + 3) / 4;
+  const uint32_t blocks = std::min(((uint32_t)a.T * (uint32_t)a.n_item_cols + 3) / 4, 1u << 22);   // a launch has less than 2^32 threads
   switch (vec) {
     case 8: rope_kernel<T, 8><<<blocks, 256, 0, s>>>(a); break;
     case 4: rope_kernel<T, 4><<<blocks, 256, 0, s>>>(a); break;

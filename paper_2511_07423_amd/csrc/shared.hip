@@ -306,6 +306,17 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
   }
 }
 
+struct Range { uintptr_t from, to; };
+static bool meet(const Range& a, const Range& b) { return a.from < b.to && b.from < a.to; }
+static Range heads_range(const void* p, int64_t ts, int64_t hs, int64_t heads, int64_t n, int hd, int bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return {at, at + (uintptr_t)(((n - 1) * ts + (heads - 1) * hs + hd) * bytes)};
+}
+static Range pool_range(const synera_batch* b, const void* p) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return {at, at + (uintptr_t)b->n_pages * b->lim.Hkv * SY_PAGE * b->lim.hd * 2};
+}
+
 template <typename TI>
 static hipError_t launch_append(const AppendArgs& a, int vec, uint32_t blocks, hipStream_t s) {
   switch (vec) {
@@ -334,32 +345,21 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   if (st == SYNERA_OK) st = turn_check(*v, n1, hd, bytes, 2, false);
   if (st == SYNERA_OK && q) st = turn_check(*q, n1, hd, bytes, 2, true);
   if (st != SYNERA_OK || v->d_gain) return SYNERA_EINVAL;
-  // whole pools as ranges, so that no output lies on an input or on another output
-  const int64_t layer = (int64_t)b->n_pages * l.Hkv * SY_PAGE * hd;
-  const void* pools[2] = {d_k_layer, d_v_layer};
-  const synera_heads* ins[3] = {k, v, q};
-  const uintptr_t kp = reinterpret_cast<uintptr_t>(d_k_layer), vp = reinterpret_cast<uintptr_t>(d_v_layer);
-  if (kp < vp + 2 * layer && vp < kp + 2 * layer) return SYNERA_EINVAL;
-  for (const synera_heads* i : ins) {
+  // no output lies on an input or on another output; the pools are taken as whole ranges
+  const Range pools[2] = {pool_range(b, d_k_layer), pool_range(b, d_v_layer)};
+  if (meet(pools[0], pools[1])) return SYNERA_EINVAL;
+  for (const synera_heads* i : {k, v, q}) {
     if (!i) continue;
-    const int64_t span = ((n1 - 1) * i->in_token + (int64_t)(i->n_heads - 1) * i->in_head + hd) * bytes;
-    const uintptr_t ip = reinterpret_cast<uintptr_t>(i->d_in);
-    for (const void* pool : pools) {
-      const uintptr_t pp = reinterpret_cast<uintptr_t>(pool);
-      if (ip < pp + 2 * layer && pp < ip + span) return SYNERA_EINVAL;
-    }
+    const Range in = heads_range(i->d_in, i->in_token, i->in_head, i->n_heads, n1, hd, bytes);
+    if (meet(in, pools[0]) || meet(in, pools[1])) return SYNERA_EINVAL;
     if (!q) continue;
     if (i == q && dtype == 1 && q->d_in == q->d_out && (n1 == 1 || q->in_token == q->out_token) && (q->n_heads == 1 || q->in_head == q->out_head)) continue;
     if (turn_overlap(q->d_out, q->out_token, q->out_head, q->n_heads, 2, i->d_in, i->in_token, i->in_head, i->n_heads, bytes, n1, hd))
       return SYNERA_EINVAL;
   }
   if (q) {
-    const uintptr_t op = reinterpret_cast<uintptr_t>(q->d_out);
-    const int64_t span = ((n1 - 1) * q->out_token + (int64_t)(q->n_heads - 1) * q->out_head + hd) * 2;
-    for (const void* pool : pools) {
-      const uintptr_t pp = reinterpret_cast<uintptr_t>(pool);
-      if (op < pp + 2 * layer && pp < op + span) return SYNERA_EINVAL;
-    }
+    const Range out = heads_range(q->d_out, q->out_token, q->out_head, q->n_heads, n1, hd, 2);
+    if (meet(out, pools[0]) || meet(out, pools[1])) return SYNERA_EINVAL;
   }
   if (!rope_device_ok(b->device) || rope->device != b->device) return SYNERA_EINVAL;
   AppendArgs a = {};
@@ -941,6 +941,12 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   if ((reinterpret_cast<uintptr_t>(q->d_in) | (uint64_t)(2 * q->in_token) | (uint64_t)(2 * q->in_head)) % 16) return SYNERA_EINVAL;
   if ((reinterpret_cast<uintptr_t>(q->d_out) | (uint64_t)(2 * q->out_token) | (uint64_t)(2 * q->out_head)) % 8) return SYNERA_EINVAL;
   if (turn_overlap(q->d_out, q->out_token, q->out_head, l.Hq, 2, q->d_in, q->in_token, q->in_head, l.Hq, 2, n1, l.hd)) return SYNERA_EINVAL;
+  const Range out = heads_range(q->d_out, q->out_token, q->out_head, l.Hq, n1, l.hd, 2), k = pool_range(b, d_k_layer), v = pool_range(b, d_v_layer);
+  if (meet(out, k) || meet(out, v)) return SYNERA_EINVAL;
+  if (d_lse) {
+    const Range lse = heads_range(d_lse, l.Hq, 1, l.Hq, n1, 1, 4), in = heads_range(q->d_in, q->in_token, q->in_head, l.Hq, n1, l.hd, 2);
+    if (meet(lse, k) || meet(lse, v) || meet(lse, out) || meet(lse, in)) return SYNERA_EINVAL;
+  }
   if (!rope_device_ok(b->device)) return SYNERA_EINVAL;
   SharedAttnArgs a = {};
   a.q = static_cast<const bf16_t*>(q->d_in);

@@ -2,9 +2,8 @@
 // work into items.  No HIP call, no arithmetic of the method.
 #include <algorithm>
 #include <cstring>
-#include <functional>
+#include <map>
 #include <new>
-#include <queue>
 
 #include "shared.h"
 
@@ -241,15 +240,17 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx, const int32_t* n_
           sizes.emplace_back(c.w * ((double)c.keys / (double)n + (n > 1 ? SH_KEYS_A_CUT : SH_KEYS_AN_ITEM)), n * c.tiles * l.Hkv);
         }
       std::sort(sizes.rbegin(), sizes.rend());
-      std::priority_queue<double, std::vector<double>, std::greater<double>> place;
-      for (int64_t i = 0; i < l.slots; ++i) place.push(0);
+      std::map<double, int64_t> places{{0.0, l.slots}};         // when they are free, how many of them
       double end = 0;
-      for (const auto& [size, n] : sizes)
-        for (int64_t i = 0; i < n; ++i) {
-          const double t = place.top() + size;
-          place.pop();
-          place.push(t);
+      for (auto [size, n] : sizes)
+        while (n > 0) {
+          const auto first = places.begin();
+          const int64_t k = std::min(n, first->second);
+          const double t = first->first + size;
+          if ((first->second -= k) == 0) places.erase(first);
+          places[t] += k;
           end = std::max(end, t);
+          n -= k;
         }
       if (end < best) {
         best = end;

@@ -90,6 +90,19 @@ def test_many_tokens(T, heads):
     check(ok, k, pos, ref.frequencies(128), "half", "k")
 
 
+def test_very_many_small_heads():
+    """More items than one launch has wavefronts: 2^25 tokens of one pair, turned by their positions' parity."""
+    s = synera()
+    rope = s.Rope(2, inv_freq=[np.pi])
+    n = (1 << 25) + 3
+    pos = torch.arange(n, device=DEV, dtype=torch.int32)
+    x = draw((n, 1, 2), torch.bfloat16, 1)
+    got, _ = rope.apply(pos, x)
+    want = torch.where((pos % 2 == 0)[:, None, None], x, -x)
+    assert (got.float() - want.float()).abs().max() <= 2.0 ** -8 * 6 + 1e-5        # |x| < 6: one rounding, and pi in 64 bits
+    assert torch.equal(got[::2][: 1 << 10], x[::2][: 1 << 10])
+
+
 def test_strides_and_alignment():
     """Rows that start on any element, tokens inside heads, heads that are one head repeated, outputs with gaps that stay."""
     s = synera()
@@ -182,5 +195,11 @@ def test_refusals():
     assert status(lambda: rope.apply(pos, q, q, out_q=same, out_k=same)) == s.EINVAL             # two outputs on one another
     one = torch.empty((6, 1, 64), dtype=torch.bfloat16, device=DEV)
     assert status(lambda: rope.apply(pos, q, out_q=one.expand(6, 4, 64))) == s.EINVAL            # an output on itself
+    from paper_2511_07423_amd import binding as b
+    far = b._pack_heads(q.data_ptr(), q.data_ptr(), 0, 4, 256, 64, 256, 64)                      # nothing is launched
+    assert b._lib.synera_rope_apply(rope._h, 1, 1 << 29, pos.data_ptr(), far, None, None) == s.EUNSUP
+    assert b._lib.synera_rope_apply(rope._h, 1, -1, pos.data_ptr(), far, None, None) == s.EINVAL
+    assert b._lib.synera_rope_apply(rope._h, 3, 6, pos.data_ptr(), far, None, None) == s.EINVAL
+    assert b._lib.synera_rope_apply(rope._h, 1, 6, pos.data_ptr() + 1, far, None, None) == s.EINVAL
     rope.apply(pos, wide[:, :4], out_q=wide[:, 5:])                                              # slices side by side are fine
     torch.cuda.synchronize()

@@ -370,4 +370,10 @@ def test_refusals():
     odd = torch.empty(T * hq * hd + 8, dtype=torch.bfloat16, device=DEV)
     assert status(lambda: b.attention(odd[1: 1 + T * hq * hd].view(T, hq, hd), kp, vp)) == s.EINVAL
     assert status(lambda: b.attention(good, kp, vp, out=odd[2: 2 + T * hq * hd].view(T, hq, hd))) == s.EINVAL
+    pool_as_out = kp.view(-1)[: T * hq * hd].view(T, hq, hd)
+    assert status(lambda: b.attention(good, kp, vp, out=pool_as_out)) == s.EINVAL   # out on the keys
+    assert status(lambda: b.append_rope(rope, q, k, v, kp, vp, out_q=pool_as_out)) == s.EINVAL
+    pool_as_out = kp.view(-1)[: T * hq * hd].view(T, hq, hd)
+    assert status(lambda: b.attention(good, kp, vp, out=pool_as_out)) == s.EINVAL   # out on the keys
+    assert status(lambda: b.append_rope(rope, q, k, v, kp, vp, out_q=pool_as_out)) == s.EINVAL
     assert torch.equal(b.attention(good, kp, vp), o)
