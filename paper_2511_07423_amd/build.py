@@ -18,6 +18,9 @@ SOURCES = ["gemm_nf4_high.hip", "gemm_nf4_low.hip", "gemm_nf2.hip", "gemm_k64.hi
 ASM_CHECKED = {"gemm_nf4_high.hip": "proj_kernel", "gemm_nf4_low.hip": "proj_kernel", "gemm_nf2.hip": "proj_kernel", "gemm_k64.hip": "proj_kernel",
                "gemm_k64_once.hip": "proj_kernel",
                "ceilings.hip": "ceiling_mfma_f16"}
+# sources whose assembly is kept because a test reads it: the attention's inner loops over asynchronous copies, which a wait or a spill
+# of the compiler's would drain
+ASM_KEPT = ["shared.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # The attention kernel's builtin MFMAs take their accumulators in VGPRs: in AGPRs (the compiler's default choice)
@@ -34,7 +37,7 @@ def _quiet(stderr):
 def _compile(src):
     obj = os.path.join(OBJ_DIR, os.path.splitext(src)[0] + ".o")
     cmd = ["hipcc", *FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
-    if src in ASM_CHECKED:
+    if src in ASM_CHECKED or src in ASM_KEPT:
         cmd.append("-save-temps=obj")
     res = subprocess.run(cmd, capture_output=True, text=True, cwd=OBJ_DIR)
     if res.returncode != 0:

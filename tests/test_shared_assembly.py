@@ -1,0 +1,45 @@
+"""The attention over shared prefixes keeps its copies in flight: in the inner loops over tiles the compiler must neither wait for vector
+memory by itself (it would drain the copies, which it does not know of) nor spill registers (a reload waits likewise)."""
+import os
+import re
+
+import pytest
+
+import paper_2511_07423_amd as synera
+
+ASM = os.path.join(os.path.dirname(synera.lib_path()), "_build", "shared-hip-amdgcn-amd-amdhsa-gfx950.s")
+
+
+def inner_loops(text, kernel):
+    """Innermost loops of a kernel that copy to LDS and multiply: lists of (line, inside inline assembly)."""
+    body = re.search(rf"^{kernel}:(.*?)^\s*s_endpgm", text, re.S | re.M).group(1).split("\n")
+    label = {m.group(1): i for i, line in enumerate(body) if (m := re.match(r"(\.LBB\S+):", line))}
+    loops = []
+    for i, line in enumerate(body):
+        m = re.search(r"s_c?branch\S*\s+(\.LBB\S+)", line)
+        if m and label.get(m.group(1), i) < i:
+            loops.append((label[m.group(1)], i))
+    inline, marked = False, []
+    for line in body:
+        inline = (inline or "#ASMSTART" in line) and "#ASMEND" not in line
+        marked.append((line, inline))
+    found = []
+    for a, b in loops:
+        if any(a <= c and d <= b and (a, b) != (c, d) for c, d in loops):
+            continue
+        part = marked[a: b + 1]
+        if sum("v_mfma" in x for x, _ in part) and any("global_load_lds" in x for x, _ in part):
+            found.append(part)
+    return found
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_inner_loops_do_not_drain_their_copies(head_dim):
+    if not os.path.exists(ASM):
+        pytest.skip("the library was built elsewhere: no assembly here")
+    loops = inner_loops(open(ASM).read(), rf"_Z18shared_attn_kernelILi{head_dim}EEv14SharedAttnArgs")
+    assert len(loops) >= 3                        # wavefronts alone, four to the keys, two by two or four to the rows
+    for part in loops:
+        spills = [x for x, _ in part if "scratch_" in x]
+        waits = [x for x, inline in part if "s_waitcnt" in x and "vmcnt" in x and not inline]
+        assert not spills and not waits, (spills[:3], waits[:3])
