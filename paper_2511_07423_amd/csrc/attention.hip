@@ -75,7 +75,13 @@ __device__ __forceinline__ void store_o(const AttnLaunch& a, size_t tok, int col
   }
 }
 
-// copy_to_lds (common.h), the lines marked as not wanted again (nt), for keys and values that no cache holds until the next call: they come faster
+// Asynchronous 16-byte-per-lane copy global -> LDS; lane i lands at lds_addr + 16 i (m0 carries the
+// wavefront-uniform LDS address).
+__device__ __forceinline__ void copy_to_lds(const void* gptr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
+
+// The same, the lines marked as not wanted again (nt), for keys and values that no cache holds until the next call: they come faster
 // from HBM.  256 requests in a shuffled pool (447 K keys, 1.8 GB): 316 -> 290 us a launch; the headline
 // batch 85 -> 80; one request of 900 keys 11.9 -> 11.0. 
 __device__ __forceinline__ void copy_to_lds_once(const void* gptr, uint32_t lds_addr) {

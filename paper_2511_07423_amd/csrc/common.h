@@ -56,12 +56,6 @@ __device__ __forceinline__ void rotate_pair(float v0, float v1, float c, float s
   r1 = __builtin_fmaf(v1, c, v0 * s);
 }
 
-// Asynchronous 16-byte-per-lane copy global -> LDS; lane i lands at lds_addr + 16 i (m0 carries the
-// wavefront-uniform LDS address).
-__device__ __forceinline__ void copy_to_lds(const void* gptr, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
-}
-
 // ---------------------------------------------------------------- elementwise.hip
 struct BatchMeta {        // device pointers into one uploaded metadata blob (all int32)
   const int32_t* ctx_len;      // [B]
