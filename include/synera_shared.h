@@ -7,8 +7,8 @@
  * Element types: 0 = f32, 1 = bf16, 2 = f16.  The cache is bf16, gains are bf16.
  * Arithmetic is 32-bit throughout, angles are 64-bit; each output is rounded once, to nearest even.
  * The handles belong to the HIP device that was current when they were made: a call with another device current is
- * refused (EINVAL).  They must outlive the graphs that captured calls with them.  Nothing here waits for the GPU except the creates and destroys, and
- * synera_batch_plan if it runs more than four plans ahead of its uploads.
+ * refused (EINVAL).  They must outlive the graphs that captured calls with them.  Nothing here waits for the GPU except
+ * the creates and destroys, and synera_batch_plan if it runs more than four plans ahead of its uploads.
  */
 #ifndef SYNERA_SHARED_H
 #define SYNERA_SHARED_H
@@ -27,7 +27,7 @@ extern "C" {
  *   SYNERA_ROPE_BANDS   with r = original * f_i / (2 pi) turns over the original context: f_i / factor for r <= low,
  *                       f_i for r >= high, and (1 - t) f_i / factor + t f_i, t = (r - low) / (high - low), between
  * or the caller's own table.  pos * f_i / (2 pi) is formed in 64 bits and only what is left of whole turns is rounded to
- * 32: any int32 position is good to 5e-7 rad.
+ * 32: with |f_i| <= 1 any int32 position is good to 5e-7 rad.
  */
 #define SYNERA_ROPE_INTERLEAVED 0
 #define SYNERA_ROPE_HALF 1
@@ -44,7 +44,7 @@ typedef struct synera_rope_desc {
   double factor;             /* LINEAR, BANDS: > 0                                          */
   double low, high;          /* BANDS: 0 <= low < high                                      */
   double original;           /* BANDS: > 0                                                  */
-  double magnitude;          /* of cos and sin; 1 for a rotation proper                     */
+  double magnitude;          /* of cos and sin, finite in f32; 1 for a rotation proper      */
   const double* h_inv_freq;  /* HOST [rot_dim / 2] f_i in place of base and scaling, or NULL */
 } synera_rope_desc;
 
@@ -91,7 +91,8 @@ int32_t synera_qk_norm_rope(const synera_rope* rope, int32_t dtype, int64_t n_to
 typedef struct synera_batch synera_batch;
 
 /* head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, at most 1024; room for max_batch requests, max_tokens new tokens
- * a plan, max_pages block-table columns.  Errors: EINVAL, EUNSUP, EHIP, ENOMEM. */
+ * a plan, max_pages block-table columns.  Keeps 0.3 to 0.6 GB of device memory (head_dim 128; half of it at 64) for partial
+ * results, and the plan on the device and four times in pinned host memory.  Errors: EINVAL, EUNSUP, EHIP, ENOMEM. */
 int32_t synera_batch_create(synera_batch** out, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_batch,
                             int32_t max_tokens, int32_t max_pages);
 /* Waits for the device.  NULL is allowed. */
@@ -112,7 +113,8 @@ int32_t synera_validate_shared(int32_t B, const int32_t* h_ctx_len, const int32_
  * Plans a batch: finds the shared prefixes, cuts the attention's work, and uploads both on `stream`.  The calls below
  * must be on the same stream, or ordered behind it by the caller; so must a plan behind calls that use the one before.
  * Not while the stream is being captured (EINVAL).  Calls that were captured into a graph work for any later plan of
- * this batch: what is planned is read on the device.  max_pages: columns of h_block_table (<= the batch's).  A refused
+ * this batch: what is planned is read on the device; their tensors and pools need room for the tokens and pages of those
+ * plans, which nothing checks.  max_pages: columns of h_block_table (<= the batch's).  A refused
  * plan leaves the one before as it was.  Errors: as synera_validate_shared, EHIP, ENOMEM.
  */
 int32_t synera_batch_plan(synera_batch* batch, int32_t B, const int32_t* h_ctx_len, const int32_t* h_n_new,
@@ -139,8 +141,8 @@ int32_t synera_append_rope(synera_batch* batch, const synera_rope* rope, int32_t
  *   scale               finite, > 0 (0 takes 1 / sqrt(head_dim))
  *   d_lse               f32 [T][n_q_heads], ln sum exp(scale q k), or NULL
  * Softmax statistics and sums are 32-bit; the probabilities meet the bf16 values as bf16.  Keys and values that a
- * row does not see may hold anything, infinities and NaN too.  Outputs must not lie on inputs.  Calls with one batch must be ordered (they share its scratch), in
- * graphs as well.  Errors: EINVAL, EHIP.
+ * row does not see may hold anything, infinities and NaN too.  Outputs must not lie on inputs.  Calls with one batch
+ * must be ordered (they share its scratch), in graphs as well.  Errors: EINVAL, EHIP.
  */
 int32_t synera_shared_attention(synera_batch* batch, const synera_heads* q, const void* d_k_layer, const void* d_v_layer,
                                 float scale, float* d_lse, void* stream);

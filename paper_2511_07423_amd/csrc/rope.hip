@@ -15,7 +15,7 @@ extern "C" int32_t synera_rope_create(synera_rope** out, const synera_rope_desc*
   const synera_rope_desc& d = *desc;
   if (d.head_dim < 2 || d.head_dim % 2 || d.rot_dim < 2 || d.rot_dim % 2 || d.rot_dim > d.head_dim) return SYNERA_EINVAL;
   if (d.layout != SYNERA_ROPE_INTERLEAVED && d.layout != SYNERA_ROPE_HALF) return SYNERA_EINVAL;
-  if (!std::isfinite(d.magnitude)) return SYNERA_EINVAL;
+  if (!std::isfinite((float)d.magnitude)) return SYNERA_EINVAL;
   const int half = d.rot_dim / 2;
   if (!d.h_inv_freq) {
     if (!std::isfinite(d.base) || !(d.base > 1.0)) return SYNERA_EINVAL;

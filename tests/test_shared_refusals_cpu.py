@@ -65,3 +65,10 @@ def test_null_handles():
         assert lib.synera_validate_shared(*args, 1, 1, 1, 1) == s.EINVAL
     with pytest.raises(ValueError):
         s.validate_shared([1, 2], [1], table, 1, 1, 1)
+
+
+def test_a_magnitude_has_to_be_finite_in_32_bits():
+    for bad in (1e39, -1e300):
+        with pytest.raises(s.SyneraError) as e:
+            s.Rope(64, magnitude=bad)
+        assert e.value.status == s.EINVAL
