@@ -915,7 +915,7 @@ template <int HD>
 static hipError_t launch_shared(const SharedAttnArgs& a, int blocks, int joined, hipStream_t s) {
   const size_t lds = shared_lds<HD>();
   hipError_t e = hipSuccess;
-  if (blocks > 0) shared_attn_kernel<HD><<<blocks, 256, lds, s>>>(a);
+  if (blocks > 0) shared_attn_kernel<HD><<<std::min(blocks, 1 << 22), 256, lds, s>>>(a);   // a launch has less than 2^32 threads
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (joined > 0) shared_join_kernel<HD><<<dim3(joined, (a.Hq * (HD / 4) + 255) / 256), 256, 0, s>>>(a, a.block_groups < 0 ? -1 : joined);
   return hipGetLastError();
