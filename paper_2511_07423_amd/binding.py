@@ -693,7 +693,8 @@ def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max
 
 class SharedBatch:
     """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
-    attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too.
+    attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too; their tensors
+    and pools need room for the tokens and pages of those plans.
     Belongs to the device that is current when it is made."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):
@@ -754,8 +755,8 @@ class SharedBatch:
         -> o bf16 (out, new if None), or (o, lse f32 [T, Hq])."""
         if scale is None:
             scale = 0.0
-        elif not scale > 0:
-            raise ValueError("scale is positive")
+        elif not scale >= 2.0 ** -126:
+            raise ValueError("scale is positive (from 2^-126 on: what 32 bits round to 0 would take the default)")
         index = self._index
         h, out = _heads(q, out, None, torch.bfloat16, self.n_tokens, self.n_q_heads, self.head_dim, index, "q", None, False)
         lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None

@@ -377,3 +377,47 @@ def test_refusals():
     assert status(lambda: b.attention(good, kp, vp, out=pool_as_out)) == s.EINVAL   # out on the keys
     assert status(lambda: b.append_rope(rope, q, k, v, kp, vp, out_q=pool_as_out)) == s.EINVAL
     assert torch.equal(b.attention(good, kp, vp), o)
+
+
+def test_a_scale_that_32_bits_round_to_zero_is_refused():
+    s = synera()
+    b = s.SharedBatch(2, 1, 64, 1, 1, 1)
+    b.plan([4], [1], [[0]], 1)
+    kp, vp, q = draw((1, 1, P, 64), 1), draw((1, 1, 64, P), 2), draw((1, 2, 64), 3)
+    with pytest.raises(ValueError):
+        b.attention(q, kp, vp, scale=1e-60)                                          # (0 would mean 1 / sqrt(head_dim))
+    # the smallest scale weighs all keys alike
+    o = b.attention(q, kp, vp, scale=2.0 ** -126)
+    want = vp[0, 0, :, :5].double().mean(1)
+    assert torch.allclose(o[0].double(), want.expand(2, 64), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+@pytest.mark.parametrize("hq,hkv,hd,ctx,new", [(1024, 1, 64, 200, 3), (300, 2, 128, 90, 5), (2, 2, 128, 131077, 1), (1, 1, 64, 70001, 3)])
+def test_attention_wide_groups_and_long_contexts(hq, hkv, hd, ctx, new):
+    """Tokens whose heads fill several tiles of rows or straddle two; single contexts that all units share."""
+    n = -(-(ctx + new) // P)
+    table = np.random.RandomState(ctx).permutation(n).astype(np.int32)[None]
+    check_attention(hq, hkv, hd, np.array([ctx], np.int32), np.array([new], np.int32), table, n, ctx + new)
+
+
+def test_pages_whose_offsets_pass_32_bits():
+    """The last pages of pools of over 2^32 bytes: what is appended and attended there is what it is in a small pool, bit for bit."""
+    s, hq, hkv, hd = synera(), 16, 8, 128
+    ctx, new, table, n = shared_batch(5, 20, np.array([0, 3, 16, 90, 200]), np.array([1, 2, 17, 40, 1]))
+    many = (1 << 32) // (hkv * P * hd * 2) + n
+    T = int(new.sum())
+    x = draw((T, hq + 2 * hkv, hd), 1)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    rope = s.Rope(hd)
+    small = [draw((n, hkv, P, hd), 2), draw((n, hkv, hd, P), 3)]
+    large = [torch.empty((many, *p.shape[1:]), dtype=p.dtype, device=DEV) for p in small]
+    for p, whole in zip(small, large):
+        whole[many - n:] = p
+    got = []
+    for pools, at, pages in ((small, 0, n), (large, many - n, many)):
+        b = s.SharedBatch(hq, hkv, hd, len(ctx), T, table.shape[1])
+        b.plan(ctx, new, np.where(table >= 0, table + at, -1), pages)
+        turned = b.append_rope(rope, q, k, v, *pools)
+        got.append((turned, b.attention(turned, *pools), pools[0][at:], pools[1][at:]))
+    for a, c in zip(*got):
+        assert torch.equal(a, c)
