@@ -8,7 +8,8 @@
 // heads at a time.
 //
 // Bound by HBM: every value is read and written once.  The angle costs a lane one 64-bit product and 40 instructions a
-// pair, for all its heads.
+// pair, for all its heads.  Measured: 8192 tokens of 40 x 128 bf16, half of each head turned, 34 us, 4.9 TB/s; 16000 tokens 64 us, 5.2; 6000 in
+// f32, normed, 47 to 52 us, 4.7 to 5.2; one token 3.4 us, 64 normed ones 4.7.
 #pragma once
 #include "common.h"
 #include "../../include/synera_shared.h"
