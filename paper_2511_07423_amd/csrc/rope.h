@@ -8,8 +8,8 @@
 // heads at a time.
 //
 // Bound by HBM: every value is read and written once.  The angle costs a lane one 64-bit product and 40 instructions a
-// pair, for all its heads.  Measured: 8192 tokens of 40 x 128 bf16, half of each head turned, 34 us, 4.9 TB/s; 16000 tokens 64 us, 5.2; 6000 in
-// f32, normed, 47 to 52 us, 4.7 to 5.2; one token 3.4 us, 64 normed ones 4.7.
+// pair, for all its heads.  Measured, on new inputs each time: 8192 tokens of 40 x 128 bf16, half of each head turned, 38 us, 4.4 TB/s; 16000 tokens 60 us, 5.4;
+// 6000 in f32, normed, 59 us, 4.2; one token 3.1 us, 64 normed ones 4.8.
 #pragma once
 #include "common.h"
 #include "../../include/synera_shared.h"
@@ -20,6 +20,7 @@ struct synera_rope {
   double* rev;                 // device [rot_dim / 2]: turns from one position to the next
 };
 
+enum { TURN_KEPT, TURN_ONCE_IN, TURN_ONCE_BOTH };   // nothing, inputs, inputs and outputs
 struct TurnSeg {
   const void* in;
   void* out;
@@ -35,6 +36,7 @@ struct TurnArgs {
   float magnitude, eps;
   int32_t T, hd, rot, half;
   int32_t lanes_log2, groups, groups_per_item, n_item_cols;   // lanes of a head; head groups of a token, of an item; items of a token
+  int32_t once;                // what is marked as not wanted again: TURN_ONCE_*
   // appends: keys go to their pages
   const int32_t* slot;         // [T] page x 16 + slot
   bf16_t* k_layer;
@@ -46,7 +48,7 @@ template <> struct TurnType<bf16_t> { typedef uint16_t raw; };
 template <> struct TurnType<_Float16> { typedef _Float16 raw; };
 
 template <int N> struct TurnBits { typedef u32x4 v; };
-template <> struct TurnBits<8> { typedef uint2 v; };
+template <> struct TurnBits<8> { typedef __attribute__((ext_vector_type(2))) uint32_t v; };
 template <> struct TurnBits<4> { typedef uint32_t v; };
 template <> struct TurnBits<2> { typedef uint16_t v; };
 
@@ -55,17 +57,27 @@ template <typename T, int VEC>
 struct TurnChunk {
   static constexpr int BYTES = VEC * (int)sizeof(T), PIECE = BYTES > 16 ? 16 : BYTES, N = BYTES / PIECE;
   typename TurnBits<PIECE>::v p[N];
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(const T* from) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = reinterpret_cast<const typename TurnBits<PIECE>::v*>(from)[i];
+    for (int i = 0; i < N; ++i) {
+      const auto* at = reinterpret_cast<const typename TurnBits<PIECE>::v*>(from) + i;
+      if constexpr (ONCE) p[i] = __builtin_nontemporal_load(at);
+      else p[i] = *at;
+    }
   }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < N; ++i) p[i] = typename TurnBits<PIECE>::v{};
   }
+  template <bool ONCE>
   __device__ __forceinline__ void store(T* to) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) reinterpret_cast<typename TurnBits<PIECE>::v*>(to)[i] = p[i];
+    for (int i = 0; i < N; ++i) {
+      auto* at = reinterpret_cast<typename TurnBits<PIECE>::v*>(to) + i;
+      if constexpr (ONCE) __builtin_nontemporal_store(p[i], at);
+      else *at = p[i];
+    }
   }
   __device__ __forceinline__ void widen(float* f) const;
   __device__ __forceinline__ void round(const float* f);
@@ -110,7 +122,7 @@ __device__ __forceinline__ void turn_angle(double pos, double rev, float magnitu
 }
 
 // Item `item` of the call: the head groups item % n_item_cols of token item / n_item_cols.  TI, TO: element types in and out.
-template <typename TI, typename TO, int VEC, bool PAGED>
+template <typename TI, typename TO, int VEC, bool PAGED, int ONCE>
 __device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item) {
   constexpr int NU = VEC == 1 ? 2 : 1;                      // single values: up to 128 units on 64 lanes
   // Heads of a lane whose loads are on their way together: 64 bytes in all.  (128: fewer wavefronts fit; 6000 tokens of 40 x 128 f32 normed
@@ -165,8 +177,8 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item
         xa[i][n].zero();
         xb[i][n].zero();
         if (on && (turned[n] || tail)) {
-          if (ca[n] >= 0) xa[i][n].load(in + ca[n]);
-          if (cb[n] >= 0) xb[i][n].load(in + cb[n]);
+          if (ca[n] >= 0) xa[i][n].template load<ONCE != TURN_KEPT>(in + ca[n]);
+          if (cb[n] >= 0) xb[i][n].template load<ONCE != TURN_KEPT>(in + cb[n]);
         }
       }
     }
@@ -248,11 +260,11 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item
         TurnChunk<TO, VEC> y;
         if (ca[n] >= 0) {
           y.round(va[n]);
-          y.store(out + ca[n]);
+          y.template store<ONCE == TURN_ONCE_BOTH>(out + ca[n]);
         }
         if (cb[n] >= 0) {
           y.round(vb[n]);
-          y.store(out + cb[n]);
+          y.template store<ONCE == TURN_ONCE_BOTH>(out + cb[n]);
         }
       }
     }

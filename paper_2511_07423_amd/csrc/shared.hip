@@ -207,8 +207,9 @@ extern "C" int32_t synera_batch_plan(synera_batch* b, int32_t B, const int32_t* 
 // ------------------------------------------------------------------------------------ append
 // Wavefronts take queries' and keys' head groups (rope.h), or the values of one page window: 128 of a token's Hkv hd values for up
 // to 16 consecutive tokens, turned in LDS from token-major to the page's [dim][slot] order so that a whole page leaves in
-// 16-byte pieces.  In a page that other tokens share only the appended slots are written.
-// Bound by HBM where there are many tokens: 31 585 of 32 + 2 x 8 heads of 128 (776 MB) 169 us, 4.6 TB/s; a decoding step of 64 tokens 4.8 us.
+// 16-byte pieces.  In a page that other tokens share only the appended slots are written.  (Values are read as usual where all else is marked,
+// turn_setup: marked too, 31 585 tokens 139 -> 153 us.)
+// Bound by HBM where there are many tokens: 31 585 of 32 + 2 x 8 heads of 128 (776 MB) 139 us, 5.6 TB/s; a decoding step of 64 tokens 4.8 us.
 struct AppendArgs {
   TurnArgs turn;
   const ShHeader* head;
@@ -238,7 +239,7 @@ __device__ __forceinline__ uint32_t value_pair(const TI* v, bool pairs) {    // 
   return pack_bf2(f[0], f[1]);
 }
 
-template <typename TI>
+template <typename TI, int ONCE>
 __device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindow w, const int e0, uint32_t* turn) {
   const int lane = threadIdx.x & 63, e = e0 + 2 * lane;
   const bool on = e < a.n;
@@ -279,7 +280,8 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindo
     const int slot0 = (piece & 1) * 8;          // the piece's first slot
     bf16_t* to = dst + piece * 8;
     if (slot0 >= w.s0 && slot0 + 8 <= w.s1) {
-      *reinterpret_cast<u32x4*>(to) = x;
+      if constexpr (ONCE == TURN_ONCE_BOTH) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to));
+      else *reinterpret_cast<u32x4*>(to) = x;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -293,18 +295,18 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindo
   __builtin_amdgcn_wave_barrier();              // the next window's values come into the same words
 }
 
-template <typename TI, int VEC>
+template <typename TI, int VEC, int ONCE>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t turn[4][64 * 16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.v_blocks) {
     const uint32_t slabs = (uint32_t)(a.n + 127) / 128, items = (uint32_t)a.head->n_windows * slabs;
     for (uint32_t i = blockIdx.x * 4 + wave; i < items; i += (uint32_t)a.v_blocks * 4)
-      append_values<TI>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
+      append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
   } else {
     const uint32_t items = (uint32_t)a.head->n_tokens * (uint32_t)a.turn.n_item_cols;
     for (uint32_t i = (blockIdx.x - a.v_blocks) * 4 + wave; i < items; i += (gridDim.x - a.v_blocks) * 4)
-      turn_item<TI, bf16_t, VEC, true>(a.turn, i);
+      turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, i);
   }
 }
 
@@ -319,13 +321,21 @@ static Range pool_range(const synera_batch* b, const void* p) {
   return {at, at + (uintptr_t)b->n_pages * b->lim.Hkv * SY_PAGE * b->lim.hd * 2};
 }
 
+template <typename TI, int VEC>
+static void append_vec(const AppendArgs& a, uint32_t blocks, hipStream_t s) {
+  if constexpr (VEC >= 4) {
+    if (a.turn.once == TURN_ONCE_BOTH) return append_rope_kernel<TI, VEC, TURN_ONCE_BOTH><<<blocks, 256, 0, s>>>(a);
+    if (a.turn.once == TURN_ONCE_IN) return append_rope_kernel<TI, VEC, TURN_ONCE_IN><<<blocks, 256, 0, s>>>(a);
+  }
+  append_rope_kernel<TI, VEC, TURN_KEPT><<<blocks, 256, 0, s>>>(a);
+}
 template <typename TI>
 static hipError_t launch_append(const AppendArgs& a, int vec, uint32_t blocks, hipStream_t s) {
   switch (vec) {
-    case 8: append_rope_kernel<TI, 8><<<blocks, 256, 0, s>>>(a); break;
-    case 4: append_rope_kernel<TI, 4><<<blocks, 256, 0, s>>>(a); break;
-    case 2: append_rope_kernel<TI, 2><<<blocks, 256, 0, s>>>(a); break;
-    default: append_rope_kernel<TI, 1><<<blocks, 256, 0, s>>>(a);
+    case 8: append_vec<TI, 8>(a, blocks, s); break;
+    case 4: append_vec<TI, 4>(a, blocks, s); break;
+    case 2: append_vec<TI, 2>(a, blocks, s); break;
+    default: append_vec<TI, 1>(a, blocks, s);
   }
   return hipGetLastError();
 }

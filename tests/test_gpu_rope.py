@@ -203,3 +203,20 @@ def test_refusals():
     assert b._lib.synera_rope_apply(rope._h, 1, 6, pos.data_ptr() + 1, far, None, None) == s.EINVAL
     rope.apply(pos, wide[:, :4], out_q=wide[:, 5:])                                              # slices side by side are fine
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,heads,rot,dtype", [(9000, (32, 8, 128), 128, "bf16"), (6000, (32, 8, 128), 64, "f32"), (16000, (32, 8, 128), 128, "f16"),
+                                               (9001, (40, 8, 96), 24, "bf16"), (16001, (40, 8, 96), 24, "bf16")])
+def test_sizes_that_no_cache_holds(T, heads, rot, dtype):
+    """Large calls, whose inputs or outputs pass the caches by, give the bits of the same tokens in small calls."""
+    hq, hkv, hd = heads
+    rope = synera().Rope(hd, rot, layout="half")
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, hq + hkv, hd), generator=gen, device="cuda").to({"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype])
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    gains = [(1 + 0.1 * torch.randn(hd, generator=gen, device="cuda")).to(torch.bfloat16) for _ in range(2)]
+    for call in (lambda p, q, k: rope.apply(p, q, k), lambda p, q, k: rope.norm_apply(p, q, k, *gains, 1e-5)):
+        whole = call(pos, x[:, :hq], x[:, hq:])
+        for t in range(0, T, 1500):
+            part = call(pos[t: t + 1500], x[t: t + 1500, :hq], x[t: t + 1500, hq:])
+            assert all(torch.equal(w[t: t + 1500], p) for w, p in zip(whole, part)), t

@@ -421,3 +421,33 @@ def test_pages_whose_offsets_pass_32_bits():
         got.append((turned, b.attention(turned, *pools), pools[0][at:], pools[1][at:]))
     for a, c in zip(*got):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("T", [8001, 29003])
+def test_appends_that_no_cache_holds(T):
+    """Large appends, whose inputs or outputs pass the caches by: the bits of Rope.apply in small calls, and the values as they are."""
+    s, hq, hkv, hd = synera(), 32, 8, 128
+    ctx, new = np.array([5, 0, 64], np.int32), np.array([T // 2, 1, T - T // 2 - 1], np.int32)
+    need = -(-(ctx + new) // P)
+    n = int(need.sum())
+    perm = np.random.RandomState(T).permutation(n).astype(np.int32)
+    table = np.full((3, int(need.max())), -1, np.int32)
+    for i in range(3):
+        table[i, : need[i]] = perm[need[:i].sum(): need[: i + 1].sum()]
+    x = draw((T, hq + 2 * hkv, hd), 1)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    rope = s.Rope(hd, layout="half")
+    kp, vp = bits((n, hkv, P, hd), 0x1234), bits((n, hkv, hd, P), 0x4321)
+    turned = planned(hq, hkv, hd, ctx, new, table, n).append_rope(rope, q, k, v, kp, vp)
+    at = np.concatenate([c + np.arange(m) for c, m in zip(ctx, new)])
+    req = np.repeat(np.arange(3), new)
+    page, slot = torch.from_numpy(table[req, at // P].astype(np.int64)).to(DEV), torch.from_numpy(at % P).to(DEV)
+    pos = torch.from_numpy(at.astype(np.int32)).to(DEV)
+    for t in range(0, T, 1500):
+        e = min(T, t + 1500)
+        wq, wk = rope.apply(pos[t: e], q[t: e], k[t: e])
+        assert torch.equal(turned[t: e], wq) and torch.equal(kp[page[t: e], :, slot[t: e]], wk), t
+        assert torch.equal(vp[page[t: e], :, :, slot[t: e]], v[t: e]), t
+    kp[page, :, slot] = bits((), 0x1234)
+    vp[page, :, :, slot] = bits((), 0x4321)
+    assert (kp.view(torch.int16) == 0x1234).all() and (vp.view(torch.int16) == 0x4321).all()
