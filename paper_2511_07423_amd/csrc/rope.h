@@ -9,7 +9,7 @@
 //
 // Bound by HBM: every value is read and written once.  The angle costs a lane one 64-bit product and 40 instructions a
 // pair, for all its heads.  Measured, on new inputs each time: 8192 tokens of 40 x 128 bf16, half of each head turned, 38 us, 4.4 TB/s; 16000 tokens 60 us, 5.4;
-// 6000 in f32, normed, 59 us, 4.2; one token 3.1 us, 64 normed ones 4.8.
+// 6000 in f32, normed, 51 us, 4.8; one token 3.1 us, 64 normed ones 4.8.
 #pragma once
 #include "common.h"
 #include "../../include/synera_shared.h"
@@ -127,7 +127,7 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item
   constexpr int NU = VEC == 1 ? 2 : 1;                      // single values: up to 128 units on 64 lanes
   // Heads of a lane whose loads are on their way together: 64 bytes in all.  (128: fewer wavefronts fit; 6000 tokens of 40 x 128 f32 normed
   // 54.7 -> 46.8 us, 31585 tokens appended 173 -> 169.)
-  constexpr int IT = NU == 1 && sizeof(TI) == 2 ? 2 : 1;
+  constexpr int IT = NU == 1 && VEC * (int)sizeof(TI) <= 16 ? 2 : 1;
   const int lane = threadIdx.x & 63;
   const uint32_t t = item / (uint32_t)a.n_item_cols;
   const int g0 = (int)(item - t * (uint32_t)a.n_item_cols) * a.groups_per_item;
@@ -197,12 +197,20 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item
       }
       if (a.q.gain || a.k.gain) {                           // uniform; heads without gains pass by
         // (The gains come from the nearest cache each time.  Kept from the beginning, they were waited for before the heads: 47 -> 64 us.)
+        // (Neighbours first, in a lane and between lanes: the order of the sum does not depend on VEC, which goes by sizes and alignment.)
         float ss = 0.f;
 #pragma unroll
-        for (int n = 0; n < NU; ++n)
+        for (int n = 0; n < NU; ++n) {
+          float sq[VEC];
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) ss += va[n][j] * va[n][j] + vb[n][j] * vb[n][j];
-        for (int o = (1 << a.lanes_log2) >> 1; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
+          for (int j = 0; j < VEC; ++j) sq[j] = __builtin_fmaf(va[n][j], va[n][j], vb[n][j] * vb[n][j]);
+#pragma unroll
+          for (int o = 1; o < VEC; o *= 2)
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2 * o) sq[j] += sq[j + o];
+          ss += sq[0];
+        }
+        for (int o = 1; o < 1 << a.lanes_log2; o *= 2) ss += __shfl_xor(ss, o);
         const float inv = 1.0f / sqrtf(ss / (float)a.hd + a.eps);
         if (gain && on) {
 #pragma unroll

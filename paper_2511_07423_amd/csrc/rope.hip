@@ -152,7 +152,10 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   a.hd = hd;
   a.rot = rot;
   a.half = rope->desc.layout == SYNERA_ROPE_HALF;
-  int vec = 8;
+  const int64_t moved = (n_tokens * (a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes)) >> 20;      // MB
+  // (f32: a chunk of 8 is two vectors, each of which fills half a line.  Where the lines do not wait in a cache for their other halves, 4: 6000 tokens
+  // of 40 x 128 normed 59 -> 51 us, 9000 82 -> 80; but 4000 tokens 36 -> 38, 4096 appended 37 -> 41.)
+  int vec = in_bytes == 4 && !paged && moved >= 224 ? 4 : 8;
   while (vec > 1 && !(fits(vec, rope, q, in_bytes, out_bytes, true) && fits(vec, rope, k, in_bytes, out_bytes, !paged))) vec /= 2;
   const int units = rot / (2 * vec) + (hd / vec - rot / vec + 1) / 2;
   a.lanes_log2 = 0;
@@ -170,7 +173,6 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   // then: 12 000 tokens and their reader 94 -> 84 us, but 8192 and theirs 55 -> 63; appends, whose keys the attention reads with all
   // else: 31 585 tokens 169 -> 139 us (with their attention 656 -> 656), 11 400 with theirs 206 -> 215.  (Chunks of one or two values are bound by their
   // instructions: 2.5 TB/s.)
-  const int64_t moved = (n_tokens * (a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes)) >> 20;      // MB
   a.once = vec < 4 || moved < 128 ? TURN_KEPT : moved < (paged ? 512 : 224) ? TURN_ONCE_IN : TURN_ONCE_BOTH;
   return vec;
 }
