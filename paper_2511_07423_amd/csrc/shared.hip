@@ -468,12 +468,12 @@ template <int N>
 __device__ __forceinline__ void copy_page(const bf16_t* base, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3, uint32_t lds_addr, bool once) {
 #define SH_COPY_4(MARK)                                                                                                            \
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5" MARK                                               \
-               "\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024" MARK "\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048" MARK          \
-               "\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base) \
+               "\n\tglobal_load_lds_dwordx4 %2, %5 offset:0x400" MARK "\n\tglobal_load_lds_dwordx4 %3, %5 offset:0x800" MARK          \
+               "\n\tglobal_load_lds_dwordx4 %4, %5 offset:0xc00" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(base) \
                : "memory", "m0")
 #define SH_COPY_2(MARK)                                                                                                            \
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" MARK                                               \
-               "\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "s"(base) : "memory", "m0")
+               "\n\tglobal_load_lds_dwordx4 %2, %3 offset:0x400" MARK ::"s"(lds_addr), "v"(o0), "v"(o1), "s"(base) : "memory", "m0")
   if constexpr (N == 4) {
     if (once) SH_COPY_4(" nt");
     else SH_COPY_4("");
