@@ -621,7 +621,7 @@ class Rope:
     """Rotary positions of heads of head_dim values, of which the first rot_dim turn (all by default): pairs (2i, 2i+1)
     with layout "interleaved", (i, i + rot_dim/2) with "half".  scaling: None, ("linear", factor) or ("bands", factor, low, high,
     original context); inv_freq: rot_dim/2 numbers in place of base and scaling; magnitude multiplies cosines and sines.
-    Belongs to the device that is current when it is made."""
+    Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
 
     def __init__(self, head_dim, rot_dim=None, layout="interleaved", base=10000.0, scaling=None, inv_freq=None, magnitude=1.0):
         self._h = _vp()
@@ -695,7 +695,7 @@ class SharedBatch:
     """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
     attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too; their tensors
     and pools need room for the tokens and pages of those plans.
-    Belongs to the device that is current when it is made."""
+    Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):
         self._h = _vp()
