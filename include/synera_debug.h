@@ -135,7 +135,7 @@ int32_t synera_debug_attention_plan(const synera_model_desc* desc, int32_t attn_
                                     int32_t* h_cuts, int64_t cut_cap, int32_t* h_counts);
 
 /*
- * Test hook, host only: what synera_batch_plan would upload for one batch (not validated here) on a chip that runs `slots`
+ * Test hook, host only: what synera_batch_plan would upload for one batch (page ids are not validated here) on a chip that runs `slots`
  * blocks at once.  `which` picks a region: 0 header (tokens, page windows, tokens with several partial results, groups of 8 items that a
  * block takes each, groups of 32 that a wavefront takes each, 0 ..), 1 positions, 2 page x 16 + slot, 3 windows [n][4] = page, first
  * token, slots from, to, 4 items [n][32] = flags (1 = one request's rows, 2 = keys not wanted again), KV head, rows, first row in the node, first token or entry
@@ -143,7 +143,8 @@ int32_t synera_debug_attention_plan(const synera_model_desc* desc, int32_t attn_
  * pages from the first key on, 5 token list, 6 page list, 7 tokens with several partial results [n][4] = token, first entry of the list,
  * entries, 0, 8 that list [n][2] = partial row of head 0, step to the next KV head's.
  * n_words: size of the region, in 32-bit words; h_out: the region (ENOSPC where cap words are too few); limits (or NULL) [7]: room
- * for items, list, partial results, pages, windows, partial rows, rows of shared nodes.  Errors: EINVAL, ENOSPC, ENOMEM.
+ * for items, list, partial results, pages, windows, partial rows, rows of shared nodes.  Errors: EINVAL (null, sizes < 1, head counts that do not
+ * divide, `which`, lengths < 0 or beyond the table's columns or max_tokens), ENOSPC, ENOMEM.
  */
 int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t slots, int32_t max_tokens, int32_t B,
                                  const int32_t* h_ctx_len, const int32_t* h_n_new, const int32_t* h_block_table, int32_t max_pages,

@@ -1009,7 +1009,16 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
 extern "C" int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t slots, int32_t max_tokens, int32_t B,
                                             const int32_t* h_ctx_len, const int32_t* h_n_new, const int32_t* h_block_table, int32_t max_pages,
                                             int32_t which, int32_t* h_out, int64_t cap, int64_t* n_words, int64_t* limits) {
-  if (!h_ctx_len || !h_n_new || !h_block_table || !n_words || (cap > 0 && !h_out) || B < 1 || slots < 1 || n_kv_heads < 1) return SYNERA_EINVAL;
+  if (!h_ctx_len || !h_n_new || !h_block_table || !n_words || (cap > 0 && !h_out) || B < 1 || slots < 1 || max_tokens < 1 || max_pages < 1 ||
+      n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || which < 0 || which >= N_REGIONS)
+    return SYNERA_EINVAL;
+  int64_t tokens = 0;
+  for (int i = 0; i < B; ++i) {                      // what the planner reads lies inside the table; page ids are only passed on
+    const int64_t end = (int64_t)h_ctx_len[i] + h_n_new[i];
+    if (h_ctx_len[i] < 0 || h_n_new[i] < 0 || end > INT32_MAX - SY_SH_STEP || end > (int64_t)max_pages * SYNERA_PAGE_SIZE) return SYNERA_EINVAL;
+    tokens += h_n_new[i];
+  }
+  if (tokens > max_tokens) return SYNERA_EINVAL;
   try {
     ShLimits l = {};
     l.Hq = n_q_heads;
@@ -1030,7 +1039,6 @@ extern "C" int32_t synera_debug_shared_plan(int32_t n_q_heads, int32_t n_kv_head
                                    p.pages.data(), p.joined.data(), p.parts.data()};
     const size_t words[N_REGIONS] = {sizeof(ShHeader) / 4, p.tok_pos.size(), p.tok_slot.size(), p.windows.size() * 4, p.items.size() * 32,
                                      p.list.size(), p.pages.size(), p.joined.size() * 4, p.parts.size() * 2};
-    if (which < 0 || which >= N_REGIONS) return SYNERA_EINVAL;
     *n_words = (int64_t)words[which];
     if ((int64_t)words[which] > cap) return SYNERA_ENOSPC;
     if (words[which]) std::memcpy(h_out, from[which], words[which] * 4);

@@ -72,3 +72,25 @@ def test_a_magnitude_has_to_be_finite_in_32_bits():
         with pytest.raises(s.SyneraError) as e:
             s.Rope(64, magnitude=bad)
         assert e.value.status == s.EINVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n_q_heads=1), dict(n_q_heads=3), dict(n_q_heads=0), dict(n_q_heads=-2), dict(n_kv_heads=0), dict(n_kv_heads=-2), dict(slots=0), dict(max_tokens=0),
+    dict(max_tokens=2), dict(max_pages=0), dict(max_pages=1), dict(B=0), dict(which=-1), dict(which=9), dict(ctx=-1), dict(new=-1),
+    dict(ctx=(1 << 31) - 100, max_pages=1 << 27)])
+def test_the_planning_hook_refuses_what_it_cannot_plan(bad):
+    """Head counts that do not divide, sizes below one, lengths beyond the table: no division by zero, no read past the table."""
+    a = {**dict(n_q_heads=2, n_kv_heads=2, slots=4, max_tokens=3, B=1, ctx=15, new=3, max_pages=2, which=0), **bad}
+    ctx, new, table = np.array([a["ctx"]], np.int32), np.array([a["new"]], np.int32), np.array([[0, 1]], np.int32)
+    p = lambda v: v.ctypes.data_as(C.POINTER(C.c_int32))                                   # noqa: E731
+    out, n = np.zeros(64, np.int32), C.c_int64(0)
+    assert b._lib.synera_debug_shared_plan(a["n_q_heads"], a["n_kv_heads"], a["slots"], a["max_tokens"], a["B"], p(ctx), p(new), p(table),
+                                           a["max_pages"], a["which"], p(out), 64, C.byref(n), None) == s.EINVAL
+
+
+def test_the_planning_hook_from_python():
+    for hq, hkv in ((1, 2), (3, 2), (2, 0)):
+        with pytest.raises(s.SyneraError) as e:
+            s.debug_shared_plan(hq, hkv, 4, [3], [1], [[0]])
+        assert e.value.status == s.EINVAL
+    assert s.debug_shared_plan(2, 2, 4, [3], [1], [[0]])["head"][0, 0] == 1
