@@ -63,6 +63,7 @@ typedef struct synera_heads {
   void* d_out;
   const void* d_gain;        /* bf16 [head_dim]: the norm's gains, or NULL where the heads are not normed */
   int32_t n_heads;
+  int32_t n_rows;            /* tokens that d_in and d_out have room for, 0: not said.  Calls with a batch look at it */
   int64_t in_token, in_head;
   int64_t out_token, out_head;
 } synera_heads;
@@ -114,7 +115,8 @@ int32_t synera_validate_shared(int32_t B, const int32_t* h_ctx_len, const int32_
  * must be on the same stream, or ordered behind it by the caller; so must a plan behind calls that use the one before.
  * Not while the stream is being captured (EINVAL).  Calls that were captured into a graph work for any later plan of
  * this batch: what is planned is read on the device; their tensors and pools need room for the tokens and pages of those
- * plans, which nothing checks.  max_pages: columns of h_block_table (<= the batch's).  A refused
+ * plans, which nothing checks.  That no output lies on an input or on itself is checked, when they are captured, for as many tokens as
+ * the smallest n_rows of the call (for two, or those of the plan at hand, where none is said).  max_pages: columns of h_block_table (<= the batch's).  A refused
  * plan leaves the one before as it was.  Errors: as synera_validate_shared, EHIP, ENOMEM.
  */
 int32_t synera_batch_plan(synera_batch* batch, int32_t B, const int32_t* h_ctx_len, const int32_t* h_n_new,
@@ -126,7 +128,7 @@ int32_t synera_batch_plan(synera_batch* batch, int32_t B, const int32_t* h_ctx_l
  * with gains (not v).  k->d_out, v->d_out and their strides are not looked at.  d_k_layer, d_v_layer: one layer of the pools,
  * 16-byte aligned, of at least the planned n_pages_in_pool pages.  Slots that are not appended to stay as they were.
  * Outputs must not lie on inputs (but for q in place, bf16) nor on the pools.
- * Errors: EINVAL (also: no plan, head counts or head_dim other than the batch's), EHIP.
+ * Errors: EINVAL (also: no plan, head counts or head_dim other than the batch's, n_rows below the plan's tokens), EHIP.
  */
 int32_t synera_append_rope(synera_batch* batch, const synera_rope* rope, int32_t dtype, const synera_heads* q,
                            const synera_heads* k, const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer,

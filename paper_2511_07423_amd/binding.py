@@ -125,9 +125,10 @@ class _RopeDesc(C.Structure):
                 ("original", C.c_double), ("magnitude", C.c_double), ("h_inv_freq", C.POINTER(C.c_double))]
 
 
-# synera_heads as bytes: d_in, d_out, d_gain, n_heads, strides in and out of tokens and heads.  (Filling a ctypes structure field
+# synera_heads as bytes: d_in, d_out, d_gain, n_heads (n_rows: 0), strides in and out of tokens and heads.  (Filling a ctypes structure field
 # by field, and asking torch for the stream object, took longer than the kernels of a decoding step.)
 _pack_heads = struct.Struct("@PPPi4xqqqq").pack
+_pack_heads_rows = struct.Struct("@PPPiiqqqq").pack     # n_rows behind n_heads
 _lib.synera_rope_create.restype = C.c_int32
 _lib.synera_rope_create.argtypes = [C.POINTER(_vp), C.POINTER(_RopeDesc)]
 _lib.synera_rope_destroy.restype = C.c_int32
@@ -605,16 +606,17 @@ def _heads(x, out, gain, dtype, n, n_heads, hd, index, name, out_dtype=None, exa
         if gain.dtype != torch.bfloat16 or gain.shape != shape[2:] or not gain.is_contiguous() or gain.get_device() != index:
             raise ValueError(f"{name}: gains are bf16 [{hd}] on cuda:{index}")
         at_gain = gain.data_ptr()
+    rows = 0 if exact else min(shape[0], 0x7FFFFFFF)
     if out is False:
-        return _pack_heads(x.data_ptr(), 0, at_gain, shape[1], strides[0], strides[1], 0, 0), None
+        return _pack_heads_rows(x.data_ptr(), 0, at_gain, shape[1], rows, strides[0], strides[1], 0, 0), None
     if out is None:
         out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
-        return _pack_heads(x.data_ptr(), out.data_ptr(), at_gain, shape[1], strides[0], strides[1], shape[1] * hd, hd), out
+        return _pack_heads_rows(x.data_ptr(), out.data_ptr(), at_gain, shape[1], rows, strides[0], strides[1], shape[1] * hd, hd), out
     out_strides = out.stride()
     if out.shape != shape or out.dtype != (out_dtype or dtype) or (out_strides[2] != 1 and hd > 1) or out.get_device() != index:
         raise ValueError(f"{name}: the output is {out_dtype or dtype} {tuple(shape)} on cuda:{index}, the values of a head side by side; "
                          f"got {out.dtype} {tuple(out.shape)}, strides {out_strides}, on {out.device}")
-    return _pack_heads(x.data_ptr(), out.data_ptr(), at_gain, shape[1], strides[0], strides[1], out_strides[0], out_strides[1]), out
+    return _pack_heads_rows(x.data_ptr(), out.data_ptr(), at_gain, shape[1], rows, strides[0], strides[1], out_strides[0], out_strides[1]), out
 
 
 class Rope:
@@ -694,7 +696,7 @@ def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max
 class SharedBatch:
     """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
     attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too; their tensors
-    and pools need room for the tokens and pages of those plans.
+    and pools need room for the tokens and pages of those plans, and all rows of their outputs lie apart from each other and from inputs.
     Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):

@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <type_traits>
 
@@ -321,6 +322,20 @@ static Range pool_range(const synera_batch* b, const void* p) {
   return {at, at + (uintptr_t)b->n_pages * b->lim.Hkv * SY_PAGE * b->lim.hd * 2};
 }
 
+// Tokens that the checks of a call go by: the plan's; of a captured call, which serves later plans too, as many as all its tensors have room
+// for.  -1: a tensor lacks room for the plan at hand.
+static int64_t tokens_to_check(const synera_batch* b, bool graph, std::initializer_list<const synera_heads*> heads) {
+  const int64_t T = b->plan.head.n_tokens;
+  int64_t room = 0;
+  for (const synera_heads* h : heads) {
+    if (!h || !h->n_rows) continue;
+    if (h->n_rows < T) return -1;
+    room = room ? std::min<int64_t>(room, h->n_rows) : h->n_rows;
+  }
+  if (!graph) return std::max<int64_t>(T, 1);
+  return std::max<int64_t>({T, 1, std::min<int64_t>(room ? room : 2, b->lim.max_tokens)});
+}
+
 template <typename TI, int VEC>
 static void append_vec(const AppendArgs& a, uint32_t blocks, hipStream_t s) {
   if constexpr (VEC >= 4) {
@@ -352,7 +367,8 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   const ShLimits& l = b->lim;
   const int bytes = dtype == 0 ? 4 : 2, hd = l.hd;
   if (rope->desc.head_dim != hd || k->n_heads != l.Hkv || v->n_heads != l.Hkv || (q && q->n_heads != l.Hq)) return SYNERA_EINVAL;
-  const int64_t T = b->plan.head.n_tokens, n1 = std::max<int64_t>(T, 1);
+  const int64_t n1 = tokens_to_check(b, graph, {q, k, v});
+  if (n1 < 0) return SYNERA_EINVAL;
   int32_t st = turn_check(*k, n1, hd, bytes, 2, false);
   if (st == SYNERA_OK) st = turn_check(*v, n1, hd, bytes, 2, false);
   if (st == SYNERA_OK && q) st = turn_check(*q, n1, hd, bytes, 2, true);
@@ -375,7 +391,8 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   }
   if (!rope_device_ok(b->device) || rope->device != b->device) return SYNERA_EINVAL;
   AppendArgs a = {};
-  const int vec = turn_setup(a.turn, rope, n1, q, k, bytes, 2, true, eps);
+  const int64_t T = std::max<int64_t>(b->plan.head.n_tokens, 1);
+  const int vec = turn_setup(a.turn, rope, T, q, k, bytes, 2, true, eps);
   a.turn.pos = b->region<int32_t>(R_POS);
   a.turn.slot = b->region<int32_t>(R_SLOT);
   a.turn.k_layer = static_cast<bf16_t*>(d_k_layer);
@@ -393,7 +410,7 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   a.v_pairs = va % (2 * bytes) == 0;
   const int64_t v_items = std::max<int64_t>(1, (int64_t)b->plan.head.n_windows * ((a.n + 127) / 128));
   a.v_blocks = (int32_t)std::min<int64_t>((v_items + 3) / 4, 1 << 16);
-  const int64_t t_blocks = std::min<int64_t>((n1 * a.turn.n_item_cols + 3) / 4, 1 << 20);
+  const int64_t t_blocks = std::min<int64_t>((T * a.turn.n_item_cols + 3) / 4, 1 << 20);
   const uint32_t blocks = (uint32_t)(a.v_blocks + t_blocks);
   const hipError_t e = dtype == 0   ? launch_append<float>(a, vec, blocks, s)
                        : dtype == 1 ? launch_append<bf16_t>(a, vec, blocks, s)
@@ -954,7 +971,8 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16 || reinterpret_cast<uintptr_t>(d_lse) % 4) return SYNERA_EINVAL;
   const ShLimits& l = b->lim;
   if (q->n_heads != l.Hq) return SYNERA_EINVAL;
-  const int64_t T = b->plan.head.n_tokens, n1 = std::max<int64_t>(T, 1);
+  const int64_t n1 = tokens_to_check(b, graph, {q});
+  if (n1 < 0) return SYNERA_EINVAL;
   if (turn_check(*q, n1, l.hd, 2, 2, true) != SYNERA_OK) return SYNERA_EINVAL;
   if ((reinterpret_cast<uintptr_t>(q->d_in) | (uint64_t)(2 * q->in_token) | (uint64_t)(2 * q->in_head)) % 16) return SYNERA_EINVAL;
   if ((reinterpret_cast<uintptr_t>(q->d_out) | (uint64_t)(2 * q->out_token) | (uint64_t)(2 * q->out_head)) % 8) return SYNERA_EINVAL;

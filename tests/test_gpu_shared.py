@@ -451,3 +451,70 @@ def test_appends_that_no_cache_holds(T):
     kp[page, :, slot] = bits((), 0x1234)
     vp[page, :, :, slot] = bits((), 0x4321)
     assert (kp.view(torch.int16) == 0x1234).all() and (vp.view(torch.int16) == 0x4321).all()
+
+
+def captured(call):
+    """A graph of the call, captured on a stream of its own; it never runs."""
+    graph, side = torch.cuda.CUDAGraph(keep_graph=True), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    return graph
+
+
+def test_captured_calls_are_checked_for_later_plans():
+    """Behind a plan of one token, tensors whose later rows lie on one another: an eager call touches none of those, a captured one would for
+    a later plan, and is refused."""
+    s, hq, hkv, hd, rows = synera(), 4, 2, 64, 32
+    rope = s.Rope(hd)
+    b = s.SharedBatch(hq, hkv, hd, 4, rows, 4)
+    b.plan([3], [1], [[0]], 16)
+    kp, vp = draw((16, hkv, P, hd), 1), draw((16, hkv, hd, P), 2)
+    width = hq * hd
+    flat = draw((2 * (rows + 2) * width,), 3)
+    q, k, v = flat[: rows * width].view(rows, hq, hd), draw((rows, hkv, hd), 4), draw((rows, hkv, hd), 5)
+    stretched = flat.as_strided((rows, hq, hd), (2 * width, hd, 1))                  # q's first row, other later ones
+    behind = flat[8 * width: (rows + 8) * width].view(rows, hq, hd)                  # q's rows 8 ..
+    same = draw((1, hq, hd), 6).expand(rows, hq, hd)                                 # one row for all
+    inside = flat[rows * width:].as_strided((rows, hq, hd), (hd, 8 * hd, 1))         # heads apart for eight tokens
+    free = flat[rows * width: 2 * rows * width].view(rows, hq, hd)
+
+    def refused(call):
+        with pytest.raises(s.SyneraError) as e:
+            call()
+        assert e.value.status == s.EINVAL
+
+    def all_captured():
+        for out in (stretched, behind, same, inside):
+            refused(lambda: b.append_rope(rope, q, k, v, kp, vp, out_q=out))
+        for out in (behind, same, inside):
+            refused(lambda: b.attention(q, kp, vp, out=out))
+        refused(lambda: b.append_rope(rope, q, behind[:, :2], v, kp, vp, out_q=q))   # queries in place, keys in their later rows
+        b.append_rope(rope, q, k, v, kp, vp, out_q=free)
+        b.append_rope(rope, q, k, v, kp, vp, out_q=q)                                # in place
+        b.append_rope(rope, q[:8], k[:8], v[:8], kp, vp, out_q=behind[:8])           # room for eight tokens
+        by_head = free.view(hq, rows, hd).transpose(0, 1)
+        b.append_rope(rope, q, k, v, kp, vp, out_q=by_head)
+        b.attention(q, kp, vp, out=by_head)
+        one = free.view(-1)[: hq * hd].view(hq, 1, hd).transpose(0, 1)               # one row, heads outermost
+        b.append_rope(rope, q[:1], k[:1], v[:1], kp, vp, out_q=one)
+        b.attention(q[:1], kp, vp, out=one)
+    captured(all_captured)
+    for out in (stretched, behind, same, inside):                                    # the first rows are apart
+        b.append_rope(rope, q, k, v, kp, vp, out_q=out)
+    b.attention(q, kp, vp, out=behind)
+    # without row counts, captured calls are checked for two tokens at least
+    from paper_2511_07423_amd import binding as raw
+    heads = [raw._pack_heads(t.data_ptr(), o.data_ptr(), 0, t.shape[1], t.stride(0), t.stride(1), o.stride(0), o.stride(1))
+             for t, o in ((q, stretched), (k, k), (v, v), (q, free))]
+
+    def append(at):
+        stream = torch.cuda.current_stream().cuda_stream
+        return raw._lib.synera_append_rope(b._h, rope._h, 1, heads[at], heads[1], heads[2], 0.0, kp.data_ptr(), vp.data_ptr(), stream)
+    got = []
+    captured(lambda: got.extend((append(0), append(3))))
+    assert got == [s.EINVAL, s.OK] and append(0) == s.OK
+    short = raw._pack_heads_rows(k.data_ptr(), 0, 0, hkv, 1, hkv * hd, hd, 0, 0)
+    b.plan([3], [2], [[0]], 16)
+    assert raw._lib.synera_append_rope(b._h, rope._h, 1, None, short, heads[2], 0.0, kp.data_ptr(), vp.data_ptr(), None) == s.EINVAL
+    torch.cuda.synchronize()
