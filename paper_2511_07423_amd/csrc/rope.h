@@ -21,6 +21,25 @@ struct synera_rope {
 };
 
 enum { TURN_KEPT, TURN_ONCE_IN, TURN_ONCE_BOTH };   // nothing, inputs, inputs and outputs
+// How a token's head groups are dealt to wavefronts: `groups` to an item, n items.  They share the token's cosines and sines, and are
+// spread while there are too few items.
+struct TurnCols {
+  int32_t groups, n;
+};
+__host__ __device__ inline TurnCols turn_cols(int32_t groups, int32_t n_tokens) {
+  const int32_t want = 4096 / (n_tokens > 1 ? n_tokens : 1), cols = want > groups ? groups : want > 1 ? want : 1;
+  const int32_t each = (groups + cols - 1) / cols;
+  return TurnCols{each, (groups + each - 1) / each};
+}
+// What the last-level cache (256 MB) could not hold for the next call anyway is marked as not wanted again, so that the rest stays there.
+// Inputs are read for the last time: a producer, 8192 tokens of 40 x 128 bf16 turned, a reader of the queries 81 -> 74 us; below, where
+// the producer left them in the caches, 2000 tokens alone 10.4 -> 12.1.  Outputs come next, so they are marked only where they are gone by
+// then: 12 000 tokens and their reader 94 -> 84 us, but 8192 and theirs 55 -> 63; appends, whose keys the attention reads with all
+// else: 31 585 tokens 169 -> 139 us (with their attention 656 -> 656), 11 400 with theirs 206 -> 215.  (Chunks of one or two values are bound by their
+// instructions: 2.5 TB/s.)  moved: MB in and out.
+__host__ __device__ inline int32_t turn_once(int vec, int64_t moved, bool paged) {
+  return vec < 4 || moved < 128 ? TURN_KEPT : moved < (paged ? 512 : 224) ? TURN_ONCE_IN : TURN_ONCE_BOTH;
+}
 struct TurnSeg {
   const void* in;
   void* out;
@@ -35,7 +54,9 @@ struct TurnArgs {
   const double* rev;
   float magnitude, eps;
   int32_t T, hd, rot, half;
-  int32_t lanes_log2, groups, groups_per_item, n_item_cols;   // lanes of a head; head groups of a token, of an item; items of a token
+  int32_t lanes_log2, groups;  // lanes of a head; head groups of a token
+  TurnCols cols;
+  int64_t token_bytes;         // moved for a token, in and out
   int32_t once;                // what is marked as not wanted again: TURN_ONCE_*
   // appends: keys go to their pages
   const int32_t* slot;         // [T] page x 16 + slot
@@ -121,17 +142,17 @@ __device__ __forceinline__ void turn_angle(double pos, double rev, float magnitu
   s *= magnitude;
 }
 
-// Item `item` of the call: the head groups item % n_item_cols of token item / n_item_cols.  TI, TO: element types in and out.
+// Item `item` of the call: the item % cols.n th head groups of token item / cols.n.  TI, TO: element types in and out.
 template <typename TI, typename TO, int VEC, bool PAGED, int ONCE>
-__device__ __forceinline__ void turn_item(const TurnArgs& a, const uint32_t item) {
+__device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols, const uint32_t item) {
   constexpr int NU = VEC == 1 ? 2 : 1;                      // single values: up to 128 units on 64 lanes
   // Heads of a lane whose loads are on their way together: 64 bytes in all.  (128: fewer wavefronts fit; 6000 tokens of 40 x 128 f32 normed
   // 54.7 -> 46.8 us, 31585 tokens appended 173 -> 169.)
   constexpr int IT = NU == 1 && VEC * (int)sizeof(TI) <= 16 ? 2 : 1;
   const int lane = threadIdx.x & 63;
-  const uint32_t t = item / (uint32_t)a.n_item_cols;
-  const int g0 = (int)(item - t * (uint32_t)a.n_item_cols) * a.groups_per_item;
-  const int g1 = min(a.groups, g0 + a.groups_per_item);
+  const uint32_t t = item / (uint32_t)cols.n;
+  const int g0 = (int)(item - t * (uint32_t)cols.n) * cols.groups;
+  const int g1 = min(a.groups, g0 + cols.groups);
   const int per = 64 >> a.lanes_log2, sub = lane >> a.lanes_log2, u0 = lane & ((1 << a.lanes_log2) - 1);
   const int R = a.rot / (2 * VEC), rest = a.hd / VEC - 2 * R, rest_units = (rest + 1) / 2;
   const bool apart = VEC == 1 && !a.half;                   // single interleaved values: a unit is one pair

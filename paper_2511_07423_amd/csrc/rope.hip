@@ -152,7 +152,8 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   a.hd = hd;
   a.rot = rot;
   a.half = rope->desc.layout == SYNERA_ROPE_HALF;
-  const int64_t moved = (n_tokens * (a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes)) >> 20;      // MB
+  a.token_bytes = (int64_t)(a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes);
+  const int64_t moved = (n_tokens * a.token_bytes) >> 20;        // MB
   // (f32: a chunk of 8 is two vectors, each of which fills half a line.  Where the lines do not wait in a cache for their other halves, 4: 6000 tokens
   // of 40 x 128 normed 59 -> 51 us, 9000 82 -> 80; but 4000 tokens 36 -> 38, 4096 appended 37 -> 41.)
   int vec = in_bytes == 4 && !paged && moved >= 224 ? 4 : 8;
@@ -162,27 +163,17 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   while ((1 << a.lanes_log2) < std::min(units, 64)) ++a.lanes_log2;
   const int per = 64 >> a.lanes_log2;
   a.groups = (a.q.n_heads + a.k.n_heads + per - 1) / per;
-  // A token's head groups share its cosines and sines; they are spread over wavefronts while there are too few of those.
-  const int want = 4096;
-  int cols = (int)std::min<int64_t>(a.groups, std::max<int64_t>(1, want / std::max<int64_t>(1, n_tokens)));
-  a.groups_per_item = (a.groups + cols - 1) / cols;
-  a.n_item_cols = (a.groups + a.groups_per_item - 1) / a.groups_per_item;
-  // What the last-level cache (256 MB) could not hold for the next call anyway is marked as not wanted again, so that the rest stays there.
-  // Inputs are read for the last time: a producer, 8192 tokens of 40 x 128 bf16 turned, a reader of the queries 81 -> 74 us; below, where
-  // the producer left them in the caches, 2000 tokens alone 10.4 -> 12.1.  Outputs come next, so they are marked only where they are gone by
-  // then: 12 000 tokens and their reader 94 -> 84 us, but 8192 and theirs 55 -> 63; appends, whose keys the attention reads with all
-  // else: 31 585 tokens 169 -> 139 us (with their attention 656 -> 656), 11 400 with theirs 206 -> 215.  (Chunks of one or two values are bound by their
-  // instructions: 2.5 TB/s.)
-  a.once = vec < 4 || moved < 128 ? TURN_KEPT : moved < (paged ? 512 : 224) ? TURN_ONCE_IN : TURN_ONCE_BOTH;
+  a.cols = turn_cols(a.groups, a.T);
+  a.once = turn_once(vec, moved, paged);
   return vec;
 }
 
 // ------------------------------------------------------------------------------------ whole tensors
 template <typename T, int VEC, int ONCE>
 __global__ __launch_bounds__(256) void rope_kernel(TurnArgs a) {
-  const uint32_t items = (uint32_t)a.T * (uint32_t)a.n_item_cols;
+  const uint32_t items = (uint32_t)a.T * (uint32_t)a.cols.n;
   for (uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += gridDim.x * 4)
-    turn_item<T, T, VEC, false, ONCE>(a, item);
+    turn_item<T, T, VEC, false, ONCE>(a, a.cols, item);
 }
 
 template <typename T, int VEC>
@@ -195,7 +186,7 @@ static void launch_vec(const TurnArgs& a, uint32_t blocks, hipStream_t s) {
 }
 template <typename T>
 static hipError_t launch_rope(const TurnArgs& a, int vec, hipStream_t s) {
-  const uint32_t blocks = std::min(((uint32_t)a.T * (uint32_t)a.n_item_cols + 3) / 4, 1u << 22);   // a launch has less than 2^32 threads
+  const uint32_t blocks = std::min(((uint32_t)a.T * (uint32_t)a.cols.n + 3) / 4, 1u << 22);   // a launch has less than 2^32 threads
   switch (vec) {
     case 8: launch_vec<T, 8>(a, blocks, s); break;
     case 4: launch_vec<T, 4>(a, blocks, s); break;

@@ -14,6 +14,10 @@
 #include "shared.h"
 
 #define SH_STAGES 4            // plans that may run ahead of their uploads
+// Blocks of a captured append for each place of the attention (two a compute unit).  One kind, whose plans all fit the caches: a 64-token step 4.5 us,
+// in tensors of 3000 rows 5.4 (eager 4.4).  Any plan (33 000 rows): two, 24 prompts of 31 800 tokens 148 us (eager 138), a 64-token step 5.0; four, 148 and 5.1.
+#define SH_APPEND_KEPT 4
+#define SH_APPEND_ANY 2
 #define SH_CONST_AS __attribute__((address_space(4)))
 
 // ------------------------------------------------------------------------------------ the handle
@@ -219,8 +223,8 @@ struct AppendArgs {
   int64_t v_ts, v_hs;
   bf16_t* v_layer;
   int32_t n, hd;               // n = Hkv hd
+  int32_t v_blocks;            // the first blocks take values, the others heads (append_rows)
   int32_t v_pairs;             // whether two values of v can be loaded together
-  int32_t v_blocks;            // the first blocks take values, the others heads
 };
 
 template <typename TI>
@@ -297,17 +301,46 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindo
 }
 
 template <typename TI, int VEC, int ONCE>
-__global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
-  __shared__ __attribute__((aligned(16))) uint32_t turn[4][64 * 16];
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.v_blocks) {
     const uint32_t slabs = (uint32_t)(a.n + 127) / 128, items = (uint32_t)a.head->n_windows * slabs;
     for (uint32_t i = blockIdx.x * 4 + wave; i < items; i += (uint32_t)a.v_blocks * 4)
       append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
   } else {
-    const uint32_t items = (uint32_t)a.head->n_tokens * (uint32_t)a.turn.n_item_cols;
+    const uint32_t items = (uint32_t)a.head->n_tokens * (uint32_t)cols.n;
     for (uint32_t i = (blockIdx.x - a.v_blocks) * 4 + wave; i < items; i += (gridDim.x - a.v_blocks) * 4)
-      turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, i);
+      turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i);
+  }
+}
+// PLAN_KNOWN: an eager launch.  A captured one serves later plans, so how their heads are dealt out goes by the plan that it finds.  PLAN_KEPT: no
+// plan that its tensors have room for is marked.  PLAN_ANY: what is marked goes by the plan too, and, since the launch cannot have an item for each
+// wavefront of the largest, values and heads are taken from one list, so that both end together.
+enum { PLAN_KNOWN, PLAN_KEPT, PLAN_ANY };
+template <typename TI, int VEC, int ONCE>
+__device__ __forceinline__ void append_listed(const AppendArgs& a, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t slabs = (uint32_t)(a.n + 127) / 128, values = (uint32_t)a.head->n_windows * slabs;
+  const uint32_t all = values + (uint32_t)a.head->n_tokens * (uint32_t)cols.n;
+  for (uint32_t i = blockIdx.x * 4 + wave; i < all; i += gridDim.x * 4) {
+    if (i < values) append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
+    else turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i - values);
+  }
+}
+template <typename TI, int VEC, int ONCE, int PLAN>
+__global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint32_t turn[4][64 * 16];
+  if constexpr (PLAN == PLAN_KNOWN) {
+    append_rows<TI, VEC, ONCE>(a, a.turn.cols, turn);
+  } else if constexpr (PLAN == PLAN_KEPT) {
+    append_rows<TI, VEC, ONCE>(a, turn_cols(a.turn.groups, a.head->n_tokens), turn);
+  } else {
+    const int32_t T = a.head->n_tokens;
+    const TurnCols cols = turn_cols(a.turn.groups, T);
+    const int32_t once = turn_once(VEC, (T * a.turn.token_bytes) >> 20, true);
+    if (once == TURN_ONCE_BOTH) append_listed<TI, VEC, TURN_ONCE_BOTH>(a, cols, turn);
+    else if (once == TURN_ONCE_IN) append_listed<TI, VEC, TURN_ONCE_IN>(a, cols, turn);
+    else append_listed<TI, VEC, TURN_KEPT>(a, cols, turn);
   }
 }
 
@@ -323,34 +356,38 @@ static Range pool_range(const synera_batch* b, const void* p) {
 }
 
 // Tokens that the checks of a call go by: the plan's; of a captured call, which serves later plans too, as many as all its tensors have room
-// for.  -1: a tensor lacks room for the plan at hand.
-static int64_t tokens_to_check(const synera_batch* b, bool graph, std::initializer_list<const synera_heads*> heads) {
+// for.  -1: a tensor lacks room for the plan at hand.  room: tokens that any plan may bring to these tensors.
+static int64_t tokens_to_check(const synera_batch* b, bool graph, std::initializer_list<const synera_heads*> heads, int64_t& room) {
   const int64_t T = b->plan.head.n_tokens;
-  int64_t room = 0;
+  room = 0;
   for (const synera_heads* h : heads) {
     if (!h || !h->n_rows) continue;
     if (h->n_rows < T) return -1;
     room = room ? std::min<int64_t>(room, h->n_rows) : h->n_rows;
   }
+  const int64_t said = room;
+  room = std::min<int64_t>(said ? said : INT64_MAX, b->lim.max_tokens);
   if (!graph) return std::max<int64_t>(T, 1);
-  return std::max<int64_t>({T, 1, std::min<int64_t>(room ? room : 2, b->lim.max_tokens)});
+  return std::max<int64_t>({T, 1, said ? room : std::min<int64_t>(room, 2)});
 }
 
 template <typename TI, int VEC>
-static void append_vec(const AppendArgs& a, uint32_t blocks, hipStream_t s) {
+static void append_vec(const AppendArgs& a, int plan, uint32_t blocks, hipStream_t s) {
   if constexpr (VEC >= 4) {
-    if (a.turn.once == TURN_ONCE_BOTH) return append_rope_kernel<TI, VEC, TURN_ONCE_BOTH><<<blocks, 256, 0, s>>>(a);
-    if (a.turn.once == TURN_ONCE_IN) return append_rope_kernel<TI, VEC, TURN_ONCE_IN><<<blocks, 256, 0, s>>>(a);
+    if (plan == PLAN_ANY) return append_rope_kernel<TI, VEC, TURN_KEPT, PLAN_ANY><<<blocks, 256, 0, s>>>(a);
+    if (plan == PLAN_KNOWN && a.turn.once == TURN_ONCE_BOTH) return append_rope_kernel<TI, VEC, TURN_ONCE_BOTH, PLAN_KNOWN><<<blocks, 256, 0, s>>>(a);
+    if (plan == PLAN_KNOWN && a.turn.once == TURN_ONCE_IN) return append_rope_kernel<TI, VEC, TURN_ONCE_IN, PLAN_KNOWN><<<blocks, 256, 0, s>>>(a);
   }
-  append_rope_kernel<TI, VEC, TURN_KEPT><<<blocks, 256, 0, s>>>(a);
+  if (plan == PLAN_KNOWN) return append_rope_kernel<TI, VEC, TURN_KEPT, PLAN_KNOWN><<<blocks, 256, 0, s>>>(a);
+  append_rope_kernel<TI, VEC, TURN_KEPT, PLAN_KEPT><<<blocks, 256, 0, s>>>(a);
 }
 template <typename TI>
-static hipError_t launch_append(const AppendArgs& a, int vec, uint32_t blocks, hipStream_t s) {
+static hipError_t launch_append(const AppendArgs& a, int plan, int vec, uint32_t blocks, hipStream_t s) {
   switch (vec) {
-    case 8: append_vec<TI, 8>(a, blocks, s); break;
-    case 4: append_vec<TI, 4>(a, blocks, s); break;
-    case 2: append_vec<TI, 2>(a, blocks, s); break;
-    default: append_vec<TI, 1>(a, blocks, s);
+    case 8: append_vec<TI, 8>(a, plan, blocks, s); break;
+    case 4: append_vec<TI, 4>(a, plan, blocks, s); break;
+    case 2: append_vec<TI, 2>(a, plan, blocks, s); break;
+    default: append_vec<TI, 1>(a, plan, blocks, s);
   }
   return hipGetLastError();
 }
@@ -367,7 +404,8 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   const ShLimits& l = b->lim;
   const int bytes = dtype == 0 ? 4 : 2, hd = l.hd;
   if (rope->desc.head_dim != hd || k->n_heads != l.Hkv || v->n_heads != l.Hkv || (q && q->n_heads != l.Hq)) return SYNERA_EINVAL;
-  const int64_t n1 = tokens_to_check(b, graph, {q, k, v});
+  int64_t room;
+  const int64_t n1 = tokens_to_check(b, graph, {q, k, v}, room);
   if (n1 < 0) return SYNERA_EINVAL;
   int32_t st = turn_check(*k, n1, hd, bytes, 2, false);
   if (st == SYNERA_OK) st = turn_check(*v, n1, hd, bytes, 2, false);
@@ -408,13 +446,22 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
   a.hd = hd;
   const uint64_t va = reinterpret_cast<uintptr_t>(v->d_in) | (uint64_t)(v->in_token * bytes) | (uint64_t)(v->in_head * bytes);
   a.v_pairs = va % (2 * bytes) == 0;
-  const int64_t v_items = std::max<int64_t>(1, (int64_t)b->plan.head.n_windows * ((a.n + 127) / 128));
-  a.v_blocks = (int32_t)std::min<int64_t>((v_items + 3) / 4, 1 << 16);
-  const int64_t t_blocks = std::min<int64_t>((T * a.turn.n_item_cols + 3) / 4, 1 << 20);
-  const uint32_t blocks = (uint32_t)(a.v_blocks + t_blocks);
-  const hipError_t e = dtype == 0   ? launch_append<float>(a, vec, blocks, s)
-                       : dtype == 1 ? launch_append<bf16_t>(a, vec, blocks, s)
-                                    : launch_append<_Float16>(a, vec, blocks, s);
+  // A wavefront for each item: of the plan at hand, or, in a captured call, of the largest that the tensors have room for; but no more than
+  // fill the chip a few times, since a small plan finds them all, too.
+  const int64_t slabs = (a.n + 127) / 128;
+  int64_t v_items = std::max<int64_t>(1, b->plan.head.n_windows * slabs), t_items = T * a.turn.cols.n, most_v = 1 << 16, most = 1 << 20;
+  int plan = PLAN_KNOWN;
+  if (graph) {
+    plan = turn_once(vec, (room * a.turn.token_bytes) >> 20, true) == TURN_KEPT ? PLAN_KEPT : PLAN_ANY;
+    v_items = std::min(room, 2 * std::min<int64_t>(l.max_batch, room) + room / SY_PAGE) * slabs;      // (sh_limits)
+    t_items = std::min(room * a.turn.groups, std::max<int64_t>(room, 4096));                          // (turn_cols)
+    most_v = most = SH_APPEND_KEPT * (int64_t)l.slots;
+  }
+  a.v_blocks = (int32_t)std::min((v_items + 3) / 4, most_v);
+  const uint32_t blocks = (uint32_t)(plan == PLAN_ANY ? SH_APPEND_ANY * (int64_t)l.slots : a.v_blocks + std::min((t_items + 3) / 4, most));
+  const hipError_t e = dtype == 0   ? launch_append<float>(a, plan, vec, blocks, s)
+                       : dtype == 1 ? launch_append<bf16_t>(a, plan, vec, blocks, s)
+                                    : launch_append<_Float16>(a, plan, vec, blocks, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
@@ -971,7 +1018,8 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16 || reinterpret_cast<uintptr_t>(d_lse) % 4) return SYNERA_EINVAL;
   const ShLimits& l = b->lim;
   if (q->n_heads != l.Hq) return SYNERA_EINVAL;
-  const int64_t n1 = tokens_to_check(b, graph, {q});
+  int64_t room;
+  const int64_t n1 = tokens_to_check(b, graph, {q}, room);
   if (n1 < 0) return SYNERA_EINVAL;
   if (turn_check(*q, n1, l.hd, 2, 2, true) != SYNERA_OK) return SYNERA_EINVAL;
   if ((reinterpret_cast<uintptr_t>(q->d_in) | (uint64_t)(2 * q->in_token) | (uint64_t)(2 * q->in_head)) % 16) return SYNERA_EINVAL;

@@ -1,5 +1,6 @@
 """GPU parity of appends with the rotation and of attention over shared prefixes with float64: element by element, over random trees of
 shared pages whose unwritten slots hold NaN."""
+import ctypes as C
 import random
 
 import numpy as np
@@ -518,3 +519,110 @@ def test_captured_calls_are_checked_for_later_plans():
     b.plan([3], [2], [[0]], 16)
     assert raw._lib.synera_append_rope(b._h, rope._h, 1, None, short, heads[2], 0.0, kp.data_ptr(), vp.data_ptr(), None) == s.EINVAL
     torch.cuda.synchronize()
+
+
+def blocks_of_kernels(graph):
+    """Grids of the kernels in a captured graph, from the runtime itself."""
+    class Params(C.Structure):                                 # hipKernelNodeParams
+        _fields_ = [("block", C.c_uint * 3), ("extra", C.c_void_p), ("func", C.c_void_p), ("grid", C.c_uint * 3), ("args", C.c_void_p), ("lds", C.c_uint)]
+    path = next(line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line)
+    hip = C.CDLL(path)
+    at, n = C.c_void_p(graph.raw_cuda_graph()), C.c_size_t(0)
+    assert hip.hipGraphGetNodes(at, None, C.byref(n)) == 0
+    nodes = (C.c_void_p * n.value)()
+    assert hip.hipGraphGetNodes(at, nodes, C.byref(n)) == 0
+    grids = []
+    for node in nodes:
+        kind = C.c_int(-1)
+        assert hip.hipGraphNodeGetType(C.c_void_p(node), C.byref(kind)) == 0
+        if kind.value == 0:                                    # hipGraphNodeTypeKernel
+            params = Params()
+            assert hip.hipGraphKernelNodeGetParams(C.c_void_p(node), C.byref(params)) == 0
+            grids.append(tuple(params.grid))
+    return grids
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
+def test_captured_appends_are_launched_for_the_room_they_have(dtype, hd):
+    """Behind a plan of one token: a captured append fills the chip if its tensors have the rows for it, and no more blocks than their rows can
+    use if not."""
+    s, hq, hkv, rows = synera(), 32, 8, 4096
+    rope = s.Rope(hd)
+    b = s.SharedBatch(hq, hkv, hd, 64, rows, 300)
+    b.plan([3], [1], [[0]], 16)
+    kp, vp = draw((16, hkv, P, hd), 1), draw((16, hkv, hd, P), 2)
+    x = draw((rows, hq + 2 * hkv, hd), 3, TYPES[dtype])
+    out = torch.empty((rows, hq, hd), dtype=torch.bfloat16, device=DEV)
+    places = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+
+    def grid(n):
+        part = x[:n]
+        (blocks, _, _), = blocks_of_kernels(captured(lambda: b.append_rope(rope, part[:, :hq], part[:, hq: hq + hkv], part[:, hq + hkv:], kp, vp,
+                                                                           out_q=out[:n])))
+        return blocks
+    slabs = hkv * hd // 128                                    # pieces of a token's values, one a wavefront
+    assert grid(rows) >= 2 * places
+    assert grid(1) <= slabs + hq + hkv
+    assert grid(8) <= 8 * (slabs + hq + hkv)
+
+
+def test_a_captured_append_serves_batches_of_any_size():
+    """Captured behind one token, replayed for steps, drafts and prompts in every element type: the eager call's bits."""
+    s, hq, hkv, hd, rows = synera(), 32, 8, 128, 6000
+    rope = s.Rope(hd, 64, layout="half")
+    b = s.SharedBatch(hq, hkv, hd, 64, rows, 400)
+    n_pages = 1000
+    pools = draw((n_pages, hkv, P, hd), 1), draw((n_pages, hkv, hd, P), 2)
+    gains = draw((hd,), 3) + 1, draw((hd,), 4) + 1
+    plans = [(np.zeros(64, np.int32), np.ones(64, np.int32)), (np.arange(64) * 3, 1 + np.arange(64) % 16), (np.array([5]), np.array([6000])),
+             (np.array([0, 7, 31]), np.array([900, 1, 2000])), (np.array([3]), np.array([1]))]
+    for dtype in TYPES:
+        x = draw((rows, hq + 2 * hkv, hd), 5, TYPES[dtype])
+        q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+        out = torch.zeros((rows, hq, hd), dtype=torch.bfloat16, device=DEV)
+        b.plan([3], [1], [[0]], n_pages)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.append_rope(rope, q, k, v, *pools, q_gain=gains[0], k_gain=gains[1], out_q=out)
+        for ctx, new in plans + plans[::-1]:
+            need = -(-(ctx + new) // P)
+            table = np.full((len(ctx), int(need.max())), -1, np.int32)
+            perm = np.random.RandomState(len(ctx)).permutation(n_pages)
+            for i in range(len(ctx)):
+                table[i, : need[i]] = perm[need[:i].sum(): need[: i + 1].sum()]
+            b.plan(ctx, new, table, n_pages)
+            T = int(new.sum())
+            wanted = [p.clone() for p in pools]
+            want = b.append_rope(rope, q, k, v, *wanted, q_gain=gains[0], k_gain=gains[1])
+            out.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[:T], want[:T]) and (out[T:] == 7).all(), (dtype, T)
+            assert all(torch.equal(a, c) for a, c in zip(pools, wanted)), (dtype, T)
+
+
+def test_captured_appends_that_no_cache_holds():
+    """A captured append whose plans pass the caches by or do not, with tensors that have room for both: the eager call's bits."""
+    s, hq, hkv, hd, rows = synera(), 32, 8, 128, 17500
+    rope, b = s.Rope(hd, layout="half"), s.SharedBatch(hq, hkv, hd, 1, rows, 1100)
+    n_pages = 1100
+    table = np.random.RandomState(1).permutation(n_pages).astype(np.int32)[None]
+    pools = [torch.zeros((n_pages, hkv, P, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((n_pages, hkv, hd, P), dtype=torch.bfloat16, device=DEV)]
+    x = draw((rows, hq + 2 * hkv, hd), 1, torch.float32)                             # 537 MB moved for all rows, 31 KB for one
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    out = torch.zeros((rows, hq, hd), dtype=torch.bfloat16, device=DEV)
+    b.plan([3], [1], table[:, :1], n_pages)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.append_rope(rope, q, k, v, *pools, out_q=out)
+    for T in (rows - 3, 1, 5001):                                                    # marked, kept, inputs marked
+        b.plan([7], [T], table, n_pages)
+        wanted = [p.clone() for p in pools]
+        want = b.append_rope(rope, q, k, v, *wanted)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:T], want[:T]) and (out[T:] == 7).all(), T
+        assert all(torch.equal(a, c) for a, c in zip(pools, wanted)), T
