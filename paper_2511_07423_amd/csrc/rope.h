@@ -54,6 +54,9 @@ struct TurnArgs {
   const double* rev;
   float magnitude, eps;
   int32_t T, hd, rot, half;
+  int32_t rest_half;           // value i of the rest of a head (from rot on) shares a unit with value i + rest_half: goes by hd and rot alone
+  int32_t as_wide;             // 1, 2 (more than 64 units): single values whose squares are summed in the order of the wider chunks that other calls
+                               // for such heads take
   int32_t lanes_log2, groups;  // lanes of a head; head groups of a token
   TurnCols cols;
   int64_t token_bytes;         // moved for a token, in and out
@@ -154,7 +157,7 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols
   const int g0 = (int)(item - t * (uint32_t)cols.n) * cols.groups;
   const int g1 = min(a.groups, g0 + cols.groups);
   const int per = 64 >> a.lanes_log2, sub = lane >> a.lanes_log2, u0 = lane & ((1 << a.lanes_log2) - 1);
-  const int R = a.rot / (2 * VEC), rest = a.hd / VEC - 2 * R, rest_units = (rest + 1) / 2;
+  const int R = a.rot / (2 * VEC), rest_units = a.rest_half / VEC;
   const bool apart = VEC == 1 && !a.half;                   // single interleaved values: a unit is one pair
   int ca[NU], cb[NU];                                       // first value of the unit's chunks, -1: none
   float cs[NU][VEC], sn[NU][VEC];
@@ -180,7 +183,7 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols
       }
     } else if (u - R < rest_units) {
       ca[n] = (2 * R + u - R) * VEC;
-      if (u - R + rest_units < rest) cb[n] = ca[n] + rest_units * VEC;
+      if (ca[n] + a.rest_half < a.hd) cb[n] = ca[n] + a.rest_half;
     }
   }
   for (int g = g0; g < g1; g += IT) {
@@ -218,7 +221,14 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols
       }
       if (a.q.gain || a.k.gain) {                           // uniform; heads without gains pass by
         // (The gains come from the nearest cache each time.  Kept from the beginning, they were waited for before the heads: 47 -> 64 us.)
-        // (Neighbours first, in a lane and between lanes: the order of the sum does not depend on VEC, which goes by sizes and alignment.)
+        // The order of the sum goes by hd, rot and layout alone, not by VEC, which goes by sizes and alignment too: squares x[p]^2 + x[p + rot / 2]^2
+        // of the turned part, then x[p]^2 + x[p + rest_half]^2 of the rest, in a binary tree over p, neighbours first.  (Heads that only single values
+        // divide have an order of their own: in this one 2000 x 20 of 250 take 33 in place of 30 us.  Rows of other heads that start on odd elements pay for it:
+        // 3000 x 40 of 128 71 -> 76 us, interleaved 72 -> 82.)
+        auto across = [&](float v) {
+          for (int o = 1; o < 1 << a.lanes_log2; o *= 2) v += __shfl_xor(v, o);
+          return v;
+        };
         float ss = 0.f;
 #pragma unroll
         for (int n = 0; n < NU; ++n) {
@@ -229,9 +239,23 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols
           for (int o = 1; o < VEC; o *= 2)
 #pragma unroll
             for (int j = 0; j < VEC; j += 2 * o) sq[j] += sq[j + o];
+          if (VEC == 1 && a.as_wide) {
+            if (apart && on && turned[n]) {                 // the lane holds a pair: the two values that are summed together are read again
+              const TI* in = static_cast<const TI*>(is_q ? a.q.in : a.k.in) + (int64_t)t * (is_q ? a.q.in_ts : a.k.in_ts) +
+                             (int64_t)(is_q ? h : h - a.q.n_heads) * (is_q ? a.q.in_hs : a.k.in_hs) + u0 + 64 * n;
+              TurnChunk<TI, 1> x, y;
+              float fx, fy;
+              x.load(in);
+              y.load(in + R);
+              x.widen(&fx);
+              y.widen(&fy);
+              sq[0] = __builtin_fmaf(fx, fx, fy * fy);
+            }
+            if (a.as_wide > n) sq[0] = across(sq[0]);
+          }
           ss += sq[0];
         }
-        for (int o = 1; o < 1 << a.lanes_log2; o *= 2) ss += __shfl_xor(ss, o);
+        if (!(VEC == 1 && a.as_wide)) ss = across(ss);
         const float inv = 1.0f / sqrtf(ss / (float)a.hd + a.eps);
         if (gain && on) {
 #pragma unroll

@@ -152,13 +152,17 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   a.hd = hd;
   a.rot = rot;
   a.half = rope->desc.layout == SYNERA_ROPE_HALF;
+  int widest = 8;                                            // chunk that the head takes where everything is aligned
+  while (hd % widest || rot % (2 * widest)) widest /= 2;
+  a.rest_half = ((hd - rot) / widest + 1) / 2 * widest;
   a.token_bytes = (int64_t)(a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes);
   const int64_t moved = (n_tokens * a.token_bytes) >> 20;        // MB
   // (f32: a chunk of 8 is two vectors, each of which fills half a line.  Where the lines do not wait in a cache for their other halves, 4: 6000 tokens
   // of 40 x 128 normed 59 -> 51 us, 9000 82 -> 80; but 4000 tokens 36 -> 38, 4096 appended 37 -> 41.)
   int vec = in_bytes == 4 && !paged && moved >= 224 ? 4 : 8;
   while (vec > 1 && !(fits(vec, rope, q, in_bytes, out_bytes, true) && fits(vec, rope, k, in_bytes, out_bytes, !paged))) vec /= 2;
-  const int units = rot / (2 * vec) + (hd / vec - rot / vec + 1) / 2;
+  const int units = rot / (2 * vec) + a.rest_half / vec;
+  a.as_wide = vec == 1 && widest > 1 ? (units > 64 ? 2 : 1) : 0;
   a.lanes_log2 = 0;
   while ((1 << a.lanes_log2) < std::min(units, 64)) ++a.lanes_log2;
   const int per = 64 >> a.lanes_log2;

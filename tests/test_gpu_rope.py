@@ -220,3 +220,34 @@ def test_sizes_that_no_cache_holds(T, heads, rot, dtype):
         for t in range(0, T, 1500):
             part = call(pos[t: t + 1500], x[t: t + 1500, :hq], x[t: t + 1500, hq:])
             assert all(torch.equal(w[t: t + 1500], p) for w, p in zip(whole, part)), t
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("hd,rot", [(128, 128), (120, 16), (120, 40), (80, 20), (104, 16), (256, 256), (250, 250), (200, 64), (72, 36)])
+def test_norms_do_not_depend_on_alignment(hd, rot, dtype, layout):
+    """The order of a norm's sum goes by the head alone: rows that start on any element give the bits of aligned ones."""
+    rope, T, heads = synera().Rope(hd, rot, layout=layout), 40, 10
+    x, pos = draw((T, heads, hd), TYPES[dtype], hd + rot, 2.0), positions(T, 1)
+    gain = draw((hd,), torch.bfloat16, 5) + 1
+    want, _ = rope.norm_apply(pos, x, None, gain, None, 1e-5)
+    for shift in (1, 2, 4):
+        flat = torch.empty((x.numel() + 8,), dtype=x.dtype, device=DEV)
+        odd = flat[shift: shift + x.numel()].view(x.shape)
+        odd.copy_(x)
+        got, _ = rope.norm_apply(pos, odd, None, gain, None, 1e-5)
+        assert torch.equal(got, want), (shift, (got != want).sum().item())
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("hd,rot", [(120, 16), (120, 120)])
+def test_norms_do_not_depend_on_other_tokens(hd, rot, layout):
+    """f32 calls of more than 224 MB go in narrower chunks: the bits of the same tokens in small calls, where the part that does not turn is an
+    odd number of chunks too."""
+    rope, T, heads = synera().Rope(hd, rot, layout=layout), 6400, 40                # 246 MB in and out
+    x, pos = draw((T, heads, hd), torch.float32, rot, 2.0), positions(T, 1)
+    gain = draw((hd,), torch.bfloat16, 5) + 1
+    whole, _ = rope.norm_apply(pos, x, None, gain, None, 1e-5)
+    for t in range(0, T, 1600):
+        part, _ = rope.norm_apply(pos[t: t + 1600], x[t: t + 1600], None, gain, None, 1e-5)
+        assert torch.equal(whole[t: t + 1600], part), t
