@@ -140,7 +140,8 @@ int32_t synera_append_rope(synera_batch* batch, const synera_rope* rope, int32_t
  * read once for all of them where that is the shorter way.
  *   q->d_in, q->d_out   bf16 [T][n_q_heads][head_dim], rotated queries in, o out; gains unused.  Not in place.  d_in and its
  *                       strides on 16 bytes, d_out and its strides on 8
- *   scale               finite, > 0 (0 takes 1 / sqrt(head_dim))
+ *   scale               > 0, finite in 32 bits times log2 e: below 2.35e38 (0 takes 1 / sqrt(head_dim)).  Scores scale q k beyond that do
+ *                       not fit 32 bits either: their rows may be NaN
  *   d_lse               f32 [T][n_q_heads], ln sum exp(scale q k), or NULL
  * Softmax statistics and sums are 32-bit; the probabilities meet the bf16 values as bf16.  Keys and values that a
  * row does not see may hold anything, infinities and NaN too.  Outputs must not lie on inputs.  Calls with one batch

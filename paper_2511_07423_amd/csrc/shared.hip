@@ -1012,6 +1012,8 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
                                            float scale, float* d_lse, void* stream) {
   if (!b || !q || !d_k_layer || !d_v_layer || !b->planned) return SYNERA_EINVAL;
   if (!std::isfinite(scale) || scale < 0.f) return SYNERA_EINVAL;
+  const float c = (scale > 0.f ? scale : 1.0f / sqrtf((float)b->lim.hd)) * 1.4426950408889634f;
+  if (!std::isfinite(c)) return SYNERA_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool graph = capturing(s);
   if (b->plan.head.n_tokens == 0 && !graph) return SYNERA_OK;
@@ -1050,7 +1052,7 @@ extern "C" int32_t synera_shared_attention(synera_batch* b, const synera_heads* 
   a.part_o = b->part_o;
   a.part_ml = b->part_ml;
   a.lse = d_lse;
-  a.c = (scale > 0.f ? scale : 1.0f / sqrtf((float)l.hd)) * 1.4426950408889634f;
+  a.c = c;
   a.m0 = a.c > 1.f ? -3e38f / a.c : -3e38f;
   a.Hq = l.Hq;
   a.Hkv = l.Hkv;

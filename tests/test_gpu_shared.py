@@ -626,3 +626,19 @@ def test_captured_appends_that_no_cache_holds():
         torch.cuda.synchronize()
         assert torch.equal(out[:T], want[:T]) and (out[T:] == 7).all(), T
         assert all(torch.equal(a, c) for a, c in zip(pools, wanted)), T
+
+
+def test_a_scale_that_is_not_finite_in_the_exponent_is_refused():
+    """The scale meets log2 e in 32 bits: beyond 2.35e38 there is no such number, and no weight could be formed."""
+    s = synera()
+    b = s.SharedBatch(2, 1, 64, 1, 1, 1)
+    b.plan([4], [1], [[0]], 1)
+    kp, vp, q = draw((1, 1, P, 64), 1), draw((1, 1, 64, P), 2), draw((1, 2, 64), 3)
+    for scale in (3e38, 2.4e38):
+        with pytest.raises(s.SyneraError) as e:
+            b.attention(q, kp, vp, scale=scale)
+        assert e.value.status == s.EINVAL
+    tiny = (q.float() * 2.0 ** -60).to(torch.bfloat16)         # the largest scales weigh the largest score alone
+    o = b.attention(tiny, kp, vp, scale=2.0 ** 80)
+    best = (tiny[0].double() @ kp[0, 0, :5].double().T).argmax(1)
+    assert torch.equal(o[0], vp[0, 0].T[best])
