@@ -641,4 +641,7 @@ def test_a_scale_that_is_not_finite_in_the_exponent_is_refused():
     tiny = (q.float() * 2.0 ** -60).to(torch.bfloat16)         # the largest scales weigh the largest score alone
     o = b.attention(tiny, kp, vp, scale=2.0 ** 80)
     best = (tiny[0].double() @ kp[0, 0, :5].double().T).argmax(1)
-    assert torch.equal(o[0], vp[0, 0].T[best])
+    # One key has all the weight, p = 2^(s c - m c) with m c rounded to 32 bits: near 2^23 that is up to half a unit off, so p is not 1.  It meets
+    # the value as bf16 (2^-8) and is divided by itself unrounded; the output is bf16 (2^-8): (1 + 2^-8)^2 - 1 < 2^-7 + 2^-15, and 32-bit steps.
+    want = vp[0, 0].T[best].double()
+    assert ((o[0].double() - want).abs() <= want.abs() * (2.0 ** -7 + 2.0 ** -14)).all()
