@@ -645,3 +645,16 @@ def test_a_scale_that_is_not_finite_in_the_exponent_is_refused():
     # the value as bf16 (2^-8) and is divided by itself unrounded; the output is bf16 (2^-8): (1 + 2^-8)^2 - 1 < 2^-7 + 2^-15, and 32-bit steps.
     want = vp[0, 0].T[best].double()
     assert ((o[0].double() - want).abs() <= want.abs() * (2.0 ** -7 + 2.0 ** -14)).all()
+
+
+def test_attention_refuses_outputs_on_the_values():
+    s, hq, hkv, hd = synera(), 4, 2, 64
+    b = s.SharedBatch(hq, hkv, hd, 1, 2, 1)
+    b.plan([4], [2], [[0]], 2)
+    kp, vp, q, k = draw((2, hkv, P, hd), 1), draw((2, hkv, hd, P), 2), draw((2, hq, hd), 3), draw((2, hkv, hd), 4)
+    on_values = vp.view(-1)[: q.numel()].view(q.shape)
+    for call in (lambda: b.attention(q, kp, vp, out=on_values), lambda: b.append_rope(s.Rope(hd), q, k, k, kp, vp, out_q=on_values),
+                 lambda: b.append_rope(s.Rope(hd), None, k, vp.view(-1, hkv, hd)[:2], kp, vp)):
+        with pytest.raises(s.SyneraError) as e:
+            call()
+        assert e.value.status == s.EINVAL

@@ -43,3 +43,39 @@ def test_inner_loops_do_not_drain_their_copies(head_dim):
         spills = [x for x, _ in part if "scratch_" in x]
         waits = [x for x, inline in part if "s_waitcnt" in x and "vmcnt" in x and not inline]
         assert not spills and not waits, (spills[:3], waits[:3])
+
+
+def whole_loops(text, kernel):
+    """All loops of a kernel, up to the function's own end: lists of (line, inside inline assembly), and the line numbers they span."""
+    body = re.search(rf"^{kernel}:(.*?)^\.Lfunc_end\d+:", text, re.S | re.M).group(1).split("\n")
+    label = {m.group(1): i for i, line in enumerate(body) if (m := re.match(r"(\.LBB\S+):", line))}
+    inline, marked = False, []
+    for line in body:
+        inline = (inline or "#ASMSTART" in line) and "#ASMEND" not in line
+        marked.append((line, inline))
+    spans = {(label[m.group(1)], i) for i, line in enumerate(body)
+             if (m := re.search(r"s_c?branch\S*\s+(\.LBB\S+)", line)) and label.get(m.group(1), i) < i}
+    return marked, spans
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_each_form_of_the_attention_has_its_loop(head_dim):
+    """Four loops over tiles that need no mask, each found and each checked from end to end: wavefronts alone and four to the keys (no barrier), two
+    by two (one), four to the rows (one for two tiles)."""
+    if not os.path.exists(ASM):
+        pytest.skip("the library was built elsewhere: no assembly here")
+    marked, spans = whole_loops(open(ASM).read(), rf"_Z18shared_attn_kernelILi{head_dim}EEv14SharedAttnArgs")
+    tile = head_dim // 8                          # products of a tile: head_dim / 16 of the scores, 2 x head_dim / 32 of the values
+
+    def count(span, word):
+        return sum(word in x for x, _ in marked[span[0]: span[1] + 1])
+    # (the masked tiles' loops hold one that goes key by key: products, no copies)
+    by_key = [s for s in spans if count(s, "v_mfma") and not count(s, "global_load_lds")]
+    free = [s for s in spans if count(s, "v_mfma") in (tile, 2 * tile) and count(s, "global_load_lds") and
+            not any(s[0] <= k[0] and k[1] <= s[1] for k in by_key)]
+    free = [s for s in free if not any(o[0] <= s[0] and s[1] <= o[1] and o != s for o in free)]
+    assert sorted((count(s, "v_mfma") // tile, count(s, "s_barrier")) for s in free) == [(1, 0), (1, 0), (1, 1), (2, 1)]
+    for a, b in free:
+        spills = [x for x, _ in marked[a: b + 1] if "scratch_" in x]
+        waits = [x for x, inline in marked[a: b + 1] if "s_waitcnt" in x and "vmcnt" in x and not inline]
+        assert not spills and not waits, (spills[:3], waits[:3])
