@@ -50,7 +50,7 @@ typedef struct synera_rope_desc {
 
 typedef struct synera_rope synera_rope;
 
-/* Errors: EINVAL (null, a value outside the ranges above or not finite), EUNSUP (head_dim > 256), EHIP, ENOMEM. */
+/* Errors: EINVAL (null, a value outside the ranges above or not finite, an f_i whose 2^31 f_i / (2 pi) is not finite in 64 bits), EUNSUP (head_dim > 256), EHIP, ENOMEM. */
 int32_t synera_rope_create(synera_rope** out, const synera_rope_desc* desc);
 /* Waits for the device.  NULL is allowed. */
 int32_t synera_rope_destroy(synera_rope* rope);

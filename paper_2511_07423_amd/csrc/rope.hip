@@ -43,6 +43,7 @@ extern "C" int32_t synera_rope_create(synera_rope** out, const synera_rope_desc*
       }
     }
     rev[i] = f / two_pi;
+    if (!std::isfinite(rev[i] * 2147483648.0)) return SYNERA_EINVAL;     // the turns of the farthest position
   }
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) {

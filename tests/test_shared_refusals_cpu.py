@@ -94,3 +94,12 @@ def test_the_planning_hook_from_python():
             s.debug_shared_plan(hq, hkv, 4, [3], [1], [[0]])
         assert e.value.status == s.EINVAL
     assert s.debug_shared_plan(2, 2, 4, [3], [1], [[0]])["head"][0, 0] == 1
+
+
+@pytest.mark.parametrize("bad", [dict(scaling=("linear", 5e-324)), dict(scaling=("bands", 5e-324, 1.0, 4.0, 8192.0)), dict(scaling=("linear", 1e-300)),
+                                 dict(inv_freq=np.full(32, 1e308)), dict(inv_freq=np.r_[np.ones(31), -1e300])])
+def test_frequencies_turn_by_finite_angles_at_every_position(bad):
+    """pos f / 2 pi is formed in 64 bits for any int32 position: frequencies that are infinite there, or become so, are refused."""
+    with pytest.raises(s.SyneraError) as e:
+        s.Rope(64, **bad)
+    assert e.value.status == s.EINVAL
