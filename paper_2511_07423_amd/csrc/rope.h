@@ -329,6 +329,8 @@ int32_t turn_check(const synera_heads& s, int64_t n_tokens, int hd, int in_bytes
 // Whether an output and an input of one call, or two outputs, lie on one another other than as one tensor in place.
 bool turn_overlap(const void* a, int64_t a_ts, int64_t a_hs, int a_heads, int a_bytes, const void* b, int64_t b_ts, int64_t b_hs,
                   int b_heads, int b_bytes, int64_t n_tokens, int hd);
+// Whether `size` bytes of an input lie on the heads that an output writes (between tokens they may).
+bool turn_on_output(const synera_heads& s, int64_t n_tokens, int hd, int out_bytes, const void* at, int64_t size);
 // Fills the segments, VEC and the lane geometry of `a` from the rope and the heads (q or k may be null).
 int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const synera_heads* q, const synera_heads* k, int in_bytes,
                int out_bytes, bool paged, float eps);

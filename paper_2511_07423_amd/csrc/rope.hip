@@ -115,6 +115,17 @@ bool turn_overlap(const void* a, int64_t a_ts, int64_t a_hs, int a_heads, int a_
   return true;
 }
 
+bool turn_on_output(const synera_heads& s, int64_t n, int hd, int out_bytes, const void* at, int64_t size) {
+  const uintptr_t out = reinterpret_cast<uintptr_t>(s.d_out), in = reinterpret_cast<uintptr_t>(at);
+  const int64_t step = s.out_token * out_bytes, span = ((int64_t)(s.n_heads - 1) * s.out_head + hd) * out_bytes;
+  if (!at || in + size <= out || out + (n - 1) * step + span <= in) return false;
+  if (in > out && span <= step) {                    // in the gap between two tokens?
+    const int64_t d = (int64_t)((in - out) % step);
+    if (d >= span && d + size <= step) return false;
+  }
+  return true;
+}
+
 // The widest chunk that divides the head as the layout needs and whose vectors everything is aligned for.  6000 tokens of 40 x 128 bf16 in
 // chunks of 8, 4, 2, 1 values: 24.7, 21.7, 32.7, 43.8 us; normed on the way into their pages (16 K tokens) 8 beats 4, 95 against 106 us.
 static bool fits(int vec, const synera_rope* rope, const synera_heads* s, int in_bytes, int out_bytes, bool out) {
@@ -225,6 +236,9 @@ static int32_t turn_tensors(const synera_rope* rope, int32_t dtype, int64_t n, c
   if (k && turn_overlap(q->d_out, q->out_token, q->out_head, q->n_heads, bytes, k->d_out, k->out_token, k->out_head, k->n_heads, bytes, n, hd))
     return SYNERA_EINVAL;
   if (n * ((int64_t)q->n_heads + (k ? k->n_heads : 0)) >= (int64_t)1 << 31) return SYNERA_EUNSUP;
+  for (const synera_heads* o : both)
+    for (const synera_heads* i : both)
+      if (o && i && (turn_on_output(*o, n, hd, bytes, d_pos, 4 * n) || turn_on_output(*o, n, hd, bytes, i->d_gain, 2 * hd))) return SYNERA_EINVAL;
   if (!rope_device_ok(rope->device)) return SYNERA_EINVAL;
   TurnArgs a = {};
   const int vec = turn_setup(a, rope, n, q, k, bytes, bytes, false, eps);

@@ -418,6 +418,10 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
     if (!i) continue;
     const Range in = heads_range(i->d_in, i->in_token, i->in_head, i->n_heads, n1, hd, bytes);
     if (meet(in, pools[0]) || meet(in, pools[1])) return SYNERA_EINVAL;
+    if (i->d_gain) {
+      const Range gain = heads_range(i->d_gain, 0, 0, 1, 1, hd, 2);
+      if (meet(gain, pools[0]) || meet(gain, pools[1]) || (q && turn_on_output(*q, n1, hd, 2, i->d_gain, 2 * hd))) return SYNERA_EINVAL;
+    }
     if (!q) continue;
     if (i == q && dtype == 1 && q->d_in == q->d_out && (n1 == 1 || q->in_token == q->out_token) && (q->n_heads == 1 || q->in_head == q->out_head)) continue;
     if (turn_overlap(q->d_out, q->out_token, q->out_head, q->n_heads, 2, i->d_in, i->in_token, i->in_head, i->n_heads, bytes, n1, hd))

@@ -251,3 +251,25 @@ def test_norms_do_not_depend_on_other_tokens(hd, rot, layout):
     for t in range(0, T, 1600):
         part, _ = rope.norm_apply(pos[t: t + 1600], x[t: t + 1600], None, gain, None, 1e-5)
         assert torch.equal(whole[t: t + 1600], part), t
+
+
+def test_outputs_on_positions_or_gains_are_refused():
+    """Positions and gains are read while outputs are written: an output on them is refused as on any other input."""
+    s = synera()
+    rope, T = s.Rope(64), 6
+    flat = torch.zeros(T * 4 * 64, dtype=torch.bfloat16, device=DEV)
+    on = flat.view(T, 4, 64)
+    q, k, gain, pos = draw((T, 4, 64), torch.bfloat16, 1), draw((T, 4, 64), torch.bfloat16, 2), torch.ones(64, dtype=torch.bfloat16, device=DEV), positions(T, 1)
+    on_pos, on_gain = flat[-2 * T:].view(torch.int32), flat[640: 704]
+    for call in (lambda: rope.apply(on_pos, q, out_q=on), lambda: rope.apply(on_pos, q, k, out_k=on), lambda: rope.norm_apply(pos, q, None, on_gain, None, 0.1, out_q=on),
+                 lambda: rope.norm_apply(pos, q, k, gain, on_gain, 0.1, out_q=on), lambda: rope.norm_apply(pos, q, k, on_gain, gain, 0.1, out_k=on)):
+        with pytest.raises(s.SyneraError) as e:
+            call()
+        assert e.value.status == s.EINVAL
+    beside = flat[: 4 * 64 * 2].view(2, 4, 64)
+    rope.apply(on_pos[:2], q[:2], out_q=beside)                                      # beside the output they are fine
+    wide = torch.zeros((T, 5, 64), dtype=torch.bfloat16, device=DEV)                 # and in its gaps, too
+    gap = wide[3, 4]
+    gap.fill_(1.0)
+    got, _ = rope.norm_apply(pos, q, None, gap, None, 0.1, out_q=wide[:, :4])
+    assert torch.equal(got, rope.norm_apply(pos, q, None, gain, None, 0.1)[0])

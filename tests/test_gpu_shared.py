@@ -658,3 +658,18 @@ def test_attention_refuses_outputs_on_the_values():
         with pytest.raises(s.SyneraError) as e:
             call()
         assert e.value.status == s.EINVAL
+
+
+def test_appends_refuse_outputs_on_gains():
+    """Gains are read while queries and pages are written."""
+    s, hq, hkv, hd = synera(), 4, 2, 64
+    b, rope = s.SharedBatch(hq, hkv, hd, 1, 2, 1), s.Rope(hd)
+    b.plan([4], [2], [[0]], 2)
+    kp, vp, q, k = draw((2, hkv, P, hd), 1), draw((2, hkv, hd, P), 2), draw((2, hq, hd), 3), draw((2, hkv, hd), 4)
+    out, gain = torch.zeros_like(q), torch.ones(hd, dtype=torch.bfloat16, device=DEV)
+    for q_gain, k_gain in ((out.view(-1)[64: 128], gain), (gain, out.view(-1)[-64:]), (kp.view(-1)[:64], gain), (gain, vp.view(-1)[-64:]), (None, kp.view(-1)[64: 128])):
+        with pytest.raises(s.SyneraError) as e:
+            b.append_rope(rope, q, k, k, kp, vp, q_gain=q_gain, k_gain=k_gain, out_q=out)
+        assert e.value.status == s.EINVAL
+    b.append_rope(rope, q, k, k, kp, vp, q_gain=gain, k_gain=gain, out_q=out)
+    torch.cuda.synchronize()
