@@ -606,7 +606,7 @@ def _heads(x, out, gain, dtype, n, n_heads, hd, index, name, out_dtype=None, exa
         if gain.dtype != torch.bfloat16 or gain.shape != shape[2:] or not gain.is_contiguous() or gain.get_device() != index:
             raise ValueError(f"{name}: gains are bf16 [{hd}] on cuda:{index}")
         at_gain = gain.data_ptr()
-    rows = 0 if exact else min(shape[0], 0x7FFFFFFF)
+    rows = 0 if exact else shape[0] if shape[0] < 0x80000000 else 0x7FFFFFFF
     if out is False:
         return _pack_heads_rows(x.data_ptr(), 0, at_gain, shape[1], rows, strides[0], strides[1], 0, 0), None
     if out is None:
