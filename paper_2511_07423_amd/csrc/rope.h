@@ -35,8 +35,8 @@ __host__ __device__ inline TurnCols turn_cols(int32_t groups, int32_t n_tokens) 
 // Inputs are read for the last time: a producer, 8192 tokens of 40 x 128 bf16 turned, a reader of the queries 81 -> 74 us; below, where
 // the producer left them in the caches, 2000 tokens alone 10.4 -> 12.1.  Outputs come next, so they are marked only where they are gone by
 // then: 12 000 tokens and their reader 94 -> 84 us, but 8192 and theirs 55 -> 63; appends, whose keys the attention reads with all
-// else: 31 585 tokens 169 -> 139 us (with their attention 656 -> 656), 11 400 with theirs 206 -> 215.  (Chunks of one or two values are bound by their
-// instructions: 2.5 TB/s.)  moved: MB in and out.
+// else: 31 585 tokens 169 -> 139 us (with their attention 656 -> 656), 11 400 with theirs 206 -> 215.  (Chunks of one or two values, which
+// have too few bytes on their way for more than 2.5 TB/s, are not marked.)  moved: MB in and out.
 __host__ __device__ inline int32_t turn_once(int vec, int64_t moved, bool paged) {
   return vec < 4 || moved < 128 ? TURN_KEPT : moved < (paged ? 512 : 224) ? TURN_ONCE_IN : TURN_ONCE_BOTH;
 }
@@ -149,8 +149,9 @@ __device__ __forceinline__ void turn_angle(double pos, double rev, float magnitu
 template <typename TI, typename TO, int VEC, bool PAGED, int ONCE>
 __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols, const uint32_t item) {
   constexpr int NU = VEC == 1 ? 2 : 1;                      // single values: up to 128 units on 64 lanes
-  // Heads of a lane whose loads are on their way together: 64 bytes in all.  (128: fewer wavefronts fit; 6000 tokens of 40 x 128 f32 normed
-  // 54.7 -> 46.8 us, 31585 tokens appended 173 -> 169.)
+  // Heads of a lane whose loads are on their way together: 64 bytes in all for chunks of 8 values, 32 for 4 in 16 bits.  (Twice that: fewer wavefronts
+  // fit; 6000 tokens of 40 x 128 f32 normed 54.7 -> 46.8 us, 31585 tokens appended 173 -> 169.)  Chunks of 2 and 1 are on their way for one head at a time: the
+  // generated code widens each masked chunk in its own branch and waits for it there.
   constexpr int IT = NU == 1 && VEC * (int)sizeof(TI) <= 16 ? 2 : 1;
   const int lane = threadIdx.x & 63;
   const uint32_t t = item / (uint32_t)cols.n;

@@ -169,8 +169,10 @@ int turn_setup(TurnArgs& a, const synera_rope* rope, int64_t n_tokens, const syn
   a.rest_half = ((hd - rot) / widest + 1) / 2 * widest;
   a.token_bytes = (int64_t)(a.q.n_heads + a.k.n_heads) * hd * (in_bytes + out_bytes);
   const int64_t moved = (n_tokens * a.token_bytes) >> 20;        // MB
-  // (f32: a chunk of 8 is two vectors, each of which fills half a line.  Where the lines do not wait in a cache for their other halves, 4: 6000 tokens
-  // of 40 x 128 normed 59 -> 51 us, 9000 82 -> 80; but 4000 tokens 36 -> 38, 4096 appended 37 -> 41.)
+  // (f32: a chunk of 8 is two vectors, each of which fills half a line.  Where the lines do not wait in a cache for their other halves, 4.  Chunks of 8
+  // and 4, us, on new inputs each time: 40 x 128 normed, interleaved: 96 MB in and out 22.7, 25.0; 160 37.5, 39.0; 180 44.2, 41.7; 200 44.8, 44.7; 224 56.0, 47.8;
+  // 256 61.4, 57.1; 288 68.6, 71.3; 352 82.3, 79.8; 640 141, 132.  40 x 128, half of each turned: 224 53.8, 44.1; 640 141, 125.  40 x 96: 224 67.9, 63.0; 640 176,
+  // 148.  20 x 64, 10 x 256: 8 to 19 % less from 224 on, and 4 to 17 % less from 128 on.  4096 tokens of 40 x 128 appended: 37, 41.)
   int vec = in_bytes == 4 && !paged && moved >= 224 ? 4 : 8;
   while (vec > 1 && !(fits(vec, rope, q, in_bytes, out_bytes, true) && fits(vec, rope, k, in_bytes, out_bytes, !paged))) vec /= 2;
   const int units = rot / (2 * vec) + a.rest_half / vec;

@@ -487,8 +487,9 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
 //     wavefronts that share keys; a slot holds a page for each wavefront of the group.  80 KB in all: two blocks a compute
 //     unit, whose matrix and softmax work overlap.  K chunks are swizzled by slot, V halves by dim on the way in, for
 //     LDS reads without bank conflicts.
-//   * The probabilities are rounded to bf16 (to nearest): 2^-8 of each at most, which a sum over keys averages out to less than the
-//     rounding of the bf16 output; where one key has all the weight both are alike.  The sum l takes them as they were.
+//   * The probabilities are rounded to bf16 (to nearest), the sum l takes them as they were: 2^-8 of each at most, so the output is off by at most
+//     2^-8 of the values' mean magnitude, as much as by its own rounding.  Measured against 64 bits, in root mean square: 0.0018 to 0.0023 of the output,
+//     0.0016 to 0.0017 with 32-bit probabilities.  Kept in two terms they would take half as many matrix products again.
 // Few rows: bound by HBM.  256 requests of one token behind 8192 shared ones and 64 .. 1024 of their own (405 MB): 83 us, 4.9 TB/s.
 // Many rows: by the matrix cores and the softmax's vector instructions, which take turns on a SIMD (97 % of its cycles in all, 53 % the
 // matrix cores), at the clock that the power limit leaves: 1620 tokens of 64 heads against 16384 keys 870 us, 1.0 PFLOP/s.

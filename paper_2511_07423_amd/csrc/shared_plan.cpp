@@ -100,7 +100,8 @@ struct Node {                       // pages [first, last) of the rows of `who`
 };
 
 // What a key costs `rows` query rows of one KV head, in keys fetched: fetching bounds up to two tiles of rows, the matrix
-// cores more (0.45 of a fetch for each tile).
+// cores more.  0.45 of a fetch for each tile is fitted, not derived: launches of nothing but full tiles reach 1.03 PFLOP/s, where it would be 0.62
+// (65536 operations against 512 bytes at 4.99 TB/s); what a tile costs beside fetches has not been measured by itself.
 double key_cost(int64_t rows) {
   const int64_t tiles = (rows + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
   return std::max(1.0, 0.45 * (double)tiles);
