@@ -8,7 +8,8 @@
  * Arithmetic is 32-bit throughout, angles are 64-bit; each output is rounded once, to nearest even.
  * The handles belong to the HIP device that was current when they were made: a call with another device current is
  * refused (EINVAL).  They must outlive the graphs that captured calls with them.  Nothing here waits for the GPU except
- * the creates and destroys, and synera_batch_plan if it runs more than four plans ahead of its uploads.
+ * the creates and destroys, and synera_batch_plan if it runs more than four plans ahead of its uploads.  Destroys leave a capture of
+ * any stream alone; creates, like other allocations, end one that is under way.
  */
 #ifndef SYNERA_SHARED_H
 #define SYNERA_SHARED_H

@@ -334,14 +334,14 @@ extern "C" int32_t synera_create(synera_ctx** out, const synera_model_desc* desc
 
 extern "C" int32_t synera_destroy(synera_ctx* c) {
   if (!c) return SYNERA_OK;
-  (void)hipDeviceSynchronize();
+  const BesideCaptures beside;
+  if (c->arena) (void)hipFree(c->arena);               // waits for the device: nothing reads the rest from here on
   for (int s = 0; s < N_STAGE; ++s) {
     if (c->done[s]) (void)hipEventDestroy(c->done[s]);
     if (c->h_meta[s]) (void)hipHostFree(c->h_meta[s]);
     if (c->d_meta[s]) (void)hipFree(c->d_meta[s]);
   }
   for (hipEvent_t e : c->prof_events) (void)hipEventDestroy(e);
-  if (c->arena) (void)hipFree(c->arena);
   delete c;
   return SYNERA_OK;
 }

@@ -14,6 +14,21 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 #define SY_PAGE 16
 
+// While it lives, frees of this thread leave captures of any stream alone, which they would end in the usual mode.  For destroys: a collector may
+// end a handle's life at any time.  Frees wait for the device that the memory lies on, so device memory goes first; hipDeviceSynchronize ends captures
+// in this mode, too.
+struct BesideCaptures {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  BesideCaptures() {
+    if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) (void)hipGetLastError();
+  }
+  ~BesideCaptures() {
+    if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) (void)hipGetLastError();
+  }
+  BesideCaptures(const BesideCaptures&) = delete;
+  BesideCaptures& operator=(const BesideCaptures&) = delete;
+};
+
 // fp32 -> bf16, round-to-nearest-even, two at a time with gfx950's v_cvt_pk_bf16_f32.
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;

@@ -73,7 +73,7 @@ extern "C" int32_t synera_rope_create(synera_rope** out, const synera_rope_desc*
 
 extern "C" int32_t synera_rope_destroy(synera_rope* r) {
   if (!r) return SYNERA_OK;
-  (void)hipDeviceSynchronize();
+  const BesideCaptures beside;                       // (the free waits for the device)
   (void)hipFree(r->rev);
   delete r;
   return SYNERA_OK;

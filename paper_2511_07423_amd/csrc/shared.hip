@@ -45,12 +45,12 @@ static size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
 extern "C" int32_t synera_batch_destroy(synera_batch* b) {
   if (!b) return SYNERA_OK;
-  (void)hipDeviceSynchronize();
+  const BesideCaptures beside;
+  if (b->dev) (void)hipFree(b->dev);                 // waits for the device: nothing reads the pinned memory from here on
   for (int s = 0; s < SH_STAGES; ++s) {
     if (b->done[s]) (void)hipEventDestroy(b->done[s]);
     if (b->host[s]) (void)hipHostFree(b->host[s]);
   }
-  if (b->dev) (void)hipFree(b->dev);
   delete b;
   return SYNERA_OK;
 }

@@ -673,3 +673,51 @@ def test_appends_refuse_outputs_on_gains():
         assert e.value.status == s.EINVAL
     b.append_rope(rope, q, k, k, kp, vp, q_gain=gain, k_gain=gain, out_q=out)
     torch.cuda.synchronize()
+
+
+def small_verifier():
+    from helpers import drawn_model, small_shape
+    shape = small_shape(d_model=256, n_q_heads=4, n_kv_heads=4, head_dim=64, d_ffn=128, vocab=128, n_layers=1)
+    head, layers = drawn_model(shape, 1, DEV)
+    return synera().Verifier(shape, head, layers, 4, 200, 8)
+
+
+def test_handles_that_go_while_a_graph_is_captured():
+    """A collector may end the life of handles at any time, also while some stream is captured: the capture stands, and what was captured runs."""
+    s, hq, hkv, hd = synera(), 4, 2, 64
+    b, rope = s.SharedBatch(hq, hkv, hd, 1, 2, 1), s.Rope(hd)
+    b.plan([4], [2], [[0]], 1)
+    kp, vp, x = draw((1, hkv, P, hd), 1), draw((1, hkv, hd, P), 2), draw((2, hq + 2 * hkv, hd), 3)
+    q, k, v = x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:]
+    others = [s.Rope(hd), s.SharedBatch(hq, hkv, hd, 1, 2, 1), s.SharedBatch(hq, hkv, hd, 1, 2, 1), small_verifier()]
+    others[2].plan([4], [2], [[0]], 1)
+    out_q, out = torch.zeros((2, hq, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((2, hq, hd), dtype=torch.bfloat16, device=DEV)
+    pools = kp.clone(), vp.clone()
+    want_q = b.append_rope(rope, q, k, v, *pools)
+    want = b.attention(want_q, *pools)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.append_rope(rope, q, k, v, kp, vp, out_q=out_q)
+        for h in others:
+            h.close()
+        b.attention(out_q, kp, vp, out=out)
+    for _ in range(3):
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out_q, want_q) and torch.equal(out, want)
+
+
+def test_destroys_wait_for_the_device():
+    """Handles go behind the work that may still read them, on whatever stream it runs."""
+    s = synera()
+    for handle in (s.Rope(64), s.SharedBatch(4, 2, 64, 1, 2, 1), small_verifier()):
+        torch.cuda.synchronize()
+        side, done = torch.cuda.Stream(), torch.cuda.Event()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                      # some milliseconds
+            done.record()
+        assert not done.query()
+        handle.close()
+        assert done.query()
