@@ -1,6 +1,7 @@
 """GPU parity of appends with the rotation and of attention over shared prefixes with float64: element by element, over random trees of
 shared pages whose unwritten slots hold NaN."""
 import ctypes as C
+import gc
 import random
 
 import numpy as np
@@ -458,8 +459,13 @@ def captured(call):
     """A graph of the call, captured on a stream of its own; it never runs."""
     graph, side = torch.cuda.CUDAGraph(keep_graph=True), torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.graph(graph, stream=side):
-        call()
+    gc.collect()                                               # graphs that other tests left behind wait for the device when they go,
+    gc.disable()                                               # which ends a capture
+    try:
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    finally:
+        gc.enable()
     return graph
 
 
