@@ -16,6 +16,13 @@ DEV, P = "cuda:0", 16
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
 
+@pytest.fixture(autouse=True)
+def nothing_left_behind():
+    """What a test's refusals leave in cycles (graphs among it) goes with the test, not inside a later test's capture."""
+    yield
+    gc.collect()
+
+
 def synera():
     import paper_2511_07423_amd as s
     return s
