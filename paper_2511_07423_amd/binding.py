@@ -155,6 +155,35 @@ _lib.synera_debug_shared_plan.restype = C.c_int32
 _lib.synera_debug_shared_plan.argtypes = [C.c_int32] * 5 + [_i32p] * 3 + [C.c_int32] * 2 + [_i32p, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
 
 
+class _LogitsDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64), ("in_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("d_cu", _vp), ("d_history", _vp), ("d_history_len", _vp), ("d_n_prompt", _vp), ("history_columns", C.c_int32),
+                ("bias_columns", C.c_int32), ("d_repetition", _vp), ("d_presence", _vp), ("d_frequency", _vp), ("d_bias_id", _vp),
+                ("d_bias", _vp), ("d_mask", _vp), ("d_tokens", _vp), ("d_parent", _vp)]
+
+
+# synera_logits_desc as bytes, in that order
+_pack_logits = struct.Struct("@iiqqqqPPPPiiPPPPPPPP").pack
+_lib.synera_pages_update.restype = C.c_int32
+_lib.synera_pages_update.argtypes = [C.c_int32, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, C.c_int32, C.c_int64, _vp, _vp, _vp, _vp, _vp]
+_lib.synera_tree_create.restype = C.c_int32
+_lib.synera_tree_create.argtypes = [C.POINTER(_vp)] + [C.c_int32] * 6
+_lib.synera_tree_destroy.restype = C.c_int32
+_lib.synera_tree_destroy.argtypes = [_vp]
+_lib.synera_tree_plan.restype = C.c_int32
+_lib.synera_tree_plan.argtypes = [_vp, C.c_int32, _vp, _vp, _vp, C.c_int64, _vp, C.c_int32, C.c_int32, _vp, _vp]
+_lib.synera_tree_append_rope.restype = C.c_int32
+_lib.synera_tree_append_rope.argtypes = [_vp, _vp, C.c_int32, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
+_lib.synera_tree_attention.restype = C.c_int32
+_lib.synera_tree_attention.argtypes = [_vp, _vp, _vp, _vp, C.c_float, _vp, _vp]
+_lib.synera_tree_accept.restype = C.c_int32
+_lib.synera_tree_accept.argtypes = [_vp, C.c_int64] + [_vp] * 9
+_lib.synera_tree_commit.restype = C.c_int32
+_lib.synera_tree_commit.argtypes = [_vp, C.c_int64, _vp, _vp, C.c_int32, C.c_int64, _vp, _vp, _vp]
+_lib.synera_logits_adjust.restype = C.c_int32
+_lib.synera_logits_adjust.argtypes = [C.c_char_p, _vp, _vp, _vp]
+
+
 class SyneraError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -693,16 +722,15 @@ def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max
     return _lib.synera_validate_shared(len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool, max_batch, max_tokens)
 
 
-class SharedBatch:
-    """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
-    attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too; their tensors
-    and pools need room for the tokens and pages of those plans, and all rows of their outputs lie apart from each other and from inputs.
-    Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
+class _PagedBatch:
+    """What batches over a paged cache have in common: a handle whose plan says where each token goes and what it sees."""
+    _names = ()                                           # of the C functions: create, destroy, append, attention
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):
         self._h = _vp()
-        _check(_lib.synera_batch_create(C.byref(self._h), n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages),
-               "synera_batch_create")
+        create, _, append, attend = self._names
+        self._append, self._attend = getattr(_lib, append), getattr(_lib, attend)
+        _check(getattr(_lib, create)(C.byref(self._h), n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages), create)
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
@@ -711,7 +739,7 @@ class SharedBatch:
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
-            _lib.synera_batch_destroy(self._h)
+            getattr(_lib, self._names[1])(self._h)
             self._h = None
 
     def __del__(self):
@@ -719,16 +747,6 @@ class SharedBatch:
             self.close()
         except Exception:
             pass
-
-    def plan(self, ctx_len, n_new, block_table, n_pages_in_pool):
-        """Host: cached and new tokens of each request, block_table [B, columns]; shared pages first in their rows."""
-        bt = np.ascontiguousarray(block_table, dtype=np.int32)
-        (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
-        if bt.ndim != 2 or len(ctx) != len(new) or len(bt) != len(ctx):
-            raise ValueError("ctx_len, n_new and the rows of block_table belong together")
-        _check(_lib.synera_batch_plan(self._h, len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool,
-                                      _raw_stream(self._index)), "synera_batch_plan")
-        self.n_tokens, self.n_pages = int(new.sum()), n_pages_in_pool
 
     def _pool(self, pool, tile):
         shape = pool.shape
@@ -746,10 +764,10 @@ class SharedBatch:
         hq = None
         if q is not None:
             hq, out_q = _heads(q, out_q, q_gain, dtype, n, self.n_q_heads, hd, index, "q", torch.bfloat16, False)
-        st = _lib.synera_append_rope(self._h, rope._h, _head_type(dtype), hq, hk, hv, eps, self._pool(k_pool, self._tiles[0]),
-                                     self._pool(v_pool, self._tiles[1]), _raw_stream(index))
+        st = self._append(self._h, rope._h, _head_type(dtype), hq, hk, hv, eps, self._pool(k_pool, self._tiles[0]),
+                          self._pool(v_pool, self._tiles[1]), _raw_stream(index))
         if st:
-            raise SyneraError(st, "synera_append_rope")
+            raise SyneraError(st, self._names[2])
         return out_q
 
     def attention(self, q, k_pool, v_pool, scale=None, out=None, want_lse=False):
@@ -762,11 +780,30 @@ class SharedBatch:
         index = self._index
         h, out = _heads(q, out, None, torch.bfloat16, self.n_tokens, self.n_q_heads, self.head_dim, index, "q", None, False)
         lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
-        st = _lib.synera_shared_attention(self._h, h, self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1]), scale,
-                                          lse.data_ptr() if want_lse else None, _raw_stream(index))
+        st = self._attend(self._h, h, self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1]), scale,
+                          lse.data_ptr() if want_lse else None, _raw_stream(index))
         if st:
-            raise SyneraError(st, "synera_shared_attention")
+            raise SyneraError(st, self._names[3])
         return (out, lse) if want_lse else out
+
+
+class SharedBatch(_PagedBatch):
+    """A ragged batch over a paged bf16 cache whose requests may share pages: plan() once a step, then append_rope() and
+    attention() for each layer, all on one stream.  Calls captured into a graph serve later plans of this batch too; their tensors
+    and pools need room for the tokens and pages of those plans, and all rows of their outputs lie apart from each other and from inputs.
+    Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
+
+    _names = "synera_batch_create", "synera_batch_destroy", "synera_append_rope", "synera_shared_attention"
+
+    def plan(self, ctx_len, n_new, block_table, n_pages_in_pool):
+        """Host: cached and new tokens of each request, block_table [B, columns]; shared pages first in their rows."""
+        bt = np.ascontiguousarray(block_table, dtype=np.int32)
+        (ctx, p_ctx), (new, p_new) = _host_i32(ctx_len), _host_i32(n_new)
+        if bt.ndim != 2 or len(ctx) != len(new) or len(bt) != len(ctx):
+            raise ValueError("ctx_len, n_new and the rows of block_table belong together")
+        _check(_lib.synera_batch_plan(self._h, len(ctx), p_ctx, p_new, bt.ctypes.data_as(_i32p), bt.shape[1], n_pages_in_pool,
+                                      _raw_stream(self._index)), "synera_batch_plan")
+        self.n_tokens, self.n_pages = int(new.sum()), n_pages_in_pool
 
 
 _SHARED_REGIONS = {"head": (0, 16), "pos": (1, 1), "slot": (2, 1), "windows": (3, 4), "items": (4, 32), "list": (5, 1), "pages": (6, 1),
@@ -799,6 +836,141 @@ def debug_shared_block(block_groups, wave_groups, run, block):
     at = C.c_int32(0)
     _check(_lib.synera_debug_shared_block(block_groups, wave_groups, run, block, C.byref(at)), "synera_debug_shared_block")
     return at.value, at.value < 8 * block_groups
+
+
+# ---------------------------------------------------------------------------------- trees of drafted tokens, lengths on the GPU
+TREE_NODES = 256
+
+
+def _ints(t, shape, index, name, dtype=torch.int32):
+    """The address of a contiguous int32 tensor of this shape (None: none); -1 in the shape stands for any size."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != index or not t.is_contiguous() or t.dim() != len(shape) or \
+            any(a != b and b >= 0 for a, b in zip(t.shape, shape)):
+        raise ValueError(f"{name}: expected {dtype} {list(shape)} on cuda:{index}, contiguous; got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _current(t, name):
+    """The index of the current device, which t has to be on."""
+    index = torch._C._cuda_getDevice() if t.is_cuda else -1
+    if index < 0 or t.get_device() != index:
+        raise ValueError(f"{name}: expected a tensor on the current GPU, got one on {t.device}")
+    return index
+
+
+def update_pages(table, held, free, n_free, ctx_len, n_new, n_rows, shared=None):
+    """Pages for each request's ctx_len + n_new tokens, in place: rows of `table` [B, columns], of whose pages request i holds its first
+    held[i], take what they lack from the stack `free` [n_pages] of n_free [1] pages and give back what they have too much, but for their first
+    shared[i] columns.  -> (cu [B + 1], pos [n_rows], slot [n_rows], status [B]): where each request's tokens begin in the flattened rows, each
+    token's position and its place page * 16 + slot, and what refused a request (0: nothing).  All int32 on the GPU."""
+    index = _current(table, "table")
+    B, columns = table.shape
+    pages = _ints(free, (-1,), index, "free")
+    args = (_ints(ctx_len, (B,), index, "ctx_len"), _ints(n_new, (B,), index, "n_new"), _ints(shared, (B,), index, "shared"),
+            _ints(table, (B, columns), index, "table"), columns, _ints(held, (B,), index, "held"), pages, _ints(n_free, (1,), index, "n_free"))
+    # one tensor for all outputs: cu, status, pos, slot
+    out = torch.empty(2 * B + 1 + 2 * n_rows, dtype=torch.int32, device=table.device)
+    at = out.data_ptr()
+    st = _lib.synera_pages_update(B, *args, free.numel(), n_rows, at, at + 4 * (2 * B + 1), at + 4 * (2 * B + 1 + n_rows), at + 4 * (B + 1),
+                                  _raw_stream(index))
+    if st:
+        raise SyneraError(st, "synera_pages_update")
+    cu, status, pos, slot = out.split((B + 1, B, n_rows, n_rows))
+    return cu, pos, slot, status
+
+
+class TreeBatch(_PagedBatch):
+    """Trees of drafted tokens over a paged bf16 cache, their lengths on the GPU: plan() once a step, append_rope() and attention() for each
+    layer (as SharedBatch's), accept() and commit() behind the last, all on one stream.  All but the making of the handle can be captured into a
+    graph; captured calls serve later plans too, for which their tensors and pools need room.  Rows of a tree: node j of request i is row
+    cu[i] + j, cu the prefix sums of n_nodes.  Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
+    _names = "synera_tree_create", "synera_tree_destroy", "synera_tree_append_rope", "synera_tree_attention"
+
+    def plan(self, ctx_len, n_nodes, parent, block_table, n_pages_in_pool):
+        """int32 on the GPU: cached tokens and nodes (at most TREE_NODES) of each request, each node's parent among the nodes before it
+        in its request (-1: a child of the context) [rows], block_table [B, columns] -> status [B], 0 for requests that are not refused."""
+        index = self._index
+        B, n = ctx_len.numel(), parent.numel()
+        table = _ints(block_table, (B, -1), index, "block_table")
+        status = torch.empty(B, dtype=torch.int32, device=self.device)
+        st = _lib.synera_tree_plan(self._h, B, _ints(ctx_len, (B,), index, "ctx_len"), _ints(n_nodes, (B,), index, "n_nodes"),
+                                   _ints(parent, (n,), index, "parent"), n, table, block_table.shape[1], n_pages_in_pool, status.data_ptr(),
+                                   _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_tree_plan")
+        self.n_requests, self.n_tokens, self.n_pages = B, n, n_pages_in_pool
+        return status
+
+    n_requests = 0
+
+    def accept(self, tokens, target, anchor=None, n_given=None):
+        """The path of each tree that the targets (int32 [rows]: the token after each node) follow.  Its first n_given[i] nodes are
+        accepted as they are; anchor[i] is the token after the context of requests without such nodes.  -> dict of int32 tensors: accept_len [B]
+        (nodes behind the given ones), token [B] (the target at the path's end), path [rows] (node indices, then -1), n_path [B]."""
+        index, B, n = self._index, self.n_requests, tokens.numel()
+        out = torch.empty(3 * B + n, dtype=torch.int32, device=self.device)
+        at = out.data_ptr()
+        st = _lib.synera_tree_accept(self._h, n, _ints(tokens, (n,), index, "tokens"), _ints(target, (n,), index, "target"),
+                                     _ints(anchor, (B,), index, "anchor"), _ints(n_given, (B,), index, "n_given"), at, at + 4 * B, at + 12 * B,
+                                     at + 8 * B, _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_tree_accept")
+        accept_len, token, n_path, path = out.split((B, B, B, n))
+        return {"accept_len": accept_len, "token": token, "path": path, "n_path": n_path}
+
+    def commit(self, path, n_path, k_pool, v_pool):
+        """Moves the keys and values of each path to the positions behind its context, in one layer's pools or in all layers'
+        [n_layers, pages, ...]; n_path is then to be added to the cached lengths."""
+        index, k_tile, v_tile = self._index, self._tiles[0], self._tiles[1]
+        for pool, tile in ((k_pool, k_tile), (v_pool, v_tile)):
+            shape = pool.shape
+            if pool.dtype != torch.bfloat16 or len(shape) not in (4, 5) or shape[-3:] != tile or shape[-4] < self.n_pages or \
+                    shape[:-3] != k_pool.shape[:-3] or pool.stride(0) != k_pool.stride(0) or pool.get_device() != index or \
+                    not (pool[0] if len(shape) == 5 and shape[0] > 0 else pool).is_contiguous():
+                raise ValueError(f"expected pools bf16 [(layers,) >= {self.n_pages}, ...] on {self.device}, each layer contiguous, alike for keys and values")
+        layers, stride = (k_pool.shape[0], k_pool.stride(0)) if k_pool.dim() == 5 else (1, 0)
+        n = path.numel()
+        st = _lib.synera_tree_commit(self._h, n, _ints(path, (n,), index, "path"), _ints(n_path, (self.n_requests,), index, "n_path"), layers, stride,
+                                     k_pool.data_ptr(), v_pool.data_ptr(), _raw_stream(index))
+        if st:
+            raise SyneraError(st, "synera_tree_commit")
+
+
+def adjust_logits(logits, cu=None, history=None, history_len=None, n_prompt=None, repetition=None, presence=None, frequency=None,
+                  bias_id=None, bias=None, mask=None, tokens=None, parent=None, out=None):
+    """Logits [rows, vocab] (f32, bf16 or f16) with penalties, biases and masks, as a new tensor or in `out` (logits itself for in place).
+    Row r belongs to request r or, with cu [B + 1], to the request whose rows cu[i] .. cu[i + 1] - 1 it is among.  Of request i: history [B, columns],
+    of which the first history_len[i] tokens were seen, those from n_prompt[i] on generated; repetition, presence, frequency f32 [B]; bias
+    f32 [B, n] for the tokens bias_id [B, n] (of entries that name a token twice the last).  mask: bits [rows, ceil(vocab / 32)] of
+    tokens that are allowed; all others become -inf.  tokens and parent [rows]: a row is a node of its request's tree, whose path
+    from the root, itself included, was generated too.  Integers are int32.  No gradients."""
+    index = _current(logits, "logits")
+    rows, vocab = logits.shape
+    dtype = _head_type(logits.dtype)
+    if logits.stride(1) != 1 and vocab > 1:
+        raise ValueError("logits: values of a row lie side by side")
+    B = rows if cu is None else cu.numel() - 1
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or (out.stride(1) != 1 and vocab > 1) or out.get_device() != index:
+        raise ValueError(f"out: expected {logits.dtype} {list(logits.shape)} on cuda:{index}, values of a row side by side")
+    columns = 0 if history is None else history.shape[1]
+    biases = 0 if bias_id is None else bias_id.shape[1]
+    f32 = torch.float32
+    desc = _pack_logits(
+        B, dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, out.stride(0) if rows > 1 else vocab,
+        _ints(cu, (B + 1,), index, "cu") or 0, _ints(history, (B, columns), index, "history") or 0,
+        _ints(history_len, (B,), index, "history_len") or 0, _ints(n_prompt, (B,), index, "n_prompt") or 0, columns, biases,
+        _ints(repetition, (B,), index, "repetition", f32) or 0, _ints(presence, (B,), index, "presence", f32) or 0,
+        _ints(frequency, (B,), index, "frequency", f32) or 0, _ints(bias_id, (B, biases), index, "bias_id") or 0,
+        _ints(bias, (B, biases), index, "bias", f32) or 0, _ints(mask, (rows, (vocab + 31) // 32), index, "mask") or 0,
+        _ints(tokens, (rows,), index, "tokens") or 0, _ints(parent, (rows,), index, "parent") or 0)
+    st = _lib.synera_logits_adjust(desc, logits.data_ptr(), out.data_ptr(), _raw_stream(index))
+    if st:
+        raise SyneraError(st, "synera_logits_adjust")
+    return out
 
 
 # ---------------------------------------------------------------------------------- scheduler (host only)

@@ -167,6 +167,7 @@ __device__ __forceinline__ void turn_item(const TurnArgs& a, const TurnCols cols
   size_t page_at = 0;
   if (PAGED) {
     const int32_t at = a.slot[t];
+    if (at < 0) return;                                     // (uniform) a token that goes nowhere
     page_at = ((size_t)(at / SY_PAGE) * a.k.n_heads * SY_PAGE + at % SY_PAGE) * a.hd;   // of head 0; heads lie SY_PAGE x hd apart
   }
 #pragma unroll

@@ -95,3 +95,19 @@ struct ShPlan {
 // The batch has been validated.  Throws std::bad_alloc.
 void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx_len, const int32_t* n_new, const int32_t* table, int32_t max_pages,
              ShPlan& p);
+
+// ---------------------------------------------------------------- shared.hip
+// Where the new tokens of a batch go: of a planned synera_batch, or of a tree's plan, whose sizes only the device knows.
+struct ShTarget {
+  const ShLimits* lim;
+  int device;
+  int32_t n_pages;
+  int64_t n_tokens;            // known: of the plan; else rows that it may fill
+  int32_t n_windows;
+  bool known;
+  const int32_t *pos, *slot;   // device, as ShPlan's; a slot below 0: the token goes nowhere
+  const ShHeader* head;
+  const ShWindow* windows;     // empty ones (s1 <= s0) are passed by
+};
+int32_t sh_append(const ShTarget& target, const synera_rope* rope, int32_t dtype, const synera_heads* q, const synera_heads* k,
+                  const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer, void* stream);
