@@ -1,4 +1,6 @@
 // Block tables and slot maps from request lengths, on the GPU: the pages of each row follow its lengths, from and to a stack of free ones.
+#include <algorithm>
+
 #include "../../include/synera.h"
 #include "../../include/synera_tree.h"
 #include "common.h"
@@ -62,71 +64,105 @@ __device__ __forceinline__ Sum3 scan3(Sum3 v, Sum3* wave_sums, Sum3& total) {
   return Sum3{before.rows + v.rows - in.rows, before.grow + v.grow - in.grow, before.back + v.back - in.back};
 }
 
+// The n entries of a row and of the stack, from x and y on, that a request moves: a few by its own thread, more by its whole wavefront.
+#define PG_FEW 4
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
+}
+template <typename F>
+__device__ __forceinline__ void each_page(int32_t n, int64_t x, int64_t y, F move) {
+  if (n <= PG_FEW)
+    for (int c = 0; c < n; ++c) move(x, y, c);
+  uint64_t many = __builtin_amdgcn_ballot_w64(n > PG_FEW);
+  while (many) {
+    const int owner = __builtin_ctzll(many);
+    many &= many - 1;
+    const int all = __builtin_amdgcn_readlane(n, owner);
+    const int64_t ox = lane_value(x, owner), oy = lane_value(y, owner);
+    for (int c = threadIdx.x & 63; c < all; c += 64) move(ox, oy, c);
+  }
+}
+
 // One block.  First what each row takes (from the stack as it was) and where its tokens begin, then, when all have taken theirs, what
-// rows return, then the tokens' places.
-__global__ __launch_bounds__(1024) void pages_kernel(PagesArgs a) {
-  __shared__ Sum3 wave_sums[16];
+// rows return.  Bound by latency: two loads behind each other, three barriers for the sums, the pages.
+__device__ __forceinline__ void pages_step(const PagesArgs& a, Sum3* wave_sums, int32_t* taken) {
   const int tid = threadIdx.x;
   const int32_t n_free = min(max(a.n_free[0], 0), a.n_pages);
   Sum3 done = {0, 0, 0};
-  __shared__ int32_t taken;
-  if (tid == 0) taken = 0;
+  if (tid == 0) *taken = 0;
   __syncthreads();
-  int64_t all_back = 0;
+  PageStep s;
+  Sum3 at, total;
   for (int i0 = 0; i0 < a.B; i0 += 1024) {
     const int i = i0 + tid;
-    PageStep s = {0, 0, 0, 0, 0, 0, SYNERA_OK};
+    s = PageStep{0, 0, 0, 0, 0, 0, SYNERA_OK};
     if (i < a.B) s = page_step(a, i);
-    Sum3 total;
-    Sum3 at = scan3(Sum3{s.rows, s.grow, s.back}, wave_sums, total);
+    at = scan3(Sum3{s.rows, s.grow, s.back}, wave_sums, total);
     at.rows += done.rows;
     at.grow += done.grow;
+    at.back += done.back;
+    if (s.grow > 0 && at.grow + s.grow > n_free) s.status = SYNERA_ENOSPC;
+    const int32_t takes = s.status == SYNERA_OK ? s.grow : 0;
+    each_page(takes, (int64_t)i * a.columns + s.held, n_free - 1 - at.grow, [&](int64_t to, int64_t top, int c) { a.table[to + c] = a.free_[top - c]; });
+    if (takes > 0) atomicMax(taken, (int32_t)(at.grow + s.grow));
     if (i < a.B) {
-      if (s.grow > 0 && at.grow + s.grow > n_free) s.status = SYNERA_ENOSPC;
-      if (s.status == SYNERA_OK && s.grow > 0) {
-        for (int c = 0; c < s.grow; ++c) a.table[(size_t)i * a.columns + s.held + c] = a.free_[n_free - 1 - (int32_t)(at.grow + c)];
-        atomicMax(&taken, (int32_t)(at.grow + s.grow));
-      }
       a.cu[i] = (int32_t)at.rows;
       a.status[i] = s.status;
       if (i == a.B - 1) a.cu[a.B] = (int32_t)(at.rows + s.rows);
     }
     done.rows += total.rows;
     done.grow += total.grow;
-    all_back += total.back;
+    done.back += total.back;
   }
-  __syncthreads();
-  const int32_t left = n_free - taken;
+  __syncthreads();                                           // all have taken theirs
+  const int64_t left = n_free - *taken;
+  const bool one = a.B <= 1024;                              // what this thread knows of its only request is still there
   int64_t back = 0;
   for (int i0 = 0; i0 < a.B; i0 += 1024) {
     const int i = i0 + tid;
-    PageStep s = {0, 0, 0, 0, 0, 0, SYNERA_OK};
-    if (i < a.B) s = page_step(a, i);
-    Sum3 total;
-    const Sum3 at = scan3(Sum3{0, 0, s.back}, wave_sums, total);
-    if (i < a.B && a.status[i] == SYNERA_OK) {
-      for (int c = 0; c < s.back; ++c) {
-        const int64_t to = left + all_back - 1 - (back + at.back + c);
-        if (to < a.n_pages) a.free_[to] = a.table[(size_t)i * a.columns + s.keep + c];
+    if (!one) {
+      s = PageStep{0, 0, 0, 0, 0, 0, SYNERA_OK};
+      if (i < a.B) {
+        s = page_step(a, i);
+        s.status = a.status[i];
       }
-      a.held[i] = s.keep;
+      at = scan3(Sum3{0, 0, s.back}, wave_sums, total);
+      at.back += back;
+      back += total.back;
     }
-    back += total.back;
+    each_page(s.status == SYNERA_OK ? s.back : 0, (int64_t)i * a.columns + s.keep, left + done.back - 1 - at.back, [&](int64_t from, int64_t top, int c) {
+      if (top - c < a.n_pages) a.free_[top - c] = a.table[from + c];
+    });
+    if (i < a.B && s.status == SYNERA_OK) a.held[i] = s.keep;
   }
-  if (tid == 0) a.n_free[0] = (int32_t)min(left + all_back, (int64_t)a.n_pages);
-  __syncthreads();
-  const int wave = tid >> 6, lane = tid & 63;
-  for (int i = wave; i < a.B; i += 16) {
-    const int32_t first = a.cu[i], rows = a.cu[i + 1] - first, ctx = a.ctx[i];
-    const bool ok = a.status[i] == SYNERA_OK;
-    for (int j = lane; j < rows; j += 64) {
-      if ((int64_t)first + j >= a.n_rows) break;
-      const int32_t p = ctx + j;
-      a.pos[first + j] = ok ? p : -1;
-      a.slot[first + j] = ok ? a.table[(size_t)i * a.columns + p / SY_PAGE] * SY_PAGE + p % SY_PAGE : -1;
-    }
+  if (tid == 0) a.n_free[0] = (int32_t)min(left + done.back, (int64_t)a.n_pages);
+}
+
+// The places of a request's tokens, by `lanes` threads of which this is number `lane`.
+__device__ __forceinline__ void pages_places(const PagesArgs& a, int i, int lane, int lanes) {
+  const int32_t first = a.cu[i], rows = a.cu[i + 1] - first, ctx = a.ctx[i];
+  const bool ok = a.status[i] == SYNERA_OK;
+  for (int j = lane; j < rows; j += lanes) {
+    if ((int64_t)first + j >= a.n_rows) break;
+    const int32_t p = ctx + j;
+    a.pos[first + j] = ok ? p : -1;
+    a.slot[first + j] = ok ? a.table[(size_t)i * a.columns + p / SY_PAGE] * SY_PAGE + p % SY_PAGE : -1;
   }
 }
+
+// PLACES: the same block writes the tokens' places too.  It writes some 40 GB/s: beyond PG_ROWS tokens a second launch over all requests is shorter.
+#define PG_ROWS 4096
+template <bool PLACES>
+__global__ __launch_bounds__(1024) void pages_kernel(PagesArgs a) {
+  __shared__ Sum3 wave_sums[16];
+  __shared__ int32_t taken;
+  pages_step(a, wave_sums, &taken);
+  if constexpr (PLACES) {
+    __syncthreads();
+    for (int i = threadIdx.x >> 6; i < a.B; i += 16) pages_places(a, i, threadIdx.x & 63, 64);
+  }
+}
+__global__ __launch_bounds__(256) void pages_places_kernel(PagesArgs a) { pages_places(a, blockIdx.x, blockIdx.y * 256 + threadIdx.x, gridDim.y * 256); }
 
 extern "C" int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_new, const int32_t* d_shared, int32_t* d_table,
                                        int32_t columns, int32_t* d_held, int32_t* d_free, int32_t* d_n_free, int32_t n_pages, int64_t n_rows,
@@ -140,6 +176,14 @@ extern "C" int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, cons
   if (bits % 4) return SYNERA_EINVAL;
   if (n_pages >= 1 << 27 || (int64_t)B * columns >= (int64_t)1 << 27) return SYNERA_EUNSUP;
   const PagesArgs a = {d_ctx_len, d_n_new, d_shared, d_table, d_held, d_free, d_n_free, d_cu, d_pos, d_slot, d_status, n_rows, B, columns, n_pages};
-  pages_kernel<<<1, 1024, 0, static_cast<hipStream_t>(stream)>>>(a);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (n_rows <= PG_ROWS) {
+    pages_kernel<true><<<1, 1024, 0, s>>>(a);
+  } else {
+    pages_kernel<false><<<1, 1024, 0, s>>>(a);
+    if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
+    // (requests of a prompt's length take several blocks)
+    pages_places_kernel<<<dim3(B, (uint32_t)std::min<int64_t>(64, std::max<int64_t>(1, n_rows / B / 1024))), 256, 0, s>>>(a);
+  }
   return hipGetLastError() == hipSuccess ? SYNERA_OK : SYNERA_EHIP;
 }
