@@ -122,7 +122,7 @@ typedef struct synera_logits_desc {
   const int32_t* d_history_len;    /* [B] clamped to 0 .. history_columns; NULL with d_history                            */
   const int32_t* d_n_prompt;   /* [B] or NULL: 0                                                                        */
   int32_t history_columns;     /* below 2^19                                                                            */
-  int32_t bias_columns;        /* <= 2046                                                                               */
+  int32_t bias_columns;        /* <= 1022                                                                               */
   const float* d_repetition;   /* [B], above 0, or NULL: 1                                                              */
   const float* d_presence;     /* [B] or NULL: 0                                                                        */
   const float* d_frequency;    /* [B] or NULL: 0                                                                        */

@@ -6,16 +6,22 @@
 #include "rope.h"
 
 // A block takes a slice of the vocabulary for some rows of one request.  What is known of a token lies in one word in LDS: how often it was
-// generated (bits 0 .. 19), whether it was part of the prompt (20), the last bias entry that names it, from 1 on (21 .. 31).  The words are
-// made from the history once for all rows of the block; a row's path is added before the row and taken away behind it.  All counts are integers,
-// so the order of the atomics does not show.  A bit for each 16 bytes of logits says whether any of their words may be set: what has none and is
-// allowed passes as it is, without a conversion.
+// generated (bits 0 .. 19), whether it was part of the prompt (20), whether it is on some row's path (21), the last bias entry that names it, from 1
+// on (22 .. 31); a bit for each token says that its word is not 0.  They are made from the history once for all rows of the block.  All counts are
+// integers, so the order of the atomics does not show.
+// Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides, and a lane goes through those of its
+// piece that have a word and are allowed, one at a time.  (Nearly every wavefront meets some: with a test for each value of each piece, 2048 x 128256 masked
+// took 325 us; formed behind the others, from memory, 300.)
+// Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Longer ones are
+// added to the words before a row and taken away behind it.
 #define LG_SLICE 8192
+#define LG_THREADS 512
 #define LG_PROMPT (1u << 20)
 #define LG_SEEN (2 * LG_PROMPT - 1)
-#define LG_BIAS 21
+#define LG_PATH (1u << 21)
+#define LG_BIAS 22
 #define LG_MOST_STEPS 65536      // of a path
-#define LG_NODES 512             // of a tree whose parents and tokens are read once, into LDS
+#define LG_NODES 256
 #define LG_FLY 4                 // 16-byte pieces of a thread on their way together
 
 struct LogitsArgs {
@@ -23,13 +29,10 @@ struct LogitsArgs {
   const void* in;
   void* out;
   int32_t splits;                // blocks that share the rows of a request
-  bool in_place;
+  bool in_place, once;
 };
 
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) LgBits {   // 16 bytes at any address that T allows
-  u32x4 v;
-};
+typedef u32x4 __attribute__((aligned(2))) lg_piece;            // 16 bytes at any address that a type of logits allows
 
 struct LgParams {
   float rho, pres, freq;
@@ -42,6 +45,34 @@ __device__ __forceinline__ float lg_adjust(const LgParams& p, float x, uint32_t 
   const uint32_t entry = w >> LG_BIAS;
   if (entry) x += p.bias[entry - 1];
   return x;
+}
+
+// Value k of a piece, and another in its place.
+template <typename T> __device__ __forceinline__ float lg_get(u32x4 v, int k) {
+  if constexpr (sizeof(T) == 4) {
+    return __uint_as_float(k & 2 ? (k & 1 ? v[3] : v[2]) : (k & 1 ? v[1] : v[0]));
+  } else {
+    const uint32_t w = (k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> (16 * (k & 1));
+    const uint16_t h = (uint16_t)w;
+    TurnChunk<T, 1> c;
+    float f;
+    c.p[0] = h;
+    c.widen(&f);
+    return f;
+  }
+}
+template <typename T> __device__ __forceinline__ u32x4 lg_put(u32x4 v, int k, float f) {
+  TurnChunk<T, 1> c;
+  c.round(&f);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] = w == k ? c.p[0] : v[w];
+  } else {
+    const uint32_t shift = 16 * (k & 1), bits = (uint32_t)c.p[0] << shift, keep = 0xFFFF0000u >> shift;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] = w == k / 2 ? (v[w] & keep) | bits : v[w];
+  }
+  return v;
 }
 
 // The bits of a piece as they are where its VEC mask bits are set, -infinity elsewhere.
@@ -63,14 +94,17 @@ __device__ __forceinline__ u32x4 lg_masked16(u32x4 v, uint32_t bits) {
 template <> __device__ __forceinline__ u32x4 lg_masked<bf16_t>(u32x4 v, uint32_t bits) { return lg_masked16<0xFF80u>(v, bits); }
 template <> __device__ __forceinline__ u32x4 lg_masked<_Float16>(u32x4 v, uint32_t bits) { return lg_masked16<0xFC00u>(v, bits); }
 
-template <typename T, bool MASK>
-__global__ __launch_bounds__(256) void logits_kernel(LogitsArgs a) {
-  constexpr int VEC = 16 / (int)sizeof(T), PIECES = LG_SLICE / VEC;
+// ONCE: the output is marked as not wanted again.
+template <typename T, bool MASK, bool ONCE>
+__global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
+  constexpr int VEC = 16 / (int)sizeof(T), PIECES = LG_SLICE / VEC, EACH = PIECES / LG_THREADS, ROWS = LG_FLY / EACH;
   constexpr uint32_t ALL = (1u << VEC) - 1;
-  typedef LgBits<T> Bits;
   __shared__ __attribute__((aligned(16))) uint32_t word[LG_SLICE];
-  __shared__ uint32_t maybe[PIECES / 32];
-  __shared__ int32_t node_token[LG_NODES], node_parent[LG_NODES];
+  __shared__ uint32_t has_word[LG_SLICE / 32];
+  __shared__ uint32_t on_path[LG_NODES][LG_NODES / 32 + 1];   // (+ 1: neighbours on other banks)
+  __shared__ int32_t parents[LG_NODES];
+  __shared__ uint32_t listed[LG_NODES];                       // token in the slice | node << 16
+  __shared__ int32_t n_listed;
   const int tid = threadIdx.x, i = blockIdx.y;
   const int v0 = blockIdx.x * LG_SLICE, n = min(LG_SLICE, (int)a.d.vocab - v0);
   int64_t first = i, rows = 1;
@@ -79,26 +113,55 @@ __global__ __launch_bounds__(256) void logits_kernel(LogitsArgs a) {
     rows = min(max((int64_t)a.d.d_cu[i + 1], first), a.d.rows) - first;
   }
   if (blockIdx.z >= rows) return;
-  // ---- the words
-  auto mark = [&](uint32_t t) { atomicOr(&maybe[t / VEC / 32], 1u << (t / VEC % 32)); };
-  for (int w = tid; w < (n + 3) / 4; w += 256) reinterpret_cast<u32x4*>(word)[w] = u32x4{0, 0, 0, 0};
-  if (tid < PIECES / 32) maybe[tid] = 0;
-  const bool staged = a.d.d_tokens && rows <= LG_NODES;
-  if (staged)
-    for (int t = tid; t < (int)rows; t += 256) {
-      node_token[t] = a.d.d_tokens[first + t];
-      node_parent[t] = a.d.d_parent[first + t];
+  // ---- the first rows are asked for before anything else
+  const int64_t words = (a.d.vocab + 31) / 32;
+  const int whole = n / VEC;
+  auto in_of = [&](int64_t j) { return static_cast<const T*>(a.in) + (first + j) * a.d.in_stride + v0; };
+  auto out_of = [&](int64_t j) { return static_cast<T*>(a.out) + (first + j) * a.d.out_stride + v0; };
+  auto mask_of = [&](int64_t j) { return reinterpret_cast<const uint32_t*>(a.d.d_mask) + (first + j) * words + v0 / 32; };
+  struct Rows {                                               // pieces of rows j0, j0 + splits, .., `most` of them
+    uint32_t bits[ROWS][EACH];
+    u32x4 x[ROWS][EACH];
+  };
+  auto on = [&](int64_t j0, int most, int g, int p) { return g < most && j0 + (int64_t)g * a.splits < rows && tid + p * LG_THREADS < whole; };
+  auto load = [&](Rows& r, int64_t j0, int most) {
+    if constexpr (MASK) {
+#pragma unroll
+      for (int g = 0; g < ROWS; ++g)
+#pragma unroll
+        for (int p = 0; p < EACH; ++p) {
+          const int c = tid + p * LG_THREADS;
+          r.bits[g][p] = on(j0, most, g, p) ? (mask_of(j0 + (int64_t)g * a.splits)[c * VEC / 32] >> (c * VEC % 32)) & ALL : 0;
+        }
     }
-  __syncthreads();
-  if (a.d.d_bias_id) {
-    for (int e = tid; e < a.d.bias_columns; e += 256) {
-      const uint32_t t = (uint32_t)(a.d.d_bias_id[(size_t)i * a.d.bias_columns + e] - v0);
-      if (t < (uint32_t)n) {
-        atomicMax(&word[t], (uint32_t)(e + 1) << LG_BIAS);
-        mark(t);
+#pragma unroll
+    for (int g = 0; g < ROWS; ++g)
+#pragma unroll
+      for (int p = 0; p < EACH; ++p) {
+        r.x[g][p] = u32x4{0, 0, 0, 0};
+        if (MASK ? r.bits[g][p] != 0 : on(j0, most, g, p))
+          r.x[g][p] = reinterpret_cast<const lg_piece*>(in_of(j0 + (int64_t)g * a.splits))[tid + p * LG_THREADS];
       }
+  };
+  const bool masked_paths = a.d.d_tokens && rows <= LG_NODES, added_paths = a.d.d_tokens && !masked_paths;
+  const int most = added_paths ? 1 : ROWS;
+  Rows now;
+  load(now, blockIdx.z, most);
+  // ---- the words
+  for (int w = tid; w < (n + 3) / 4; w += LG_THREADS) reinterpret_cast<u32x4*>(word)[w] = u32x4{0, 0, 0, 0};
+  if (tid < LG_SLICE / 32) has_word[tid] = 0;
+  if (tid == 0) n_listed = 0;
+  if (masked_paths && tid < rows) parents[tid] = a.d.d_parent[first + tid];
+  __syncthreads();
+  auto touch = [&](uint32_t t, uint32_t before) {             // by the first one that finds nothing
+    if (before == 0) atomicOr(&has_word[t / 32], 1u << (t % 32));
+  };
+  if (a.d.d_bias_id) {
+    for (int e = tid; e < a.d.bias_columns; e += LG_THREADS) {
+      const uint32_t t = (uint32_t)(a.d.d_bias_id[(size_t)i * a.d.bias_columns + e] - v0);
+      if (t < (uint32_t)n) touch(t, atomicMax(&word[t], (uint32_t)(e + 1) << LG_BIAS));
     }
-    __syncthreads();
+    __syncthreads();                                          // (the largest entry is sought among entries alone)
   }
   if (a.d.d_history) {
     const int len = min(max(a.d.d_history_len[i], 0), a.d.history_columns);
@@ -106,112 +169,123 @@ __global__ __launch_bounds__(256) void logits_kernel(LogitsArgs a) {
     const int32_t* h = a.d.d_history + (size_t)i * a.d.history_columns;
     auto count = [&](int e, int32_t id) {
       const uint32_t t = (uint32_t)(id - v0);
-      if (t >= (uint32_t)n) return;
-      if (e < prompt) atomicOr(&word[t], LG_PROMPT);
-      else atomicAdd(&word[t], 1u);
-      mark(t);
+      if (t < (uint32_t)n) touch(t, e < prompt ? atomicOr(&word[t], LG_PROMPT) : atomicAdd(&word[t], 1u));
     };
     int e = tid;
-    for (; e + 3 * 256 < len; e += 4 * 256) {
-      const int32_t t0 = h[e], t1 = h[e + 256], t2 = h[e + 512], t3 = h[e + 768];
+    for (; e + 3 * LG_THREADS < len; e += 4 * LG_THREADS) {
+      const int32_t t0 = h[e], t1 = h[e + LG_THREADS], t2 = h[e + 2 * LG_THREADS], t3 = h[e + 3 * LG_THREADS];
       count(e, t0);
-      count(e + 256, t1);
-      count(e + 512, t2);
-      count(e + 768, t3);
+      count(e + LG_THREADS, t1);
+      count(e + 2 * LG_THREADS, t2);
+      count(e + 3 * LG_THREADS, t3);
     }
-    for (; e < len; e += 256) count(e, h[e]);
-    __syncthreads();
+    for (; e < len; e += LG_THREADS) count(e, h[e]);
   }
+  if (masked_paths && tid < rows) {
+    uint32_t* mine = on_path[tid];
+#pragma unroll
+    for (int w = 0; w < LG_NODES / 32; ++w) mine[w] = 0;
+    for (int at = tid;;) {
+      mine[at / 32] |= 1u << (at % 32);
+      const int up = parents[at];
+      if (up < 0 || up >= at) break;
+      at = up;
+    }
+    const uint32_t t = (uint32_t)(a.d.d_tokens[first + tid] - v0);
+    if (t < (uint32_t)n) {
+      listed[atomicAdd(&n_listed, 1)] = t | (uint32_t)tid << 16;
+      touch(t, atomicOr(&word[t], LG_PATH));
+    }
+  }
+  __syncthreads();
   const LgParams params = {a.d.d_repetition ? a.d.d_repetition[i] : 1.f, a.d.d_presence ? a.d.d_presence[i] : 0.f,
                            a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + (size_t)i * a.d.bias_columns};
   // ---- the rows
-  for (int64_t j = blockIdx.z; j < rows; j += a.splits) {
-    const int64_t r = first + j;
-    auto path = [&](uint32_t by) {
-      if (!a.d.d_tokens) return;
-      if (tid == 0) {
-        int64_t at = j;
-        for (int k = 0; k < LG_MOST_STEPS; ++k) {
-          const uint32_t t = (uint32_t)((staged ? node_token[at] : a.d.d_tokens[first + at]) - v0);
-          if (t < (uint32_t)n) {
-            word[t] += by;
-            mark(t);
-          }
-          const int32_t up = staged ? node_parent[at] : a.d.d_parent[first + at];
-          if (up < 0 || up >= at) break;
-          at = up;
-        }
+  auto word_of = [&](int64_t j, int t) {                      // of token t of the slice, for row j
+    uint32_t w = word[t];
+    if (w & LG_PATH)
+      for (int k = 0; k < n_listed; ++k) {
+        const uint32_t x = listed[k];
+        if ((int)(x & 0xFFFF) == t) w += (on_path[j][x >> 21] >> ((x >> 16) & 31)) & 1;
       }
+    return w & ~LG_PATH;
+  };
+  auto finish = [&](const Rows& r, int64_t j0) {
+#pragma unroll
+    for (int g = 0; g < ROWS; ++g)
+#pragma unroll
+      for (int p = 0; p < EACH; ++p) {
+        if (!on(j0, most, g, p)) continue;
+        const int64_t j = j0 + (int64_t)g * a.splits;
+        const int c = tid + p * LG_THREADS;
+        const uint32_t allowed = MASK ? r.bits[g][p] : ALL;
+        u32x4 v = r.x[g][p];
+        uint32_t todo = (has_word[c * VEC / 32] >> (c * VEC % 32)) & allowed;
+        if (a.in_place && !todo && allowed == ALL) continue;
+        while (todo) {
+          const int k = __builtin_ctz(todo);
+          todo &= todo - 1;
+          const uint32_t w = word_of(j, c * VEC + k);
+          if (w) v = lg_put<T>(v, k, lg_adjust(params, lg_get<T>(v, k), w));
+        }
+        v = MASK ? lg_masked<T>(v, allowed) : v;
+        lg_piece* to = reinterpret_cast<lg_piece*>(out_of(j)) + c;
+        if constexpr (ONCE) __builtin_nontemporal_store(v, to);
+        else *to = v;
+      }
+    if (whole * VEC < n)                                      // the rows' last values, less than a piece
+      for (int g = 0; g < most; ++g) {
+        const int64_t j = j0 + (int64_t)g * a.splits;
+        const int e = whole * VEC + tid;
+        if (j >= rows || e >= n) continue;
+        TurnChunk<T, 1> y;
+        float f;
+        y.load(in_of(j) + e);
+        const bool allowed = !MASK || (mask_of(j)[e / 32] >> (e % 32)) & 1;
+        const uint32_t w = word_of(j, e);
+        if (w || !allowed) {
+          y.widen(&f);
+          f = allowed ? lg_adjust(params, f, w) : -INFINITY;
+          y.round(&f);
+        }
+        y.template store<false>(out_of(j) + e);
+      }
+  };
+  auto path = [&](int64_t j, uint32_t by) {                   // a long path, into the words and out of them
+    int64_t at = j;
+    for (int k = 0; k < LG_MOST_STEPS; ++k) {
+      const uint32_t t = (uint32_t)(a.d.d_tokens[first + at] - v0);
+      if (t < (uint32_t)n) {
+        word[t] += by;
+        has_word[t / 32] |= 1u << (t % 32);
+      }
+      const int32_t up = a.d.d_parent[first + at];
+      if (up < 0 || up >= at) break;
+      at = up;
+    }
+  };
+  for (int64_t j0 = blockIdx.z, step = (int64_t)a.splits * most; j0 < rows; j0 += step) {
+    Rows next;
+    if (j0 + step < rows) load(next, j0 + step, most);
+    if (added_paths) {
+      if (tid == 0) path(j0, 1u);
       __syncthreads();
-    };
-    path(1u);
-    const T* in = static_cast<const T*>(a.in) + r * a.d.in_stride + v0;
-    T* out = static_cast<T*>(a.out) + r * a.d.out_stride + v0;
-    const uint32_t* mask = MASK ? reinterpret_cast<const uint32_t*>(a.d.d_mask) + r * ((a.d.vocab + 31) / 32) + v0 / 32 : nullptr;
-    auto piece = [&](int c, u32x4 x, uint32_t bits) {
-      const bool seen = (maybe[c / 32] >> (c % 32)) & 1;
-      bool changed = MASK && bits != ALL;
-      if (seen) {
-        TurnChunk<T, VEC> y;
-        float f[VEC];
-        y.p[0] = x;
-        y.widen(f);
-        uint32_t any = 0;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-          const uint32_t w = word[c * VEC + k];
-          any |= w;
-          if (w) f[k] = lg_adjust(params, f[k], w);
-        }
-        y.round(f);
-        if (any) {
-          x = y.p[0];
-          changed = true;
-        }
-      }
-      if (MASK) x = lg_masked<T>(x, bits);
-      if (a.in_place && !changed) return;
-      Bits z;
-      z.v = x;
-      reinterpret_cast<Bits*>(out)[c] = z;
-    };
-    const int whole = n / VEC;
-    int c = tid;
-    for (; c + (LG_FLY - 1) * 256 < whole; c += LG_FLY * 256) {
-      uint32_t bits[LG_FLY];
-      u32x4 x[LG_FLY];
-#pragma unroll
-      for (int f = 0; f < LG_FLY; ++f) bits[f] = MASK ? (mask[(c + f * 256) * VEC / 32] >> ((c + f * 256) * VEC % 32)) & ALL : ALL;
-#pragma unroll
-      for (int f = 0; f < LG_FLY; ++f) x[f] = reinterpret_cast<const Bits*>(in)[c + f * 256].v;
-#pragma unroll
-      for (int f = 0; f < LG_FLY; ++f) piece(c + f * 256, x[f], bits[f]);
     }
-    for (; c < whole; c += 256) piece(c, reinterpret_cast<const Bits*>(in)[c].v, MASK ? (mask[c * VEC / 32] >> (c * VEC % 32)) & ALL : ALL);
-    for (int e = whole * VEC + tid; e < n; e += 256) {
-      TurnChunk<T, 1> x;
-      float f;
-      x.load(in + e);
-      const uint32_t w = word[e];
-      const bool allowed = !MASK || (mask[e / 32] >> (e % 32)) & 1;
-      if (a.in_place && !w && allowed) continue;
-      if (w || !allowed) {
-        x.widen(&f);
-        if (w) f = lg_adjust(params, f, w);
-        if (!allowed) f = -INFINITY;
-        x.round(&f);
-      }
-      x.template store<false>(out + e);
+    finish(now, j0);
+    if (added_paths) {
+      __syncthreads();
+      if (tid == 0) path(j0, ~0u);
     }
-    __syncthreads();
-    path(~0u);
+    now = next;
   }
 }
 
 template <typename T>
 static void launch_logits(const LogitsArgs& a, dim3 grid, hipStream_t s) {
-  if (a.d.d_mask) logits_kernel<T, true><<<grid, 256, 0, s>>>(a);
-  else logits_kernel<T, false><<<grid, 256, 0, s>>>(a);
+  if (a.once && a.d.d_mask) logits_kernel<T, true, true><<<grid, LG_THREADS, 0, s>>>(a);
+  else if (a.once) logits_kernel<T, false, true><<<grid, LG_THREADS, 0, s>>>(a);
+  else if (a.d.d_mask) logits_kernel<T, true, false><<<grid, LG_THREADS, 0, s>>>(a);
+  else logits_kernel<T, false, false><<<grid, LG_THREADS, 0, s>>>(a);
 }
 
 static bool lg_meet(const void* a, int64_t na, const void* b, int64_t nb) {
@@ -227,7 +301,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if (!d.d_cu && d.rows != d.B) return SYNERA_EINVAL;
   if ((!d.d_tokens) != (!d.d_parent) || (d.d_tokens && !d.d_cu)) return SYNERA_EINVAL;
   if ((d.d_history && !d.d_history_len) || (!d.d_bias_id) != (!d.d_bias)) return SYNERA_EINVAL;
-  if (d.vocab > (int64_t)1 << 30 || d.bias_columns > 2046 || d.history_columns >= 1 << 19 || d.B > 65535 || d.rows >= (int64_t)1 << 31) return SYNERA_EUNSUP;
+  if (d.vocab > (int64_t)1 << 30 || d.bias_columns > 1022 || d.history_columns >= 1 << 19 || d.B > 65535 || d.rows >= (int64_t)1 << 31) return SYNERA_EUNSUP;
   if (d.rows == 0 || d.B == 0) return SYNERA_OK;
   if (!d_in || !d_out || (d.rows > 1 && (d.in_stride < d.vocab || d.out_stride < d.vocab))) return SYNERA_EINVAL;
   const int size = d.dtype == 0 ? 4 : 2;
@@ -244,7 +318,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if (bits % 4 || (reinterpret_cast<uintptr_t>(d_in) | reinterpret_cast<uintptr_t>(d_out)) % size) return SYNERA_EINVAL;
   const bool in_place = d_in == d_out && (d.rows == 1 || d.in_stride == d.out_stride);
   if (!in_place && lg_meet(d_out, out_bytes, d_in, in_bytes)) return SYNERA_EINVAL;
-  LogitsArgs a = {d, d_in, d_out, 1, in_place};
+  LogitsArgs a = {d, d_in, d_out, 1, in_place, !in_place && beyond_caches((size_t)(d.rows * d.vocab * size))};
   const int64_t slices = (d.vocab + LG_SLICE - 1) / LG_SLICE, each = (d.rows + B - 1) / B;
   a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 2048 / (slices * B))), 65535);
   const dim3 grid((uint32_t)slices, (uint32_t)B, (uint32_t)a.splits);

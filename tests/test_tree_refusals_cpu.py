@@ -57,7 +57,7 @@ def test_the_description_is_as_long_as_the_structure():
     (dict(B=-1), s.EINVAL), (dict(rows=-1), s.EINVAL), (dict(vocab=0), s.EINVAL), (dict(dtype=3), s.EINVAL), (dict(rows=3), s.EINVAL),
     (dict(in_stride=39), s.EINVAL), (dict(out_stride=39), s.EINVAL), (dict(d_history=64), s.EINVAL), (dict(d_bias_id=64), s.EINVAL),
     (dict(d_bias=64), s.EINVAL), (dict(d_tokens=64, d_cu=64), s.EINVAL), (dict(d_tokens=64, d_parent=64), s.EINVAL), (dict(d_mask=66), s.EINVAL),
-    (dict(history_columns=-1), s.EINVAL), (dict(bias_columns=-1), s.EINVAL), (dict(vocab=(1 << 30) + 1), s.EUNSUP), (dict(bias_columns=2047), s.EUNSUP),
+    (dict(history_columns=-1), s.EINVAL), (dict(bias_columns=-1), s.EINVAL), (dict(vocab=(1 << 30) + 1), s.EUNSUP), (dict(bias_columns=1023), s.EUNSUP),
     (dict(history_columns=1 << 19), s.EUNSUP), (dict(B=65536, rows=65536), s.EUNSUP)])
 def test_logits(bad, status):
     assert b._lib.synera_logits_adjust(desc(**bad), 1 << 20, 1 << 21, None) == status
