@@ -22,6 +22,8 @@
 #define LG_BIAS 22
 #define LG_MOST_STEPS 65536      // of a path
 #define LG_NODES 256
+#define LG_MOST_BIASES 1022
+#define LG_EARLY 4               // tokens of the history that a thread asks for together
 #define LG_FLY 4                 // 16-byte pieces of a thread on their way together
 
 struct LogitsArgs {
@@ -147,51 +149,67 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
   const int most = added_paths ? 1 : ROWS;
   Rows now;
   load(now, blockIdx.z, most);
-  // ---- the words
+  // ---- the words.  What they are made from is on its way before the barrier, behind which LDS is clear
+  const size_t biases = (size_t)i * a.d.bias_columns;
+  const int len = a.d.d_history ? min(max(a.d.d_history_len[i], 0), a.d.history_columns) : 0;
+  const int prompt = a.d.d_n_prompt ? a.d.d_n_prompt[i] : 0;
+  const int32_t* h = a.d.d_history + (size_t)i * a.d.history_columns;
+  int32_t seen[LG_EARLY], named[2], up0 = -1, token0 = -1;
+  static_assert(2 * LG_THREADS >= LG_MOST_BIASES, "entries of a thread");
+#pragma unroll
+  for (int u = 0; u < LG_EARLY; ++u) seen[u] = tid + u * LG_THREADS < len ? h[tid + u * LG_THREADS] : -1;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) named[u] = a.d.d_bias_id && tid + u * LG_THREADS < a.d.bias_columns ? a.d.d_bias_id[biases + tid + u * LG_THREADS] : -1;
+  if (masked_paths && tid < rows) {
+    up0 = a.d.d_parent[first + tid];
+    token0 = a.d.d_tokens[first + tid];
+  }
   for (int w = tid; w < (n + 3) / 4; w += LG_THREADS) reinterpret_cast<u32x4*>(word)[w] = u32x4{0, 0, 0, 0};
   if (tid < LG_SLICE / 32) has_word[tid] = 0;
   if (tid == 0) n_listed = 0;
-  if (masked_paths && tid < rows) parents[tid] = a.d.d_parent[first + tid];
+  if (tid < LG_NODES) parents[tid] = up0;
   __syncthreads();
+  auto slot = [&](int32_t id) { return id < 0 ? 0xFFFFFFFFu : (uint32_t)(id - v0); };      // of a token in the slice: below n
   auto touch = [&](uint32_t t, uint32_t before) {             // by the first one that finds nothing
     if (before == 0) atomicOr(&has_word[t / 32], 1u << (t % 32));
   };
-  if (a.d.d_bias_id) {
-    for (int e = tid; e < a.d.bias_columns; e += LG_THREADS) {
-      const uint32_t t = (uint32_t)(a.d.d_bias_id[(size_t)i * a.d.bias_columns + e] - v0);
-      if (t < (uint32_t)n) touch(t, atomicMax(&word[t], (uint32_t)(e + 1) << LG_BIAS));
-    }
-    __syncthreads();                                          // (the largest entry is sought among entries alone)
+  auto count = [&](int e, int32_t id) {
+    const uint32_t t = slot(id);
+    if (t < (uint32_t)n) touch(t, e < prompt ? atomicOr(&word[t], LG_PROMPT) : atomicAdd(&word[t], 1u));
+  };
+#pragma unroll
+  for (int u = 0; u < LG_EARLY; ++u) count(tid + u * LG_THREADS, seen[u]);
+  for (int e = tid + LG_EARLY * LG_THREADS; e < len; e += LG_EARLY * LG_THREADS) {
+#pragma unroll
+    for (int u = 0; u < LG_EARLY; ++u) seen[u] = e + u * LG_THREADS < len ? h[e + u * LG_THREADS] : -1;
+#pragma unroll
+    for (int u = 0; u < LG_EARLY; ++u) count(e + u * LG_THREADS, seen[u]);
   }
-  if (a.d.d_history) {
-    const int len = min(max(a.d.d_history_len[i], 0), a.d.history_columns);
-    const int prompt = a.d.d_n_prompt ? a.d.d_n_prompt[i] : 0;
-    const int32_t* h = a.d.d_history + (size_t)i * a.d.history_columns;
-    auto count = [&](int e, int32_t id) {
-      const uint32_t t = (uint32_t)(id - v0);
-      if (t < (uint32_t)n) touch(t, e < prompt ? atomicOr(&word[t], LG_PROMPT) : atomicAdd(&word[t], 1u));
-    };
-    int e = tid;
-    for (; e + 3 * LG_THREADS < len; e += 4 * LG_THREADS) {
-      const int32_t t0 = h[e], t1 = h[e + LG_THREADS], t2 = h[e + 2 * LG_THREADS], t3 = h[e + 3 * LG_THREADS];
-      count(e, t0);
-      count(e + LG_THREADS, t1);
-      count(e + 2 * LG_THREADS, t2);
-      count(e + 3 * LG_THREADS, t3);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t t = slot(named[u]), entry = tid + u * LG_THREADS + 1;
+    if (t >= (uint32_t)n) continue;
+    uint32_t old = word[t];                                   // counts may come in between
+    while (old >> LG_BIAS < entry) {
+      const uint32_t was = atomicCAS(&word[t], old, (old & ((1u << LG_BIAS) - 1)) | entry << LG_BIAS);
+      if (was == old) {
+        touch(t, old);
+        break;
+      }
+      old = was;
     }
-    for (; e < len; e += LG_THREADS) count(e, h[e]);
   }
   if (masked_paths && tid < rows) {
     uint32_t* mine = on_path[tid];
 #pragma unroll
     for (int w = 0; w < LG_NODES / 32; ++w) mine[w] = 0;
-    for (int at = tid;;) {
+    for (int at = tid, up = up0;;) {
       mine[at / 32] |= 1u << (at % 32);
-      const int up = parents[at];
       if (up < 0 || up >= at) break;
       at = up;
+      up = parents[at];
     }
-    const uint32_t t = (uint32_t)(a.d.d_tokens[first + tid] - v0);
+    const uint32_t t = slot(token0);
     if (t < (uint32_t)n) {
       listed[atomicAdd(&n_listed, 1)] = t | (uint32_t)tid << 16;
       touch(t, atomicOr(&word[t], LG_PATH));
@@ -199,7 +217,7 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
   }
   __syncthreads();
   const LgParams params = {a.d.d_repetition ? a.d.d_repetition[i] : 1.f, a.d.d_presence ? a.d.d_presence[i] : 0.f,
-                           a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + (size_t)i * a.d.bias_columns};
+                           a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + biases};
   // ---- the rows
   auto word_of = [&](int64_t j, int t) {                      // of token t of the slice, for row j
     uint32_t w = word[t];
@@ -301,7 +319,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if (!d.d_cu && d.rows != d.B) return SYNERA_EINVAL;
   if ((!d.d_tokens) != (!d.d_parent) || (d.d_tokens && !d.d_cu)) return SYNERA_EINVAL;
   if ((d.d_history && !d.d_history_len) || (!d.d_bias_id) != (!d.d_bias)) return SYNERA_EINVAL;
-  if (d.vocab > (int64_t)1 << 30 || d.bias_columns > 1022 || d.history_columns >= 1 << 19 || d.B > 65535 || d.rows >= (int64_t)1 << 31) return SYNERA_EUNSUP;
+  if (d.vocab > (int64_t)1 << 30 || d.bias_columns > LG_MOST_BIASES || d.history_columns >= 1 << 19 || d.B > 65535 || d.rows >= (int64_t)1 << 31) return SYNERA_EUNSUP;
   if (d.rows == 0 || d.B == 0) return SYNERA_OK;
   if (!d_in || !d_out || (d.rows > 1 && (d.in_stride < d.vocab || d.out_stride < d.vocab))) return SYNERA_EINVAL;
   const int size = d.dtype == 0 ? 4 : 2;
