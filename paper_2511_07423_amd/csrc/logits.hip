@@ -9,9 +9,9 @@
 // generated (bits 0 .. 19), whether it was part of the prompt (20), whether it is on some row's path (21), the last bias entry that names it, from 1
 // on (22 .. 31); a bit for each token says that its word is not 0.  They are made from the history once for all rows of the block.  All counts are
 // integers, so the order of the atomics does not show.
-// Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides, and a lane goes through those of its
-// piece that have a word and are allowed, one at a time.  (Nearly every wavefront meets some: with a test for each value of each piece, 2048 x 128256 masked
-// took 325 us; formed behind the others, from memory, 300.)
+// Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides; those that are allowed and have a word
+// are formed on the way.  (Nearly every wavefront meets some: with a branch for each value 2048 x 128256 masked took 325 us; formed behind the
+// others, from memory, 300; this way 198, as long as a plain copy of the logits.)
 // Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Longer ones are
 // added to the words before a row and taken away behind it.
 #define LG_SLICE 8192
@@ -37,16 +37,18 @@ struct LogitsArgs {
 typedef u32x4 __attribute__((aligned(2))) lg_piece;            // 16 bytes at any address that a type of logits allows
 
 struct LgParams {
-  float rho, pres, freq;
+  float rho, inv, pres, freq;    // inv: 1 / rho, rounded; x inv is within two half steps of x / rho
   const float* bias;
 };
+// Without branches: values without a word (w = 0) come out as they are.
 __device__ __forceinline__ float lg_adjust(const LgParams& p, float x, uint32_t w) {
-  if (w & LG_SEEN) x = x > 0.f ? x / p.rho : x * p.rho;
   const uint32_t g = w & (LG_PROMPT - 1);
-  if (g) x -= __builtin_fmaf(p.freq, (float)g, p.pres);
+  x *= w & LG_SEEN ? (x > 0.f ? p.inv : p.rho) : 1.f;
+  return x - (g ? __builtin_fmaf(p.freq, (float)g, p.pres) : 0.f);
+}
+__device__ __forceinline__ float lg_bias(const LgParams& p, float x, uint32_t w) {
   const uint32_t entry = w >> LG_BIAS;
-  if (entry) x += p.bias[entry - 1];
-  return x;
+  return entry ? x + p.bias[entry - 1] : x;
 }
 
 // Value k of a piece, and another in its place.
@@ -54,11 +56,9 @@ template <typename T> __device__ __forceinline__ float lg_get(u32x4 v, int k) {
   if constexpr (sizeof(T) == 4) {
     return __uint_as_float(k & 2 ? (k & 1 ? v[3] : v[2]) : (k & 1 ? v[1] : v[0]));
   } else {
-    const uint32_t w = (k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> (16 * (k & 1));
-    const uint16_t h = (uint16_t)w;
     TurnChunk<T, 1> c;
     float f;
-    c.p[0] = h;
+    c.p[0] = (uint16_t)((k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> (16 * (k & 1)));
     c.widen(&f);
     return f;
   }
@@ -100,6 +100,7 @@ template <> __device__ __forceinline__ u32x4 lg_masked<_Float16>(u32x4 v, uint32
 template <typename T, bool MASK, bool ONCE>
 __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T), PIECES = LG_SLICE / VEC, EACH = PIECES / LG_THREADS, ROWS = LG_FLY / EACH;
+  static_assert(EACH >= 1 && ROWS >= 1 && LG_THREADS >= LG_NODES && 2 * LG_THREADS >= LG_MOST_BIASES, "what a thread takes");
   constexpr uint32_t ALL = (1u << VEC) - 1;
   __shared__ __attribute__((aligned(16))) uint32_t word[LG_SLICE];
   __shared__ uint32_t has_word[LG_SLICE / 32];
@@ -115,7 +116,6 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
     rows = min(max((int64_t)a.d.d_cu[i + 1], first), a.d.rows) - first;
   }
   if (blockIdx.z >= rows) return;
-  // ---- the first rows are asked for before anything else
   const int64_t words = (a.d.vocab + 31) / 32;
   const int whole = n / VEC;
   auto in_of = [&](int64_t j) { return static_cast<const T*>(a.in) + (first + j) * a.d.in_stride + v0; };
@@ -147,15 +147,14 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
   };
   const bool masked_paths = a.d.d_tokens && rows <= LG_NODES, added_paths = a.d.d_tokens && !masked_paths;
   const int most = added_paths ? 1 : ROWS;
+  // ---- the first rows, and what the words are made from, are on their way before the barrier behind which LDS is clear
   Rows now;
   load(now, blockIdx.z, most);
-  // ---- the words.  What they are made from is on its way before the barrier, behind which LDS is clear
   const size_t biases = (size_t)i * a.d.bias_columns;
   const int len = a.d.d_history ? min(max(a.d.d_history_len[i], 0), a.d.history_columns) : 0;
   const int prompt = a.d.d_n_prompt ? a.d.d_n_prompt[i] : 0;
   const int32_t* h = a.d.d_history + (size_t)i * a.d.history_columns;
   int32_t seen[LG_EARLY], named[2], up0 = -1, token0 = -1;
-  static_assert(2 * LG_THREADS >= LG_MOST_BIASES, "entries of a thread");
 #pragma unroll
   for (int u = 0; u < LG_EARLY; ++u) seen[u] = tid + u * LG_THREADS < len ? h[tid + u * LG_THREADS] : -1;
 #pragma unroll
@@ -216,8 +215,9 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
     }
   }
   __syncthreads();
-  const LgParams params = {a.d.d_repetition ? a.d.d_repetition[i] : 1.f, a.d.d_presence ? a.d.d_presence[i] : 0.f,
-                           a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + biases};
+  LgParams params = {a.d.d_repetition ? a.d.d_repetition[i] : 1.f, 1.f, a.d.d_presence ? a.d.d_presence[i] : 0.f,
+                     a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + biases};
+  params.inv = 1.f / params.rho;
   // ---- the rows
   auto word_of = [&](int64_t j, int t) {                      // of token t of the slice, for row j
     uint32_t w = word[t];
@@ -240,11 +240,36 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
         u32x4 v = r.x[g][p];
         uint32_t todo = (has_word[c * VEC / 32] >> (c * VEC % 32)) & allowed;
         if (a.in_place && !todo && allowed == ALL) continue;
-        while (todo) {
-          const int k = __builtin_ctz(todo);
-          todo &= todo - 1;
-          const uint32_t w = word_of(j, c * VEC + k);
-          if (w) v = lg_put<T>(v, k, lg_adjust(params, lg_get<T>(v, k), w));
+        // Under a mask few values of a piece are to be formed: one at a time.  Without one, all alike and without branches.  (2048 x 128256 bf16: under a mask
+        // that leaves 3 % 198 and 226 us, without a mask 234 and 200; both ways in one kernel take too many registers.)
+        if constexpr (MASK) {
+          while (todo) {
+            const int k = __builtin_ctz(todo);
+            todo &= todo - 1;
+            const uint32_t w = word_of(j, c * VEC + k);
+            v = lg_put<T>(v, k, lg_bias(params, lg_adjust(params, lg_get<T>(v, k), w), w));
+          }
+        } else if (todo) {
+          uint32_t w[VEC], any = 0;
+          float f[VEC];
+          TurnChunk<T, VEC> y;
+          y.p[0] = v;
+          y.widen(f);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) any |= w[k] = word[c * VEC + k];
+          if (any & LG_PATH) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+              if (w[k] & LG_PATH) w[k] = word_of(j, c * VEC + k);
+          }
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) f[k] = lg_adjust(params, f[k], w[k]);
+          if (any >> LG_BIAS) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) f[k] = lg_bias(params, f[k], w[k]);
+          }
+          y.round(f);
+          v = y.p[0];
         }
         v = MASK ? lg_masked<T>(v, allowed) : v;
         lg_piece* to = reinterpret_cast<lg_piece*>(out_of(j)) + c;
@@ -263,7 +288,7 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
         const uint32_t w = word_of(j, e);
         if (w || !allowed) {
           y.widen(&f);
-          f = allowed ? lg_adjust(params, f, w) : -INFINITY;
+          f = allowed ? lg_bias(params, lg_adjust(params, f, w), w) : -INFINITY;
           y.round(&f);
         }
         y.template store<false>(out_of(j) + e);
@@ -338,7 +363,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if (!in_place && lg_meet(d_out, out_bytes, d_in, in_bytes)) return SYNERA_EINVAL;
   LogitsArgs a = {d, d_in, d_out, 1, in_place, !in_place && beyond_caches((size_t)(d.rows * d.vocab * size))};
   const int64_t slices = (d.vocab + LG_SLICE - 1) / LG_SLICE, each = (d.rows + B - 1) / B;
-  a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 2048 / (slices * B))), 65535);
+  a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 4096 / (slices * B))), 65535);
   const dim3 grid((uint32_t)slices, (uint32_t)B, (uint32_t)a.splits);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.dtype == 0) launch_logits<float>(a, grid, s);
