@@ -14,22 +14,38 @@
 #define TR_STEP SY_SH_STEP       // keys of one step, the unit of work
 
 // ------------------------------------------------------------------------------------ the plan on the device
-// The attention's work is one line: for each request in turn its streams (KV head, then tile of rows), for each stream its steps of TR_STEP keys
-// and TR_START more for what it takes to begin and end one.  Block b takes the share-th part b of the line.  So only the
-// places where parts begin are written down, and which parts a stream lies in follows from them.
-#define TR_START 2
-#define TR_SHARE 6               // the least that a block takes
+// The attention's work: a request's keys are cut into `ranges` of whole steps of TR_STEP keys, and a block takes one range of one KV head for one tile of
+// rows.  The tiles of a range follow each other on one XCD, so that its keys are fetched once and met in L2: each XCD has a list of its own,
+// the same for all but for the groups (head, range): list x has groups x, x + 8, .. of each request, whose tiles are the items.  Requests
+// come in the order of their items' cost, the longest first, since blocks take items as places become free.
+// How long a range may be is chosen from TR_LENGTHS candidates by an estimate of the time (tr_estimate).
+// (With the heads and tiles in one line that blocks took equal parts of, tiles of one head read its keys at different times:
+// 32 requests of 48 .. 160 nodes 414 us, 64 of 8 .. 64 nodes 125.)
+#define TR_LENGTHS 24
+#define TR_GRID 4                // blocks of the launch for each place
+__host__ __device__ inline int32_t tr_length(int c) {         // steps: 2, 3, 4, 6, 8, 12, .. 2048, 3072 and any
+  return c == TR_LENGTHS - 1 ? 1 << 30 : (2 + (c & 1)) << (c / 2);
+}
+// In 16ths of what a step takes a block when all places are taken and HBM is the bound (64 KB each: 6.8 us).
+#define TR_ONE 16                // a step of a request's only tile
+#define TR_MORE 11               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
+#define TR_START 32              // what it takes to begin and end an item
+#define TR_JOIN_LAUNCH 8         // to join anything at all
+#define TR_JOIN_ROWS 1024        // partial rows written and read in one 16th
 struct TrHead {
   ShHeader sh;                   // tokens and windows, for the append
-  int32_t n_blocks, share, B, pad[13];
+  int32_t items, B;              // items of an XCD's list
+  int32_t pad[14];
 };
-struct TrReq {                   // 32 bytes, scalar loads
+struct TrReq {                   // 64 bytes, scalar loads
   int32_t ctx, n, tok;           // n: 0 where the request has no nodes or is refused
-  int32_t steps, cost, streams, tiles;   // as the line counts them, refused or not
   int32_t rows;                  // of its n_nodes, those that there is room for
+  int32_t steps, ranges, tiles;  // as the lists count them, refused or not
+  int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
+  int32_t pad[8];
 };
-struct TrStart {                 // where a block's part begins
-  int32_t req, stream, step, pad;
+struct TrItem {                  // 8 bytes: a place in each XCD's list
+  int32_t req, at;               // the at-th item of the request in the list
 };
 
 struct synera_tree {
@@ -40,15 +56,15 @@ struct synera_tree {
   int64_t n_rows;
   int32_t pitch;                 // columns of the table's copy
   char* dev;
+  int32_t items_room, part_rows;
   TrHead* head;
   TrReq* req;
-  TrStart* start;
+  TrItem* items;
   ShWindow* windows;
   int32_t *pos, *slot, *parent, *table;
   uint32_t* masks;
   float* part_o;
   float2* part_ml;
-  int32_t grid;                  // blocks of the attention
 };
 
 static size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -70,6 +86,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   if (n_q_heads < 1 || n_kv_heads < 1 || max_batch < 1 || max_tokens < 1 || max_pages < 1) return SYNERA_EINVAL;
   if ((head_dim != 64 && head_dim != 128) || n_q_heads % n_kv_heads || n_q_heads > 1024) return SYNERA_EUNSUP;
   if ((int64_t)max_tokens * n_q_heads >= (int64_t)1 << 30 || (int64_t)max_batch * ((int64_t)max_pages + TR_AHEAD) >= (int64_t)1 << 30) return SYNERA_EUNSUP;
+  if ((int64_t)max_batch * n_q_heads >= (int64_t)1 << 26) return SYNERA_EUNSUP;
   int dev = 0;
   hipDeviceProp_t prop;
   if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess || prepare_attention(head_dim) != hipSuccess) {
@@ -87,9 +104,12 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   t->lim.max_pages = max_pages;
   t->lim.slots = 2 * std::max(1, prop.multiProcessorCount);
   t->pitch = max_pages + TR_AHEAD;
-  t->grid = (t->lim.slots + SY_SH_DEAL - 1) / SY_SH_DEAL * SY_SH_DEAL;
-  const size_t B = (size_t)max_batch, T = (size_t)max_tokens, parts = 2 * (size_t)t->lim.slots * SY_SH_TILE_ROWS;
-  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), ((size_t)t->lim.slots + 1) * sizeof(TrStart), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
+  // uncut, a request has an item in each list for every tile and eighth head, also one whose rows there is no room for
+  const size_t B = (size_t)max_batch, T = (size_t)max_tokens, G = (size_t)(n_q_heads / n_kv_heads);
+  t->items_room = (int32_t)std::max<size_t>((size_t)t->lim.slots, (size_t)((n_kv_heads + SY_SH_DEAL - 1) / SY_SH_DEAL) * B * (TR_NODES * G / SY_SH_TILE_ROWS + 1));
+  t->part_rows = 2 * t->lim.slots * SY_SH_TILE_ROWS;
+  const size_t parts = (size_t)t->part_rows;
+  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * sizeof(TrItem), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
                           T * 4, T * 4, T * 4, B * t->pitch * 4, T * SY_TREE_MASK * 4, parts * head_dim * 4, parts * 8};
   size_t all = 0;
   for (size_t s : sizes) all += up(s);
@@ -105,7 +125,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   };
   take(t->head);
   take(t->req);
-  take(t->start);
+  take(t->items);
   take(t->windows);
   take(t->pos);
   take(t->slot);
@@ -124,74 +144,134 @@ struct PlanArgs {
   int32_t* status;
   TrHead* head;
   TrReq* req;
-  TrStart* start;
+  TrItem* items;
   ShWindow* windows;
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
-  int32_t B, columns, pitch, n_pages, Hkv, G, slots;
+  int32_t B, columns, pitch, n_pages, Hkv, G, slots, items_room, part_rows;
   int64_t n_rows;
 };
 
 // What a request's lengths alone say of it; every block forms it for all of them.
 struct TrSize {
-  int32_t rows, windows, steps, cost, streams, tiles;
+  int32_t rows, windows, steps, tiles;
 };
 __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_t n) {
-  TrSize s = {0, 0, 0, 0, 0, 0};
+  TrSize s = {0, 0, 0, 0};
   if (n < 0 || n > TR_NODES) return s;
   s.rows = n;
   const int64_t keys = (int64_t)ctx + n;
-  if (n == 0 || ctx < 0 || (keys + SY_PAGE - 1) / SY_PAGE > a.columns) return s;
+  if (n == 0 || ctx < 0 || (keys + SY_PAGE - 1) / SY_PAGE > a.columns || keys > 0x7FFFFFFF - TR_STEP) return s;
   s.windows = (int32_t)((keys - 1) / SY_PAGE - ctx / SY_PAGE + 1);
   s.steps = (int32_t)((keys + TR_STEP - 1) / TR_STEP);
-  s.cost = s.steps + TR_START;
   s.tiles = (n * a.G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
-  s.streams = s.tiles * a.Hkv;
   return s;
 }
+__device__ __forceinline__ int32_t ranges_of(int32_t steps, int32_t length) { return steps == 0 ? 0 : (steps - 1) / length + 1; }
+__device__ __forceinline__ int32_t item_cost(const TrSize& s, int32_t ranges) {
+  return ((s.steps + ranges - 1) / ranges) * (s.tiles > 1 ? TR_MORE : TR_ONE) + TR_START;
+}
+__device__ __forceinline__ int64_t items_of(const PlanArgs& a, const TrSize& s, int32_t ranges) {      // in each list
+  return ((int64_t)a.Hkv * ranges + SY_SH_DEAL - 1) / SY_SH_DEAL * s.tiles;
+}
+// What each candidate comes to, over all requests; whole numbers, so that every block finds the same.
+struct TrTotals {
+  unsigned long long cost, parts, items;
+  int32_t longest;
+};
+__device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals& t) {
+  if (t.items > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
+  return (int64_t)(t.cost / (unsigned)(a.slots / SY_SH_DEAL)) + t.longest / 2 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
+}
 
-// Block i plans request i.  It sums up the requests before it by itself (a few thousand numbers at most, which lie in the caches), so that one launch
+// Block i plans request i.  It looks at all requests by itself (a few thousand numbers at most, which lie in the caches), so that one launch
 // does.  Paths by doubling: in each round a node takes over what its forefather has gathered, and that one's forefather.
 __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
+  constexpr int LANES = 256 / TR_LENGTHS;
   const int tid = threadIdx.x, me = blockIdx.x;
-  __shared__ int64_t sums[4][5];
-  int64_t v[5] = {0, 0, 0, 0, 0};                            // rows, windows and work before this request; rows and work of all
-  int32_t windows_all = 0;
-  for (int i = tid; i < a.B; i += 256) {
-    const TrSize s = size_of(a, a.ctx[i], a.n_nodes[i]);
-    const int64_t work = (int64_t)s.streams * s.cost;
-    if (i < me) {
-      v[0] += s.rows;
-      v[1] += s.windows;
-      v[2] += work;
-    }
-    v[3] += s.rows;
-    v[4] += work;
-    windows_all += s.windows;
-  }
-#pragma unroll
-  for (int k = 0; k < 5; ++k)
-    for (int o = 1; o < 64; o <<= 1) v[k] += __shfl_xor(v[k], o);
-  if ((tid & 63) == 0)
-    for (int k = 0; k < 5; ++k) sums[tid >> 6][k] = v[k];
-  __shared__ int32_t all_windows;
+  __shared__ TrTotals totals[TR_LENGTHS];
+  __shared__ TrSize sizes[256];
+  __shared__ int32_t best;
+  __shared__ unsigned long long sums[5];                      // rows, windows, items and partial rows before this request; rows of all
+  __shared__ int32_t all_windows, all_items;
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
-  if (tid == 0) all_windows = 0;
-  __syncthreads();
-  if (windows_all) atomicAdd(&all_windows, windows_all);
-#pragma unroll
-  for (int k = 0; k < 5; ++k) v[k] = sums[0][k] + sums[1][k] + sums[2][k] + sums[3][k];
-  const int64_t first = v[0];
+  if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0};
+  if (tid < 5) sums[tid] = 0;
+  if (tid == 0) all_windows = all_items = 0;
   const int32_t ctx = a.ctx[me], n = a.n_nodes[me];
   const TrSize s = size_of(a, ctx, n);
-  const int64_t share64 = max((int64_t)TR_SHARE, (v[4] + a.slots - 1) / a.slots);
-  const int32_t share = (int32_t)min(share64, (int64_t)0x7FFFFFFF);
+  // ---- how long a range may be
+  for (int i0 = 0; i0 < a.B; i0 += 256) {
+    __syncthreads();
+    if (i0 + tid < a.B) sizes[tid] = size_of(a, a.ctx[i0 + tid], a.n_nodes[i0 + tid]);
+    __syncthreads();
+    const int c = tid / LANES, m = min(256, a.B - i0);
+    if (c < TR_LENGTHS) {
+      TrTotals t = {0, 0, 0, 0};
+      for (int i = tid % LANES; i < m; i += LANES) {
+        const TrSize z = sizes[i];
+        if (z.steps == 0) continue;
+        const int32_t r = ranges_of(z.steps, tr_length(c)), cost = item_cost(z, r);
+        const unsigned long long items = items_of(a, z, r);
+        t.items += items;
+        t.cost += items * cost;
+        t.longest = max(t.longest, cost);
+        if (r > 1) t.parts += (unsigned long long)r * a.Hkv * z.rows * a.G;
+      }
+      atomicAdd(&totals[c].cost, t.cost);
+      atomicAdd(&totals[c].parts, t.parts);
+      atomicAdd(&totals[c].items, t.items);
+      atomicMax(&totals[c].longest, t.longest);
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int b = TR_LENGTHS - 1;                                   // (always has room)
+    int64_t least = INT64_MAX;
+    for (int c = 0; c < TR_LENGTHS; ++c) {
+      const int64_t e = tr_estimate(a, totals[c]);
+      if (e < least) {
+        least = e;
+        b = c;
+      }
+    }
+    best = b;
+  }
+  __syncthreads();
+  // ---- what lies before this request: rows, windows and partial rows by number, items by cost
+  const int32_t length = tr_length(best), ranges = ranges_of(s.steps, length), items = (int32_t)items_of(a, s, ranges), cost = s.steps ? item_cost(s, ranges) : 0;
+  {
+    unsigned long long v[5] = {0, 0, 0, 0, 0};
+    int32_t windows = 0;
+    for (int i = tid; i < a.B; i += 256) {
+      const TrSize z = size_of(a, a.ctx[i], a.n_nodes[i]);
+      const int32_t r = ranges_of(z.steps, length);
+      v[4] += z.rows;
+      windows += z.windows;
+      if (i < me) {
+        v[0] += z.rows;
+        v[1] += z.windows;
+        if (r > 1) v[3] += (unsigned long long)r * a.Hkv * z.rows * a.G;
+      }
+      if (z.steps) {
+        const int32_t k = item_cost(z, r);
+        if (k > cost || (k == cost && i < me)) v[2] += items_of(a, z, r);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+      if (v[k]) atomicAdd(&sums[k], v[k]);
+    if (windows) atomicAdd(&all_windows, windows);
+    if (tid == 0) all_items = (int32_t)totals[best].items;
+  }
+  __syncthreads();
+  const int64_t first = (int64_t)sums[0], windows0 = (int64_t)sums[1];
 
   // ---- what only this block looks at: parents and pages
   int32_t status = n < 0 || n > TR_NODES ? SYNERA_EINVAL : ctx < 0 ? SYNERA_ERANGE : SYNERA_OK;
   const int64_t keys = (int64_t)ctx + (status == SYNERA_OK ? n : 0);
-  if (status == SYNERA_OK && (first + s.rows > a.n_rows || (n > 0 && s.streams == 0))) status = SYNERA_ENOSPC;
+  if (status == SYNERA_OK && (first + s.rows > a.n_rows || (n > 0 && s.steps == 0))) status = SYNERA_ENOSPC;
   const bool fits = status == SYNERA_OK && n > 0;
   bool bad_parent = false, bad_page = false;
   int32_t up = -1;
@@ -259,22 +339,18 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     const int32_t page = ctx / SY_PAGE + w, from = max(ctx, page * SY_PAGE), to = min(ctx + n, (page + 1) * SY_PAGE);
     ShWindow x = {0, 0, 0, 0};
     if (live) x = ShWindow{row[page], (int32_t)first + from - ctx, from - page * SY_PAGE, to - page * SY_PAGE};
-    a.windows[v[1] + w] = x;
+    a.windows[windows0 + w] = x;
   }
-  // ---- the line
-  const int64_t work = (int64_t)s.streams * s.cost;
-  for (int64_t b = (v[2] + share - 1) / share + tid; b * share < v[2] + work; b += 256) {
-    const int64_t at = b * share - v[2];
-    a.start[b] = TrStart{me, (int32_t)(at / s.cost), (int32_t)(at % s.cost), 0};
-  }
+  // ---- the lists
+  for (int k = tid; k < items; k += 256) a.items[sums[2] + k] = TrItem{me, k};
   if (tid == 0) {
-    a.req[me] = TrReq{ctx, live ? n : 0, (int32_t)first, s.steps, s.cost, s.streams, s.tiles, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first))};
+    a.req[me] = TrReq{ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles,
+                      (int32_t)sums[3], {}};
     if (a.status) a.status[me] = status;
     if (me == 0) {
-      a.head->sh.n_tokens = (int32_t)min(v[3], a.n_rows);
+      a.head->sh.n_tokens = (int32_t)min((int64_t)sums[4], a.n_rows);
       a.head->sh.n_windows = all_windows;
-      a.head->n_blocks = (int32_t)((v[4] + share - 1) / share);
-      a.head->share = share;
+      a.head->items = all_items;
       a.head->B = a.B;
     }
   }
@@ -296,8 +372,8 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   const ShLimits& l = t->lim;
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
-  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->start, t->windows, t->pos, t->slot, t->parent, t->table,
-                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, l.slots, n_rows};
+  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->windows, t->pos, t->slot, t->parent, t->table,
+                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, l.slots, t->items_room, t->part_rows, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
   t->planned = true;
@@ -320,85 +396,63 @@ extern "C" int32_t synera_tree_append_rope(synera_tree* t, const synera_rope* ro
 struct TreeAttnArgs : SharedAttnArgs {
   const TrHead* th;
   const TrReq* req;
-  const TrStart* start;
+  const TrItem* places;
   const uint32_t* masks;
   int32_t pitch;
 };
 typedef SH_CONST_AS sh_i32x8v tr_i32x8;
-typedef SH_CONST_AS sh_i32x4v tr_i32x4;
+typedef SH_CONST_AS sh_i32x2v tr_i32x2;
 
 __device__ __forceinline__ TrReq req_of(const TreeAttnArgs& a, int r) {
   const sh_i32x8v w = *reinterpret_cast<const tr_i32x8*>((uintptr_t)(a.req + r));
-  return TrReq{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+  return TrReq{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], {}};
 }
-__device__ __forceinline__ TrStart start_of(const TreeAttnArgs& a, int b) {
-  const sh_i32x4v w = *reinterpret_cast<const tr_i32x4*>((uintptr_t)(a.start + b));
-  return TrStart{w[0], w[1], w[2], 0};
-}
-// Rows of tile `tile` of a request: its first one, and how many.
-__device__ __forceinline__ int tile_rows(const TreeAttnArgs& a, const TrReq& q, int tile) { return min(SY_SH_TILE_ROWS, q.n * a.G - tile * SY_SH_TILE_ROWS); }
 
 template <int HD>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int n_blocks = a.th->n_blocks, share = a.th->share, B = a.th->B;
-  // each XCD takes a run of the line, so that tiles of rows that read the same keys meet in its L2
-  const int per = (n_blocks + SY_SH_DEAL - 1) / SY_SH_DEAL, b = (int)(blockIdx.x % SY_SH_DEAL) * per + (int)(blockIdx.x / SY_SH_DEAL);
-  if ((int)(blockIdx.x / SY_SH_DEAL) >= per || b >= n_blocks) return;
-  const TrStart st = start_of(a, b);
-  int r = st.req, s = st.stream, k0 = st.step, left = share;
-  while (r < B) {
-    const TrReq q = req_of(a, r);
-    for (; left > 0 && s < q.streams; ++s, k0 = 0) {
-      const int len = min(q.cost - k0, left), end = min(k0 + len, q.steps);
-      left -= len;
-      if (k0 >= q.steps || q.n == 0) continue;
-      const int tile = s % q.tiles, keys = q.ctx + q.n;
-      const bool whole = k0 == 0 && end == q.steps;
-      ShItem it;
-      it.flags = SY_SH_LEAF | (q.tiles == 1 ? SY_SH_ONCE : 0);
-      it.kv_head = s / q.tiles;
-      it.n_rows = tile_rows(a, q, tile);
-      it.row0 = tile * SY_SH_TILE_ROWS;
-      it.tok = q.tok;
-      it.page = r * a.pitch;
-      it.n_pages = (keys + SY_PAGE - 1) / SY_PAGE;
-      it.key_begin = k0 * TR_STEP;
-      it.key_end = min(keys, end * TR_STEP);
-      it.lim0 = q.ctx;
-      it.part = whole ? -1 : (2 * b + (k0 > 0 ? 0 : 1)) * SY_SH_TILE_ROWS;
-      const int32_t* first = a.pages + it.page + it.key_begin / SY_PAGE;
-      if (it.n_rows <= 32) attend<HD, 1, 4, true>(a, it, first, lds);
-      else if (it.n_rows <= 64) attend<HD, 2, 2, true>(a, it, first, lds);
-      else attend<HD, 4, 1, true>(a, it, first, lds);
-      __syncthreads();                                        // the next item's copies come into the same LDS
-    }
-    if (left <= 0) return;
-    ++r;
-    s = 0;
-    k0 = 0;
+  const int x = blockIdx.x % SY_SH_DEAL, items = a.th->items;
+  for (int k = blockIdx.x / SY_SH_DEAL; k < items; k += gridDim.x / SY_SH_DEAL) {
+    const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(a.places + k));
+    const TrReq q = req_of(a, at[0]);
+    const int tile = at[1] % q.tiles, group = at[1] / q.tiles * SY_SH_DEAL + x, kh = group % a.Hkv, range = group / a.Hkv;
+    if (q.n == 0 || range >= q.ranges) continue;
+    const int rows = q.n * a.G, keys = q.ctx + q.n;
+    // (products of steps and ranges may pass 32 bits)
+    const int begin = (int)((uint64_t)q.steps * (uint32_t)range / (uint32_t)q.ranges), end = (int)((uint64_t)q.steps * (uint32_t)(range + 1) / (uint32_t)q.ranges);
+    ShItem it;
+    it.flags = SY_SH_LEAF | (q.tiles == 1 ? SY_SH_ONCE : 0);
+    it.kv_head = kh;
+    it.row0 = tile * SY_SH_TILE_ROWS;
+    it.n_rows = min(SY_SH_TILE_ROWS, rows - it.row0);
+    it.tok = q.tok;
+    it.page = at[0] * a.pitch;
+    it.n_pages = (keys + SY_PAGE - 1) / SY_PAGE;
+    it.key_begin = begin * TR_STEP;
+    it.key_end = min(keys, end * TR_STEP);
+    it.lim0 = q.ctx;
+    it.part = q.ranges == 1 ? -1 : q.part + group * rows + it.row0;
+    const int32_t* first = a.pages + it.page + it.key_begin / SY_PAGE;
+    if (it.n_rows <= 32) attend<HD, 1, 4, true>(a, it, first, lds);
+    else if (it.n_rows <= 64) attend<HD, 2, 2, true>(a, it, first, lds);
+    else attend<HD, 4, 1, true>(a, it, first, lds);
+    __syncthreads();                                          // the next item's copies come into the same LDS
   }
 }
 
-// Joins the parts of streams that are cut: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  Row b of the launch's blocks stands for the end of block
-// b's part of the line; those that cut one stream share its rows, so that a stream of many parts is joined by many blocks (one row of them for
-// each stream: 60 parts of 104 rows took 42 us).  A thread takes four values of a row.
-#define TR_JOIN 4
-struct TrJoin {                  // a stream that is cut
-  int count, first;              // its parts; the block that begins it
-  int tile, kh;
-};
-template <int HD, int FLY>        // FLY parts are asked for together
-__device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, const TrJoin& j, const int row, const int d4) {
+// Joins the ranges of the requests that have several: o = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A thread takes four values of a row; FLY ranges
+// are asked for together.
+template <int HD, int FLY>
+__device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, const int kh, const int row, const int d4) {
+  const int rows = q.n * a.G, step = a.Hkv * rows;
   float M = -3e38f, l = 0.f;
   float4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < j.count; s0 += FLY) {
+  for (int s0 = 0; s0 < q.ranges; s0 += FLY) {
     float2 ml[FLY];
     float4 v[FLY];
 #pragma unroll
     for (int s = 0; s < FLY; ++s) {
-      const int p = min(s0 + s, j.count - 1);
-      const size_t at = (size_t)(2 * (j.first + p) + (p == 0 ? 1 : 0)) * SY_SH_TILE_ROWS + row;
+      const size_t at = (size_t)q.part + (size_t)min(s0 + s, q.ranges - 1) * step + kh * rows + row;
       ml[s] = a.part_ml[at];
       v[s] = *reinterpret_cast<const float4*>(a.part_o + at * HD + d4);
     }
@@ -411,13 +465,13 @@ __device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, 
     sum.x *= f; sum.y *= f; sum.z *= f; sum.w *= f;
 #pragma unroll
     for (int s = 0; s < FLY; ++s)
-      if (s0 + s < j.count) {
+      if (s0 + s < q.ranges) {
         const float w = sh_ex2(ml[s].x - M);
         l += ml[s].y * w;
         sum.x += v[s].x * w; sum.y += v[s].y * w; sum.z += v[s].z * w; sum.w += v[s].w * w;
       }
   }
-  const int in_node = j.tile * SY_SH_TILE_ROWS + row, tok = q.tok + in_node / a.G, head = j.kh * a.G + in_node % a.G;
+  const int tok = q.tok + row / a.G, head = kh * a.G + row % a.G;
   const float inv = 1.0f / l;
   *reinterpret_cast<uint2*>(a.o + (int64_t)tok * a.o_ts + (int64_t)head * a.o_hs + d4) =
       make_uint2(pack_bf2(sum.x * inv, sum.y * inv), pack_bf2(sum.z * inv, sum.w * inv));
@@ -426,30 +480,26 @@ __device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, 
 
 template <int HD>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnArgs a) {
-  const int n_blocks = a.th->n_blocks, share = a.th->share, b = blockIdx.x;
-  if (b + 1 >= n_blocks) return;
-  const TrStart st = start_of(a, b + 1);
-  const TrReq q = req_of(a, st.req);
-  if (st.step <= 0 || st.step >= q.steps || q.n == 0) return;
-  const int before = (st.step + share - 1) / share, cuts = before + (q.steps - st.step + share - 1) / share - 1;
-  const TrJoin j = {cuts + 1, b + 1 - before, st.stream % q.tiles, st.stream / q.tiles};
-  const int n = tile_rows(a, q, j.tile) * (HD / 4);
-  for (int i = ((before - 1) * TR_JOIN + blockIdx.y) * 256 + threadIdx.x; i < n; i += cuts * TR_JOIN * 256) {
+  if ((int)blockIdx.x >= a.th->B) return;
+  const TrReq q = req_of(a, blockIdx.x);
+  if (q.ranges <= 1 || q.n == 0) return;
+  const int rows = q.n * a.G;
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < a.Hkv * rows * (HD / 4); i += gridDim.y * 256) {
     const int row = i / (HD / 4), d4 = i % (HD / 4) * 4;
-    if (j.count <= 2) join_row<HD, 2>(a, q, j, row, d4);
-    else if (j.count <= 4) join_row<HD, 4>(a, q, j, row, d4);
-    else join_row<HD, 8>(a, q, j, row, d4);
+    if (q.ranges <= 2) join_row<HD, 2>(a, q, row / rows, row % rows, d4);
+    else if (q.ranges <= 4) join_row<HD, 4>(a, q, row / rows, row % rows, d4);
+    else join_row<HD, 8>(a, q, row / rows, row % rows, d4);
   }
 }
 
 template <int HD>
 static constexpr size_t tree_lds() { return (size_t)20 * SY_PAGE * HD * 2; }
 template <int HD>
-static hipError_t launch_tree(const TreeAttnArgs& a, int grid, hipStream_t s) {
+static hipError_t launch_tree(const TreeAttnArgs& a, int grid, int B, hipStream_t s) {
   tree_attn_kernel<HD><<<grid, 256, tree_lds<HD>(), s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  tree_join_kernel<HD><<<dim3(grid, TR_JOIN), 256, 0, s>>>(a);
+  tree_join_kernel<HD><<<dim3(B, std::max(1, std::min(128, 1024 / B))), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 static hipError_t prepare_attention(int hd) {
@@ -463,7 +513,8 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   const ShLimits& l = t->lim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   TreeAttnArgs a = {};
-  const int32_t st = sh_attention_args(a, l, t->n_pages, t->n_rows, capturing(s), q, d_k_layer, d_v_layer, scale, d_lse);
+  const bool captured = capturing(s);
+  const int32_t st = sh_attention_args(a, l, t->n_pages, t->n_rows, captured, q, d_k_layer, d_v_layer, scale, d_lse);
   if (st != SYNERA_OK) return st == SH_NOTHING ? SYNERA_OK : st;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   a.pages = t->table;
@@ -471,10 +522,12 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.part_ml = t->part_ml;
   a.th = t->head;
   a.req = t->req;
-  a.start = t->start;
+  a.places = t->items;
   a.masks = t->masks;
   a.pitch = t->pitch;
-  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, t->grid, s) : launch_tree<64>(a, t->grid, s);
+  // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
+  const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL, B = captured ? l.max_batch : t->B;
+  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, B, s) : launch_tree<64>(a, grid, B, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
