@@ -26,7 +26,7 @@
 __host__ __device__ inline int32_t tr_length(int c) {         // steps: 2, 3, 4, 6, 8, 12, .. 2048, 3072 and any
   return c == TR_LENGTHS - 1 ? 1 << 30 : (2 + (c & 1)) << (c / 2);
 }
-// In 16ths of what a step takes a block when all places are taken and HBM is the bound (64 KB each: 6.8 us).
+// In 16ths of what a step takes a block when all places are taken and HBM is the bound (64 KB for each: 4.5 us).
 #define TR_ONE 16                // a step of a request's only tile
 #define TR_MORE 11               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
 #define TR_START 32              // what it takes to begin and end an item
@@ -181,7 +181,10 @@ struct TrTotals {
 };
 __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals& t) {
   if (t.items > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
-  return (int64_t)(t.cost / (unsigned)(a.slots / SY_SH_DEAL)) + t.longest / 2 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
+  // All places busy, or the longest item, which has three times the rate where few are: one request's range of 48 steps 104 us, 24 66.  The longest come first, so
+  // that little is left at the end: 256 requests of up to 64 steps uncut 277 us, cut to 24 301, to 12 323.
+  const int64_t busy = (int64_t)(t.cost / (unsigned)(a.slots / SY_SH_DEAL)), alone = (int64_t)t.longest * 3 / 8;
+  return max(busy, alone) + t.longest / 8 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
 }
 
 // Block i plans request i.  It looks at all requests by itself (a few thousand numbers at most, which lie in the caches), so that one launch
