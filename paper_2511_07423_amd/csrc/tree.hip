@@ -23,8 +23,10 @@
 // 32 requests of 48 .. 160 nodes 414 us, 64 of 8 .. 64 nodes 125.)
 #define TR_LENGTHS 24
 #define TR_GRID 4                // blocks of the launch for each place
-__host__ __device__ inline int32_t tr_length(int c) {         // steps: 2, 3, 4, 6, 8, 12, .. 2048, 3072 and any
-  return c == TR_LENGTHS - 1 ? 1 << 30 : (2 + (c & 1)) << (c / 2);
+// Candidate c: 2, 3, 4, 6, 8, 12, .. 2048, 3072 steps, and any.
+__device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
+  const int32_t x = (steps - 1) >> (c / 2);
+  return steps == 0 ? 0 : c == TR_LENGTHS - 1 ? 1 : (c & 1 ? x / 3 : x / 2) + 1;
 }
 // In 16ths of what a step takes a block when all places are taken and HBM is the bound (64 KB for each: 4.5 us).
 #define TR_ONE 16                // a step of a request's only tile
@@ -86,7 +88,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   if (n_q_heads < 1 || n_kv_heads < 1 || max_batch < 1 || max_tokens < 1 || max_pages < 1) return SYNERA_EINVAL;
   if ((head_dim != 64 && head_dim != 128) || n_q_heads % n_kv_heads || n_q_heads > 1024) return SYNERA_EUNSUP;
   if ((int64_t)max_tokens * n_q_heads >= (int64_t)1 << 30 || (int64_t)max_batch * ((int64_t)max_pages + TR_AHEAD) >= (int64_t)1 << 30) return SYNERA_EUNSUP;
-  if ((int64_t)max_batch * n_q_heads >= (int64_t)1 << 26) return SYNERA_EUNSUP;
+  if ((int64_t)max_batch * n_q_heads >= (int64_t)1 << 26 || max_batch > 1 << 20) return SYNERA_EUNSUP;
   int dev = 0;
   hipDeviceProp_t prop;
   if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess || prepare_attention(head_dim) != hipSuccess) {
@@ -148,7 +150,8 @@ struct PlanArgs {
   ShWindow* windows;
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
-  int32_t B, columns, pitch, n_pages, Hkv, G, slots, items_room, part_rows;
+  int32_t B, columns, pitch, n_pages, Hkv, G, items_room, part_rows;
+  double per_place;              // 1 / places of an XCD
   int64_t n_rows;
 };
 
@@ -167,12 +170,12 @@ __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_
   s.tiles = (n * a.G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
   return s;
 }
-__device__ __forceinline__ int32_t ranges_of(int32_t steps, int32_t length) { return steps == 0 ? 0 : (steps - 1) / length + 1; }
+// (A quotient in 32 bits of floating point: the same for every block, and no more than an estimate.)
 __device__ __forceinline__ int32_t item_cost(const TrSize& s, int32_t ranges) {
-  return ((s.steps + ranges - 1) / ranges) * (s.tiles > 1 ? TR_MORE : TR_ONE) + TR_START;
+  return (int32_t)((float)s.steps * (s.tiles > 1 ? TR_MORE : TR_ONE) * __builtin_amdgcn_rcpf((float)ranges)) + TR_START;
 }
-__device__ __forceinline__ int64_t items_of(const PlanArgs& a, const TrSize& s, int32_t ranges) {      // in each list
-  return ((int64_t)a.Hkv * ranges + SY_SH_DEAL - 1) / SY_SH_DEAL * s.tiles;
+__device__ __forceinline__ uint64_t items_of(const PlanArgs& a, const TrSize& s, int32_t ranges) {      // in each list
+  return ((uint64_t)a.Hkv * (uint32_t)ranges + SY_SH_DEAL - 1) / SY_SH_DEAL * (uint32_t)s.tiles;
 }
 // What each candidate comes to, over all requests; whole numbers, so that every block finds the same.
 struct TrTotals {
@@ -183,8 +186,22 @@ __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals
   if (t.items > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
   // All places busy, or the longest item, which has three times the rate where few are: one request's range of 48 steps 104 us, 24 66.  The longest come first, so
   // that little is left at the end: 256 requests of up to 64 steps uncut 277 us, cut to 24 301, to 12 323.
-  const int64_t busy = (int64_t)(t.cost / (unsigned)(a.slots / SY_SH_DEAL)), alone = (int64_t)t.longest * 3 / 8;
+  const int64_t busy = (int64_t)((double)t.cost * a.per_place), alone = (int64_t)t.longest * 3 / 8;
   return max(busy, alone) + t.longest / 8 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
+}
+
+// The sum over the block's threads, for all of them.
+template <int N>
+__device__ __forceinline__ void block_sums(int32_t (&v)[N], int32_t (*parts)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    for (int o = 1; o < 64; o <<= 1) v[k] += __shfl_xor(v[k], o);
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) parts[threadIdx.x >> 6][k] = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = parts[0][k] + parts[1][k] + parts[2][k] + parts[3][k];
 }
 
 // Block i plans request i.  It looks at all requests by itself (a few thousand numbers at most, which lie in the caches), so that one launch
@@ -194,82 +211,29 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   const int tid = threadIdx.x, me = blockIdx.x;
   __shared__ TrTotals totals[TR_LENGTHS];
   __shared__ TrSize sizes[256];
-  __shared__ int32_t best;
-  __shared__ unsigned long long sums[5];                      // rows, windows, items and partial rows before this request; rows of all
-  __shared__ int32_t all_windows, all_items;
+  __shared__ unsigned long long best;                         // estimate << 8 | candidate
+  __shared__ int32_t sums_a[4][4], sums_b[4][2];
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
   if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0};
-  if (tid < 5) sums[tid] = 0;
-  if (tid == 0) all_windows = all_items = 0;
+  if (tid == 0) best = ~0ull;
   const int32_t ctx = a.ctx[me], n = a.n_nodes[me];
   const TrSize s = size_of(a, ctx, n);
-  // ---- how long a range may be
-  for (int i0 = 0; i0 < a.B; i0 += 256) {
-    __syncthreads();
-    if (i0 + tid < a.B) sizes[tid] = size_of(a, a.ctx[i0 + tid], a.n_nodes[i0 + tid]);
-    __syncthreads();
-    const int c = tid / LANES, m = min(256, a.B - i0);
-    if (c < TR_LENGTHS) {
-      TrTotals t = {0, 0, 0, 0};
-      for (int i = tid % LANES; i < m; i += LANES) {
-        const TrSize z = sizes[i];
-        if (z.steps == 0) continue;
-        const int32_t r = ranges_of(z.steps, tr_length(c)), cost = item_cost(z, r);
-        const unsigned long long items = items_of(a, z, r);
-        t.items += items;
-        t.cost += items * cost;
-        t.longest = max(t.longest, cost);
-        if (r > 1) t.parts += (unsigned long long)r * a.Hkv * z.rows * a.G;
-      }
-      atomicAdd(&totals[c].cost, t.cost);
-      atomicAdd(&totals[c].parts, t.parts);
-      atomicAdd(&totals[c].items, t.items);
-      atomicMax(&totals[c].longest, t.longest);
+  const bool few = a.B <= 256;                                // all sizes are in LDS
+  // ---- rows and windows before this request, and of all
+  int32_t rows[4] = {0, 0, 0, 0};
+  for (int i = tid; i < a.B; i += 256) {
+    const TrSize z = size_of(a, a.ctx[i], a.n_nodes[i]);
+    if (few) sizes[i] = z;
+    if (i < me) {
+      rows[0] += z.rows;
+      rows[1] += z.windows;
     }
+    rows[2] += z.rows;
+    rows[3] += z.windows;
   }
-  __syncthreads();
-  if (tid == 0) {
-    int b = TR_LENGTHS - 1;                                   // (always has room)
-    int64_t least = INT64_MAX;
-    for (int c = 0; c < TR_LENGTHS; ++c) {
-      const int64_t e = tr_estimate(a, totals[c]);
-      if (e < least) {
-        least = e;
-        b = c;
-      }
-    }
-    best = b;
-  }
-  __syncthreads();
-  // ---- what lies before this request: rows, windows and partial rows by number, items by cost
-  const int32_t length = tr_length(best), ranges = ranges_of(s.steps, length), items = (int32_t)items_of(a, s, ranges), cost = s.steps ? item_cost(s, ranges) : 0;
-  {
-    unsigned long long v[5] = {0, 0, 0, 0, 0};
-    int32_t windows = 0;
-    for (int i = tid; i < a.B; i += 256) {
-      const TrSize z = size_of(a, a.ctx[i], a.n_nodes[i]);
-      const int32_t r = ranges_of(z.steps, length);
-      v[4] += z.rows;
-      windows += z.windows;
-      if (i < me) {
-        v[0] += z.rows;
-        v[1] += z.windows;
-        if (r > 1) v[3] += (unsigned long long)r * a.Hkv * z.rows * a.G;
-      }
-      if (z.steps) {
-        const int32_t k = item_cost(z, r);
-        if (k > cost || (k == cost && i < me)) v[2] += items_of(a, z, r);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 5; ++k)
-      if (v[k]) atomicAdd(&sums[k], v[k]);
-    if (windows) atomicAdd(&all_windows, windows);
-    if (tid == 0) all_items = (int32_t)totals[best].items;
-  }
-  __syncthreads();
-  const int64_t first = (int64_t)sums[0], windows0 = (int64_t)sums[1];
+  block_sums(rows, sums_a);
+  const int64_t first = rows[0];
 
   // ---- what only this block looks at: parents and pages
   int32_t status = n < 0 || n > TR_NODES ? SYNERA_EINVAL : ctx < 0 ? SYNERA_ERANGE : SYNERA_OK;
@@ -278,11 +242,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   const bool fits = status == SYNERA_OK && n > 0;
   bool bad_parent = false, bad_page = false;
   int32_t up = -1;
-  if (fits && tid < n) {
-    up = a.parent[first + tid];
-    bad_parent = up < -1 || up >= tid;
-    if (bad_parent) up = -1;
-  }
+  if (fits && tid < n) up = a.parent[first + tid];
   const int32_t need = fits ? (int32_t)((keys + SY_PAGE - 1) / SY_PAGE) : 0;
   const int32_t* row = a.table + (size_t)me * a.columns;
   int32_t* copy = a.pages + (size_t)me * a.pitch;
@@ -292,10 +252,59 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     bad_page |= id < 0 || id >= a.n_pages;
     copy[c] = id;
   }
-  const int any = __syncthreads_or((bad_parent ? 1 : 0) | (bad_page ? 2 : 0));
-  const int parent_bad = __syncthreads_or(bad_parent);
+  const int32_t parent = up;
+  bad_parent = up < -1 || up >= tid;
+  if (bad_parent) up = -1;
+  bad_parent &= fits && tid < n;
+
+  // ---- how long a range may be
+  for (int i0 = 0; i0 < a.B; i0 += 256) {
+    if (!few) {
+      __syncthreads();
+      if (i0 + tid < a.B) sizes[tid] = size_of(a, a.ctx[i0 + tid], a.n_nodes[i0 + tid]);
+      __syncthreads();
+    }
+    const int c = tid / LANES, m = min(256, a.B - i0);
+    if (c < TR_LENGTHS) {
+      TrTotals t = {0, 0, 0, 0};
+      for (int i = tid % LANES; i < m; i += LANES) {
+        const TrSize z = sizes[i];
+        if (z.steps == 0) continue;
+        const int32_t r = tr_ranges(z.steps, c), cost = item_cost(z, r);
+        const uint64_t items = items_of(a, z, r);
+        t.items += items;
+        t.cost += items * (uint32_t)cost;
+        t.longest = max(t.longest, cost);
+        if (r > 1) t.parts += (uint64_t)(uint32_t)r * (uint32_t)(a.Hkv * a.G * z.rows);
+      }
+      if (t.items) {
+        atomicAdd(&totals[c].cost, t.cost);
+        atomicAdd(&totals[c].parts, t.parts);
+        atomicAdd(&totals[c].items, t.items);
+        atomicMax(&totals[c].longest, t.longest);
+      }
+    }
+  }
+  const int any = __syncthreads_or(bad_parent || bad_page), parent_bad = __syncthreads_or(bad_parent);
   if (any) status = parent_bad ? SYNERA_EINVAL : SYNERA_ERANGE;
   const bool live = fits && !any;
+  if (tid < TR_LENGTHS) {
+    const int64_t e = tr_estimate(a, totals[tid]);
+    if (e < INT64_MAX) atomicMin(&best, (unsigned long long)e << 8 | (unsigned)tid);      // (the last candidate always has room)
+  }
+  __syncthreads();
+  const int chosen = (int)(best & 255);
+  // ---- partial rows before this request by number, items by cost
+  const int32_t ranges = tr_ranges(s.steps, chosen), items = s.steps ? (int32_t)items_of(a, s, ranges) : 0, cost = s.steps ? item_cost(s, ranges) : 0;
+  int32_t before[2] = {0, 0};
+  for (int i = tid; i < a.B; i += 256) {
+    const TrSize z = few ? sizes[i] : size_of(a, a.ctx[i], a.n_nodes[i]);
+    if (z.steps == 0) continue;
+    const int32_t r = tr_ranges(z.steps, chosen), k = item_cost(z, r);
+    if (i < me && r > 1) before[0] += r * a.Hkv * z.rows * a.G;
+    if (k > cost || (k == cost && i < me)) before[1] += (int32_t)items_of(a, z, r);
+  }
+  block_sums(before, sums_b);
 
   // ---- paths
   uint32_t word[8];
@@ -326,7 +335,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
       const int32_t p = ctx + tid;
       a.pos[at] = ctx + depth;
       a.slot[at] = row[p / SY_PAGE] * SY_PAGE + p % SY_PAGE;
-      a.parents[at] = a.parent[at];
+      a.parents[at] = parent;
       uint32_t* m = a.masks + at * SY_TREE_MASK;
       m[0] = m[1] = 0xFFFFFFFFu;
 #pragma unroll
@@ -342,18 +351,18 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     const int32_t page = ctx / SY_PAGE + w, from = max(ctx, page * SY_PAGE), to = min(ctx + n, (page + 1) * SY_PAGE);
     ShWindow x = {0, 0, 0, 0};
     if (live) x = ShWindow{row[page], (int32_t)first + from - ctx, from - page * SY_PAGE, to - page * SY_PAGE};
-    a.windows[windows0 + w] = x;
+    a.windows[rows[1] + w] = x;
   }
   // ---- the lists
-  for (int k = tid; k < items; k += 256) a.items[sums[2] + k] = TrItem{me, k};
+  for (int k = tid; k < items; k += 256) a.items[before[1] + k] = TrItem{me, k};
   if (tid == 0) {
     a.req[me] = TrReq{ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles,
-                      (int32_t)sums[3], {}};
+                      before[0], {}};
     if (a.status) a.status[me] = status;
     if (me == 0) {
-      a.head->sh.n_tokens = (int32_t)min((int64_t)sums[4], a.n_rows);
-      a.head->sh.n_windows = all_windows;
-      a.head->items = all_items;
+      a.head->sh.n_tokens = (int32_t)min((int64_t)rows[2], a.n_rows);
+      a.head->sh.n_windows = rows[3];
+      a.head->items = (int32_t)totals[chosen].items;
       a.head->B = a.B;
     }
   }
@@ -376,7 +385,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->windows, t->pos, t->slot, t->parent, t->table,
-                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, l.slots, t->items_room, t->part_rows, n_rows};
+                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, (double)SY_SH_DEAL / l.slots, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
   t->planned = true;
