@@ -308,8 +308,9 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
     }
   };
   for (int64_t j0 = blockIdx.z, step = (int64_t)a.splits * most; j0 < rows; j0 += step) {
+    // (the next rows are asked for before these are written where a row is few registers: in 32 bits that takes a block of three off each compute unit)
     Rows next;
-    if (j0 + step < rows) load(next, j0 + step, most);
+    if (VEC == 8 && j0 + step < rows) load(next, j0 + step, most);
     if (added_paths) {
       if (tid == 0) path(j0, 1u);
       __syncthreads();
@@ -319,7 +320,8 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
       __syncthreads();
       if (tid == 0) path(j0, ~0u);
     }
-    now = next;
+    if (VEC == 8) now = next;
+    else if (j0 + step < rows) load(now, j0 + step, most);
   }
 }
 

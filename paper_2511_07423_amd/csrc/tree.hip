@@ -54,7 +54,7 @@ struct synera_tree {
   ShLimits lim;                  // (head counts and sizes; no room of a host plan)
   int device;
   bool planned;
-  int32_t B, n_pages;
+  int32_t B, n_pages, columns;
   int64_t n_rows;
   int32_t pitch;                 // columns of the table's copy
   char* dev;
@@ -392,6 +392,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   t->B = B;
   t->n_rows = n_rows;
   t->n_pages = n_pages_in_pool;
+  t->columns = columns;
   return SYNERA_OK;
 }
 
@@ -507,10 +508,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnArgs a) {
 template <int HD>
 static constexpr size_t tree_lds() { return (size_t)20 * SY_PAGE * HD * 2; }
 template <int HD>
-static hipError_t launch_tree(const TreeAttnArgs& a, int grid, int B, hipStream_t s) {
+static hipError_t launch_tree(const TreeAttnArgs& a, int grid, int B, bool cuts, hipStream_t s) {
   tree_attn_kernel<HD><<<grid, 256, tree_lds<HD>(), s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || !cuts) return e;
   tree_join_kernel<HD><<<dim3(B, std::max(1, std::min(128, 1024 / B))), 256, 0, s>>>(a);
   return hipGetLastError();
 }
@@ -539,7 +540,8 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.pitch = t->pitch;
   // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
   const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL, B = captured ? l.max_batch : t->B;
-  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, B, s) : launch_tree<64>(a, grid, B, s);
+  const bool cuts = (captured ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
+  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, B, cuts, s) : launch_tree<64>(a, grid, B, cuts, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
