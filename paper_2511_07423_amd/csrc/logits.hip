@@ -13,14 +13,14 @@
 // are formed on the way.  (Nearly every wavefront meets some: with a branch for each value 2048 x 128256 masked took 325 us; formed behind the
 // others, from memory, 300; this way 198, as long as a plain copy of the logits.)
 // Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Longer ones are
-// added to the words before a row and taken away behind it.
+// added to the words before a row, and taken away where the next row is not behind it.
 #define LG_SLICE 8192
 #define LG_THREADS 512
 #define LG_PROMPT (1u << 20)
 #define LG_SEEN (2 * LG_PROMPT - 1)
 #define LG_PATH (1u << 21)
 #define LG_BIAS 22
-#define LG_MOST_STEPS 65536      // of a path
+#define LG_MOST_ROWS (1 << 19)   // of calls with paths: counts stay below 2^20
 #define LG_NODES 256
 #define LG_MOST_BIASES 1022
 #define LG_EARLY 4               // tokens of the history that a thread asks for together
@@ -294,32 +294,36 @@ __global__ __launch_bounds__(LG_THREADS) void logits_kernel(LogitsArgs a) {
         y.template store<false>(out_of(j) + e);
       }
   };
-  auto path = [&](int64_t j, uint32_t by) {                   // a long path, into the words and out of them
-    int64_t at = j;
-    for (int k = 0; k < LG_MOST_STEPS; ++k) {
-      const uint32_t t = (uint32_t)(a.d.d_tokens[first + at] - v0);
-      if (t < (uint32_t)n) {
-        word[t] += by;
-        has_word[t / 32] |= 1u << (t % 32);
-      }
-      const int32_t up = a.d.d_parent[first + at];
-      if (up < 0 || up >= at) break;
-      at = up;
+  // Long paths, by one thread: the words hold that of node `held`.  If it is an ancestor of the next row, only what lies between is added.
+  int64_t held = -1;
+  auto add = [&](int64_t at, uint32_t by) {
+    const uint32_t t = slot(a.d.d_tokens[first + at]);
+    if (t < (uint32_t)n) {
+      word[t] += by;
+      has_word[t / 32] |= 1u << (t % 32);
     }
+    const int32_t up = a.d.d_parent[first + at];
+    return up >= 0 && up < at ? (int64_t)up : (int64_t)-1;
+  };
+  auto hold = [&](int64_t j) {
+    int64_t at = j;
+    while (at > held) at = add(at, 1u);
+    if (at != held) {
+      for (int64_t old = held; old >= 0;) old = add(old, ~0u);
+      while (at >= 0) at = add(at, 1u);
+    }
+    held = j;
   };
   for (int64_t j0 = blockIdx.z, step = (int64_t)a.splits * most; j0 < rows; j0 += step) {
     // (the next rows are asked for before these are written where a row is few registers: in 32 bits that takes a block of three off each compute unit)
     Rows next;
     if (VEC == 8 && j0 + step < rows) load(next, j0 + step, most);
     if (added_paths) {
-      if (tid == 0) path(j0, 1u);
+      __syncthreads();
+      if (tid == 0) hold(j0);
       __syncthreads();
     }
     finish(now, j0);
-    if (added_paths) {
-      __syncthreads();
-      if (tid == 0) path(j0, ~0u);
-    }
     if (VEC == 8) now = next;
     else if (j0 + step < rows) load(now, j0 + step, most);
   }
@@ -347,6 +351,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if ((!d.d_tokens) != (!d.d_parent) || (d.d_tokens && !d.d_cu)) return SYNERA_EINVAL;
   if ((d.d_history && !d.d_history_len) || (!d.d_bias_id) != (!d.d_bias)) return SYNERA_EINVAL;
   if (d.vocab > (int64_t)1 << 30 || d.bias_columns > LG_MOST_BIASES || d.history_columns >= 1 << 19 || d.B > 65535 || d.rows >= (int64_t)1 << 31) return SYNERA_EUNSUP;
+  if (d.d_tokens && d.rows > LG_MOST_ROWS) return SYNERA_EUNSUP;
   if (d.rows == 0 || d.B == 0) return SYNERA_OK;
   if (!d_in || !d_out || (d.rows > 1 && (d.in_stride < d.vocab || d.out_stride < d.vocab))) return SYNERA_EINVAL;
   const int size = d.dtype == 0 ? 4 : 2;

@@ -192,6 +192,14 @@ extern "C" int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, cons
     bits |= reinterpret_cast<uintptr_t>(p);
   if (bits % 4) return SYNERA_EINVAL;
   if (n_pages >= 1 << 27 || (int64_t)B * columns >= (int64_t)1 << 27) return SYNERA_EUNSUP;
+  // what is written lies on nothing else
+  const struct { const void* p; int64_t n; } all[11] = {{d_table, (int64_t)B * columns}, {d_held, B}, {d_free, n_pages}, {d_n_free, 1}, {d_cu, (int64_t)B + 1},
+                                                        {d_pos, n_rows}, {d_slot, n_rows}, {d_status, B}, {d_ctx_len, B}, {d_n_new, B}, {d_shared, B}};
+  for (int i = 0; i < 8; ++i)
+    for (int k = i + 1; k < 11; ++k) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(all[i].p), y = reinterpret_cast<uintptr_t>(all[k].p);
+      if (x && y && x < y + 4 * (uintptr_t)all[k].n && y < x + 4 * (uintptr_t)all[i].n) return SYNERA_EINVAL;
+    }
   const PagesArgs a = {d_ctx_len, d_n_new, d_shared, d_table, d_held, d_free, d_n_free, d_cu, d_pos, d_slot, d_status, n_rows, B, columns, n_pages};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (n_rows > 0 && n_rows <= PG_ROWS && B <= PG_THREADS) {

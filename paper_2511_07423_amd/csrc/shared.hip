@@ -214,6 +214,7 @@ struct AppendArgs {
   int32_t n, hd;               // n = Hkv hd
   int32_t v_blocks;            // the first blocks take values, the others heads (append_rows)
   int32_t v_pairs;             // whether two values of v can be loaded together
+  int32_t most;                // tokens that the tensors of this call have room for
 };
 
 template <typename TI>
@@ -234,7 +235,8 @@ __device__ __forceinline__ uint32_t value_pair(const TI* v, bool pairs) {    // 
 }
 
 template <typename TI, int ONCE>
-__device__ __forceinline__ void append_values(const AppendArgs& a, const ShWindow w, const int e0, uint32_t* turn) {
+__device__ __forceinline__ void append_values(const AppendArgs& a, ShWindow w, const int e0, uint32_t* turn) {
+  w.s1 = w.s0 + min(w.s1 - w.s0, a.most - w.row);
   if (w.s1 <= w.s0) return;
   const int lane = threadIdx.x & 63, e = e0 + 2 * lane;
   const bool on = e < a.n;
@@ -298,7 +300,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const TurnCols 
     for (uint32_t i = blockIdx.x * 4 + wave; i < items; i += (uint32_t)a.v_blocks * 4)
       append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
   } else {
-    const uint32_t items = (uint32_t)a.head->n_tokens * (uint32_t)cols.n;
+    const uint32_t items = (uint32_t)min(a.head->n_tokens, a.most) * (uint32_t)cols.n;
     for (uint32_t i = (blockIdx.x - a.v_blocks) * 4 + wave; i < items; i += (gridDim.x - a.v_blocks) * 4)
       turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i);
   }
@@ -311,7 +313,7 @@ template <typename TI, int VEC, int ONCE>
 __device__ __forceinline__ void append_listed(const AppendArgs& a, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t slabs = (uint32_t)(a.n + 127) / 128, values = (uint32_t)a.head->n_windows * slabs;
-  const uint32_t all = values + (uint32_t)a.head->n_tokens * (uint32_t)cols.n;
+  const uint32_t all = values + (uint32_t)min(a.head->n_tokens, a.most) * (uint32_t)cols.n;
   for (uint32_t i = blockIdx.x * 4 + wave; i < all; i += gridDim.x * 4) {
     if (i < values) append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
     else turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i - values);
@@ -323,9 +325,9 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
   if constexpr (PLAN == PLAN_KNOWN) {
     append_rows<TI, VEC, ONCE>(a, a.turn.cols, turn);
   } else if constexpr (PLAN == PLAN_KEPT) {
-    append_rows<TI, VEC, ONCE>(a, turn_cols(a.turn.groups, a.head->n_tokens), turn);
+    append_rows<TI, VEC, ONCE>(a, turn_cols(a.turn.groups, min(a.head->n_tokens, a.most)), turn);
   } else {
-    const int32_t T = a.head->n_tokens;
+    const int32_t T = min(a.head->n_tokens, a.most);
     const TurnCols cols = turn_cols(a.turn.groups, T);
     const int32_t once = turn_once(VEC, (T * a.turn.token_bytes) >> 20, true);
     if (once == TURN_ONCE_BOTH) append_listed<TI, VEC, TURN_ONCE_BOTH>(a, cols, turn);
@@ -404,6 +406,9 @@ int32_t sh_append(const ShTarget& b, const synera_rope* rope, int32_t dtype, con
   a.turn.q.tail = a.turn.k.tail = 1;
   if (dtype == 1 && q && q->d_in == q->d_out && !q->d_gain) a.turn.q.tail = 0;
   a.head = b.head;
+  a.most = INT32_MAX;
+  for (const synera_heads* h : {q, k, v})
+    if (h && h->n_rows) a.most = std::min(a.most, h->n_rows);
   a.windows = b.windows;
   a.v = v->d_in;
   a.v_ts = v->in_token;

@@ -54,6 +54,7 @@ struct synera_tree {
   ShLimits lim;                  // (head counts and sizes; no room of a host plan)
   int device;
   bool planned;
+  bool replays;                  // a plan was captured: the one on the device may be another than the last one that was called
   int32_t B, n_pages, columns;
   int64_t n_rows;
   int32_t pitch;                 // columns of the table's copy
@@ -368,6 +369,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   }
 }
 
+static Range ints(const int32_t* p, int64_t n) { return {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (p ? 4 * (uintptr_t)n : 0)}; }
 static bool off4(std::initializer_list<const void*> all) {
   uintptr_t bits = 0;
   for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
@@ -380,6 +382,8 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   if (!t || !d_ctx_len || !d_n_nodes || !d_table || B < 1 || n_rows < 0 || columns < 1 || n_pages_in_pool < 1) return SYNERA_EINVAL;
   if (n_rows > 0 && !d_parent) return SYNERA_EINVAL;
   if (off4({d_ctx_len, d_n_nodes, d_parent, d_table, d_status})) return SYNERA_EINVAL;
+  for (const Range& in : {ints(d_ctx_len, B), ints(d_n_nodes, B), ints(d_parent, n_rows), ints(d_table, (int64_t)B * columns)})
+    if (meet(ints(d_status, B), in)) return SYNERA_EINVAL;
   if (n_pages_in_pool >= 1 << 27) return SYNERA_EUNSUP;
   const ShLimits& l = t->lim;
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
@@ -389,6 +393,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
   t->planned = true;
+  t->replays = t->replays || capturing(static_cast<hipStream_t>(stream));
   t->B = B;
   t->n_rows = n_rows;
   t->n_pages = n_pages_in_pool;
@@ -412,6 +417,7 @@ struct TreeAttnArgs : SharedAttnArgs {
   const TrItem* places;
   const uint32_t* masks;
   int32_t pitch;
+  int32_t rows;                  // that the tensors of this call have: a plan that was replayed may have more
 };
 typedef SH_CONST_AS sh_i32x8v tr_i32x8;
 typedef SH_CONST_AS sh_i32x2v tr_i32x2;
@@ -429,7 +435,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a) {
     const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(a.places + k));
     const TrReq q = req_of(a, at[0]);
     const int tile = at[1] % q.tiles, group = at[1] / q.tiles * SY_SH_DEAL + x, kh = group % a.Hkv, range = group / a.Hkv;
-    if (q.n == 0 || range >= q.ranges) continue;
+    if (q.n == 0 || range >= q.ranges || q.tok + q.n > a.rows) continue;
     const int rows = q.n * a.G, keys = q.ctx + q.n;
     // (products of steps and ranges may pass 32 bits)
     const int begin = (int)((uint64_t)q.steps * (uint32_t)range / (uint32_t)q.ranges), end = (int)((uint64_t)q.steps * (uint32_t)(range + 1) / (uint32_t)q.ranges);
@@ -493,15 +499,17 @@ __device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, 
 
 template <int HD>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnArgs a) {
-  if ((int)blockIdx.x >= a.th->B) return;
-  const TrReq q = req_of(a, blockIdx.x);
-  if (q.ranges <= 1 || q.n == 0) return;
-  const int rows = q.n * a.G;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < a.Hkv * rows * (HD / 4); i += gridDim.y * 256) {
-    const int row = i / (HD / 4), d4 = i % (HD / 4) * 4;
-    if (q.ranges <= 2) join_row<HD, 2>(a, q, row / rows, row % rows, d4);
-    else if (q.ranges <= 4) join_row<HD, 4>(a, q, row / rows, row % rows, d4);
-    else join_row<HD, 8>(a, q, row / rows, row % rows, d4);
+  const int B = a.th->B;
+  for (int r = blockIdx.x; r < B; r += gridDim.x) {
+    const TrReq q = req_of(a, r);
+    if (q.ranges <= 1 || q.n == 0 || q.tok + q.n > a.rows) continue;
+    const int rows = q.n * a.G;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < a.Hkv * rows * (HD / 4); i += gridDim.y * 256) {
+      const int row = i / (HD / 4), d4 = i % (HD / 4) * 4;
+      if (q.ranges <= 2) join_row<HD, 2>(a, q, row / rows, row % rows, d4);
+      else if (q.ranges <= 4) join_row<HD, 4>(a, q, row / rows, row % rows, d4);
+      else join_row<HD, 8>(a, q, row / rows, row % rows, d4);
+    }
   }
 }
 
@@ -538,9 +546,10 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.places = t->items;
   a.masks = t->masks;
   a.pitch = t->pitch;
+  a.rows = q->n_rows ? q->n_rows : INT32_MAX;
   // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
   const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL, B = captured ? l.max_batch : t->B;
-  const bool cuts = (captured ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
+  const bool cuts = (captured || t->replays ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
   const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, B, cuts, s) : launch_tree<64>(a, grid, B, cuts, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
@@ -554,12 +563,16 @@ struct AcceptArgs {
   const TrReq* req;
   const int32_t *parent, *tokens, *target, *anchor, *n_given;
   int32_t *accept_len, *token, *path, *n_path;
+  const TrHead* head;
+  int32_t rows;                  // that the arrays of this call have
 };
 // A wavefront walks a request's tree.  Lane l holds nodes l, l + 64, ..; a step asks all of them at once which hang on the node at hand
 // with the wanted token, and the first one is the next.  Bound by latency: a few loads, then some 30 cycles a step.
 __global__ __launch_bounds__(64) void tree_accept_kernel(AcceptArgs a) {
   const int i = blockIdx.x, lane = threadIdx.x;
-  const TrReq q = a.req[i];
+  if (i >= a.head->B) return;                                 // (a plan that was replayed may have fewer requests, or more rows, than the call)
+  TrReq q = a.req[i];
+  if (q.tok + q.rows > a.rows) q.n = q.rows = 0;
   int32_t parent[4], token[4], target[4];
   int mine[4];                                                // the node's place on the path
 #pragma unroll
@@ -619,14 +632,14 @@ extern "C" int32_t synera_tree_accept(synera_tree* t, int64_t n_rows, const int3
   if (off4({d_tokens, d_target, d_anchor, d_n_given, d_accept_len, d_token, d_path, d_n_path})) return SYNERA_EINVAL;
   // no output on an input or on another one
   const int64_t B = t->B, T = t->n_rows;
-  auto range = [](const int32_t* p, int64_t n) { return Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (p ? 4 * n : 0)}; };
-  const Range outs[4] = {range(d_accept_len, B), range(d_token, B), range(d_path, T), range(d_n_path, B)};
-  const Range ins[4] = {range(d_tokens, T), range(d_target, T), range(d_anchor, B), range(d_n_given, B)};
+  const Range outs[4] = {ints(d_accept_len, B), ints(d_token, B), ints(d_path, T), ints(d_n_path, B)};
+  const Range ins[4] = {ints(d_tokens, T), ints(d_target, T), ints(d_anchor, B), ints(d_n_given, B)};
   for (int i = 0; i < 4; ++i)
     for (int k = 0; k < 4; ++k)
       if (meet(outs[i], ins[k]) || (i != k && meet(outs[i], outs[k]))) return SYNERA_EINVAL;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
-  const AcceptArgs a = {t->req, t->parent, d_tokens, d_target, d_anchor, d_n_given, d_accept_len, d_token, d_path, d_n_path};
+  const AcceptArgs a = {t->req, t->parent, d_tokens, d_target, d_anchor, d_n_given, d_accept_len, d_token, d_path, d_n_path, t->head,
+                        (int32_t)std::min<int64_t>(n_rows, INT32_MAX)};
   tree_accept_kernel<<<t->B, 64, 0, static_cast<hipStream_t>(stream)>>>(a);
   return hipGetLastError() == hipSuccess ? SYNERA_OK : SYNERA_EHIP;
 }
@@ -639,6 +652,8 @@ struct CommitArgs {
   int64_t layer_stride;
   int32_t n, hd;                 // n = Hkv hd
   int32_t k_parts;               // of a layer's blocks, those that move keys; the others move values
+  const TrHead* head;
+  int32_t rows;                  // that the arrays of this call have
 };
 // A block moves a part of one layer's values, or keys, of one request.  A thread keeps to its own 16 bytes of a key, or its own dim of the
 // values, and takes the path in order: node k's place was read, if at all, by one before it, since path[k] >= k.  A batch's loads are on their way
@@ -647,8 +662,9 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
   constexpr int FLY = 8;
   __shared__ int32_t from[TR_NODES], to[TR_NODES], in_wave[4];
   const int tid = threadIdx.x, wave = tid >> 6, i = blockIdx.x;
+  if (i >= a.head->B) return;
   const TrReq q = a.req[i];
-  const int n = min(a.n_path[i], q.n);
+  const int n = q.tok + q.n > a.rows ? 0 : min(a.n_path[i], q.n);
   int p = -1;
   if (tid < n) p = a.path[q.tok + tid];
   const bool moves = p > tid && p < q.n;
@@ -708,10 +724,13 @@ extern "C" int32_t synera_tree_commit(synera_tree* t, int64_t n_rows, const int3
   const Range k = {reinterpret_cast<uintptr_t>(d_k_pool), reinterpret_cast<uintptr_t>(d_k_pool) + 2 * (uintptr_t)all};
   const Range v = {reinterpret_cast<uintptr_t>(d_v_pool), reinterpret_cast<uintptr_t>(d_v_pool) + 2 * (uintptr_t)all};
   if (meet(k, v)) return SYNERA_EINVAL;
+  for (const Range& in : {ints(d_path, n_rows), ints(d_n_path, t->B)})
+    if (meet(k, in) || meet(v, in)) return SYNERA_EINVAL;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   if (t->n_rows == 0 && !capturing(static_cast<hipStream_t>(stream))) return SYNERA_OK;
   const int32_t n = l.Hkv * l.hd;
-  CommitArgs a = {t->req, t->slot, d_path, d_n_path, static_cast<bf16_t*>(d_k_pool), static_cast<bf16_t*>(d_v_pool), layer_stride, n, l.hd, (n / 8 + 255) / 256};
+  CommitArgs a = {t->req, t->slot, d_path, d_n_path, static_cast<bf16_t*>(d_k_pool), static_cast<bf16_t*>(d_v_pool), layer_stride, n, l.hd, (n / 8 + 255) / 256, t->head,
+                  (int32_t)std::min<int64_t>(n_rows, INT32_MAX)};
   tree_commit_kernel<<<dim3(t->B, n_layers, a.k_parts + (n + 255) / 256), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return hipGetLastError() == hipSuccess ? SYNERA_OK : SYNERA_EHIP;
 }

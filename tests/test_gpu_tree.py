@@ -207,6 +207,89 @@ def test_attention_one_request(ctx, n, hd):
         check_attention(hq, hkv, hd, np.array([ctx]), [grow(rng, n, shape)], table, need, ctx + n)
 
 
+def test_attention_many_requests():
+    """More requests than a block has threads; most of them short, one long, some without nodes."""
+    args = make(random.Random(9), 700, 40, 3)
+    check_attention(2, 1, 64, *args, 3)
+    rng = random.Random(10)
+    trees = [grow(rng, rng.randrange(0, 3), "forest") for _ in range(300)] + [grow(rng, 200, "tree")]
+    ctx = np.array([rng.randrange(30) for _ in range(300)] + [9000])
+    need = [-(-(int(c) + len(t)) // P) for c, t in zip(ctx, trees)]
+    table = np.zeros((301, max(need)), np.int32)
+    at = 0
+    for i, k in enumerate(need):
+        table[i, :k] = at + np.arange(k)
+        at += k
+    check_attention(4, 2, 64, ctx, trees, table, at, 4)
+
+
+def test_pages_beyond_two_to_the_32_bytes():
+    """The last pages of pools of over 2^32 bytes, and layers that far apart: appends, attention and moves are what they are in a small pool, bit for bit."""
+    hq, hkv, hd, page = 8, 8, 128, 8 * P * 128
+    n_pages = (1 << 32) // (2 * page) + 40
+    ctx, trees, table, n = make(random.Random(11), 4, 120, 20, zero=0.0)
+    s, T = synera(), sum(map(len, trees))
+    far = table.copy()
+    far[table >= 0] = n_pages - 1 - table[table >= 0]
+    x = draw((T, hq + 2 * hkv, hd), 1)
+    rope = s.Rope(hd)
+    outs = []
+    for t, pages in ((table, n), (far, n_pages)):
+        k, v = (torch.zeros((2, pages, hkv, P, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((2, pages, hkv, hd, P), dtype=torch.bfloat16, device=DEV))
+        ids = torch.from_numpy(t[t >= 0].astype(np.int64)).to(DEV)
+        k[:, ids], v[:, ids] = draw((2, len(ids), hkv, P, hd), 2), draw((2, len(ids), hkv, hd, P), 3)
+        b = s.TreeBatch(hq, hkv, hd, 4, T, t.shape[1])
+        assert (b.plan(i32(ctx), i32([len(c) for c in trees]), i32(sum(trees, [])), i32(t), pages) == 0).all()
+        q = b.append_rope(rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], k[1], v[1])
+        o = b.attention(q, k[1], v[1])
+        acc = b.accept(i32(np.zeros(T)), i32(np.zeros(T)), n_given=i32(np.ones(4)))        # first children all the way down
+        b.commit(acc["path"], acc["n_path"], k, v)
+        outs.append((q, o, acc["path"], k[:, ids].clone(), v[:, ids].clone()))
+        del k, v
+        torch.cuda.empty_cache()
+    assert all(torch.equal(p, q) for p, q in zip(*outs))
+
+
+def test_replayed_plans_of_other_sizes():
+    """Behind a replayed plan that has more rows than a call's tensors, what lies in them is worked on and nothing behind them is touched; one that has
+    more requests than the last plan that was called is served whole."""
+    s, hq, hkv, hd = synera(), 4, 2, 64
+    ctx, trees, table, n = make(random.Random(12), 6, 700, 9, shapes=("tree",), zero=0.0)
+    new, T = [len(t) for t in trees], sum(map(len, trees))
+    k, v = filled(ctx, trees, table, n, hkv, hd, 5)
+    q = draw((T, hq, hd), 6)
+    b = planned(hq, hkv, hd, ctx, trees, table, n)
+    want = b.attention(q, k, v)
+    args = i32(ctx), i32(new), i32(sum(trees, [])), i32(table), n
+    first = [x[:2].contiguous() for x in args[:2]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            b.plan(*args)
+        few = new[0] + new[1]
+        for _ in range(3):
+            b.plan(*first, args[2][:few].contiguous(), args[3][:2].contiguous(), n)
+            assert torch.equal(b.attention(q[:few], k, v)[:few], want[:few])
+            graph.replay()
+            out = bits((T, hq, hd), 0x1234)
+            b.attention(q, k, v, out=out)                      # (the last plan that was called has two requests)
+            assert torch.equal(out, want)
+            cut = new[0] + new[1] + 1
+            out = bits((T, hq, hd), 0x1234)
+            b.attention(q[:cut], k, v, out=out[:cut])
+            rope, x = s.Rope(hd), draw((cut, hq + 2 * hkv, hd), 8)
+            out_q = bits((T, hq, hd), 0x1234)
+            kp, vp = k.clone(), v.clone()
+            b.append_rope(rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], kp, vp, out_q=out_q[:cut])
+            acc = b.accept(i32(np.zeros(cut)), i32(np.zeros(cut)), n_given=i32(np.ones(2)))
+            side.synchronize()
+            assert torch.equal(out[:few], want[:few]) and (out[few:].view(torch.int16) == 0x1234).all()
+            assert (out_q[cut:].view(torch.int16) == 0x1234).all() and (out_q[:cut].view(torch.int16) != 0x1234).any()
+            assert (acc["n_path"] >= 1).all()
+
+
 def test_attention_of_chains_is_that_of_chunks():
     """Trees whose parents are the nodes before them against the attention over chunks: both within their error of float64."""
     rng = random.Random(3)
@@ -517,6 +600,21 @@ def test_logits_long_paths_and_histories():
     x = torch.zeros((2, 9000), device=DEV)
     out = s.adjust_logits(x, history=history, history_len=i32([200000, 100001]), n_prompt=i32([0, 1]), frequency=torch.full((2,), 0.5, device=DEV))
     assert out[0, 5] == -50000 and out[0, 7] == -50000 and out[1, 5] == -50000 and (out != 0).sum() == 3
+
+
+def test_logits_of_a_long_tree_and_its_splits():
+    """Rows of one request whose paths are long and part ways: each is what it is by itself."""
+    s, rng, n, vocab = synera(), random.Random(4), 600, 3000
+    parent = [-1] + [j - 1 if rng.random() < 0.9 else rng.randrange(-1, j) for j in range(1, n)]
+    tokens = [rng.randrange(100) for _ in range(n)]
+    x = draw((n, vocab), 7, torch.float32)
+    freq = torch.full((1,), 0.25, device=DEV)
+    out = s.adjust_logits(x, cu=i32([0, n]), tokens=i32(tokens), parent=i32(parent), frequency=freq)
+    want = x.double().cpu()
+    for j, path in enumerate(tree.paths(parent)):
+        for t in path:
+            want[j, tokens[t]] -= 0.25
+    assert (out.cpu().double() - want).abs().max() < 4 * 2.0 ** -24 * (want.abs().max() + 100)
 
 
 def test_logits_rows_and_parents_that_cannot_be():

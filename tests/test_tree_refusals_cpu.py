@@ -37,6 +37,10 @@ def test_pages():
         args = list(good)
         args[at] = bad
         assert b._lib.synera_pages_update(*args) == s.EINVAL, (at, bad)
+    for at, bad in ((4, 500), (6, 128), (11, 64), (12, 380), (13, 64), (3, 384)):        # one on another
+        args = list(good)
+        args[at] = bad
+        assert b._lib.synera_pages_update(*args) == s.EINVAL, (at, bad)
     for at, bad in ((9, 1 << 27), (5, 1 << 27)):
         args = list(good)
         args[at] = bad
@@ -58,7 +62,8 @@ def test_the_description_is_as_long_as_the_structure():
     (dict(in_stride=39), s.EINVAL), (dict(out_stride=39), s.EINVAL), (dict(d_history=64), s.EINVAL), (dict(d_bias_id=64), s.EINVAL),
     (dict(d_bias=64), s.EINVAL), (dict(d_tokens=64, d_cu=64), s.EINVAL), (dict(d_tokens=64, d_parent=64), s.EINVAL), (dict(d_mask=66), s.EINVAL),
     (dict(history_columns=-1), s.EINVAL), (dict(bias_columns=-1), s.EINVAL), (dict(vocab=(1 << 30) + 1), s.EUNSUP), (dict(bias_columns=1023), s.EUNSUP),
-    (dict(history_columns=1 << 19), s.EUNSUP), (dict(B=65536, rows=65536), s.EUNSUP)])
+    (dict(history_columns=1 << 19), s.EUNSUP), (dict(B=65536, rows=65536), s.EUNSUP),
+    (dict(d_cu=64, d_tokens=64, d_parent=64, rows=(1 << 19) + 1), s.EUNSUP)])
 def test_logits(bad, status):
     assert b._lib.synera_logits_adjust(desc(**bad), 1 << 20, 1 << 21, None) == status
 
