@@ -23,6 +23,7 @@
 // 32 requests of 48 .. 160 nodes 414 us, 64 of 8 .. 64 nodes 125.)
 #define TR_LENGTHS 24
 #define TR_GRID 4                // blocks of the launch for each place
+#define TR_JOIN_GRID 2           // of the joining one
 // Candidate c: 2, 3, 4, 6, 8, 12, .. 2048, 3072 steps, and any.
 __device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
   const int32_t x = (steps - 1) >> (c / 2);
@@ -32,12 +33,13 @@ __device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
 #define TR_ONE 16                // a step of a request's only tile
 #define TR_MORE 11               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
 #define TR_START 32              // what it takes to begin and end an item
-#define TR_JOIN_LAUNCH 8         // to join anything at all
+#define TR_JOIN_LAUNCH 32        // to join anything at all
 #define TR_JOIN_ROWS 1024        // partial rows written and read in one 16th
 struct TrHead {
   ShHeader sh;                   // tokens and windows, for the append
   int32_t items, B;              // items of an XCD's list
-  int32_t pad[14];
+  int32_t joins;                 // places of the joining launch
+  int32_t pad[13];
 };
 struct TrReq {                   // 64 bytes, scalar loads
   int32_t ctx, n, tok;           // n: 0 where the request has no nodes or is refused
@@ -46,9 +48,10 @@ struct TrReq {                   // 64 bytes, scalar loads
   int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
   int32_t pad[8];
 };
-struct TrItem {                  // 8 bytes: a place in each XCD's list
-  int32_t req, at;               // the at-th item of the request in the list
+struct TrItem {                  // 8 bytes: a place in each XCD's list, or of the joining launch
+  int32_t req, at;               // the at-th item of the request in the list; TR_JOIN_AT rows of it (of all KV heads) from row at on
 };
+#define TR_JOIN_AT 8
 
 struct synera_tree {
   ShLimits lim;                  // (head counts and sizes; no room of a host plan)
@@ -62,7 +65,7 @@ struct synera_tree {
   int32_t items_room, part_rows;
   TrHead* head;
   TrReq* req;
-  TrItem* items;
+  TrItem *items, *joins;
   ShWindow* windows;
   int32_t *pos, *slot, *parent, *table;
   uint32_t* masks;
@@ -112,7 +115,9 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   t->items_room = (int32_t)std::max<size_t>((size_t)t->lim.slots, (size_t)((n_kv_heads + SY_SH_DEAL - 1) / SY_SH_DEAL) * B * (TR_NODES * G / SY_SH_TILE_ROWS + 1));
   t->part_rows = 2 * t->lim.slots * SY_SH_TILE_ROWS;
   const size_t parts = (size_t)t->part_rows;
-  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * sizeof(TrItem), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
+  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * sizeof(TrItem),
+                          // (at least two partial rows for each that is joined)
+                          (parts / 2 / TR_JOIN_AT + B) * sizeof(TrItem), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
                           T * 4, T * 4, T * 4, B * t->pitch * 4, T * SY_TREE_MASK * 4, parts * head_dim * 4, parts * 8};
   size_t all = 0;
   for (size_t s : sizes) all += up(s);
@@ -129,6 +134,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   take(t->head);
   take(t->req);
   take(t->items);
+  take(t->joins);
   take(t->windows);
   take(t->pos);
   take(t->slot);
@@ -147,7 +153,7 @@ struct PlanArgs {
   int32_t* status;
   TrHead* head;
   TrReq* req;
-  TrItem* items;
+  TrItem *items, *joins;
   ShWindow* windows;
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
@@ -185,10 +191,11 @@ struct TrTotals {
 };
 __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals& t) {
   if (t.items > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
-  // All places busy, or the longest item, which has three times the rate where few are: one request's range of 48 steps 104 us, 24 66.  The longest come first, so
-  // that little is left at the end: 256 requests of up to 64 steps uncut 277 us, cut to 24 301, to 12 323.
-  const int64_t busy = (int64_t)((double)t.cost * a.per_place), alone = (int64_t)t.longest * 3 / 8;
-  return max(busy, alone) + t.longest / 8 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
+  // All places busy, or the longest item: by itself it has 1.7 times the rate, where each block has a compute unit of its own 2.7 times.  The longest come first,
+  // so that little is left at the end.  Launches without the joining one: 64 requests of up to 33 steps uncut 101 us, cut to 24 89, to 16 95; 256 of up to
+  // 64 uncut 277, cut to 48 290, to 12 323; one of 243 cut to 48 104, to 24 66, to 8 45, to 4 48.
+  const int64_t busy = (int64_t)((double)t.cost * a.per_place), alone = (int64_t)t.longest * ((double)t.items * 2 * a.per_place <= 1.0 ? 3 : 5) / 8;
+  return max(busy, alone) + t.longest / 16 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
 }
 
 // The sum over the block's threads, for all of them.
@@ -213,7 +220,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   __shared__ TrTotals totals[TR_LENGTHS];
   __shared__ TrSize sizes[256];
   __shared__ unsigned long long best;                         // estimate << 8 | candidate
-  __shared__ int32_t sums_a[4][4], sums_b[4][2];
+  __shared__ int32_t sums_a[4][4], sums_b[4][4];
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
   if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0};
@@ -297,12 +304,19 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   const int chosen = (int)(best & 255);
   // ---- partial rows before this request by number, items by cost
   const int32_t ranges = tr_ranges(s.steps, chosen), items = s.steps ? (int32_t)items_of(a, s, ranges) : 0, cost = s.steps ? item_cost(s, ranges) : 0;
-  int32_t before[2] = {0, 0};
+  int32_t before[4] = {0, 0, 0, 0};                           // and places of the joining launch, before this request and in all
   for (int i = tid; i < a.B; i += 256) {
     const TrSize z = few ? sizes[i] : size_of(a, a.ctx[i], a.n_nodes[i]);
     if (z.steps == 0) continue;
     const int32_t r = tr_ranges(z.steps, chosen), k = item_cost(z, r);
-    if (i < me && r > 1) before[0] += r * a.Hkv * z.rows * a.G;
+    if (r > 1) {
+      const int32_t all = a.Hkv * z.rows * a.G, joins = (all + TR_JOIN_AT - 1) / TR_JOIN_AT;
+      if (i < me) {
+        before[0] += r * all;
+        before[2] += joins;
+      }
+      before[3] += joins;
+    }
     if (k > cost || (k == cost && i < me)) before[1] += (int32_t)items_of(a, z, r);
   }
   block_sums(before, sums_b);
@@ -356,6 +370,8 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   }
   // ---- the lists
   for (int k = tid; k < items; k += 256) a.items[before[1] + k] = TrItem{me, k};
+  if (ranges > 1)
+    for (int k = tid; k * TR_JOIN_AT < a.Hkv * s.rows * a.G; k += 256) a.joins[before[2] + k] = TrItem{me, k * TR_JOIN_AT};
   if (tid == 0) {
     a.req[me] = TrReq{ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles,
                       before[0], {}};
@@ -365,6 +381,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
       a.head->sh.n_windows = rows[3];
       a.head->items = (int32_t)totals[chosen].items;
       a.head->B = a.B;
+      a.head->joins = before[3];
     }
   }
 }
@@ -388,7 +405,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   const ShLimits& l = t->lim;
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
-  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->windows, t->pos, t->slot, t->parent, t->table,
+  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->joins, t->windows, t->pos, t->slot, t->parent, t->table,
                       t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, (double)SY_SH_DEAL / l.slots, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
@@ -414,7 +431,7 @@ extern "C" int32_t synera_tree_append_rope(synera_tree* t, const synera_rope* ro
 struct TreeAttnArgs : SharedAttnArgs {
   const TrHead* th;
   const TrReq* req;
-  const TrItem* places;
+  const TrItem *places, *joins;
   const uint32_t* masks;
   int32_t pitch;
   int32_t rows;                  // that the tensors of this call have: a plan that was replayed may have more
@@ -498,29 +515,27 @@ __device__ __forceinline__ void join_row(const TreeAttnArgs& a, const TrReq& q, 
 }
 
 template <int HD>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnArgs a) {
-  const int B = a.th->B;
-  for (int r = blockIdx.x; r < B; r += gridDim.x) {
-    const TrReq q = req_of(a, r);
-    if (q.ranges <= 1 || q.n == 0 || q.tok + q.n > a.rows) continue;
-    const int rows = q.n * a.G;
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < a.Hkv * rows * (HD / 4); i += gridDim.y * 256) {
-      const int row = i / (HD / 4), d4 = i % (HD / 4) * 4;
-      if (q.ranges <= 2) join_row<HD, 2>(a, q, row / rows, row % rows, d4);
-      else if (q.ranges <= 4) join_row<HD, 4>(a, q, row / rows, row % rows, d4);
-      else join_row<HD, 8>(a, q, row / rows, row % rows, d4);
-    }
+__global__ __launch_bounds__(TR_JOIN_AT * HD / 4) void tree_join_kernel(TreeAttnArgs a) {
+  const int joins = a.th->joins, d4 = threadIdx.x % (HD / 4) * 4;
+  for (int k = blockIdx.x; k < joins; k += gridDim.x) {
+    const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(a.joins + k));
+    const TrReq q = req_of(a, at[0]);
+    const int rows = q.n * a.G, row = at[1] + threadIdx.x / (HD / 4);
+    if (q.n == 0 || q.tok + q.n > a.rows || row >= a.Hkv * rows) continue;
+    if (q.ranges <= 2) join_row<HD, 2>(a, q, row / rows, row % rows, d4);
+    else if (q.ranges <= 4) join_row<HD, 4>(a, q, row / rows, row % rows, d4);
+    else join_row<HD, 8>(a, q, row / rows, row % rows, d4);
   }
 }
 
 template <int HD>
 static constexpr size_t tree_lds() { return (size_t)20 * SY_PAGE * HD * 2; }
 template <int HD>
-static hipError_t launch_tree(const TreeAttnArgs& a, int grid, int B, bool cuts, hipStream_t s) {
+static hipError_t launch_tree(const TreeAttnArgs& a, int grid, int joins, hipStream_t s) {
   tree_attn_kernel<HD><<<grid, 256, tree_lds<HD>(), s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !cuts) return e;
-  tree_join_kernel<HD><<<dim3(B, std::max(1, std::min(128, 1024 / B))), 256, 0, s>>>(a);
+  if (e != hipSuccess || joins == 0) return e;
+  tree_join_kernel<HD><<<joins, TR_JOIN_AT * HD / 4, 0, s>>>(a);
   return hipGetLastError();
 }
 static hipError_t prepare_attention(int hd) {
@@ -544,13 +559,15 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.th = t->head;
   a.req = t->req;
   a.places = t->items;
+  a.joins = t->joins;
   a.masks = t->masks;
   a.pitch = t->pitch;
   a.rows = q->n_rows ? q->n_rows : INT32_MAX;
   // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
-  const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL, B = captured ? l.max_batch : t->B;
+  const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL;
   const bool cuts = (captured || t->replays ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
-  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, B, cuts, s) : launch_tree<64>(a, grid, B, cuts, s);
+  const int joins = cuts ? TR_JOIN_GRID * l.slots : 0;
+  const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, joins, s) : launch_tree<64>(a, grid, joins, s);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return SYNERA_EHIP;
