@@ -41,15 +41,19 @@ struct TrHead {
   int32_t joins;                 // places of the joining launch
   int32_t pad[13];
 };
-struct TrReq {                   // 64 bytes, scalar loads
+struct TrReq {                   // 32 bytes, scalar loads
   int32_t ctx, n, tok;           // n: 0 where the request has no nodes or is refused
   int32_t rows;                  // of its n_nodes, those that there is room for
   int32_t steps, ranges, tiles;  // as the lists count them, refused or not
   int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
-  int32_t pad[8];
 };
-struct TrItem {                  // 8 bytes: a place in each XCD's list, or of the joining launch
-  int32_t req, at;               // the at-th item of the request in the list; TR_JOIN_AT rows of it (of all KV heads) from row at on
+struct TrItem {                  // 64 bytes: a place in each XCD's list.  All that a block has to know before it can ask for keys, in one load
+  TrReq q;
+  int32_t req, at;               // the at-th item of the request in the list
+  int32_t pad[6];
+};
+struct TrJoin {                  // 8 bytes: TR_JOIN_AT rows of a request (of all KV heads) from row `at` on
+  int32_t req, at;
 };
 #define TR_JOIN_AT 8
 
@@ -65,7 +69,8 @@ struct synera_tree {
   int32_t items_room, part_rows;
   TrHead* head;
   TrReq* req;
-  TrItem *items, *joins;
+  TrItem* items;
+  TrJoin* joins;
   ShWindow* windows;
   int32_t *pos, *slot, *parent, *table;
   uint32_t* masks;
@@ -117,7 +122,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   const size_t parts = (size_t)t->part_rows;
   const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * sizeof(TrItem),
                           // (at least two partial rows for each that is joined)
-                          (parts / 2 / TR_JOIN_AT + B) * sizeof(TrItem), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
+                          (parts / 2 / TR_JOIN_AT + B) * sizeof(TrJoin), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
                           T * 4, T * 4, T * 4, B * t->pitch * 4, T * SY_TREE_MASK * 4, parts * head_dim * 4, parts * 8};
   size_t all = 0;
   for (size_t s : sizes) all += up(s);
@@ -153,7 +158,8 @@ struct PlanArgs {
   int32_t* status;
   TrHead* head;
   TrReq* req;
-  TrItem *items, *joins;
+  TrItem* items;
+  TrJoin* joins;
   ShWindow* windows;
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
@@ -369,12 +375,12 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     a.windows[rows[1] + w] = x;
   }
   // ---- the lists
-  for (int k = tid; k < items; k += 256) a.items[before[1] + k] = TrItem{me, k};
+  const TrReq q = {ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles, before[0]};
+  for (int k = tid; k < items; k += 256) a.items[before[1] + k] = TrItem{q, me, k, {}};
   if (ranges > 1)
-    for (int k = tid; k * TR_JOIN_AT < a.Hkv * s.rows * a.G; k += 256) a.joins[before[2] + k] = TrItem{me, k * TR_JOIN_AT};
+    for (int k = tid; k * TR_JOIN_AT < a.Hkv * s.rows * a.G; k += 256) a.joins[before[2] + k] = TrJoin{me, k * TR_JOIN_AT};
   if (tid == 0) {
-    a.req[me] = TrReq{ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles,
-                      before[0], {}};
+    a.req[me] = q;
     if (a.status) a.status[me] = status;
     if (me == 0) {
       a.head->sh.n_tokens = (int32_t)min((int64_t)rows[2], a.n_rows);
@@ -431,7 +437,8 @@ extern "C" int32_t synera_tree_append_rope(synera_tree* t, const synera_rope* ro
 struct TreeAttnArgs : SharedAttnArgs {
   const TrHead* th;
   const TrReq* req;
-  const TrItem *places, *joins;
+  const TrItem* places;
+  const TrJoin* joins;
   const uint32_t* masks;
   int32_t pitch;
   int32_t rows;                  // that the tensors of this call have: a plan that was replayed may have more
@@ -441,21 +448,25 @@ typedef SH_CONST_AS sh_i32x2v tr_i32x2;
 
 __device__ __forceinline__ TrReq req_of(const TreeAttnArgs& a, int r) {
   const sh_i32x8v w = *reinterpret_cast<const tr_i32x8*>((uintptr_t)(a.req + r));
-  return TrReq{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], {}};
+  return TrReq{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
 }
 
 template <int HD>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int x = blockIdx.x % SY_SH_DEAL, items = a.th->items;
-  for (int k = blockIdx.x / SY_SH_DEAL; k < items; k += gridDim.x / SY_SH_DEAL) {
-    const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(a.places + k));
-    const TrReq q = req_of(a, at[0]);
+  const int x = blockIdx.x % SY_SH_DEAL, k0 = blockIdx.x / SY_SH_DEAL, items = a.th->items;
+  // (the first place is looked at together with the number of items: the launch has no more blocks than the lists have places)
+  for (int k = k0; k == k0 || k < items; k += gridDim.x / SY_SH_DEAL) {
+    const tr_i32x8* place = reinterpret_cast<const tr_i32x8*>((uintptr_t)(a.places + k));
+    const sh_i32x8v w = place[0];
+    const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(place + 1));
+    if (k >= items) return;
+    const TrReq q = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
     const int tile = at[1] % q.tiles, group = at[1] / q.tiles * SY_SH_DEAL + x, kh = group % a.Hkv, range = group / a.Hkv;
     if (q.n == 0 || range >= q.ranges || q.tok + q.n > a.rows) continue;
     const int rows = q.n * a.G, keys = q.ctx + q.n;
-    // (products of steps and ranges may pass 32 bits)
-    const int begin = (int)((uint64_t)q.steps * (uint32_t)range / (uint32_t)q.ranges), end = (int)((uint64_t)q.steps * (uint32_t)(range + 1) / (uint32_t)q.ranges);
+    const int each = q.steps / q.ranges, more = q.steps % q.ranges;        // the first `more` ranges have a step more
+    const int begin = range * each + min(range, more), end = begin + each + (range < more ? 1 : 0);
     ShItem it;
     it.flags = SY_SH_LEAF | (q.tiles == 1 ? SY_SH_ONCE : 0);
     it.kv_head = kh;
