@@ -921,14 +921,14 @@ class TreeBatch(_PagedBatch):
     def commit(self, path, n_path, k_pool, v_pool):
         """Moves the keys and values of each path to the positions behind its context, in one layer's pools or in all layers'
         [n_layers, pages, ...]; n_path is then to be added to the cached lengths."""
-        index, k_tile, v_tile = self._index, self._tiles[0], self._tiles[1]
-        for pool, tile in ((k_pool, k_tile), (v_pool, v_tile)):
-            shape = pool.shape
-            if pool.dtype != torch.bfloat16 or len(shape) not in (4, 5) or shape[-3:] != tile or shape[-4] < self.n_pages or \
-                    shape[:-3] != k_pool.shape[:-3] or pool.stride(0) != k_pool.stride(0) or pool.get_device() != index or \
-                    not (pool[0] if len(shape) == 5 and shape[0] > 0 else pool).is_contiguous():
+        index, shape = self._index, k_pool.shape
+        for pool, tile in ((k_pool, self._tiles[0]), (v_pool, self._tiles[1])):
+            packed = tile[0] * tile[1] * tile[2], tile[1] * tile[2], tile[2], 1
+            if pool.dtype is not torch.bfloat16 or len(shape) not in (4, 5) or pool.shape[:-2] != shape[:-2] or pool.shape[-3:] != tile or \
+                    shape[-4] < self.n_pages or pool.stride(0) != k_pool.stride(0) or pool.get_device() != index or \
+                    not (pool.stride()[-4:] == packed or (pool[0] if len(shape) == 5 and shape[0] > 0 else pool).is_contiguous()):
                 raise ValueError(f"expected pools bf16 [(layers,) >= {self.n_pages}, ...] on {self.device}, each layer contiguous, alike for keys and values")
-        layers, stride = (k_pool.shape[0], k_pool.stride(0)) if k_pool.dim() == 5 else (1, 0)
+        layers, stride = (shape[0], k_pool.stride(0)) if len(shape) == 5 else (1, 0)
         n = path.numel()
         st = _lib.synera_tree_commit(self._h, n, _ints(path, (n,), index, "path"), _ints(n_path, (self.n_requests,), index, "n_path"), layers, stride,
                                      k_pool.data_ptr(), v_pool.data_ptr(), _raw_stream(index))
