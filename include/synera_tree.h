@@ -38,7 +38,8 @@ extern "C" {
  * The lengths and d_shared are device i32 [B], d_shared may be NULL (none).  d_table is i32 [B][columns], d_free i32 [n_pages], d_n_free
  * i32 [1] (taken as 0 below 0, as n_pages above).  A page must be held once or be free once; nothing checks that.  n_rows may be 0 (d_pos and
  * d_slot are not looked at).  Rows of tokens beyond n_rows are left out.
- * Errors: EINVAL (null, sizes, pointers off 4 bytes), EUNSUP (n_pages >= 2^27, B x columns >= 2^27), EHIP.
+ * What is written lies on no other array of the call.  Errors: EINVAL (null, sizes, pointers off 4 bytes, overlaps), EUNSUP (n_pages >= 2^27,
+ * B x columns >= 2^27), EHIP.
  */
 int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_new, const int32_t* d_shared, int32_t* d_table,
                             int32_t columns, int32_t* d_held, int32_t* d_free, int32_t* d_n_free, int32_t n_pages, int64_t n_rows,
@@ -64,8 +65,9 @@ int32_t synera_tree_destroy(synera_tree* tree);
 /*
  * Plans a step, once for all layers: d_ctx_len, d_n_nodes i32 [B], d_parent i32 [rows], d_table i32 [B][columns] (columns <= max_pages), all
  * read by this call alone.  The calls below must be on the same stream, or ordered behind it by the caller; so must a plan behind calls
- * that use the one before.  Captured calls work for any later plan of this handle (captured or not); their tensors and pools need
- * room for the rows and pages of those plans, which nothing checks.
+ * that use the one before.  Captured calls work for any later plan of this handle (captured or not).  Calls look at what the last plan that was
+ * called, or captured, says of rows and pages; where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
+ * the requests beyond them are left out.  That pools have room for a replayed plan's pages nothing checks.
  *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES (it has no rows), a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page
  *             id outside the pool; ENOSPC: more pages than columns, more rows than n_rows
  * Errors: EINVAL (null, sizes, alignment), ENOSPC (B > max_batch, n_rows > max_tokens, columns > max_pages), EUNSUP (n_pages_in_pool >= 2^27), EHIP.
@@ -107,14 +109,14 @@ int32_t synera_tree_commit(synera_tree* tree, int64_t n_rows, const int32_t* d_p
 /* ------------------------------------------------------------------------------------------- logits
  * For row r of request i and token t with logit x, in this order and in 32 bits:
  *   seen: t is among the first history_len[i] tokens of d_history[i] or on the row's path; g: how often it is there from n_prompt[i] on
- *   x = x / repetition (x > 0) or x * repetition     where t was seen
+ *   x = x / repetition (x > 0; times its reciprocal, rounded) or x * repetition     where t was seen
  *   x -= frequency x g + presence                    where g > 0
  *   x += bias                                        of the last entry of d_bias_id[i] that names t
  *   x = -infinity                                    where bit t % 32 of word t / 32 of d_mask[r] is not set, whatever x was
  * and rounded once to the type of the output.  A mask may leave nothing.
  */
 typedef struct synera_logits_desc {
-  int32_t B;                   /* requests                                                                              */
+  int32_t B;                   /* requests, at most 65535                                                               */
   int32_t dtype;               /* of logits, in and out: 0, 1 or 2                                                      */
   int64_t rows, vocab;         /* vocab <= 2^30                                                                         */
   int64_t in_stride, out_stride;   /* elements from row to row, >= vocab where there are several                        */
@@ -130,7 +132,7 @@ typedef struct synera_logits_desc {
   const int32_t* d_bias_id;    /* [B][bias_columns] or NULL: none.  Ids outside the vocabulary name nothing               */
   const float* d_bias;         /* [B][bias_columns]                                                                     */
   const int32_t* d_mask;       /* [rows][(vocab + 31) / 32] bits of tokens that are allowed, or NULL: all                 */
-  const int32_t* d_tokens;     /* [rows], or NULL: no paths.  With d_cu: row j of a request stands behind node j of its tree, */
+  const int32_t* d_tokens;     /* [rows], at most 2^19, or NULL: no paths.  With d_cu: row j of a request stands behind node j of its tree, */
   const int32_t* d_parent;     /* [rows]  whose path, itself included, was seen and counts for g.  A parent outside 0 .. j - 1 ends the path */
 } synera_logits_desc;
 
