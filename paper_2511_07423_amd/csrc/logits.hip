@@ -12,8 +12,10 @@
 // Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides; those that are allowed and have a word
 // are formed on the way.  (Nearly every wavefront meets some: with a branch for each value 2048 x 128256 masked took 325 us; formed behind the
 // others, from memory, 300; this way 198, as long as a plain copy of the logits.)
-// Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Longer ones are
-// added to the words before a row, and taken away where the next row is not behind it.
+// Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Rows pass those
+// tokens as they are, and behind a barrier each is formed for each row, by a lane that counts it along the list.  (198 trees of 64 nodes in a
+// vocabulary of 1096: 67 us; counted on the way, where one lane keeps its wavefront waiting, 323.)  Longer paths are added to the words before a
+// row, and taken away where the next row is not behind it.
 #define LG_SLICE 8192
 #define LG_THREADS 512
 #define LG_PROMPT (1u << 20)
@@ -22,6 +24,7 @@
 #define LG_BIAS 22
 #define LG_MOST_ROWS (1 << 19)   // of calls with paths: counts stay below 2^20
 #define LG_NODES 256
+#define LG_FIRST (1u << 31)
 #define LG_MOST_BIASES 1022
 #define LG_EARLY 4               // tokens of the history that a thread asks for together
 #define LG_FLY 4                 // 16-byte pieces of a thread on their way together
@@ -107,8 +110,9 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
   __shared__ uint32_t has_word[LG_SLICE / 32];
   __shared__ uint32_t on_path[LG_NODES][LG_NODES / 32 + 1];   // (+ 1: neighbours on other banks)
   __shared__ int32_t parents[LG_NODES];
-  __shared__ uint32_t listed[LG_NODES];                       // token in the slice | node << 16
+  __shared__ uint32_t listed[LG_NODES];                       // token in the slice | node << 16 | LG_FIRST: the first one of its token
   __shared__ int32_t n_listed;
+  __shared__ int32_t held;
   const int tid = threadIdx.x, i = blockIdx.y;
   const int v0 = blockIdx.x * LG_SLICE, n = min(LG_SLICE, (int)a.d.vocab - v0);
   int64_t first = i, rows = 1;
@@ -211,8 +215,9 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
     }
     const uint32_t t = slot(token0);
     if (t < (uint32_t)n) {
-      listed[atomicAdd(&n_listed, 1)] = t | (uint32_t)tid << 16;
-      touch(t, atomicOr(&word[t], LG_PATH));
+      const uint32_t old = atomicOr(&word[t], LG_PATH);
+      touch(t, old);
+      listed[atomicAdd(&n_listed, 1)] = t | (uint32_t)tid << 16 | (old & LG_PATH ? 0u : LG_FIRST);
     }
   }
   __syncthreads();
@@ -220,14 +225,9 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
                      a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + biases};
   params.inv = 1.f / params.rho;
   // ---- the rows
-  auto word_of = [&](int64_t j, int t) {                      // of token t of the slice, for row j
-    uint32_t w = word[t];
-    if (w & LG_PATH)
-      for (int k = 0; k < n_listed; ++k) {
-        const uint32_t x = listed[k];
-        if ((int)(x & 0xFFFF) == t) w += (on_path[j][x >> 21] >> ((x >> 16) & 31)) & 1;
-      }
-    return w & ~LG_PATH;
+  auto word_of = [&](int t) {                                 // of token t of the slice, 0 where some path has it
+    const uint32_t w = word[t];
+    return w & LG_PATH ? 0u : w;
   };
   auto finish = [&](const Rows& r, int64_t j0) {
 #pragma unroll
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
           while (todo) {
             const int k = __builtin_ctz(todo);
             todo &= todo - 1;
-            const uint32_t w = word_of(j, c * VEC + k);
+            const uint32_t w = word_of(c * VEC + k);
             v = lg_put<T>(v, k, lg_bias(params, lg_adjust(params, lg_get<T>(v, k), w), w));
           }
         } else if (todo) {
@@ -257,12 +257,7 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
           y.p[0] = v;
           y.widen(f);
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) any |= w[k] = word[c * VEC + k];
-          if (any & LG_PATH) {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k)
-              if (w[k] & LG_PATH) w[k] = word_of(j, c * VEC + k);
-          }
+          for (int k = 0; k < VEC; ++k) any |= w[k] = word_of(c * VEC + k);
 #pragma unroll
           for (int k = 0; k < VEC; ++k) f[k] = lg_adjust(params, f[k], w[k]);
           if (any >> LG_BIAS) {
@@ -286,7 +281,7 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
         float f;
         y.load(in_of(j) + e);
         const bool allowed = !MASK || (mask_of(j)[e / 32] >> (e % 32)) & 1;
-        const uint32_t w = word_of(j, e);
+        const uint32_t w = word_of(e);
         if (w || !allowed) {
           y.widen(&f);
           f = allowed ? lg_bias(params, lg_adjust(params, f, w), w) : -INFINITY;
@@ -296,21 +291,22 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
       }
   };
   // Long paths, by one thread: the words hold that of node `held`.  If it is an ancestor of the next row, only what lies between is added.
-  int64_t held = -1;
-  auto add = [&](int64_t at, uint32_t by) {
+  if (tid == 0) held = -1;
+  auto add = [&](int32_t at, uint32_t by) {
     const uint32_t t = slot(a.d.d_tokens[first + at]);
     if (t < (uint32_t)n) {
       word[t] += by;
       has_word[t / 32] |= 1u << (t % 32);
     }
     const int32_t up = a.d.d_parent[first + at];
-    return up >= 0 && up < at ? (int64_t)up : (int64_t)-1;
+    return up >= 0 && up < at ? up : -1;
   };
-  auto hold = [&](int64_t j) {
-    int64_t at = j;
-    while (at > held) at = add(at, 1u);
-    if (at != held) {
-      for (int64_t old = held; old >= 0;) old = add(old, ~0u);
+  auto hold = [&](int32_t j) {
+    const int32_t before = held;
+    int32_t at = j;
+    while (at > before) at = add(at, 1u);
+    if (at != before) {
+      for (int32_t old = before; old >= 0;) old = add(old, ~0u);
       while (at >= 0) at = add(at, 1u);
     }
     held = j;
@@ -321,12 +317,36 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
     if (VEC == 8 && j0 + step < rows) load(next, j0 + step, most);
     if (added_paths) {
       __syncthreads();
-      if (tid == 0) hold(j0);
+      if (tid == 0) hold((int32_t)j0);
       __syncthreads();
     }
     finish(now, j0);
     if (VEC == 8) now = next;
     else if (j0 + step < rows) load(now, j0 + step, most);
+  }
+  // ---- the listed tokens, which have passed as they are
+  const int n_list = n_listed;
+  if (n_list == 0) return;
+  __syncthreads();
+  const int mine = (int)((rows - blockIdx.z + a.splits - 1) / a.splits);
+  for (int e = tid; e < n_list * mine; e += LG_THREADS) {
+    const int g = e / n_list;
+    const int64_t j = blockIdx.z + (int64_t)g * a.splits;
+    const uint32_t own = listed[e - g * n_list];
+    const int t = (int)(own & 0xFFFF);
+    if (!(own & LG_FIRST) || (MASK && !((mask_of(j)[t / 32] >> (t % 32)) & 1))) continue;
+    TurnChunk<T, 1> y;
+    float f;
+    y.load(in_of(j) + t);
+    uint32_t w = word[t] & ~LG_PATH;
+    for (int k = 0; k < n_list; ++k) {
+      const uint32_t other = listed[k], node = (other >> 16) % LG_NODES;
+      if (((other ^ own) & 0xFFFF) == 0) w += (on_path[j][node / 32] >> (node % 32)) & 1;
+    }
+    y.widen(&f);
+    f = lg_bias(params, lg_adjust(params, f, w), w);
+    y.round(&f);
+    if (w) y.template store<false>(out_of(j) + t);
   }
 }
 
@@ -371,7 +391,9 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   if (!in_place && lg_meet(d_out, out_bytes, d_in, in_bytes)) return SYNERA_EINVAL;
   LogitsArgs a = {d, d_in, d_out, 1, in_place, !in_place && beyond_caches((size_t)(d.rows * d.vocab * size))};
   const int64_t slices = (d.vocab + LG_SLICE - 1) / LG_SLICE, each = (d.rows + B - 1) / B;
-  a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 4096 / (slices * B))), 65535);
+  // Blocks that share a request's rows, up to two rounds of three blocks a compute unit: with more, what each makes from the history and the paths costs more
+  // than full rounds save (3 x 64 rows of 123964, 1536 and 4096 blocks: 40 and 61 us; 64 x 16 of 32000: 42 and 42).
+  a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 1536 / (slices * B))), 65535);
   const dim3 grid((uint32_t)slices, (uint32_t)B, (uint32_t)a.splits);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.dtype == 0) launch_logits<float>(a, grid, s);

@@ -582,6 +582,17 @@ def test_logits(vocab, dtype):
         check_logits(rng, trees, B, vocab, dtype, seed + vocab, parts, pitch, in_place=seed % 2 == 1)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,vocab", ((60, 37), (50, 1096), (3, 17000)))
+def test_logits_of_trees_that_share_blocks(B, vocab, dtype):
+    """More rows than blocks take one by one, most tokens on several nodes: each row counts its own path's."""
+    rng = random.Random(B)
+    for seed, (parts, pitch) in enumerate(((EVERY, 0), (("tree", "frequency", "repetition"), vocab + 1), (("tree", "presence", "mask"), vocab + 8))):
+        trees = [grow(rng, rng.choice((64, 63, 256, 0)), rng.choice(("tree", "chain", "wide"))) for i in range(B)]
+        for in_place in (False, True):
+            check_logits(rng, trees, B, vocab, dtype, seed, parts, pitch, in_place=in_place)
+
+
 def test_logits_of_one_row_and_none():
     s = synera()
     check_logits(random.Random(1), [[], [-1], []], 3, 129, "f32", 1, EVERY)
