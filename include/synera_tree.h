@@ -67,7 +67,8 @@ int32_t synera_tree_destroy(synera_tree* tree);
  * read by this call alone.  The calls below must be on the same stream, or ordered behind it by the caller; so must a plan behind calls
  * that use the one before.  Captured calls work for any later plan of this handle (captured or not).  Calls look at what the last plan that was
  * called, or captured, says of rows and pages; where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
- * the requests beyond them are left out.  That pools have room for a replayed plan's pages nothing checks.
+ * the requests beyond them are left out, as an accept or a commit leaves out requests beyond the B of the plan that it was called behind; before a captured plan's
+ * first replay the handle has no requests.  That pools have room for a replayed plan's pages nothing checks.
  *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES (it has no rows), a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page
  *             id outside the pool; ENOSPC: more pages than columns, more rows than n_rows
  * Errors: EINVAL (null, sizes, alignment), ENOSPC (B > max_batch, n_rows > max_tokens, columns > max_pages), EUNSUP (n_pages_in_pool >= 2^27), EHIP.
@@ -89,7 +90,7 @@ int32_t synera_tree_attention(synera_tree* tree, const synera_heads* q, const vo
  * follows them, or the context where there are none, is the target of the last one, or d_anchor[i].  From there the path goes to the
  * first child whose token (d_tokens i32 [rows]) is the target, and on with that child's target.
  *   d_accept_len i32 [B]     nodes on the path behind the given ones
- *   d_token      i32 [B]     the target at the path's end, which no child has; -1: none (no given nodes and no anchor, or refused)
+ *   d_token      i32 [B]     the target at the path's end, which no child has; -1: none (no nodes, no given ones and no anchor, or refused)
  *   d_path       i32 [rows]  row cu_i + k: the k-th node of the path, the given ones first; -1 behind its end
  *   d_n_path     i32 [B]     nodes on the path, the given ones included
  * Outputs must not lie on inputs.  Errors: EINVAL (null, no plan, n_rows below the plan's, neither d_anchor nor d_n_given), EHIP.

@@ -725,6 +725,7 @@ def validate_shared(ctx_len, n_new, block_table, n_pages_in_pool, max_batch, max
 class _PagedBatch:
     """What batches over a paged cache have in common: a handle whose plan says where each token goes and what it sees."""
     _names = ()                                           # of the C functions: create, destroy, append, attention
+    _skips_none = False                                   # tensors without rows: nothing is called (to C no rows are an unknown number)
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_tokens, max_pages):
         self._h = _vp()
@@ -764,8 +765,10 @@ class _PagedBatch:
         hq = None
         if q is not None:
             hq, out_q = _heads(q, out_q, q_gain, dtype, n, self.n_q_heads, hd, index, "q", torch.bfloat16, False)
-        st = self._append(self._h, rope._h, _head_type(dtype), hq, hk, hv, eps, self._pool(k_pool, self._tiles[0]),
-                          self._pool(v_pool, self._tiles[1]), _raw_stream(index))
+        at_k, at_v, kind = self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1]), _head_type(dtype)
+        if self._skips_none and (k.shape[0] == 0 or v.shape[0] == 0 or (q is not None and q.shape[0] == 0)):
+            return out_q
+        st = self._append(self._h, rope._h, kind, hq, hk, hv, eps, at_k, at_v, _raw_stream(index))
         if st:
             raise SyneraError(st, self._names[2])
         return out_q
@@ -780,10 +783,11 @@ class _PagedBatch:
         index = self._index
         h, out = _heads(q, out, None, torch.bfloat16, self.n_tokens, self.n_q_heads, self.head_dim, index, "q", None, False)
         lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
-        st = self._attend(self._h, h, self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1]), scale,
-                          lse.data_ptr() if want_lse else None, _raw_stream(index))
-        if st:
-            raise SyneraError(st, self._names[3])
+        at_k, at_v = self._pool(k_pool, self._tiles[0]), self._pool(v_pool, self._tiles[1])
+        if not (self._skips_none and q.shape[0] == 0):
+            st = self._attend(self._h, h, at_k, at_v, scale, lse.data_ptr() if want_lse else None, _raw_stream(index))
+            if st:
+                raise SyneraError(st, self._names[3])
         return (out, lse) if want_lse else out
 
 
@@ -885,6 +889,7 @@ class TreeBatch(_PagedBatch):
     graph; captured calls serve later plans too, for which their tensors and pools need room.  Rows of a tree: node j of request i is row
     cu[i] + j, cu the prefix sums of n_nodes.  Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
     _names = "synera_tree_create", "synera_tree_destroy", "synera_tree_append_rope", "synera_tree_attention"
+    _skips_none = True
 
     def plan(self, ctx_len, n_nodes, parent, block_table, n_pages_in_pool):
         """int32 on the GPU: cached tokens and nodes (at most TREE_NODES) of each request, each node's parent among the nodes before it

@@ -148,6 +148,13 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   take(t->masks);
   take(t->part_o);
   take(t->part_ml);
+  // (no requests, rows or items until a plan has run: one that is captured has not)
+  const TrHead none = {};
+  if (hipMemcpy(t->head, &none, sizeof none, hipMemcpyHostToDevice) != hipSuccess) {
+    (void)hipGetLastError();
+    (void)synera_tree_destroy(t);
+    return SYNERA_EHIP;
+  }
   *out = t;
   return SYNERA_OK;
 }

@@ -207,6 +207,68 @@ def test_attention_one_request(ctx, n, hd):
         check_attention(hq, hkv, hd, np.array([ctx]), [grow(rng, n, shape)], table, need, ctx + n)
 
 
+def test_attention_of_a_long_context():
+    """More steps than any length of ranges but the last few covers with what room there is for partial results."""
+    rng, need = random.Random(12), -(-(150000 + 21) // P)
+    table = np.array([rng.sample(range(need), need)], np.int32)
+    check_attention(3, 1, 64, np.array([150000]), [grow(rng, 21, "tree")], table, need, 5)
+
+
+def outputs_of(b, T, q, k, v, rope, B):
+    """All calls behind a plan, on T rows, with what they leave."""
+    out = bits((T, b.n_q_heads, b.head_dim), 0x1234)
+    if T:
+        b.append_rope(rope, None, q[:T, :b.n_kv_heads], q[:T, :b.n_kv_heads], k, v)
+    else:
+        b.append_rope(rope, q[:0], q[:0, :b.n_kv_heads], q[:0, :b.n_kv_heads], k, v)
+    _, lse = b.attention(q[:T], k, v, out=out, want_lse=True)
+    tokens = i32(np.zeros(T))
+    got = b.accept(tokens, tokens, anchor=i32(np.zeros(B)))
+    b.commit(got["path"], got["n_path"], k, v)
+    return out, lse, got
+
+
+def test_steps_without_nodes_and_plans_that_have_not_run():
+    """No request has a node; and calls behind a plan that is captured and not replayed, eager ones and captured ones on no rows: nothing is written."""
+    s, (hq, hkv, hd), B, n_pages = synera(), (4, 2, 64), 3, 8
+    q = draw((10, hq, hd), 1)
+    k, v = draw((n_pages, hkv, P, hd), 2), draw((n_pages, hkv, hd, P), 3)
+    before = k.clone(), v.clone()
+    rope = s.Rope(hd, layout="half")
+    b = s.TreeBatch(hq, hkv, hd, B, 10, 2)
+    table = i32(np.arange(6).reshape(3, 2))
+    status = b.plan(i32([5, 0, 20]), i32([0, 0, 0]), i32([]), table, n_pages)
+    out, lse, got = outputs_of(b, 0, q, k, v, rope, B)
+    assert status.tolist() == [0, 0, 0] and lse.shape == (0, hq)
+    assert got["accept_len"].tolist() == got["n_path"].tolist() == [0, 0, 0] and got["token"].tolist() == [-1] * 3 and got["path"].numel() == 0
+
+    b = s.TreeBatch(hq, hkv, hd, B, 10, 2)
+    ctx, new, parent = i32([5, 0, 20]), i32([2, 1, 3]), i32([-1, 0, -1, -1, 0, 0])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        status = b.plan(ctx, new, parent, table, n_pages)
+    out, _, _ = outputs_of(b, 6, q, k, v, rope, B)
+    assert torch.equal(out.view(torch.int16), bits(out.shape, 0x1234).view(torch.int16))
+    assert torch.equal(k.view(torch.int16), before[0].view(torch.int16)) and torch.equal(v.view(torch.int16), before[1].view(torch.int16))
+    graph.replay()
+    out, _, got = outputs_of(b, 6, q, k, v, rope, B)
+    assert status.tolist() == [0, 0, 0] and not torch.equal(k.view(torch.int16), before[0].view(torch.int16))
+    assert torch.isfinite(out).all()
+
+    b.plan(i32([5, 0, 20]), i32([0, 0, 0]), i32([]), table, n_pages)
+    none, at = torch.cuda.CUDAGraph(), (k.clone(), v.clone(), q.clone())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(none):
+        b.append_rope(rope, q[:0], q[:0, :hkv], q[:0, :hkv], k, v)
+        b.attention(q[:0], k, v, out=q[:0])
+    b.plan(ctx, new, parent, table, n_pages)
+    none.replay()
+    torch.cuda.synchronize()
+    for x, y in zip((k, v, q), at):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
 def test_attention_many_requests():
     """More requests than a block has threads; most of them short, one long, some without nodes."""
     args = make(random.Random(9), 700, 40, 3)
@@ -755,8 +817,8 @@ def test_steps_of_a_server():
         b.plan(i32(ctx), v.n, v.parent, state[0], v.k.shape[1])
         x = v.x[1]
         q = b.append_rope(v.rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], pool_k, pool_v)
-        wo, _, eo, _ = tree.attention(ref.to64(q)[:T], ref.to64(pool_k), ref.to64(pool_v), ctx, trees, state[0].cpu().numpy(), hd ** -0.5)
-        ref.close(ref.to64(out["o"][1])[:T], wo, eo, f"o of step {step}")
+        wo, _, eo, _ = tree.attention(ref.to64(q[:T]), ref.to64(pool_k), ref.to64(pool_v), ctx, trees, state[0].cpu().numpy(), hd ** -0.5)
+        ref.close(ref.to64(out["o"][1][:T]), wo, eo, f"o of step {step}")
         assert k_then is None and (out["after"] == 0).all()
         assert np.array_equal(v.held.cpu().numpy(), -(-(ctx + want[3]) // P))
 
