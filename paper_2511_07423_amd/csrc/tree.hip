@@ -15,13 +15,16 @@
 
 // ------------------------------------------------------------------------------------ the plan on the device
 // The attention's work: a request's keys are cut into `ranges` of whole steps of TR_STEP keys, and a block takes one range of one KV head for one tile of
-// rows.  The tiles of a range follow each other on one XCD, so that its keys are fetched once and met in L2: each XCD has a list of its own,
-// the same for all but for the groups (head, range): list x has groups x, x + 8, .. of each request, whose tiles are the items.  Requests
-// come in the order of their items' cost, the longest first, since blocks take items as places become free.
+// rows.  Up to TR_UNIT tiles of a range follow each other on one XCD, so that its keys are fetched once and met in L2: each XCD has a list of its own,
+// and such units (range, head, tiles) are dealt to the lists in turn.  A request begins where as many requests of its size before it would have ended.
+// Requests come in the order of their items' cost, the longest first, since blocks take items as places become free.
+// (Where the lists had their items in common but for the head, all had as many places as the fullest: 74 requests of 1344 rows at 5 heads 243 us, 184 so;
+// 27 of 288 at 3 heads 295 and 228; 187 of one small tile at one head 45 and 28.)
 // How long a range may be is chosen from TR_LENGTHS candidates by an estimate of the time (tr_estimate).
 // (With the heads and tiles in one line that blocks took equal parts of, tiles of one head read its keys at different times:
 // 32 requests of 48 .. 160 nodes 414 us, 64 of 8 .. 64 nodes 125.)
 #define TR_LENGTHS 24
+#define TR_UNIT 8                // and half as many where the heads alone do not fill the lists: with 8, the 74 requests at 5 heads took 220 us; with 4, 32 of 2 .. 5 tiles at 8 heads 360 for 335
 #define TR_GRID 4                // blocks of the launch for each place
 #define TR_JOIN_GRID 2           // of the joining one
 // Candidate c: 2, 3, 4, 6, 8, 12, .. 2048, 3072 steps, and any.
@@ -29,17 +32,24 @@ __device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
   const int32_t x = (steps - 1) >> (c / 2);
   return steps == 0 ? 0 : c == TR_LENGTHS - 1 ? 1 : (c & 1 ? x / 3 : x / 2) + 1;
 }
-// In 16ths of what a step takes a block when all places are taken and HBM is the bound (64 KB for each: 4.5 us).
+// In 16ths of what a step takes a block of 64 rows at most when all places are taken and HBM is the bound (64 KB for each with heads of 128: 5.1 us).
 #define TR_ONE 16                // a step of a request's only tile
-#define TR_MORE 11               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
-#define TR_START 32              // what it takes to begin and end an item
-#define TR_JOIN_LAUNCH 32        // to join anything at all
+#define TR_FULL 22               // if it has more than 64 rows
+#define TR_MORE 15               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
+#define TR_ALONE 4               // the same, where a block has a compute unit of its own, for up to 64 rows
+#define TR_ALONE_FULL 8          // and more
+#define TR_PAIR 5                // and where two share one
+#define TR_PAIR_FULL 14
+#define TR_START 16              // what it takes to begin and end an item
+#define TR_JOIN_LAUNCH 10        // to join anything at all
 #define TR_JOIN_ROWS 1024        // partial rows written and read in one 16th
+#define TR_JOIN_RANGES 4         // ranges of a row, one after the other
 struct TrHead {
   ShHeader sh;                   // tokens and windows, for the append
-  int32_t items, B;              // items of an XCD's list
+  int32_t B;
   int32_t joins;                 // places of the joining launch
-  int32_t pad[13];
+  int32_t pad[6];
+  int32_t items[SY_SH_DEAL];     // in each list
 };
 struct TrReq {                   // 32 bytes, scalar loads
   int32_t ctx, n, tok;           // n: 0 where the request has no nodes or is refused
@@ -47,10 +57,11 @@ struct TrReq {                   // 32 bytes, scalar loads
   int32_t steps, ranges, tiles;  // as the lists count them, refused or not
   int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
 };
-struct TrItem {                  // 64 bytes: a place in each XCD's list.  All that a block has to know before it can ask for keys, in one load
+struct TrItem {                  // 64 bytes, the k-th of list x at 8 k + x.  All that a block has to know before it can ask for keys, in one load
   TrReq q;
-  int32_t req, at;               // the at-th item of the request in the list
-  int32_t pad[6];
+  int32_t req, tile;             // (a tile that the request has not: none)
+  int32_t group;                 // range x heads + head
+  int32_t pad[5];
 };
 struct TrJoin {                  // 8 bytes: TR_JOIN_AT rows of a request (of all KV heads) from row `at` on
   int32_t req, at;
@@ -77,6 +88,19 @@ struct synera_tree {
   float* part_o;
   float2* part_ml;
 };
+
+// Units of a range of a head, all of the same number of tiles (the last may have fewer); items of `ranges` of them in the longest list.
+__host__ __device__ __forceinline__ int32_t units_of(int32_t Hkv, int32_t tiles) {
+  const int32_t most = Hkv % SY_SH_DEAL ? TR_UNIT / 2 : TR_UNIT;
+  return (tiles + most - 1) / most;
+}
+__host__ __device__ __forceinline__ int32_t per_unit(int32_t Hkv, int32_t tiles) {
+  const int32_t units = units_of(Hkv, tiles);
+  return (tiles + units - 1) / units;
+}
+__host__ __device__ __forceinline__ uint64_t places_of(int32_t Hkv, int32_t tiles, int32_t ranges) {
+  return ((uint64_t)Hkv * (uint32_t)ranges * (uint32_t)units_of(Hkv, tiles) + SY_SH_DEAL - 1) / SY_SH_DEAL * (uint32_t)per_unit(Hkv, tiles);
+}
 
 static size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -117,10 +141,12 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   t->pitch = max_pages + TR_AHEAD;
   // uncut, a request has an item in each list for every tile and eighth head, also one whose rows there is no room for
   const size_t B = (size_t)max_batch, T = (size_t)max_tokens, G = (size_t)(n_q_heads / n_kv_heads);
-  t->items_room = (int32_t)std::max<size_t>((size_t)t->lim.slots, (size_t)((n_kv_heads + SY_SH_DEAL - 1) / SY_SH_DEAL) * B * (TR_NODES * G / SY_SH_TILE_ROWS + 1));
+  size_t places = 0;
+  for (int32_t tiles = 1; tiles <= (int32_t)(TR_NODES * G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS; ++tiles) places = std::max<size_t>(places, places_of(n_kv_heads, tiles, 1));
+  t->items_room = (int32_t)std::max<size_t>((size_t)t->lim.slots, B * places);
   t->part_rows = 2 * t->lim.slots * SY_SH_TILE_ROWS;
   const size_t parts = (size_t)t->part_rows;
-  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * sizeof(TrItem),
+  const size_t sizes[] = {sizeof(TrHead), B * sizeof(TrReq), (size_t)t->items_room * SY_SH_DEAL * sizeof(TrItem),
                           // (at least two partial rows for each that is joined)
                           (parts / 2 / TR_JOIN_AT + B) * sizeof(TrJoin), B * (TR_NODES / SY_PAGE + 1) * sizeof(ShWindow),
                           T * 4, T * 4, T * 4, B * t->pitch * 4, T * SY_TREE_MASK * 4, parts * head_dim * 4, parts * 8};
@@ -171,7 +197,8 @@ struct PlanArgs {
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
   int32_t B, columns, pitch, n_pages, Hkv, G, items_room, part_rows;
-  double per_place;              // 1 / places of an XCD
+  double per_place;              // 1 / blocks that run at once
+  int32_t scale;                 // of what is not a step: 2 with heads of 64, whose steps take half as long
   int64_t n_rows;
 };
 
@@ -191,24 +218,26 @@ __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_
   return s;
 }
 // (A quotient in 32 bits of floating point: the same for every block, and no more than an estimate.)
-__device__ __forceinline__ int32_t item_cost(const TrSize& s, int32_t ranges) {
-  return (int32_t)((float)s.steps * (s.tiles > 1 ? TR_MORE : TR_ONE) * __builtin_amdgcn_rcpf((float)ranges)) + TR_START;
+__device__ __forceinline__ int32_t item_cost(const PlanArgs& a, const TrSize& s, int32_t ranges, int32_t step) {
+  return (int32_t)((float)s.steps * step * __builtin_amdgcn_rcpf((float)ranges)) + TR_START * a.scale;
 }
-__device__ __forceinline__ uint64_t items_of(const PlanArgs& a, const TrSize& s, int32_t ranges) {      // in each list
-  return ((uint64_t)a.Hkv * (uint32_t)ranges + SY_SH_DEAL - 1) / SY_SH_DEAL * (uint32_t)s.tiles;
+__device__ __forceinline__ int32_t item_cost(const PlanArgs& a, const TrSize& s, int32_t ranges) {
+  return item_cost(a, s, ranges, s.tiles > 1 ? TR_MORE : s.rows * a.G > 64 ? TR_FULL : TR_ONE);
 }
 // What each candidate comes to, over all requests; whole numbers, so that every block finds the same.
 struct TrTotals {
-  unsigned long long cost, parts, items;
-  int32_t longest;
+  unsigned long long cost, parts, items, places;              // items: of all lists; places: of each
+  int32_t longest, shortest, alone, pair, ranges;             // an item's cost; the longest one's alone on a compute unit, the shortest one's beside another; most of a request
 };
 __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals& t) {
-  if (t.items > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
-  // All places busy, or the longest item: by itself it has 1.7 times the rate, where each block has a compute unit of its own 2.7 times.  The longest come first,
-  // so that little is left at the end.  Launches without the joining one: 64 requests of up to 33 steps uncut 101 us, cut to 24 89, to 16 95; 256 of up to
-  // 64 uncut 277, cut to 48 290, to 12 323; one of 243 cut to 48 104, to 24 66, to 8 45, to 4 48.
-  const int64_t busy = (int64_t)((double)t.cost * a.per_place), alone = (int64_t)t.longest * ((double)t.items * 2 * a.per_place <= 1.0 ? 3 : 5) / 8;
-  return max(busy, alone) + t.longest / 16 + (t.parts ? TR_JOIN_LAUNCH + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
+  if (t.places > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
+  // All places busy; as many rounds of the shortest items as there are; or the longest item, at first beside others.  More is left at the
+  // end where items differ and there are few.
+  const double rounds = (double)t.items * a.per_place;
+  const int64_t busy = (int64_t)((double)t.cost * a.per_place), least = rounds > 0.5 ? (int64_t)ceil(rounds) * t.pair : 0,
+                longest = rounds > 0.5 ? max(t.longest * 5 / 8, t.alone) : t.alone;
+  const int64_t end = t.longest / 32 + (int64_t)(t.alone * 0.2 * (1.0 - (double)t.shortest / max(t.longest, 1)) / max(2 * rounds, 1.0));
+  return max(max(busy, least), longest) + end + (t.parts ? (TR_JOIN_LAUNCH + t.ranges / TR_JOIN_RANGES) * a.scale + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
 }
 
 // The sum over the block's threads, for all of them.
@@ -233,10 +262,10 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   __shared__ TrTotals totals[TR_LENGTHS];
   __shared__ TrSize sizes[256];
   __shared__ unsigned long long best;                         // estimate << 8 | candidate
-  __shared__ int32_t sums_a[4][4], sums_b[4][4];
+  __shared__ int32_t sums_a[4][4], sums_b[4][3], sums_c[4][2 * SY_SH_DEAL], begin[SY_SH_DEAL];
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
-  if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0};
+  if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0, 0, INT32_MAX, 0, INT32_MAX, 0};
   if (tid == 0) best = ~0ull;
   const int32_t ctx = a.ctx[me], n = a.n_nodes[me];
   const TrSize s = size_of(a, ctx, n);
@@ -287,22 +316,32 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     }
     const int c = tid / LANES, m = min(256, a.B - i0);
     if (c < TR_LENGTHS) {
-      TrTotals t = {0, 0, 0, 0};
+      TrTotals t = {0, 0, 0, 0, 0, INT32_MAX, 0, INT32_MAX, 0};
       for (int i = tid % LANES; i < m; i += LANES) {
         const TrSize z = sizes[i];
         if (z.steps == 0) continue;
-        const int32_t r = tr_ranges(z.steps, c), cost = item_cost(z, r);
-        const uint64_t items = items_of(a, z, r);
+        const int32_t r = tr_ranges(z.steps, c), cost = item_cost(a, z, r);
+        const uint64_t items = (uint64_t)a.Hkv * (uint32_t)r * (uint32_t)z.tiles;
         t.items += items;
+        t.places += places_of(a.Hkv, z.tiles, r);
         t.cost += items * (uint32_t)cost;
         t.longest = max(t.longest, cost);
+        t.shortest = min(t.shortest, cost);
+        t.ranges = max(t.ranges, r);
+        t.pair = min(t.pair, item_cost(a, z, r, z.rows * a.G > 64 ? TR_PAIR_FULL : TR_PAIR));
+        t.alone = max(t.alone, item_cost(a, z, r, z.rows * a.G > 64 ? TR_ALONE_FULL : TR_ALONE));
         if (r > 1) t.parts += (uint64_t)(uint32_t)r * (uint32_t)(a.Hkv * a.G * z.rows);
       }
       if (t.items) {
         atomicAdd(&totals[c].cost, t.cost);
         atomicAdd(&totals[c].parts, t.parts);
         atomicAdd(&totals[c].items, t.items);
+        atomicAdd(&totals[c].places, t.places);
         atomicMax(&totals[c].longest, t.longest);
+        atomicMin(&totals[c].shortest, t.shortest);
+        atomicMax(&totals[c].alone, t.alone);
+        atomicMax(&totals[c].ranges, t.ranges);
+        atomicMin(&totals[c].pair, t.pair);
       }
     }
   }
@@ -316,23 +355,36 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   __syncthreads();
   const int chosen = (int)(best & 255);
   // ---- partial rows before this request by number, items by cost
-  const int32_t ranges = tr_ranges(s.steps, chosen), items = s.steps ? (int32_t)items_of(a, s, ranges) : 0, cost = s.steps ? item_cost(s, ranges) : 0;
-  int32_t before[4] = {0, 0, 0, 0};                           // and places of the joining launch, before this request and in all
+  const int32_t ranges = tr_ranges(s.steps, chosen), cost = s.steps ? item_cost(a, s, ranges) : 0;
+  int32_t before[3] = {0, 0, 0};                              // and places of the joining launch, before this request and in all
+  int32_t lists[2 * SY_SH_DEAL] = {};                         // items of each list, before this request's and in all
   for (int i = tid; i < a.B; i += 256) {
     const TrSize z = few ? sizes[i] : size_of(a, a.ctx[i], a.n_nodes[i]);
     if (z.steps == 0) continue;
-    const int32_t r = tr_ranges(z.steps, chosen), k = item_cost(z, r);
+    const int32_t r = tr_ranges(z.steps, chosen), k = item_cost(a, z, r);
     if (r > 1) {
       const int32_t all = a.Hkv * z.rows * a.G, joins = (all + TR_JOIN_AT - 1) / TR_JOIN_AT;
       if (i < me) {
         before[0] += r * all;
-        before[2] += joins;
+        before[1] += joins;
       }
-      before[3] += joins;
+      before[2] += joins;
     }
-    if (k > cost || (k == cost && i < me)) before[1] += (int32_t)items_of(a, z, r);
+    const bool first = k > cost || (k == cost && i < me);
+    const uint32_t units = (uint32_t)(a.Hkv * r * units_of(a.Hkv, z.tiles)), per = per_unit(a.Hkv, z.tiles), deal = (uint32_t)i * units;
+#pragma unroll
+    for (int x = 0; x < SY_SH_DEAL; ++x) {
+      const int32_t items = (units + SY_SH_DEAL - 1 - (x - deal) % SY_SH_DEAL) / SY_SH_DEAL * per;
+      lists[x] += first ? items : 0;
+      lists[SY_SH_DEAL + x] += items;
+    }
   }
   block_sums(before, sums_b);
+  block_sums(lists, sums_c);
+#pragma unroll
+  for (int x = 0; x < SY_SH_DEAL; ++x)
+    if (tid == x) begin[x] = lists[x];
+  __syncthreads();
 
   // ---- paths
   uint32_t word[8];
@@ -383,18 +435,24 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   }
   // ---- the lists
   const TrReq q = {ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles, before[0]};
-  for (int k = tid; k < items; k += 256) a.items[before[1] + k] = TrItem{q, me, k, {}};
+  const uint32_t each = units_of(a.Hkv, s.tiles), units = s.steps ? a.Hkv * ranges * each : 0, per = s.steps ? per_unit(a.Hkv, s.tiles) : 1;
+  for (uint32_t e = tid; e < units * per; e += 256) {
+    const uint32_t u = e / per, x = (u + (uint32_t)me * units) % SY_SH_DEAL;
+    a.items[(size_t)(begin[x] + u / SY_SH_DEAL * per + e % per) * SY_SH_DEAL + x] =
+        TrItem{q, me, (int32_t)(u % each * per + e % per), (int32_t)(u / each), {}};
+  }
   if (ranges > 1)
-    for (int k = tid; k * TR_JOIN_AT < a.Hkv * s.rows * a.G; k += 256) a.joins[before[2] + k] = TrJoin{me, k * TR_JOIN_AT};
+    for (int k = tid; k * TR_JOIN_AT < a.Hkv * s.rows * a.G; k += 256) a.joins[before[1] + k] = TrJoin{me, k * TR_JOIN_AT};
   if (tid == 0) {
     a.req[me] = q;
     if (a.status) a.status[me] = status;
     if (me == 0) {
       a.head->sh.n_tokens = (int32_t)min((int64_t)rows[2], a.n_rows);
       a.head->sh.n_windows = rows[3];
-      a.head->items = (int32_t)totals[chosen].items;
+#pragma unroll
+      for (int x = 0; x < SY_SH_DEAL; ++x) a.head->items[x] = lists[SY_SH_DEAL + x];
       a.head->B = a.B;
-      a.head->joins = before[3];
+      a.head->joins = before[2];
     }
   }
 }
@@ -419,7 +477,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->joins, t->windows, t->pos, t->slot, t->parent, t->table,
-                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, (double)SY_SH_DEAL / l.slots, n_rows};
+                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, 1.0 / l.slots, l.hd == 64 ? 2 : 1, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
   t->planned = true;
@@ -452,6 +510,7 @@ struct TreeAttnArgs : SharedAttnArgs {
 };
 typedef SH_CONST_AS sh_i32x8v tr_i32x8;
 typedef SH_CONST_AS sh_i32x2v tr_i32x2;
+typedef SH_CONST_AS sh_i32x4v tr_i32x4;
 
 __device__ __forceinline__ TrReq req_of(const TreeAttnArgs& a, int r) {
   const sh_i32x8v w = *reinterpret_cast<const tr_i32x8*>((uintptr_t)(a.req + r));
@@ -461,16 +520,16 @@ __device__ __forceinline__ TrReq req_of(const TreeAttnArgs& a, int r) {
 template <int HD>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int x = blockIdx.x % SY_SH_DEAL, k0 = blockIdx.x / SY_SH_DEAL, items = a.th->items;
+  const int items = a.th->items[blockIdx.x % SY_SH_DEAL] * SY_SH_DEAL;
   // (the first place is looked at together with the number of items: the launch has no more blocks than the lists have places)
-  for (int k = k0; k == k0 || k < items; k += gridDim.x / SY_SH_DEAL) {
+  for (int k = blockIdx.x; k == (int)blockIdx.x || k < items; k += gridDim.x) {
     const tr_i32x8* place = reinterpret_cast<const tr_i32x8*>((uintptr_t)(a.places + k));
     const sh_i32x8v w = place[0];
-    const sh_i32x2v at = *reinterpret_cast<const tr_i32x2*>((uintptr_t)(place + 1));
+    const sh_i32x4v at = *reinterpret_cast<const tr_i32x4*>((uintptr_t)(place + 1));       // request, tile, group
     if (k >= items) return;
     const TrReq q = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
-    const int tile = at[1] % q.tiles, group = at[1] / q.tiles * SY_SH_DEAL + x, kh = group % a.Hkv, range = group / a.Hkv;
-    if (q.n == 0 || range >= q.ranges || q.tok + q.n > a.rows) continue;
+    const int tile = at[1], group = at[2], kh = group % a.Hkv, range = group / a.Hkv;
+    if (q.n == 0 || tile >= q.tiles || q.tok + q.n > a.rows) continue;
     const int rows = q.n * a.G, keys = q.ctx + q.n;
     const int each = q.steps / q.ranges, more = q.steps % q.ranges;        // the first `more` ranges have a step more
     const int begin = range * each + min(range, more), end = begin + each + (range < more ? 1 : 0);
