@@ -91,15 +91,10 @@ struct synera_tree {
 
 // Units of a range of a head, all of the same number of tiles (the last may have fewer); items of `ranges` of them in the longest list.
 __host__ __device__ __forceinline__ int32_t units_of(int32_t Hkv, int32_t tiles) {
-  const int32_t most = Hkv % SY_SH_DEAL ? TR_UNIT / 2 : TR_UNIT;
-  return (tiles + most - 1) / most;
+  return Hkv % SY_SH_DEAL ? (tiles + TR_UNIT / 2 - 1) / (TR_UNIT / 2) : (tiles + TR_UNIT - 1) / TR_UNIT;
 }
-__host__ __device__ __forceinline__ int32_t per_unit(int32_t Hkv, int32_t tiles) {
-  const int32_t units = units_of(Hkv, tiles);
-  return (tiles + units - 1) / units;
-}
-__host__ __device__ __forceinline__ uint64_t places_of(int32_t Hkv, int32_t tiles, int32_t ranges) {
-  return ((uint64_t)Hkv * (uint32_t)ranges * (uint32_t)units_of(Hkv, tiles) + SY_SH_DEAL - 1) / SY_SH_DEAL * (uint32_t)per_unit(Hkv, tiles);
+__host__ __device__ __forceinline__ uint64_t places_of(int32_t Hkv, int32_t units, int32_t per, int32_t ranges) {
+  return ((uint64_t)(uint32_t)(Hkv * units) * (uint32_t)ranges + SY_SH_DEAL - 1) / SY_SH_DEAL * (uint32_t)per;
 }
 
 static size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -142,7 +137,10 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
   // uncut, a request has an item in each list for every tile and eighth head, also one whose rows there is no room for
   const size_t B = (size_t)max_batch, T = (size_t)max_tokens, G = (size_t)(n_q_heads / n_kv_heads);
   size_t places = 0;
-  for (int32_t tiles = 1; tiles <= (int32_t)(TR_NODES * G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS; ++tiles) places = std::max<size_t>(places, places_of(n_kv_heads, tiles, 1));
+  for (int32_t tiles = 1; tiles <= (int32_t)(TR_NODES * G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS; ++tiles) {
+    const int32_t units = units_of(n_kv_heads, tiles);
+    places = std::max<size_t>(places, places_of(n_kv_heads, units, (tiles + units - 1) / units, 1));
+  }
   t->items_room = (int32_t)std::max<size_t>((size_t)t->lim.slots, B * places);
   t->part_rows = 2 * t->lim.slots * SY_SH_TILE_ROWS;
   const size_t parts = (size_t)t->part_rows;
@@ -197,7 +195,7 @@ struct PlanArgs {
   int32_t *pos, *slot, *parents, *pages;
   uint32_t* masks;
   int32_t B, columns, pitch, n_pages, Hkv, G, items_room, part_rows;
-  double per_place;              // 1 / blocks that run at once
+  float per_place;               // 1 / blocks that run at once
   int32_t scale;                 // of what is not a step: 2 with heads of 64, whose steps take half as long
   int64_t n_rows;
 };
@@ -205,9 +203,10 @@ struct PlanArgs {
 // What a request's lengths alone say of it; every block forms it for all of them.
 struct TrSize {
   int32_t rows, windows, steps, tiles;
+  int32_t units, per;            // tiles of a unit
 };
 __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_t n) {
-  TrSize s = {0, 0, 0, 0};
+  TrSize s = {0, 0, 0, 0, 0, 1};
   if (n < 0 || n > TR_NODES) return s;
   s.rows = n;
   const int64_t keys = (int64_t)ctx + n;
@@ -215,6 +214,8 @@ __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_
   s.windows = (int32_t)((keys - 1) / SY_PAGE - ctx / SY_PAGE + 1);
   s.steps = (int32_t)((keys + TR_STEP - 1) / TR_STEP);
   s.tiles = (n * a.G + SY_SH_TILE_ROWS - 1) / SY_SH_TILE_ROWS;
+  s.units = units_of(a.Hkv, s.tiles);
+  s.per = (s.tiles + s.units - 1) / s.units;
   return s;
 }
 // (A quotient in 32 bits of floating point: the same for every block, and no more than an estimate.)
@@ -233,19 +234,20 @@ __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals
   if (t.places > (unsigned long long)a.items_room || t.parts > (unsigned long long)a.part_rows) return INT64_MAX;
   // All places busy; as many rounds of the shortest items as there are; or the longest item, at first beside others.  More is left at the
   // end where items differ and there are few.
-  const double rounds = (double)t.items * a.per_place;
-  const int64_t busy = (int64_t)((double)t.cost * a.per_place), least = rounds > 0.5 ? (int64_t)ceil(rounds) * t.pair : 0,
-                longest = rounds > 0.5 ? max(t.longest * 5 / 8, t.alone) : t.alone;
-  const int64_t end = t.longest / 32 + (int64_t)(t.alone * 0.2 * (1.0 - (double)t.shortest / max(t.longest, 1)) / max(2 * rounds, 1.0));
+  const float rounds = (float)t.items * a.per_place;
+  const int64_t busy = (int64_t)((float)t.cost * a.per_place), least = rounds > 0.5f ? (int64_t)ceilf(rounds) * t.pair : 0,
+                longest = rounds > 0.5f ? max(t.longest * 5 / 8, t.alone) : t.alone;
+  const int64_t end = t.longest / 32 + (int64_t)(t.alone * 0.2f * (1.f - (float)t.shortest * __builtin_amdgcn_rcpf((float)max(t.longest, 1))) *
+                                                 __builtin_amdgcn_rcpf(fmaxf(2.f * rounds, 1.f)));
   return max(max(busy, least), longest) + end + (t.parts ? (TR_JOIN_LAUNCH + t.ranges / TR_JOIN_RANGES) * a.scale + (int64_t)(t.parts / TR_JOIN_ROWS) : 0);
 }
 
 // The sum over the block's threads, for all of them.
 template <int N>
 __device__ __forceinline__ void block_sums(int32_t (&v)[N], int32_t (*parts)[N]) {
+  for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-    for (int o = 1; o < 64; o <<= 1) v[k] += __shfl_xor(v[k], o);
+    for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
     for (int k = 0; k < N; ++k) parts[threadIdx.x >> 6][k] = v[k];
@@ -321,10 +323,11 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
         const TrSize z = sizes[i];
         if (z.steps == 0) continue;
         const int32_t r = tr_ranges(z.steps, c), cost = item_cost(a, z, r);
-        const uint64_t items = (uint64_t)a.Hkv * (uint32_t)r * (uint32_t)z.tiles;
+        // (more items than 32 bits count are more than there is room for)
+        const uint32_t items = (uint32_t)min((uint64_t)(uint32_t)(a.Hkv * z.tiles) * (uint32_t)r, (uint64_t)0xFFFFFFFFu);
         t.items += items;
-        t.places += places_of(a.Hkv, z.tiles, r);
-        t.cost += items * (uint32_t)cost;
+        t.places += places_of(a.Hkv, z.units, z.per, r);
+        t.cost += (uint64_t)items * (uint32_t)cost;
         t.longest = max(t.longest, cost);
         t.shortest = min(t.shortest, cost);
         t.ranges = max(t.ranges, r);
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
       before[2] += joins;
     }
     const bool first = k > cost || (k == cost && i < me);
-    const uint32_t units = (uint32_t)(a.Hkv * r * units_of(a.Hkv, z.tiles)), per = per_unit(a.Hkv, z.tiles), deal = (uint32_t)i * units;
+    const uint32_t units = (uint32_t)(a.Hkv * r * z.units), per = z.per, deal = (uint32_t)i * units;
 #pragma unroll
     for (int x = 0; x < SY_SH_DEAL; ++x) {
       const int32_t items = (units + SY_SH_DEAL - 1 - (x - deal) % SY_SH_DEAL) / SY_SH_DEAL * per;
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   }
   // ---- the lists
   const TrReq q = {ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles, before[0]};
-  const uint32_t each = units_of(a.Hkv, s.tiles), units = s.steps ? a.Hkv * ranges * each : 0, per = s.steps ? per_unit(a.Hkv, s.tiles) : 1;
+  const uint32_t each = s.units, units = a.Hkv * ranges * each, per = s.per;
   for (uint32_t e = tid; e < units * per; e += 256) {
     const uint32_t u = e / per, x = (u + (uint32_t)me * units) % SY_SH_DEAL;
     a.items[(size_t)(begin[x] + u / SY_SH_DEAL * per + e % per) * SY_SH_DEAL + x] =
@@ -477,7 +480,7 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->joins, t->windows, t->pos, t->slot, t->parent, t->table,
-                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, 1.0 / l.slots, l.hd == 64 ? 2 : 1, n_rows};
+                      t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, 1.0f / l.slots, l.hd == 64 ? 2 : 1, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
   t->planned = true;

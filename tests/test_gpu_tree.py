@@ -207,6 +207,20 @@ def test_attention_one_request(ctx, n, hd):
         check_attention(hq, hkv, hd, np.array([ctx]), [grow(rng, n, shape)], table, need, ctx + n)
 
 
+@pytest.mark.parametrize("hq,hkv", [(128, 8), (80, 5), (33, 11), (10, 10), (48, 3)])
+def test_attention_of_many_rows(hq, hkv):
+    """Requests of many tiles and of one, whose units begin in different lists, some of no nodes in between, keys cut and whole."""
+    rng = random.Random(hq)
+    trees = [grow(rng, n, rng.choice(("tree", "wide", "chain"))) for n in (200, 3, 0, 77, 256, 1, 130)]
+    for ctx in ((0, 700, 5, 90, 31, 1500, 128), (20, 0, 0, 3, 0, 17, 0)):
+        need = [-(-(c + len(t)) // P) for c, t in zip(ctx, trees)]
+        ids, table, at = rng.sample(range(sum(need)), sum(need)), np.full((len(need), max(need)), -1, np.int32), 0
+        for i, k in enumerate(need):
+            table[i, :k] = ids[at:at + k]
+            at += k
+        check_attention(hq, hkv, 64, np.array(ctx), trees, table, sum(need), 4)
+
+
 def test_attention_of_a_long_context():
     """More steps than any length of ranges but the last few covers with what room there is for partial results."""
     rng, need = random.Random(12), -(-(150000 + 21) // P)
