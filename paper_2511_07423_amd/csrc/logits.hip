@@ -11,7 +11,7 @@
 // integers, so the order of the atomics does not show.
 // Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides; those that are allowed and have a word
 // are formed on the way.  (Nearly every wavefront meets some: with a branch for each value 2048 x 128256 masked took 325 us; formed behind the
-// others, from memory, 300; this way 198, as long as a plain copy of the logits.)
+// others, from memory, 300; this way 202, as long as a plain copy of the logits.)
 // Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Rows pass those
 // tokens as they are, and behind a barrier each is formed for each row, by a lane that counts it along the list.  (198 trees of 64 nodes in a
 // vocabulary of 1096: 67 us; counted on the way, where one lane keeps its wavefront waiting, 323.)  Longer paths are added to the words before a
@@ -100,7 +100,7 @@ template <> __device__ __forceinline__ u32x4 lg_masked<bf16_t>(u32x4 v, uint32_t
 template <> __device__ __forceinline__ u32x4 lg_masked<_Float16>(u32x4 v, uint32_t bits) { return lg_masked16<0xFC00u>(v, bits); }
 
 // ONCE: the output is marked as not wanted again.
-// (6 wavefronts a SIMD: three blocks a compute unit, as many as LDS holds.  Two registers more: 2048 x 128256 masked 198 -> 216 us.)
+// (6 wavefronts a SIMD: three blocks a compute unit, as many as LDS holds.  Three registers more, spilled: 2048 x 128256 masked 202 -> 220 us.)
 template <typename T, bool MASK, bool ONCE>
 __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(LogitsArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T), PIECES = LG_SLICE / VEC, EACH = PIECES / LG_THREADS, ROWS = LG_FLY / EACH;
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
         uint32_t todo = (has_word[c * VEC / 32] >> (c * VEC % 32)) & allowed;
         if (a.in_place && !todo && allowed == ALL) continue;
         // Under a mask few values of a piece are to be formed: one at a time.  Without one, all alike and without branches.  (2048 x 128256 bf16: under a mask
-        // that leaves 3 % 198 and 226 us, without a mask 234 and 200; both ways in one kernel take too many registers.)
+        // that leaves 3 % 202 and 226 us, without a mask 234 and 200; both ways in one kernel take too many registers.)
         if constexpr (MASK) {
           while (todo) {
             const int k = __builtin_ctz(todo);
