@@ -112,6 +112,7 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
   __shared__ uint32_t has_word[LG_SLICE / 32];
   __shared__ uint32_t on_path[LG_NODES][LG_NODES / 32 + 1];   // (+ 1: neighbours on other banks)
   __shared__ int32_t parents[LG_NODES];
+  __shared__ float given[2 * LG_THREADS];                     // biases
   __shared__ uint32_t listed[LG_NODES];                       // token in the slice | node << 16 | LG_FIRST: the first one of its token
   __shared__ int32_t n_listed;
   __shared__ int32_t held;
@@ -166,14 +167,22 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
   for (int u = 0; u < LG_EARLY; ++u) seen[u] = tid + u * LG_THREADS < len ? h[tid + u * LG_THREADS] : -1;
 #pragma unroll
   for (int u = 0; u < 2; ++u) named[u] = a.d.d_bias_id && tid + u * LG_THREADS < a.d.bias_columns ? a.d.d_bias_id[biases + tid + u * LG_THREADS] : -1;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (a.d.d_bias_id && tid + u * LG_THREADS < a.d.bias_columns) given[tid + u * LG_THREADS] = a.d.d_bias[biases + tid + u * LG_THREADS];
   if (masked_paths && tid < rows) {
     up0 = a.d.d_parent[first + tid];
     token0 = a.d.d_tokens[first + tid];
+    if (up0 >= tid) up0 = -1;
   }
   for (int w = tid; w < (n + 3) / 4; w += LG_THREADS) reinterpret_cast<u32x4*>(word)[w] = u32x4{0, 0, 0, 0};
   if (tid < LG_SLICE / 32) has_word[tid] = 0;
   if (tid == 0) n_listed = 0;
-  if (tid < LG_NODES) parents[tid] = up0;
+  if (tid < LG_NODES) {
+    parents[tid] = up0;
+#pragma unroll
+    for (int w = 0; w < LG_NODES / 32; ++w) on_path[tid][w] = 0;
+  }
   __syncthreads();
   auto slot = [&](int32_t id) { return id < 0 ? 0xFFFFFFFFu : (uint32_t)(id - v0); };      // of a token in the slice: below n
   auto touch = [&](uint32_t t, uint32_t before) {             // by the first one that finds nothing
@@ -206,25 +215,30 @@ __global__ __launch_bounds__(LG_THREADS, MASK ? 6 : 4) void logits_kernel(Logits
     }
   }
   if (masked_paths && tid < rows) {
-    uint32_t* mine = on_path[tid];
-#pragma unroll
-    for (int w = 0; w < LG_NODES / 32; ++w) mine[w] = 0;
-    for (int at = tid, up = up0;;) {
-      mine[at / 32] |= 1u << (at % 32);
-      if (up < 0 || up >= at) break;
-      at = up;
-      up = parents[at];
-    }
     const uint32_t t = slot(token0);
     if (t < (uint32_t)n) {
       const uint32_t old = atomicOr(&word[t], LG_PATH);
       touch(t, old);
       listed[atomicAdd(&n_listed, 1)] = t | (uint32_t)tid << 16 | (old & LG_PATH ? 0u : LG_FIRST);
     }
+    // The path of each row that this block takes: towards the root node numbers fall, so that its words are written one by one.
+    if (tid >= (int)blockIdx.z && (tid - (int)blockIdx.z) % a.splits == 0) {
+      uint32_t bits = 1u << (tid % 32);
+      int w = tid / 32;
+      for (int up = up0; up >= 0; up = parents[up]) {
+        if (up / 32 != w) {
+          on_path[tid][w] = bits;
+          bits = 0;
+          w = up / 32;
+        }
+        bits |= 1u << (up % 32);
+      }
+      on_path[tid][w] = bits;
+    }
   }
   __syncthreads();
   LgParams params = {a.d.d_repetition ? a.d.d_repetition[i] : 1.f, 1.f, a.d.d_presence ? a.d.d_presence[i] : 0.f,
-                     a.d.d_frequency ? a.d.d_frequency[i] : 0.f, a.d.d_bias + biases};
+                     a.d.d_frequency ? a.d.d_frequency[i] : 0.f, given};
   params.inv = 1.f / params.rho;
   // ---- the rows
   auto word_of = [&](int t) {                                 // of token t of the slice, 0 where some path has it
