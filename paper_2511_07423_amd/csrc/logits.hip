@@ -14,7 +14,7 @@
 // others, from memory, 300; this way 202, as long as a plain copy of the logits.)
 // Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Rows pass those
 // tokens as they are, and behind a barrier each is formed for each row, by a lane that counts it along the list.  (198 trees of 64 nodes in a
-// vocabulary of 1096: 67 us; counted on the way, where one lane keeps its wavefront waiting, 323.)  Longer paths are added to the words before a
+// vocabulary of 1096: 68 us; counted on the way, where one lane keeps its wavefront waiting, 323.)  Longer paths are added to the words before a
 // row, and taken away where the next row is not behind it.
 #define LG_SLICE 8192
 #define LG_EVEN 64               // slices are as long as each other: 9 x 64 rows of 9000 to 12000 tokens 17.6 -> 14.9 us
@@ -408,7 +408,7 @@ extern "C" int32_t synera_logits_adjust(const synera_logits_desc* desc, const vo
   LogitsArgs a = {d, d_in, d_out, 1, 0, in_place, !in_place && beyond_caches((size_t)(d.rows * d.vocab * size))};
   const int64_t slices = (d.vocab + LG_SLICE - 1) / LG_SLICE, each = (d.rows + B - 1) / B;
   // Blocks that share a request's rows, up to two rounds of three blocks a compute unit: with more, what each makes from the history and the paths costs more
-  // than full rounds save (3 x 64 rows of 123964, 1536 and 4096 blocks: 40 and 61 us; 64 x 16 of 32000: 42 and 42).
+  // than full rounds save (3 x 64 rows of 123964, 1536 and 3968 blocks: 34 and 44 us; 198 x 64 of 1096 68 and 85; 64 x 16 of 32000 41 and 42, 1024: 44).
   a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(each, 1536 / (slices * B))), 65535);
   a.slice = (int32_t)(((d.vocab + slices - 1) / slices + LG_EVEN - 1) / LG_EVEN * LG_EVEN);
   const dim3 grid((uint32_t)slices, (uint32_t)B, (uint32_t)a.splits);
