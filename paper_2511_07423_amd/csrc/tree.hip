@@ -37,7 +37,7 @@ __device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
 #define TR_FULL 22               // if it has more than 64 rows
 #define TR_MORE 15               // of one of several, which share what is fetched: the matrix cores' and the softmax's time
 #define TR_ALONE 4               // the same, where a block has a compute unit of its own, for up to 64 rows
-#define TR_ALONE_FULL 8          // and more
+#define TR_ALONE_FULL 10         // and more
 #define TR_PAIR 5                // and where two share one
 #define TR_PAIR_FULL 14
 #define TR_START 16              // what it takes to begin and end an item
