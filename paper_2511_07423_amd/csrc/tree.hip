@@ -23,11 +23,11 @@
 // How long a range may be is chosen from TR_LENGTHS candidates by an estimate of the time (tr_estimate).
 // (With the heads and tiles in one line that blocks took equal parts of, tiles of one head read its keys at different times:
 // 32 requests of 48 .. 160 nodes 414 us, 64 of 8 .. 64 nodes 125.)
-#define TR_LENGTHS 24
+#define TR_LENGTHS 22
 #define TR_UNIT 8                // and half as many where the heads alone do not fill the lists: with 8, the 74 requests at 5 heads took 220 us; with 4, 32 of 2 .. 5 tiles at 8 heads 360 for 335
 #define TR_GRID 4                // blocks of the launch for each place
 #define TR_JOIN_GRID 2           // of the joining one
-// Candidate c: 2, 3, 4, 6, 8, 12, .. 2048, 3072 steps, and any.
+// Candidate c: 2, 3, 4, 6, 8, 12, .. 1536, 2048 steps, and any.
 __device__ __forceinline__ int32_t tr_ranges(int32_t steps, int c) {
   const int32_t x = (steps - 1) >> (c / 2);
   return steps == 0 ? 0 : c == TR_LENGTHS - 1 ? 1 : (c & 1 ? x / 3 : x / 2) + 1;
