@@ -26,7 +26,7 @@ extern "C" {
  * columns.  A call makes every row hold what its lengths need, ceil((L_i + n_i) / 16) pages:
  *   - rows that hold fewer take pages from the top of the stack, in the order of requests and columns.  Where the stack as it was
  *     before the call does not cover a request's and all those before it, the request and all later ones that need pages
- *     are refused (ENOSPC);
+ *     are refused (ENOSPC): their rows stay as they were, with fewer pages than their lengths need (synera_tree_plan_held refuses such requests);
  *   - rows that hold more return those behind, all but their first d_shared[i] columns; the first one returned ends on top.
  * So a step that is taken back leaves the stack as it was.  Entries behind a row's held columns and behind the stack's top stay.
  * Then each token's place, for token j of request i in row cu[i] + j:
@@ -75,6 +75,16 @@ int32_t synera_tree_destroy(synera_tree* tree);
  */
 int32_t synera_tree_plan(synera_tree* tree, int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_nodes, const int32_t* d_parent,
                          int64_t n_rows, const int32_t* d_table, int32_t columns, int32_t n_pages_in_pool, int32_t* d_status, void* stream);
+
+/*
+ * The same behind synera_pages_update: of each row of the table only the first d_held[i] columns are the request's own (i32 [B], NULL: all).  A request that
+ * synera_pages_update refused, whose row ends in entries that are no pages or by now another request's, is refused here too:
+ * ENOSPC where its tokens and nodes need more than d_held[i] pages, EINVAL where that is outside 0 .. columns.  A plan without d_held takes
+ * all entries that a request's lengths reach for its own.
+ */
+int32_t synera_tree_plan_held(synera_tree* tree, int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_nodes, const int32_t* d_parent,
+                              int64_t n_rows, const int32_t* d_table, int32_t columns, const int32_t* d_held, int32_t n_pages_in_pool,
+                              int32_t* d_status, void* stream);
 
 /* As synera_append_rope, each node at its places in text and cache.  Tensors have room for the plan's n_rows tokens. */
 int32_t synera_tree_append_rope(synera_tree* tree, const synera_rope* rope, int32_t dtype, const synera_heads* q,

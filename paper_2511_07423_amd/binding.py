@@ -172,6 +172,8 @@ _lib.synera_tree_destroy.restype = C.c_int32
 _lib.synera_tree_destroy.argtypes = [_vp]
 _lib.synera_tree_plan.restype = C.c_int32
 _lib.synera_tree_plan.argtypes = [_vp, C.c_int32, _vp, _vp, _vp, C.c_int64, _vp, C.c_int32, C.c_int32, _vp, _vp]
+_lib.synera_tree_plan_held.restype = C.c_int32
+_lib.synera_tree_plan_held.argtypes = [_vp, C.c_int32, _vp, _vp, _vp, C.c_int64, _vp, C.c_int32, _vp, C.c_int32, _vp, _vp]
 _lib.synera_tree_append_rope.restype = C.c_int32
 _lib.synera_tree_append_rope.argtypes = [_vp, _vp, C.c_int32, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
 _lib.synera_tree_attention.restype = C.c_int32
@@ -891,16 +893,18 @@ class TreeBatch(_PagedBatch):
     _names = "synera_tree_create", "synera_tree_destroy", "synera_tree_append_rope", "synera_tree_attention"
     _skips_none = True
 
-    def plan(self, ctx_len, n_nodes, parent, block_table, n_pages_in_pool):
+    def plan(self, ctx_len, n_nodes, parent, block_table, n_pages_in_pool, held=None):
         """int32 on the GPU: cached tokens and nodes (at most TREE_NODES) of each request, each node's parent among the nodes before it
-        in its request (-1: a child of the context) [rows], block_table [B, columns] -> status [B], 0 for requests that are not refused."""
+        in its request (-1: a child of the context) [rows], block_table [B, columns] -> status [B], 0 for requests that are not refused.
+        held [B], as update_pages leaves it: the columns that are the request's own.  Behind update_pages it has to be given, or a request that
+        was refused there for want of pages is planned with whatever its row ends in."""
         index = self._index
         B, n = ctx_len.numel(), parent.numel()
         columns = block_table.shape[-1]
         status = torch.empty(B, dtype=torch.int32, device=self.device)
-        st = _lib.synera_tree_plan(self._h, B, _ints(ctx_len, (B,), index, "ctx_len"), _ints(n_nodes, (B,), index, "n_nodes"),
-                                   _ints(parent, (n,), index, "parent"), n, _ints(block_table, (B, columns), index, "block_table"), columns,
-                                   n_pages_in_pool, status.data_ptr(), _raw_stream(index))
+        st = _lib.synera_tree_plan_held(self._h, B, _ints(ctx_len, (B,), index, "ctx_len"), _ints(n_nodes, (B,), index, "n_nodes"),
+                                        _ints(parent, (n,), index, "parent"), n, _ints(block_table, (B, columns), index, "block_table"), columns,
+                                        _ints(held, (B,), index, "held"), n_pages_in_pool, status.data_ptr(), _raw_stream(index))
         if st:
             raise SyneraError(st, "synera_tree_plan")
         self.n_requests, self.n_tokens, self.n_pages = B, n, n_pages_in_pool

@@ -186,6 +186,7 @@ extern "C" int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int3
 // ------------------------------------------------------------------------------------ planning
 struct PlanArgs {
   const int32_t *ctx, *n_nodes, *parent, *table;
+  const int32_t* held;           // columns of the table that are each request's own, or null: all
   int32_t* status;
   TrHead* head;
   TrReq* req;
@@ -291,6 +292,11 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   int32_t status = n < 0 || n > TR_NODES ? SYNERA_EINVAL : ctx < 0 ? SYNERA_ERANGE : SYNERA_OK;
   const int64_t keys = (int64_t)ctx + (status == SYNERA_OK ? n : 0);
   if (status == SYNERA_OK && (first + s.rows > a.n_rows || (n > 0 && s.steps == 0))) status = SYNERA_ENOSPC;
+  if (status == SYNERA_OK && a.held) {                        // (entries behind may be pages of others by now)
+    const int32_t held = a.held[me];
+    if (held < 0 || held > a.columns) status = SYNERA_EINVAL;
+    else if ((keys + SY_PAGE - 1) / SY_PAGE > held) status = SYNERA_ENOSPC;
+  }
   const bool fits = status == SYNERA_OK && n > 0;
   bool bad_parent = false, bad_page = false;
   int32_t up = -1;
@@ -467,19 +473,19 @@ static bool off4(std::initializer_list<const void*> all) {
   return bits % 4 != 0;
 }
 
-extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_nodes, const int32_t* d_parent,
-                                    int64_t n_rows, const int32_t* d_table, int32_t columns, int32_t n_pages_in_pool, int32_t* d_status,
-                                    void* stream) {
+extern "C" int32_t synera_tree_plan_held(synera_tree* t, int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_nodes, const int32_t* d_parent,
+                                         int64_t n_rows, const int32_t* d_table, int32_t columns, const int32_t* d_held, int32_t n_pages_in_pool,
+                                         int32_t* d_status, void* stream) {
   if (!t || !d_ctx_len || !d_n_nodes || !d_table || B < 1 || n_rows < 0 || columns < 1 || n_pages_in_pool < 1) return SYNERA_EINVAL;
   if (n_rows > 0 && !d_parent) return SYNERA_EINVAL;
-  if (off4({d_ctx_len, d_n_nodes, d_parent, d_table, d_status})) return SYNERA_EINVAL;
-  for (const Range& in : {ints(d_ctx_len, B), ints(d_n_nodes, B), ints(d_parent, n_rows), ints(d_table, (int64_t)B * columns)})
+  if (off4({d_ctx_len, d_n_nodes, d_parent, d_table, d_held, d_status})) return SYNERA_EINVAL;
+  for (const Range& in : {ints(d_ctx_len, B), ints(d_n_nodes, B), ints(d_parent, n_rows), ints(d_table, (int64_t)B * columns), ints(d_held, B)})
     if (meet(ints(d_status, B), in)) return SYNERA_EINVAL;
   if (n_pages_in_pool >= 1 << 27) return SYNERA_EUNSUP;
   const ShLimits& l = t->lim;
   if (B > l.max_batch || n_rows > l.max_tokens || columns > l.max_pages) return SYNERA_ENOSPC;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
-  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_status, t->head, t->req, t->items, t->joins, t->windows, t->pos, t->slot, t->parent, t->table,
+  const PlanArgs a = {d_ctx_len, d_n_nodes, d_parent, d_table, d_held, d_status, t->head, t->req, t->items, t->joins, t->windows, t->pos, t->slot, t->parent, t->table,
                       t->masks, B, columns, t->pitch, n_pages_in_pool, l.Hkv, l.Hq / l.Hkv, t->items_room, t->part_rows, 1.0f / l.slots, l.hd == 64 ? 2 : 1, n_rows};
   tree_plan_kernel<<<B, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
@@ -490,6 +496,12 @@ extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_
   t->n_pages = n_pages_in_pool;
   t->columns = columns;
   return SYNERA_OK;
+}
+
+extern "C" int32_t synera_tree_plan(synera_tree* t, int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_nodes, const int32_t* d_parent,
+                                    int64_t n_rows, const int32_t* d_table, int32_t columns, int32_t n_pages_in_pool, int32_t* d_status,
+                                    void* stream) {
+  return synera_tree_plan_held(t, B, d_ctx_len, d_n_nodes, d_parent, n_rows, d_table, columns, nullptr, n_pages_in_pool, d_status, stream);
 }
 
 // ------------------------------------------------------------------------------------ append

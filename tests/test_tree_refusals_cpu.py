@@ -30,6 +30,10 @@ def test_null_handles():
     assert lib.synera_tree_destroy(None) == s.OK
 
 
+def test_null_handle_of_a_plan_with_held_pages():
+    assert b._lib.synera_tree_plan_held(None, 1, 16, 16, 16, 1, 16, 1, 16, 1, None, None) == s.EINVAL
+
+
 def test_pages():
     good = [1, 64, 128, None, 192, 4, 256, 320, 384, 10, 5, 448, 512, 576, 640, None]
     for at, bad in ((0, 0), (0, -1), (1, None), (2, None), (4, None), (5, 0), (6, None), (7, None), (8, None), (9, 0), (10, -1), (11, None), (12, None),
