@@ -63,13 +63,15 @@ int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int32_t n_kv_he
 int32_t synera_tree_destroy(synera_tree* tree);
 
 /*
+ * Rows are numbered as by synera_pages_update: cu_i sums up the n of the requests before, of 0 where n is below 0 or above 16 x columns, also
+ * where n is more than a tree may have or the request is refused.  So with tables of the same columns both have the same rows for all requests.
  * Plans a step, once for all layers: d_ctx_len, d_n_nodes i32 [B], d_parent i32 [rows], d_table i32 [B][columns] (columns <= max_pages), all
  * read by this call alone.  The calls below must be on the same stream, or ordered behind it by the caller; so must a plan behind calls
  * that use the one before.  Captured calls work for any later plan of this handle (captured or not).  Calls look at what the last plan that was
  * called, or captured, says of rows and pages; where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
  * the requests beyond them are left out, as an accept or a commit leaves out requests beyond the B of the plan that it was called behind; before a captured plan's
  * first replay the handle has no requests.  That pools have room for a replayed plan's pages nothing checks.
- *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES (it has no rows), a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page
+ *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES, a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page
  *             id outside the pool; ENOSPC: more pages than columns, more rows than n_rows
  * Errors: EINVAL (null, sizes, alignment), ENOSPC (B > max_batch, n_rows > max_tokens, columns > max_pages), EUNSUP (n_pages_in_pool >= 2^27), EHIP.
  */

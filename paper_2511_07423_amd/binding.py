@@ -889,7 +889,7 @@ class TreeBatch(_PagedBatch):
     """Trees of drafted tokens over a paged bf16 cache, their lengths on the GPU: plan() once a step, append_rope() and attention() for each
     layer (as SharedBatch's), accept() and commit() behind the last, all on one stream.  All but the making of the handle can be captured into a
     graph; captured calls serve later plans too, for which their tensors and pools need room.  Rows of a tree: node j of request i is row
-    cu[i] + j, cu the prefix sums of n_nodes.  Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
+    cu[i] + j, cu as update_pages returns it for a table of the same columns (the prefix sums of n_nodes).  Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
     _names = "synera_tree_create", "synera_tree_destroy", "synera_tree_append_rope", "synera_tree_attention"
     _skips_none = True
 

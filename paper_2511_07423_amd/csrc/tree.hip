@@ -11,6 +11,7 @@
 
 #define TR_NODES SYNERA_TREE_NODES
 #define TR_AHEAD 16              // columns behind a row of the table, filled with its last page: the attention's first pages are read without clamps
+#define TR_ROWS (1 << 30)        // max_tokens is below
 #define TR_STEP SY_SH_STEP       // keys of one step, the unit of work
 
 // ------------------------------------------------------------------------------------ the plan on the device
@@ -53,7 +54,7 @@ struct TrHead {
 };
 struct TrReq {                   // 32 bytes, scalar loads
   int32_t ctx, n, tok;           // n: 0 where the request has no nodes or is refused
-  int32_t rows;                  // of its n_nodes, those that there is room for
+  int32_t rows;                  // of those that are counted, the ones that there is room for
   int32_t steps, ranges, tiles;  // as the lists count them, refused or not
   int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
 };
@@ -201,15 +202,18 @@ struct PlanArgs {
   int64_t n_rows;
 };
 
-// What a request's lengths alone say of it; every block forms it for all of them.
+// What a request's lengths alone say of it; every block forms it for all of them.  Rows are counted as synera_pages_update counts them, also of requests
+// that are refused: what lies behind has the same rows for both.
 struct TrSize {
-  int32_t rows, windows, steps, tiles;
+  int32_t rows;                  // TR_ROWS at most, more than any call has
+  int32_t windows, steps, tiles;
   int32_t units, per;            // tiles of a unit
 };
 __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_t n) {
   TrSize s = {0, 0, 0, 0, 0, 1};
-  if (n < 0 || n > TR_NODES) return s;
-  s.rows = n;
+  if (n < 0 || n > (int64_t)SY_PAGE * a.columns) return s;
+  s.rows = min(n, TR_ROWS);
+  if (n > TR_NODES) return s;
   const int64_t keys = (int64_t)ctx + n;
   if (n == 0 || ctx < 0 || (keys + SY_PAGE - 1) / SY_PAGE > a.columns || keys > 0x7FFFFFFF - TR_STEP) return s;
   s.windows = (int32_t)((keys - 1) / SY_PAGE - ctx / SY_PAGE + 1);
@@ -219,6 +223,7 @@ __device__ __forceinline__ TrSize size_of(const PlanArgs& a, int32_t ctx, int32_
   s.per = (s.tiles + s.units - 1) / s.units;
   return s;
 }
+__device__ __forceinline__ int32_t tr_rows(int32_t x, int32_t y) { return (int32_t)min((uint32_t)x + (uint32_t)y, (uint32_t)TR_ROWS); }
 // (A quotient in 32 bits of floating point: the same for every block, and no more than an estimate.)
 __device__ __forceinline__ int32_t item_cost(const PlanArgs& a, const TrSize& s, int32_t ranges, int32_t step) {
   return (int32_t)((float)s.steps * step * __builtin_amdgcn_rcpf((float)ranges)) + TR_START * a.scale;
@@ -244,17 +249,21 @@ __device__ __forceinline__ int64_t tr_estimate(const PlanArgs& a, const TrTotals
 }
 
 // The sum over the block's threads, for all of them.
-template <int N>
-__device__ __forceinline__ void block_sums(int32_t (&v)[N], int32_t (*parts)[N]) {
+template <int N, typename Add>
+__device__ __forceinline__ void block_sums(int32_t (&v)[N], int32_t (*parts)[N], Add add) {
   for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
+    for (int k = 0; k < N; ++k) v[k] = add(v[k], __shfl_xor(v[k], o));
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
     for (int k = 0; k < N; ++k) parts[threadIdx.x >> 6][k] = v[k];
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = parts[0][k] + parts[1][k] + parts[2][k] + parts[3][k];
+  for (int k = 0; k < N; ++k) v[k] = add(add(parts[0][k], parts[1][k]), add(parts[2][k], parts[3][k]));
+}
+template <int N>
+__device__ __forceinline__ void block_sums(int32_t (&v)[N], int32_t (*parts)[N]) {
+  block_sums(v, parts, [](int32_t x, int32_t y) { return x + y; });
 }
 
 // Block i plans request i.  It looks at all requests by itself (a few thousand numbers at most, which lie in the caches), so that one launch
@@ -265,7 +274,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   __shared__ TrTotals totals[TR_LENGTHS];
   __shared__ TrSize sizes[256];
   __shared__ unsigned long long best;                         // estimate << 8 | candidate
-  __shared__ int32_t sums_a[4][4], sums_b[4][3], sums_c[4][2 * SY_SH_DEAL], begin[SY_SH_DEAL];
+  __shared__ int32_t sums_r[4][2], sums_w[4][2], sums_b[4][3], sums_c[4][2 * SY_SH_DEAL], begin[SY_SH_DEAL];
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
   if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0, 0, INT32_MAX, 0, INT32_MAX, 0};
@@ -274,18 +283,19 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   const TrSize s = size_of(a, ctx, n);
   const bool few = a.B <= 256;                                // all sizes are in LDS
   // ---- rows and windows before this request, and of all
-  int32_t rows[4] = {0, 0, 0, 0};
+  int32_t rows[2] = {0, 0}, windows[2] = {0, 0};
   for (int i = tid; i < a.B; i += 256) {
     const TrSize z = size_of(a, a.ctx[i], a.n_nodes[i]);
     if (few) sizes[i] = z;
     if (i < me) {
-      rows[0] += z.rows;
-      rows[1] += z.windows;
+      rows[0] = tr_rows(rows[0], z.rows);
+      windows[0] += z.windows;
     }
-    rows[2] += z.rows;
-    rows[3] += z.windows;
+    rows[1] = tr_rows(rows[1], z.rows);
+    windows[1] += z.windows;
   }
-  block_sums(rows, sums_a);
+  block_sums(rows, sums_r, [](int32_t x, int32_t y) { return tr_rows(x, y); });
+  block_sums(windows, sums_w);
   const int64_t first = rows[0];
 
   // ---- what only this block looks at: parents and pages
@@ -415,32 +425,32 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     }
   }
   // ---- each node's places
-  if (tid < s.rows && first + tid < a.n_rows) {
-    const int64_t at = first + tid;
-    if (live) {
-      int depth = -1;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) depth += __popc(word[w]);
-      const int32_t p = ctx + tid;
-      a.pos[at] = ctx + depth;
-      a.slot[at] = row[p / SY_PAGE] * SY_PAGE + p % SY_PAGE;
-      a.parents[at] = parent;
-      uint32_t* m = a.masks + at * SY_TREE_MASK;
-      m[0] = m[1] = 0xFFFFFFFFu;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) m[2 + w] = word[w];
-#pragma unroll
-      for (int w = 10; w < SY_TREE_MASK; ++w) m[w] = 0;
-    } else {
+  if (!live) {
+    for (int64_t at = first + tid; at < min(first + s.rows, a.n_rows); at += 256) {
       a.pos[at] = 0;
       a.slot[at] = -1;
     }
+  } else if (tid < n) {
+    const int64_t at = first + tid;
+    int depth = -1;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) depth += __popc(word[w]);
+    const int32_t p = ctx + tid;
+    a.pos[at] = ctx + depth;
+    a.slot[at] = row[p / SY_PAGE] * SY_PAGE + p % SY_PAGE;
+    a.parents[at] = parent;
+    uint32_t* m = a.masks + at * SY_TREE_MASK;
+    m[0] = m[1] = 0xFFFFFFFFu;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) m[2 + w] = word[w];
+#pragma unroll
+    for (int w = 10; w < SY_TREE_MASK; ++w) m[w] = 0;
   }
   for (int w = tid; w < s.windows; w += 256) {
     const int32_t page = ctx / SY_PAGE + w, from = max(ctx, page * SY_PAGE), to = min(ctx + n, (page + 1) * SY_PAGE);
     ShWindow x = {0, 0, 0, 0};
     if (live) x = ShWindow{row[page], (int32_t)first + from - ctx, from - page * SY_PAGE, to - page * SY_PAGE};
-    a.windows[rows[1] + w] = x;
+    a.windows[windows[0] + w] = x;
   }
   // ---- the lists
   const TrReq q = {ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles, before[0]};
@@ -456,8 +466,8 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     a.req[me] = q;
     if (a.status) a.status[me] = status;
     if (me == 0) {
-      a.head->sh.n_tokens = (int32_t)min((int64_t)rows[2], a.n_rows);
-      a.head->sh.n_windows = rows[3];
+      a.head->sh.n_tokens = (int32_t)min((int64_t)rows[1], a.n_rows);
+      a.head->sh.n_windows = windows[1];
 #pragma unroll
       for (int x = 0; x < SY_SH_DEAL; ++x) a.head->items[x] = lists[SY_SH_DEAL + x];
       a.head->B = a.B;
@@ -731,6 +741,7 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(AcceptArgs a) {
     if (j >= n && j < q.rows) a.path[q.tok + j] = -1;
     if (mine[w] >= 0) a.path[q.tok + mine[w]] = j;
   }
+  for (int j = lane + TR_NODES; j < q.rows; j += 64) a.path[q.tok + j] = -1;       // (refused: more rows than a tree may have)
 }
 
 extern "C" int32_t synera_tree_accept(synera_tree* t, int64_t n_rows, const int32_t* d_tokens, const int32_t* d_target, const int32_t* d_anchor,

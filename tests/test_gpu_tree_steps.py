@@ -123,3 +123,76 @@ def test_captured_steps_whose_pool_runs_out():
                 assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), step
             torch.cuda.synchronize()
     assert refused >= 2
+
+
+# ------------------------------------------------------------------------------------------------ counts out of range
+@pytest.mark.parametrize("n,columns,counted,status", [(300, 40, 300, "EINVAL"), (200, 8, 0, "ENOSPC"), (256, 16, 256, "ENOSPC"), (257, 16, 0, "EINVAL"), (257, 17, 257, "EINVAL"),
+                                                      (640, 40, 640, "EINVAL"), (641, 40, 0, "EINVAL"), (-1, 8, 0, "EINVAL"), (2 ** 31 - 1, 8, 0, "EINVAL")])
+def test_rows_of_a_step_with_a_count_out_of_range(n, columns, counted, status):
+    """Page tables, plans, logits and accepted paths number rows alike, whatever one request's count is: the others are what they are without it."""
+    s, (hq, hkv, hd), vocab = synera(), (4, 2, 64), 64
+    trees, at = [[-1, 0, 0], [-1, 0, 1, 0], [-1, 0]], [0, 2, 4]
+    ctx, new = i32([20, 9, 7, 5, 33]), i32([3, n, 4, -1, 2])
+    T = 9 + counted
+    first = [0, 3 + counted, 7 + counted]                      # rows of the three that can be
+    rows = torch.cat([torch.arange(r, r + len(t)) for r, t in zip(first, trees)]).to(DEV)
+    n_pages = 64
+    table, held, free, n_free = i32(np.zeros((5, columns))), i32(np.zeros(5)), i32(np.random.RandomState(1).permutation(n_pages)), i32([n_pages])
+    cu, pos, slot, refused = s.update_pages(table, held, free, n_free, ctx, new, T)
+    assert cu.tolist() == [0, 3, 3 + counted, 7 + counted, 7 + counted, T]
+    parent, tokens = torch.full((T,), -1, dtype=torch.int32, device=DEV), torch.full((T,), 1, dtype=torch.int32, device=DEV)
+    parent[rows] = i32(sum(trees, []))
+    tokens[rows] = i32(np.arange(9) + 2)
+    logits = torch.zeros((T, vocab), device=DEV)
+    follows = {0: 1, 1: 40, 2: 41, 3: 4, 4: 5, 5: 42, 6: 43, 7: 8, 8: 44}       # the target of each of the nine nodes, as a node's place among them or a token
+    for node, then in follows.items():
+        logits[rows[node], then + 2 if then < 9 else then] = 9.0
+    b = s.TreeBatch(hq, hkv, hd, 5, 700, 41)
+    for pages in (held, None):
+        got = b.plan(ctx, new, parent, table, n_pages, held=pages)
+        assert got.tolist() == [0, getattr(s, status), 0, s.EINVAL, 0]
+    x = torch.randn((T, hq + 2 * hkv, hd), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(torch.bfloat16)
+    k, v = torch.zeros((n_pages, hkv, P, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((n_pages, hkv, hd, P), dtype=torch.bfloat16, device=DEV)
+    k1, v1 = k.clone(), v.clone()
+    rope = s.Rope(hd)
+    mark = torch.full((T, hq, hd), 0x1234, dtype=torch.int16, device=DEV).view(torch.bfloat16)
+    out_q, out = mark.clone(), mark.clone()
+    b.append_rope(rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], k, v, out_q=out_q)
+    b.attention(out_q, k, v, out=out)
+    y = s.adjust_logits(logits, cu=cu, tokens=tokens, parent=parent, presence=torch.full((5,), 0.5, device=DEV))
+    target, _, _ = s.confidence(y, want_prob=False, want_entropy=False)
+    acc = b.accept(tokens, target, n_given=i32([1] * 5))
+    # the same without the two that cannot be
+    small = s.TreeBatch(hq, hkv, hd, 3, 9, 41)
+    live = torch.tensor(at, device=DEV)
+    assert (small.plan(ctx[live].contiguous(), new[live].contiguous(), i32(sum(trees, [])), table[live].contiguous(), n_pages) == 0).all()
+    x1 = x[rows]
+    q1 = small.append_rope(rope, x1[:, :hq], x1[:, hq: hq + hkv], x1[:, hq + hkv:], k1, v1)
+    o1 = small.attention(q1, k1, v1)
+    y1 = s.adjust_logits(logits[rows], cu=i32([0, 3, 7, 9]), tokens=tokens[rows], parent=i32(sum(trees, [])), presence=torch.full((3,), 0.5, device=DEV))
+    acc1 = small.accept(tokens[rows], target[rows], n_given=i32([1] * 3))
+    assert torch.equal(k, k1) and torch.equal(v, v1) and torch.equal(out_q[rows], q1) and torch.equal(out[rows], o1) and torch.equal(y[rows], y1)
+    assert torch.equal(acc["path"][rows], acc1["path"]) and all(torch.equal(acc[name][live], acc1[name]) for name in ("accept_len", "n_path", "token"))
+    assert acc1["accept_len"].tolist() == [1, 2, 1]
+    other = torch.ones(T, dtype=torch.bool, device=DEV)
+    other[rows] = False
+    assert (acc["path"][other] == -1).all() and (out[other].view(torch.int16) == 0x1234).all() and (out_q[other].view(torch.int16) == 0x1234).all()
+    assert (slot[rows] >= 0).all() and (refused == 0).tolist() == [True, n in (256, 257, 300, 640) and columns * P >= n + 9, True, False, True]
+
+
+def test_rows_that_a_step_has_no_room_for():
+    """Of a request that is refused for its count the rows that there are, then the requests behind are refused."""
+    s = synera()
+    b = s.TreeBatch(2, 1, 64, 4, 500, 40)
+    table = i32(np.arange(160).reshape(4, 40))
+    status = b.plan(i32([5, 0, 3, 0]), i32([2, 600, 3, 640]), i32([-1] * 400), table, 160)
+    assert status.tolist() == [0, s.EINVAL, s.ENOSPC, s.EINVAL]
+    acc = b.accept(i32(np.zeros(400)), i32(np.zeros(400)), n_given=i32([1] * 4))
+    assert acc["n_path"].tolist() == [1, 0, 0, 0] and acc["path"].tolist() == [0] + [-1] * 399
+    # sums beyond 32 bits
+    many = s.TreeBatch(2, 1, 64, 2000, 500, 40000)
+    table = i32(np.zeros((2000, 40000)))
+    status = many.plan(i32([0] * 2000), torch.full((2000,), 640000, dtype=torch.int32, device=DEV), i32([-1] * 400), table, 1)
+    assert (status == s.EINVAL).all()
+    acc = many.accept(i32(np.zeros(400)), i32(np.zeros(400)), n_given=i32([1] * 2000))
+    assert (acc["n_path"] == 0).all() and (acc["path"] == -1).all()
