@@ -8,7 +8,7 @@
  * of synera_shared.h.  What the host says (sizes, pointers) is checked on the host: a refused call has launched nothing.  What only the
  * device knows is checked there: each request has a status of its own (0, or one of the codes of synera.h), and a refused request
  * changes nothing and has no outputs but those that say so.  Arrays named [rows] are flattened, request after request, and have as many
- * places as n_rows says; those behind the last request's stay as they were.  Nothing here waits for the GPU but creates and destroys.
+ * places as n_rows says; those behind the last request's stay as they were, but for the places of synera_pages_update.  Nothing here waits for the GPU but creates and destroys.
  */
 #ifndef SYNERA_TREE_H
 #define SYNERA_TREE_H
@@ -31,7 +31,7 @@ extern "C" {
  * So a step that is taken back leaves the stack as it was.  Entries behind a row's held columns and behind the stack's top stay.
  * Then each token's place, for token j of request i in row cu[i] + j:
  *   d_cu      i32 [B + 1]   prefix sums of n_i (of 0 where n_i is below 0 or above 16 x columns)
- *   d_pos     i32 [rows]    L_i + j, or -1 where the request is refused
+ *   d_pos     i32 [rows]    L_i + j, or -1 where the request is refused and behind the last request's tokens
  *   d_slot    i32 [rows]    page x 16 + slot in the page, or -1
  *   d_status  i32 [B]       0; ERANGE: L_i or n_i below 0, or L_i + n_i beyond int32; ENOSPC: more pages than columns, or than there are;
  *                           EINVAL: d_held[i] outside 0 .. columns

@@ -869,7 +869,7 @@ def update_pages(table, held, free, n_free, ctx_len, n_new, n_rows, shared=None)
     """Pages for each request's ctx_len + n_new tokens, in place: rows of `table` [B, columns], of whose pages request i holds its first
     held[i], take what they lack from the stack `free` [n_pages] of n_free [1] pages and give back what they have too much, but for their first
     shared[i] columns.  -> (cu [B + 1], pos [n_rows], slot [n_rows], status [B]): where each request's tokens begin in the flattened rows, each
-    token's position and its place page * 16 + slot, and what refused a request (0: nothing).  All int32 on the GPU."""
+    token's position and its place page * 16 + slot (-1 for requests that are refused, and for rows behind the last token), and what refused a request (0: nothing).  All int32 on the GPU."""
     index = _current(table, "table")
     B, columns = table.shape
     n_pages = free.numel()

@@ -162,7 +162,11 @@ __global__ __launch_bounds__(PG_THREADS) void pages_kernel(PagesArgs a) {
     if (tid == PG_THREADS - 1) l.begin[PG_THREADS] = at.rows + s.rows;
     __syncthreads();
     const int32_t rows = (int32_t)min((int64_t)l.begin[PG_THREADS], a.n_rows);
-    for (int t = tid; t < rows; t += PG_THREADS) {
+    for (int t = tid; t < a.n_rows; t += PG_THREADS) {
+      if (t >= rows) {
+        a.pos[t] = a.slot[t] = -1;
+        continue;
+      }
       const int r = request_of(l.begin, t);
       const int32_t ctx = l.at[r], p = ctx + t - l.begin[r];
       a.pos[t] = ctx < 0 ? -1 : p;
@@ -179,6 +183,9 @@ __global__ __launch_bounds__(256) void pages_places_kernel(PagesArgs a) {
     a.pos[first + j] = ok ? p : -1;
     a.slot[first + j] = ok ? a.table[(size_t)i * a.columns + p / SY_PAGE] * SY_PAGE + p % SY_PAGE : -1;
   }
+  // rows behind the last token, dealt to all blocks
+  const int64_t step = (int64_t)gridDim.x * gridDim.y * 256;
+  for (int64_t t = a.cu[a.B] + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x; t < a.n_rows; t += step) a.pos[t] = a.slot[t] = -1;
 }
 
 extern "C" int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, const int32_t* d_n_new, const int32_t* d_shared, int32_t* d_table,

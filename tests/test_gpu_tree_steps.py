@@ -196,3 +196,19 @@ def test_rows_that_a_step_has_no_room_for():
     assert (status == s.EINVAL).all()
     acc = many.accept(i32(np.zeros(400)), i32(np.zeros(400)), n_given=i32([1] * 2000))
     assert (acc["n_path"] == 0).all() and (acc["path"] == -1).all()
+
+
+@pytest.mark.parametrize("B,n_rows", [(1, 1), (3, 7), (3, 50), (3, 4096), (3, 4097), (3, 70001), (1500, 2500), (1500, 1)])
+def test_places_behind_the_last_token(B, n_rows):
+    """A step whose rows have room for more tokens than there are: the others' places are none, whatever the memory held."""
+    s, rng = synera(), np.random.RandomState(B)
+    new = rng.randint(0, 3, size=B) if n_rows > 1 else np.zeros(B, np.int64)
+    ctx, columns = rng.randint(0, 40, size=B), 3
+    free = rng.permutation(3 * B)
+    for step in range(3):
+        junk = [torch.full((2 * B + 1 + 2 * n_rows,), 5, dtype=torch.int32, device=DEV) for _ in range(2)]
+        del junk                                               # what the next outputs may lie in
+        cu, pos, slot, status = s.update_pages(i32(np.zeros((B, columns))), i32(np.zeros(B)), i32(free), i32([3 * B]), i32(ctx), i32(new), n_rows)
+        T = min(int(new.sum()), n_rows)
+        assert (status == 0).all() and cu[-1] == new.sum()
+        assert (pos[:T] >= 0).all() and (slot[:T] >= 0).all() and (pos[T:] == -1).all() and (slot[T:] == -1).all()
