@@ -7,6 +7,7 @@
 
 #define PG_THREADS 1024
 #define PG_ROWS 4096
+#define PG_BLOCKS (1 << 20)      // of the second launch for requests, which may be more than a launch's threads
 
 struct PagesArgs {
   const int32_t *ctx, *n_new, *shared;
@@ -175,13 +176,14 @@ __global__ __launch_bounds__(PG_THREADS) void pages_kernel(PagesArgs a) {
   }
 }
 __global__ __launch_bounds__(256) void pages_places_kernel(PagesArgs a) {
-  const int i = blockIdx.x;
-  const int32_t first = a.cu[i], rows = a.cu[i + 1] - first, ctx = a.ctx[i];
-  const bool ok = a.status[i] == SYNERA_OK;
-  for (int j = blockIdx.y * 256 + threadIdx.x; j < rows && (int64_t)first + j < a.n_rows; j += gridDim.y * 256) {
-    const int32_t p = ctx + j;
-    a.pos[first + j] = ok ? p : -1;
-    a.slot[first + j] = ok ? a.table[(size_t)i * a.columns + p / SY_PAGE] * SY_PAGE + p % SY_PAGE : -1;
+  for (int i = blockIdx.x; i < a.B; i += gridDim.x) {
+    const int32_t first = a.cu[i], rows = a.cu[i + 1] - first, ctx = a.ctx[i];
+    const bool ok = a.status[i] == SYNERA_OK;
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < rows && (int64_t)first + j < a.n_rows; j += gridDim.y * 256) {
+      const int32_t p = ctx + j;
+      a.pos[first + j] = ok ? p : -1;
+      a.slot[first + j] = ok ? a.table[(size_t)i * a.columns + p / SY_PAGE] * SY_PAGE + p % SY_PAGE : -1;
+    }
   }
   // rows behind the last token, dealt to all blocks
   const int64_t step = (int64_t)gridDim.x * gridDim.y * 256;
@@ -216,7 +218,7 @@ extern "C" int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, cons
     if (hipGetLastError() != hipSuccess) return SYNERA_EHIP;
     if (n_rows == 0) return SYNERA_OK;
     // (requests of a prompt's length take several blocks)
-    pages_places_kernel<<<dim3(B, (uint32_t)std::min<int64_t>(64, std::max<int64_t>(1, n_rows / B / 1024))), 256, 0, s>>>(a);
+    pages_places_kernel<<<dim3(std::min(B, PG_BLOCKS), (uint32_t)std::min<int64_t>(64, std::max<int64_t>(1, n_rows / B / 1024))), 256, 0, s>>>(a);
   }
   return hipGetLastError() == hipSuccess ? SYNERA_OK : SYNERA_EHIP;
 }

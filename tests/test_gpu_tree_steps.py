@@ -212,3 +212,16 @@ def test_places_behind_the_last_token(B, n_rows):
         T = min(int(new.sum()), n_rows)
         assert (status == 0).all() and cu[-1] == new.sum()
         assert (pos[:T] >= 0).all() and (slot[:T] >= 0).all() and (pos[T:] == -1).all() and (slot[T:] == -1).all()
+
+
+def test_pages_of_more_requests_than_a_launch_has_blocks_for():
+    """2^24 requests and some: with 256 threads each the places' launch would have more than 2^32."""
+    s, B = synera(), (1 << 24) + 3
+    zeros = torch.zeros(B, dtype=torch.int32, device=DEV)
+    new, table, held = zeros.clone(), torch.full((B, 1), -5, dtype=torch.int32, device=DEV), zeros.clone()
+    some = torch.tensor([0, 1 << 20, (1 << 20) + 1, 1 << 23, (1 << 24) - 1, 1 << 24, B - 1], device=DEV)
+    new[some] = 3
+    cu, pos, slot, status = s.update_pages(table, held, i32([9, 8, 7, 6, 5, 4, 3]), i32([7]), zeros, new, 30)
+    assert (status == 0).all() and cu[-1] == 21 and int(held.sum()) == 7
+    assert pos.tolist() == [0, 1, 2] * 7 + [-1] * 9 and table[some, 0].tolist() == [3, 4, 5, 6, 7, 8, 9]
+    assert slot.tolist() == [16 * page + j for page in (3, 4, 5, 6, 7, 8, 9) for j in range(3)] + [-1] * 9
