@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   __shared__ TrTotals totals[TR_LENGTHS];
   __shared__ TrSize sizes[256];
   __shared__ unsigned long long best;                         // estimate << 8 | candidate
-  __shared__ int32_t sums_r[4][2], sums_w[4][2], sums_b[4][3], sums_c[4][2 * SY_SH_DEAL], begin[SY_SH_DEAL];
+  __shared__ int32_t sums_a[4][4], sums_b[4][3], sums_c[4][2 * SY_SH_DEAL], begin[SY_SH_DEAL];
   __shared__ int32_t up_[TR_NODES];
   __shared__ uint32_t gather[TR_NODES][9];                    // (9: neighbours on other banks)
   if (tid < TR_LENGTHS) totals[tid] = TrTotals{0, 0, 0, 0, 0, INT32_MAX, 0, INT32_MAX, 0};
@@ -283,19 +283,18 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
   const TrSize s = size_of(a, ctx, n);
   const bool few = a.B <= 256;                                // all sizes are in LDS
   // ---- rows and windows before this request, and of all
-  int32_t rows[2] = {0, 0}, windows[2] = {0, 0};
+  int32_t rows[4] = {0, 0, 0, 0};                             // (windows are far fewer than TR_ROWS)
   for (int i = tid; i < a.B; i += 256) {
     const TrSize z = size_of(a, a.ctx[i], a.n_nodes[i]);
     if (few) sizes[i] = z;
     if (i < me) {
       rows[0] = tr_rows(rows[0], z.rows);
-      windows[0] += z.windows;
+      rows[1] += z.windows;
     }
-    rows[1] = tr_rows(rows[1], z.rows);
-    windows[1] += z.windows;
+    rows[2] = tr_rows(rows[2], z.rows);
+    rows[3] += z.windows;
   }
-  block_sums(rows, sums_r, [](int32_t x, int32_t y) { return tr_rows(x, y); });
-  block_sums(windows, sums_w);
+  block_sums(rows, sums_a, [](int32_t x, int32_t y) { return tr_rows(x, y); });
   const int64_t first = rows[0];
 
   // ---- what only this block looks at: parents and pages
@@ -450,7 +449,7 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     const int32_t page = ctx / SY_PAGE + w, from = max(ctx, page * SY_PAGE), to = min(ctx + n, (page + 1) * SY_PAGE);
     ShWindow x = {0, 0, 0, 0};
     if (live) x = ShWindow{row[page], (int32_t)first + from - ctx, from - page * SY_PAGE, to - page * SY_PAGE};
-    a.windows[windows[0] + w] = x;
+    a.windows[rows[1] + w] = x;
   }
   // ---- the lists
   const TrReq q = {ctx, live ? n : 0, (int32_t)first, (int32_t)max((int64_t)0, min((int64_t)s.rows, a.n_rows - first)), s.steps, ranges, s.tiles, before[0]};
@@ -466,8 +465,8 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(PlanArgs a) {
     a.req[me] = q;
     if (a.status) a.status[me] = status;
     if (me == 0) {
-      a.head->sh.n_tokens = (int32_t)min((int64_t)rows[1], a.n_rows);
-      a.head->sh.n_windows = windows[1];
+      a.head->sh.n_tokens = (int32_t)min((int64_t)rows[2], a.n_rows);
+      a.head->sh.n_windows = rows[3];
 #pragma unroll
       for (int x = 0; x < SY_SH_DEAL; ++x) a.head->items[x] = lists[SY_SH_DEAL + x];
       a.head->B = a.B;
