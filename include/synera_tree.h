@@ -55,7 +55,7 @@ int32_t synera_pages_update(int32_t B, const int32_t* d_ctx_len, const int32_t* 
 typedef struct synera_tree synera_tree;
 
 /* head_dim, n_q_heads, n_kv_heads as synera_batch_create; room for max_batch requests, max_tokens rows, max_pages block-table columns.
- * Keeps 35 (head_dim 64) or 68 MB of device memory for partial results, beside the plan.  Errors: EINVAL, EUNSUP (also: max_batch > 2^20, max_batch x n_q_heads >= 2^26,
+ * Keeps 35 (head_dim 64) or 68 MB of device memory for partial results, beside the plan.  Errors: EINVAL, EUNSUP (also: max_batch > 2^14, max_batch x n_q_heads >= 2^26,
  * max_tokens x n_q_heads or max_batch x (max_pages + 16) >= 2^30), EHIP, ENOMEM. */
 int32_t synera_tree_create(synera_tree** out, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_batch,
                            int32_t max_tokens, int32_t max_pages);

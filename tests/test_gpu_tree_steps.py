@@ -9,7 +9,7 @@ import torch
 
 import shared_reference as ref
 import tree_reference as tree
-from test_gpu_tree import DEV, P, Server, grow, i32, same, synera
+from test_gpu_tree import DEV, P, Server, check_attention, grow, i32, make, same, synera
 
 pytestmark = pytest.mark.gpu
 
@@ -225,3 +225,8 @@ def test_pages_of_more_requests_than_a_launch_has_blocks_for():
     assert (status == 0).all() and cu[-1] == 21 and int(held.sum()) == 7
     assert pos.tolist() == [0, 1, 2] * 7 + [-1] * 9 and table[some, 0].tolist() == [3, 4, 5, 6, 7, 8, 9]
     assert slot.tolist() == [16 * page + j for page in (3, 4, 5, 6, 7, 8, 9) for j in range(3)] + [-1] * 9
+
+
+def test_as_many_requests_as_a_handle_may_have():
+    args = make(random.Random(1), 1 << 14, 40, 2, zero=0.1)
+    check_attention(2, 1, 64, *args, 3)

@@ -18,6 +18,14 @@ def test_tree_limits(args, status):
     assert e.value.status == status
 
 
+@pytest.mark.parametrize("max_batch", [(1 << 14) + 1, 1 << 16, 1 << 20, (1 << 20) + 1])
+def test_tree_limit_of_requests(max_batch):
+    """A plan's time grows as the square of the requests."""
+    with pytest.raises(s.SyneraError) as e:
+        s.TreeBatch(4, 4, 64, max_batch, 1 << 20, 1)
+    assert e.value.status == s.EUNSUP
+
+
 def test_null_handles():
     lib = b._lib
     one = b._pack_heads(16, 16, 0, 1, 64, 64, 64, 64)
