@@ -362,8 +362,8 @@ int32_t sh_append(const ShTarget& b, const synera_rope* rope, int32_t dtype, con
   if (!rope || !k || !v || !d_k_layer || !d_v_layer || dtype < 0 || dtype > 2) return SYNERA_EINVAL;
   if (!(eps >= 0.f) || !std::isfinite(eps)) return SYNERA_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool captured = capturing(s), graph = captured || !b.known;
-  if (b.n_tokens == 0 && !captured) return SYNERA_OK;                  // (an empty tensor has no address)
+  const bool captures = capturing(s), captured = captures || b.replays, graph = captured || !b.known;
+  if (b.n_tokens == 0 && !captures && (!b.replays || (k->n_rows == 0 && !k->d_in))) return SYNERA_OK;   // (an empty tensor has no address)
   if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16) return SYNERA_EINVAL;
   const ShLimits& l = *b.lim;
   const int bytes = dtype == 0 ? 4 : 2, hd = l.hd;
@@ -445,7 +445,7 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
                                       const synera_heads* k, const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer,
                                       void* stream) {
   if (!b || !b->planned) return SYNERA_EINVAL;
-  const ShTarget target = {&b->lim, b->device, b->n_pages, b->plan.head.n_tokens, b->plan.head.n_windows, true, b->region<int32_t>(R_POS),
+  const ShTarget target = {&b->lim, b->device, b->n_pages, b->plan.head.n_tokens, b->plan.head.n_windows, true, false, b->region<int32_t>(R_POS),
                            b->region<int32_t>(R_SLOT), b->region<ShHeader>(R_HEAD), b->region<ShWindow>(R_WIN)};
   return sh_append(target, rope, dtype, q, k, v, eps, d_k_layer, d_v_layer, stream);
 }

@@ -521,7 +521,7 @@ extern "C" int32_t synera_tree_append_rope(synera_tree* t, const synera_rope* ro
                                            const synera_heads* k, const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer,
                                            void* stream) {
   if (!t || !t->planned) return SYNERA_EINVAL;
-  const ShTarget target = {&t->lim, t->device, t->n_pages, t->n_rows, 0, false, t->pos, t->slot, &t->head->sh, t->windows};
+  const ShTarget target = {&t->lim, t->device, t->n_pages, t->n_rows, 0, false, t->replays, t->pos, t->slot, &t->head->sh, t->windows};
   return sh_append(target, rope, dtype, q, k, v, eps, d_k_layer, d_v_layer, stream);
 }
 
@@ -653,8 +653,10 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   const ShLimits& l = t->lim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   TreeAttnArgs a = {};
-  const bool captured = capturing(s);
-  const int32_t st = sh_attention_args(a, l, t->n_pages, t->n_rows, captured, q, d_k_layer, d_v_layer, scale, d_lse);
+  // A plan on the device that may be another than the last one that was called is served as far as the call's tensors go, as in a graph.
+  const bool captured = capturing(s), graph = captured || t->replays;
+  if (t->n_rows == 0 && !captured && q->n_rows == 0 && !q->d_in) return SYNERA_OK;         // (an empty tensor has no address)
+  const int32_t st = sh_attention_args(a, l, t->n_pages, t->n_rows, graph, q, d_k_layer, d_v_layer, scale, d_lse);
   if (st != SYNERA_OK) return st == SH_NOTHING ? SYNERA_OK : st;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   a.pages = t->table;
@@ -669,7 +671,7 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.rows = q->n_rows ? q->n_rows : INT32_MAX;
   // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
   const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL;
-  const bool cuts = (captured || t->replays ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
+  const bool cuts = (graph ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
   const int joins = cuts ? TR_JOIN_GRID * l.slots : 0;
   const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, joins, s) : launch_tree<64>(a, grid, joins, s);
   if (e != hipSuccess) {
@@ -873,7 +875,7 @@ extern "C" int32_t synera_tree_commit(synera_tree* t, int64_t n_rows, const int3
   for (const Range& in : {ints(d_path, n_rows), ints(d_n_path, t->B)})
     if (meet(k, in) || meet(v, in)) return SYNERA_EINVAL;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
-  if (t->n_rows == 0 && !capturing(static_cast<hipStream_t>(stream))) return SYNERA_OK;
+  if (t->n_rows == 0 && !t->replays && !capturing(static_cast<hipStream_t>(stream))) return SYNERA_OK;
   const int32_t n = l.Hkv * l.hd;
   CommitArgs a = {t->req, t->slot, d_path, d_n_path, static_cast<bf16_t*>(d_k_pool), static_cast<bf16_t*>(d_v_pool), layer_stride, n, l.hd, (n / 8 + 255) / 256, t->head,
                   (int32_t)std::min<int64_t>(n_rows, INT32_MAX)};

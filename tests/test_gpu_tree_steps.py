@@ -230,3 +230,79 @@ def test_pages_of_more_requests_than_a_launch_has_blocks_for():
 def test_as_many_requests_as_a_handle_may_have():
     args = make(random.Random(1), 1 << 14, 40, 2, zero=0.1)
     check_attention(2, 1, 64, *args, 3)
+
+
+# ------------------------------------------------------------------------------------------------ replayed plans
+def step_of(b, s, rope, x, k, v, tokens, target, given):
+    """All calls behind a plan, with what they leave; x [rows, heads, hd], pools of both layers."""
+    hq, hkv = b.n_q_heads, b.n_kv_heads
+    q = b.append_rope(rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], k[1], v[1])
+    o, lse = b.attention(q, k[1], v[1], want_lse=True)
+    acc = b.accept(tokens, target, n_given=given)
+    b.commit(acc["path"], acc["n_path"], k, v)
+    return [q, o, lse, acc["path"], acc["n_path"], acc["accept_len"], acc["token"]]
+
+
+@pytest.mark.parametrize("called", ["no rows", "no rows, fewer requests of no tables", "one row"])
+def test_eager_calls_behind_a_replayed_plan(called):
+    """The last plan that was called had no rows, or few; the one on the device, which a graph has replayed since, is what eager calls work on."""
+    s, (hq, hkv, hd), B = synera(), (4, 2, 64), 4
+    ctx, trees, table, n = make(random.Random(21), B, 600, 30, shapes=("tree",), zero=0.0)
+    T = sum(map(len, trees))
+    args = i32(ctx), i32([len(t) for t in trees]), i32(sum(trees, [])), i32(table), n
+    rope = s.Rope(hd)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn((T, hq + 2 * hkv, hd), generator=gen, device=DEV).to(torch.bfloat16)
+    pools = [torch.randn(d, generator=gen, device=DEV).to(torch.bfloat16) for d in ((2, n, hkv, P, hd), (2, n, hkv, hd, P))]
+    tokens, given = i32(np.zeros(T)), i32(np.ones(B))          # (every target is the first child's token)
+    plain = s.TreeBatch(hq, hkv, hd, B, T, table.shape[1])
+    assert (plain.plan(*args) == 0).all()
+    k, v = (p.clone() for p in pools)
+    want = [*step_of(plain, s, rope, x, k, v, tokens, tokens, given), k, v]
+    assert (want[4] > 1).any()
+
+    b = s.TreeBatch(hq, hkv, hd, B, T, table.shape[1])
+    b.plan(*args)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            b.plan(*args)
+        for _ in range(3):
+            if called == "one row":
+                b.plan(args[0], i32([0, 1, 0, 0]), i32([-1]), args[3], n)
+            else:
+                b.plan(args[0], i32(np.zeros(B)), i32([]), args[3] if called == "no rows" else i32(np.zeros((B, 1))), n)
+            graph.replay()
+            k, v = (p.clone() for p in pools)
+            got = [*step_of(b, s, rope, x, k, v, tokens, tokens, given), k, v]
+            side.synchronize()
+            for w, g in zip(want, got):
+                assert torch.equal(w, g)
+
+
+def test_eager_calls_on_no_rows_behind_a_replayed_plan():
+    """Plans of no rows in a handle whose plans were captured: calls on empty tensors do nothing."""
+    s, (hq, hkv, hd) = synera(), (2, 1, 64)
+    b = s.TreeBatch(hq, hkv, hd, 2, 4, 2)
+    rope, table = s.Rope(hd), i32([[0, 1], [2, 3]])
+    some, none = (i32([3, 5]), i32([2, 1]), i32([-1, 0, -1]), table, 4), (i32([3, 5]), i32([0, 0]), i32([]), table, 4)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.plan(*some)
+    graph.replay()
+    b.plan(*none)
+    k, v = torch.zeros((2, 4, hkv, P, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((2, 4, hkv, hd, P), dtype=torch.bfloat16, device=DEV)
+    x = torch.ones((0, hq + 2 * hkv, hd), dtype=torch.bfloat16, device=DEV)
+    got = step_of(b, s, rope, x, k, v, i32([]), i32([]), i32([1, 1]))
+    assert got[4].tolist() == [0, 0] and (k == 0).all() and (v == 0).all()
+    # as C sees them: no rows, no addresses
+    from paper_2511_07423_amd import binding
+    heads = [binding._pack_heads_rows(0, 0, 0, h, 0, h * hd, hd, h * hd, hd) for h in (hq, hkv)]
+    stream = torch.cuda.current_stream().cuda_stream
+    assert binding._lib.synera_tree_append_rope(b._h, rope._h, 1, heads[0], heads[1], heads[1], 0.0, k[0].data_ptr(), v[0].data_ptr(), stream) == s.OK
+    assert binding._lib.synera_tree_attention(b._h, heads[0], k[0].data_ptr(), v[0].data_ptr(), 1.0, None, stream) == s.OK
+    torch.cuda.synchronize()
+    assert (k == 0).all() and (v == 0).all()
