@@ -752,10 +752,10 @@ extern "C" int32_t synera_tree_accept(synera_tree* t, int64_t n_rows, const int3
                                       const int32_t* d_n_given, int32_t* d_accept_len, int32_t* d_token, int32_t* d_path, int32_t* d_n_path,
                                       void* stream) {
   if (!t || !t->planned || !d_accept_len || !d_token || !d_n_path || n_rows < t->n_rows || (!d_anchor && !d_n_given)) return SYNERA_EINVAL;
-  if (t->n_rows > 0 && (!d_tokens || !d_target || !d_path)) return SYNERA_EINVAL;
+  if (n_rows > 0 && (!d_tokens || !d_target || !d_path)) return SYNERA_EINVAL;
   if (off4({d_tokens, d_target, d_anchor, d_n_given, d_accept_len, d_token, d_path, d_n_path})) return SYNERA_EINVAL;
-  // no output on an input or on another one
-  const int64_t B = t->B, T = t->n_rows;
+  // no output on an input or on another one, over all rows that a replayed plan may have
+  const int64_t B = t->B, T = std::min<int64_t>(n_rows, t->lim.max_tokens);
   const Range outs[4] = {ints(d_accept_len, B), ints(d_token, B), ints(d_path, T), ints(d_n_path, B)};
   const Range ins[4] = {ints(d_tokens, T), ints(d_target, T), ints(d_anchor, B), ints(d_n_given, B)};
   for (int i = 0; i < 4; ++i)
@@ -863,7 +863,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 extern "C" int32_t synera_tree_commit(synera_tree* t, int64_t n_rows, const int32_t* d_path, const int32_t* d_n_path, int32_t n_layers,
                                       int64_t layer_stride, void* d_k_pool, void* d_v_pool, void* stream) {
   if (!t || !t->planned || !d_n_path || !d_k_pool || !d_v_pool || n_rows < t->n_rows || n_layers < 1 || n_layers > 65535) return SYNERA_EINVAL;
-  if (t->n_rows > 0 && !d_path) return SYNERA_EINVAL;
+  if (n_rows > 0 && !d_path) return SYNERA_EINVAL;
   if (off4({d_path, d_n_path}) || (reinterpret_cast<uintptr_t>(d_k_pool) | reinterpret_cast<uintptr_t>(d_v_pool)) % 16) return SYNERA_EINVAL;
   const ShLimits& l = t->lim;
   const int64_t layer = (int64_t)t->n_pages * l.Hkv * SY_PAGE * l.hd;
@@ -872,7 +872,7 @@ extern "C" int32_t synera_tree_commit(synera_tree* t, int64_t n_rows, const int3
   const Range k = {reinterpret_cast<uintptr_t>(d_k_pool), reinterpret_cast<uintptr_t>(d_k_pool) + 2 * (uintptr_t)all};
   const Range v = {reinterpret_cast<uintptr_t>(d_v_pool), reinterpret_cast<uintptr_t>(d_v_pool) + 2 * (uintptr_t)all};
   if (meet(k, v)) return SYNERA_EINVAL;
-  for (const Range& in : {ints(d_path, n_rows), ints(d_n_path, t->B)})
+  for (const Range& in : {ints(d_path, std::min<int64_t>(n_rows, l.max_tokens)), ints(d_n_path, t->B)})
     if (meet(k, in) || meet(v, in)) return SYNERA_EINVAL;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
   if (t->n_rows == 0 && !t->replays && !capturing(static_cast<hipStream_t>(stream))) return SYNERA_OK;

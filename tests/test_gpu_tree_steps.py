@@ -306,3 +306,30 @@ def test_eager_calls_on_no_rows_behind_a_replayed_plan():
     assert binding._lib.synera_tree_attention(b._h, heads[0], k[0].data_ptr(), v[0].data_ptr(), 1.0, None, stream) == s.OK
     torch.cuda.synchronize()
     assert (k == 0).all() and (v == 0).all()
+
+
+def test_accept_and_commit_are_checked_for_the_rows_that_they_say():
+    """A plan that is replayed later may have as many rows as the call's arrays: addresses and overlaps are checked for all of them."""
+    s = synera()
+    from paper_2511_07423_amd import binding
+    lib, (hq, hkv, hd) = binding._lib, (2, 1, 64)
+    b = s.TreeBatch(hq, hkv, hd, 2, 16, 2)
+    table = i32([[0, 1], [2, 3]])
+    k, v = torch.zeros((4, hkv, P, hd), dtype=torch.bfloat16, device=DEV), torch.zeros((4, hkv, hd, P), dtype=torch.bfloat16, device=DEV)
+    rows, out = torch.zeros((2, 16), dtype=torch.int32, device=DEV), torch.zeros((3, 2), dtype=torch.int32, device=DEV)
+    room = torch.zeros(64, dtype=torch.int32, device=DEV)
+    tok, tgt, path, stream = rows[0].data_ptr(), rows[1].data_ptr(), room.data_ptr(), torch.cuda.current_stream().cuda_stream
+    given = i32([1, 1]).data_ptr()
+
+    def accept(n, tokens, target, path, n_path=out[2].data_ptr()):
+        return lib.synera_tree_accept(b._h, n, tokens, target, None, given, out[0].data_ptr(), out[1].data_ptr(), path, n_path, stream)
+    for n_nodes, parent in ((i32([0, 0]), i32([])), (i32([1, 1]), i32([-1, -1]))):
+        assert (b.plan(i32([3, 5]), n_nodes, parent, table, 4) == 0).all()
+        for bad in ((16, None, tgt, path), (16, tok, None, path), (16, tok, tgt, None), (16, tok, tgt, tok + 60), (16, tok, tgt, tgt - 8),
+                    (16, tok, tgt, path, path + 60), (16, tok, tgt, path, tgt + 60)):
+            assert accept(*bad) == s.EINVAL, bad
+        assert lib.synera_tree_commit(b._h, 16, None, out[2].data_ptr(), 1, 0, k.data_ptr(), v.data_ptr(), stream) == s.EINVAL
+        assert accept(16, tok, tgt, path) == s.OK and accept(16, tok, tgt, path, path + 64) == s.OK
+        assert accept(1 << 62, tok, tgt, path, path + 60) == s.EINVAL and accept(1 << 62, tok, tgt, path, path + 64) == s.OK
+        assert lib.synera_tree_commit(b._h, 16, path, out[2].data_ptr(), 1, 0, k.data_ptr(), v.data_ptr(), stream) == s.OK
+    torch.cuda.synchronize()
