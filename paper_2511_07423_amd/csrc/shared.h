@@ -98,6 +98,7 @@ void sh_plan(const ShLimits& l, int32_t B, const int32_t* ctx_len, const int32_t
 
 // ---------------------------------------------------------------- shared.hip
 // Where the new tokens of a batch go: of a planned synera_batch, or of a tree's plan, whose sizes only the device knows.
+#define SH_FIRST_PITCH 8
 struct ShTarget {
   const ShLimits* lim;
   int device;
@@ -109,6 +110,7 @@ struct ShTarget {
   const int32_t *pos, *slot;   // device, as ShPlan's; a slot below 0: the token goes nowhere
   const ShHeader* head;
   const ShWindow* windows;     // empty ones (s1 <= s0) are passed by
+  const int32_t *first, *n_requests;   // device: each request's first token, SH_FIRST_PITCH apart, and how many there are; or null: requests are cut where tensors end
 };
 int32_t sh_append(const ShTarget& target, const synera_rope* rope, int32_t dtype, const synera_heads* q, const synera_heads* k,
                   const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer, void* stream);

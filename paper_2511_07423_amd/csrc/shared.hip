@@ -215,7 +215,20 @@ struct AppendArgs {
   int32_t v_blocks;            // the first blocks take values, the others heads (append_rows)
   int32_t v_pairs;             // whether two values of v can be loaded together
   int32_t most;                // tokens that the tensors of this call have room for
+  const int32_t *first, *n_requests;   // as ShTarget's
 };
+// Tokens of the plan on the device that this call works on: all, or, where the tensors are too short, those of the requests that lie in them whole.
+__device__ __forceinline__ int32_t append_tokens(const AppendArgs& a) {
+  const int32_t n = a.head->n_tokens;
+  if (n <= a.most || !a.first) return min(n, a.most);
+  int low = 0;                                  // the last request that begins before the end or at it
+  for (int high = a.n_requests[0] - 1; low < high;) {
+    const int mid = (low + high + 1) / 2;
+    if (a.first[(size_t)mid * SH_FIRST_PITCH] <= a.most) low = mid;
+    else high = mid - 1;
+  }
+  return a.first[(size_t)low * SH_FIRST_PITCH];
+}
 
 template <typename TI>
 __device__ __forceinline__ uint32_t value_pair(const TI* v, bool pairs) {    // two neighbouring values as bf16
@@ -235,8 +248,8 @@ __device__ __forceinline__ uint32_t value_pair(const TI* v, bool pairs) {    // 
 }
 
 template <typename TI, int ONCE>
-__device__ __forceinline__ void append_values(const AppendArgs& a, ShWindow w, const int e0, uint32_t* turn) {
-  w.s1 = w.s0 + min(w.s1 - w.s0, a.most - w.row);
+__device__ __forceinline__ void append_values(const AppendArgs& a, ShWindow w, const int32_t tokens, const int e0, uint32_t* turn) {
+  w.s1 = w.s0 + min(w.s1 - w.s0, tokens - w.row);
   if (w.s1 <= w.s0) return;
   const int lane = threadIdx.x & 63, e = e0 + 2 * lane;
   const bool on = e < a.n;
@@ -293,14 +306,14 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, ShWindow w, c
 }
 
 template <typename TI, int VEC, int ONCE>
-__device__ __forceinline__ void append_rows(const AppendArgs& a, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const int32_t tokens, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.v_blocks) {
     const uint32_t slabs = (uint32_t)(a.n + 127) / 128, items = (uint32_t)a.head->n_windows * slabs;
     for (uint32_t i = blockIdx.x * 4 + wave; i < items; i += (uint32_t)a.v_blocks * 4)
-      append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
+      append_values<TI, ONCE>(a, a.windows[i / slabs], tokens, (int)(i % slabs) * 128, turn[wave]);
   } else {
-    const uint32_t items = (uint32_t)min(a.head->n_tokens, a.most) * (uint32_t)cols.n;
+    const uint32_t items = (uint32_t)tokens * (uint32_t)cols.n;
     for (uint32_t i = (blockIdx.x - a.v_blocks) * 4 + wave; i < items; i += (gridDim.x - a.v_blocks) * 4)
       turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i);
   }
@@ -310,12 +323,12 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const TurnCols 
 // wavefront of the largest, values and heads are taken from one list, so that both end together.
 enum { PLAN_KNOWN, PLAN_KEPT, PLAN_ANY };
 template <typename TI, int VEC, int ONCE>
-__device__ __forceinline__ void append_listed(const AppendArgs& a, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
+__device__ __forceinline__ void append_listed(const AppendArgs& a, const int32_t tokens, const TurnCols cols, uint32_t (*turn)[64 * 16]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t slabs = (uint32_t)(a.n + 127) / 128, values = (uint32_t)a.head->n_windows * slabs;
-  const uint32_t all = values + (uint32_t)min(a.head->n_tokens, a.most) * (uint32_t)cols.n;
+  const uint32_t all = values + (uint32_t)tokens * (uint32_t)cols.n;
   for (uint32_t i = blockIdx.x * 4 + wave; i < all; i += gridDim.x * 4) {
-    if (i < values) append_values<TI, ONCE>(a, a.windows[i / slabs], (int)(i % slabs) * 128, turn[wave]);
+    if (i < values) append_values<TI, ONCE>(a, a.windows[i / slabs], tokens, (int)(i % slabs) * 128, turn[wave]);
     else turn_item<TI, bf16_t, VEC, true, ONCE>(a.turn, cols, i - values);
   }
 }
@@ -323,16 +336,17 @@ template <typename TI, int VEC, int ONCE, int PLAN>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t turn[4][64 * 16];
   if constexpr (PLAN == PLAN_KNOWN) {
-    append_rows<TI, VEC, ONCE>(a, a.turn.cols, turn);
+    append_rows<TI, VEC, ONCE>(a, min(a.head->n_tokens, a.most), a.turn.cols, turn);
   } else if constexpr (PLAN == PLAN_KEPT) {
-    append_rows<TI, VEC, ONCE>(a, turn_cols(a.turn.groups, min(a.head->n_tokens, a.most)), turn);
+    const int32_t T = append_tokens(a);
+    append_rows<TI, VEC, ONCE>(a, T, turn_cols(a.turn.groups, T), turn);
   } else {
-    const int32_t T = min(a.head->n_tokens, a.most);
+    const int32_t T = append_tokens(a);
     const TurnCols cols = turn_cols(a.turn.groups, T);
     const int32_t once = turn_once(VEC, (T * a.turn.token_bytes) >> 20, true);
-    if (once == TURN_ONCE_BOTH) append_listed<TI, VEC, TURN_ONCE_BOTH>(a, cols, turn);
-    else if (once == TURN_ONCE_IN) append_listed<TI, VEC, TURN_ONCE_IN>(a, cols, turn);
-    else append_listed<TI, VEC, TURN_KEPT>(a, cols, turn);
+    if (once == TURN_ONCE_BOTH) append_listed<TI, VEC, TURN_ONCE_BOTH>(a, T, cols, turn);
+    else if (once == TURN_ONCE_IN) append_listed<TI, VEC, TURN_ONCE_IN>(a, T, cols, turn);
+    else append_listed<TI, VEC, TURN_KEPT>(a, T, cols, turn);
   }
 }
 
@@ -410,6 +424,8 @@ int32_t sh_append(const ShTarget& b, const synera_rope* rope, int32_t dtype, con
   for (const synera_heads* h : {q, k, v})
     if (h && h->n_rows) a.most = std::min(a.most, h->n_rows);
   a.windows = b.windows;
+  a.first = b.first;
+  a.n_requests = b.n_requests;
   a.v = v->d_in;
   a.v_ts = v->in_token;
   a.v_hs = v->in_head;
@@ -446,7 +462,7 @@ extern "C" int32_t synera_append_rope(synera_batch* b, const synera_rope* rope, 
                                       void* stream) {
   if (!b || !b->planned) return SYNERA_EINVAL;
   const ShTarget target = {&b->lim, b->device, b->n_pages, b->plan.head.n_tokens, b->plan.head.n_windows, true, false, b->region<int32_t>(R_POS),
-                           b->region<int32_t>(R_SLOT), b->region<ShHeader>(R_HEAD), b->region<ShWindow>(R_WIN)};
+                           b->region<int32_t>(R_SLOT), b->region<ShHeader>(R_HEAD), b->region<ShWindow>(R_WIN), nullptr, nullptr};
   return sh_append(target, rope, dtype, q, k, v, eps, d_k_layer, d_v_layer, stream);
 }
 

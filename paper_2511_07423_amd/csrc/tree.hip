@@ -61,6 +61,7 @@ struct TrReq {                   // 32 bytes, scalar loads
   int32_t steps, ranges, tiles;  // as the lists count them, refused or not
   int32_t part;                  // first of its partial rows, if it has several ranges: [range][head][row]
 };
+static_assert(sizeof(TrReq) == 4 * SH_FIRST_PITCH, "how the append finds a request's first row");
 struct TrItem {                  // 64 bytes, the k-th of list x at 8 k + x.  All that a block has to know before it can ask for keys, in one load
   TrReq q;
   int32_t req, tile;             // (a tile that the request has not: none)
@@ -521,7 +522,7 @@ extern "C" int32_t synera_tree_append_rope(synera_tree* t, const synera_rope* ro
                                            const synera_heads* k, const synera_heads* v, float eps, void* d_k_layer, void* d_v_layer,
                                            void* stream) {
   if (!t || !t->planned) return SYNERA_EINVAL;
-  const ShTarget target = {&t->lim, t->device, t->n_pages, t->n_rows, 0, false, t->replays, t->pos, t->slot, &t->head->sh, t->windows};
+  const ShTarget target = {&t->lim, t->device, t->n_pages, t->n_rows, 0, false, t->replays, t->pos, t->slot, &t->head->sh, t->windows, &t->req->tok, &t->head->B};
   return sh_append(target, rope, dtype, q, k, v, eps, d_k_layer, d_v_layer, stream);
 }
 

@@ -333,3 +333,49 @@ def test_accept_and_commit_are_checked_for_the_rows_that_they_say():
         assert accept(1 << 62, tok, tgt, path, path + 60) == s.EINVAL and accept(1 << 62, tok, tgt, path, path + 64) == s.OK
         assert lib.synera_tree_commit(b._h, 16, path, out[2].data_ptr(), 1, 0, k.data_ptr(), v.data_ptr(), stream) == s.OK
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, torch.bfloat16), (128, torch.float32)])
+def test_replayed_plans_with_more_rows_than_the_tensors(hd, dtype):
+    """Wherever the tensors end, between two requests or inside one: the requests that lie in them whole are appended as ever, and of the
+    others no key, value or query is written."""
+    s, hq, hkv, B = synera(), 4, 2, 6
+    ctx, trees, table, n = make(random.Random(22), B, 100, 40, shapes=("tree",), zero=0.0)
+    trees[3], new = [], [len(t) for t in trees]
+    new[3] = 0
+    T, cu = sum(new), np.concatenate([[0], np.cumsum(new)])
+    args = i32(ctx), i32(new), i32(sum(trees, [])), i32(table), n
+    rope = s.Rope(hd)
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    x = torch.randn((T, hq + 2 * hkv, hd), generator=gen, device=DEV).to(dtype)
+    mark = lambda *shape: torch.full(shape, 0x1234, dtype=torch.int16, device=DEV).view(torch.bfloat16)       # noqa: E731
+    b = s.TreeBatch(hq, hkv, hd, B, T, table.shape[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        b.plan(*args)
+        with torch.cuda.graph(graph, stream=side):
+            b.plan(*args)
+        graph.replay()
+        k, v, q = mark(n, hkv, P, hd), mark(n, hkv, hd, P), mark(T, hq, hd)
+        b.append_rope(rope, x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:], k, v, out_q=q)
+        for cut in sorted({1, T, *cu[1:].tolist(), *(cu[1:-1] + 1).tolist(), *(cu[2:] - 1).tolist()}):
+            if not 0 < cut <= T:
+                continue
+            whole = int((cu <= cut).sum()) - 1                 # requests that end by then
+            few = int(cu[whole])
+            b.plan(*(i32([0]), i32([0]), i32([])), i32([[0]]), n)
+            graph.replay()
+            kp, vp, out_q = mark(n, hkv, P, hd), mark(n, hkv, hd, P), mark(T, hq, hd)
+            y = x[:cut]
+            b.append_rope(rope, y[:, :hq], y[:, hq: hq + hkv], y[:, hq + hkv:], kp, vp, out_q=out_q[:cut])
+            side.synchronize()
+            assert torch.equal(out_q[:few], q[:few]) and (out_q[few:].view(torch.int16) == 0x1234).all(), cut
+            there = torch.zeros((n, P), dtype=torch.bool)
+            for i in range(whole):
+                at = int(ctx[i]) + np.arange(new[i])
+                there[table[i, at // P], at % P] = True
+            there = there.to(DEV)
+            assert torch.equal(kp, torch.where(there[:, None, :, None], k, mark(1))), cut
+            assert torch.equal(vp, torch.where(there[:, None, None, :], v, mark(1))), cut
