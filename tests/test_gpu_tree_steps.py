@@ -9,7 +9,7 @@ import torch
 
 import shared_reference as ref
 import tree_reference as tree
-from test_gpu_tree import DEV, P, Server, check_attention, grow, i32, make, same, synera
+from test_gpu_tree import DEV, EVERY, P, TYPES, Server, check_attention, check_logits, grow, i32, make, same, synera
 
 pytestmark = pytest.mark.gpu
 
@@ -379,3 +379,48 @@ def test_replayed_plans_with_more_rows_than_the_tensors(hd, dtype):
             there = there.to(DEV)
             assert torch.equal(kp, torch.where(there[:, None, :, None], k, mark(1))), cut
             assert torch.equal(vp, torch.where(there[:, None, None, :], v, mark(1))), cut
+
+
+# ------------------------------------------------------------------------------------------------ wide trees, long paths that part ways
+def wide(rng, n):
+    """Parents up to 200 nodes back: in other words of the masks and, with several heads, in other tiles."""
+    return [-1] + [max(0, j - rng.randrange(1, 201)) for j in range(1, n)]
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(16, 2, 64), (12, 1, 128), (3, 3, 64)])
+def test_attention_of_wide_trees(hq, hkv, hd):
+    rng = random.Random(hq)
+    for ctx in ((0, 700, 33, 127), (129, 0, 5, 1000)):
+        trees = [wide(rng, n) for n in (256, 200, 64, 129)]
+        need = [-(-(c + len(t)) // P) for c, t in zip(ctx, trees)]
+        ids, table, at = rng.sample(range(sum(need)), sum(need)), np.full((len(need), max(need)), -1, np.int32), 0
+        for i, k in enumerate(need):
+            table[i, :k] = ids[at:at + k]
+            at += k
+        check_attention(hq, hkv, hd, np.array(ctx), trees, table, sum(need), 7)
+
+
+def test_attention_of_many_rows_behind_a_long_context():
+    """2048 rows over 315 steps of 128 keys: ranges of two steps would have 323 584 partial rows, more than there is room for on any card of up to 1264 compute
+    units (256 rows for each)."""
+    rng, need = random.Random(12), -(-(40000 + 256) // P)
+    table = np.array([rng.sample(range(need), need)], np.int32)
+    check_attention(8, 1, 64, np.array([40000]), [wide(rng, 256)], table, need, 5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,vocab,shape", [(24, 1000, "forest"), (24, 1000, "tree"), (8, 9001, "wide")])
+def test_logits_of_long_trees_that_part_ways(B, vocab, shape, dtype):
+    """Trees of more than 256 nodes of which a block takes several rows, some 64 or 96 apart (1536 blocks share them): from one to the next a path is extended,
+    or taken away and another one added.  All penalties, biases and masks, new tensors and in place."""
+    rng = random.Random(B + vocab)
+    for seed, (parts, in_place) in enumerate(((EVERY, False), (EVERY, True), (("tree", "frequency", "presence", "repetition"), True))):
+        trees = [(wide(rng, n) if shape == "wide" else grow(rng, n, shape)) for n in (rng.randrange(257, 300) for _ in range(B - 1))] + [grow(rng, 40, "tree")]
+        check_logits(rng, trees, B, vocab, dtype, seed, parts, in_place=in_place)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logits_of_wide_trees(dtype):
+    rng = random.Random(3)
+    for in_place in (False, True):
+        check_logits(rng, [wide(rng, n) for n in (256, 100, 3, 255)] * 10, 40, 1096, dtype, 5, EVERY, pitch=1097, in_place=in_place)
