@@ -7,7 +7,8 @@
  * General rules, status codes and the layout of the pools are those of synera.h, element types, heads and the ownership of handles those
  * of synera_shared.h.  What the host says (sizes, pointers) is checked on the host: a refused call has launched nothing.  What only the
  * device knows is checked there: each request has a status of its own (0, or one of the codes of synera.h), and a refused request
- * changes nothing and has no outputs but those that say so.  Arrays named [rows] are flattened, request after request, and have as many
+ * changes nothing and has no outputs but those that say so: what a call would have written for its rows stays as it was, in a tensor that nothing else
+ * filled as the memory was found.  Arrays named [rows] are flattened, request after request, and have as many
  * places as n_rows says; those behind the last request's stay as they were, but for the places of synera_pages_update.  Nothing here waits for the GPU but creates and destroys.
  */
 #ifndef SYNERA_TREE_H
@@ -70,7 +71,7 @@ int32_t synera_tree_destroy(synera_tree* tree);
  * that use the one before.  Captured calls work for any later plan of this handle (captured or not).  Calls look at what the last plan that was
  * called, or captured, says of rows and pages; once a plan was captured, they work on as many of the rows that the plan on the device has as their tensors have room for, also where the last one that was called had none. Where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
  * the requests that do not lie in them whole are left out, as an accept or a commit leaves out requests beyond the B of the plan that it was called behind; before a captured plan's
- * first replay the handle has no requests.  That pools have room for a replayed plan's pages nothing checks.
+ * first replay the handle has the requests of the plan before, or none.  That pools have room for a replayed plan's pages nothing checks.
  *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES, a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page
  *             id outside the pool; ENOSPC: more pages than columns, more rows than n_rows
  * Errors: EINVAL (null, sizes, alignment), ENOSPC (B > max_batch, n_rows > max_tokens, columns > max_pages), EUNSUP (n_pages_in_pool >= 2^27), EHIP.
@@ -133,7 +134,7 @@ typedef struct synera_logits_desc {
   int32_t dtype;               /* of logits, in and out: 0, 1 or 2                                                      */
   int64_t rows, vocab;         /* vocab <= 2^30                                                                         */
   int64_t in_stride, out_stride;   /* elements from row to row, >= vocab where there are several                        */
-  const int32_t* d_cu;         /* [B + 1] row cu[i] is the first of request i (clamped to 0 .. rows); NULL: row i is request i's, rows == B */
+  const int32_t* d_cu;         /* [B + 1] row cu[i] is the first of request i (clamped to 0 .. rows; a row of two requests, where it falls, may come out as either's); NULL: row i is request i's, rows == B */
   const int32_t* d_history;    /* [B][history_columns], or NULL: none.  Tokens outside the vocabulary do not count        */
   const int32_t* d_history_len;    /* [B] clamped to 0 .. history_columns; NULL with d_history                            */
   const int32_t* d_n_prompt;   /* [B] or NULL: 0                                                                        */
@@ -146,7 +147,7 @@ typedef struct synera_logits_desc {
   const float* d_bias;         /* [B][bias_columns]                                                                     */
   const int32_t* d_mask;       /* [rows][(vocab + 31) / 32] bits of tokens that are allowed, or NULL: all                 */
   const int32_t* d_tokens;     /* [rows], at most 2^19, or NULL: no paths.  With d_cu: row j of a request stands behind node j of its tree, */
-  const int32_t* d_parent;     /* [rows]  whose path, itself included, was seen and counts for g.  A parent outside 0 .. j - 1 ends the path */
+  const int32_t* d_parent;     /* [rows]  whose path, itself included, was seen and counts for g, beside the history, which has to end before the first node.  A parent outside 0 .. j - 1 ends the path */
 } synera_logits_desc;
 
 /*

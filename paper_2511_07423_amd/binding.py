@@ -888,7 +888,8 @@ def update_pages(table, held, free, n_free, ctx_len, n_new, n_rows, shared=None)
 class TreeBatch(_PagedBatch):
     """Trees of drafted tokens over a paged bf16 cache, their lengths on the GPU: plan() once a step, append_rope() and attention() for each
     layer (as SharedBatch's), accept() and commit() behind the last, all on one stream.  All but the making of the handle can be captured into a
-    graph; captured calls serve later plans too, for which their tensors and pools need room.  Rows of a tree: node j of request i is row
+    graph; captured calls serve later plans too, for which their tensors and pools need room.  Rows of refused requests and behind the last one's are
+    not written: in new tensors they are as the memory was.  Rows of a tree: node j of request i is row
     cu[i] + j, cu as update_pages returns it for a table of the same columns (the prefix sums of n_nodes).  Belongs to the device that is current when it is made.  For serving: outputs carry no gradients."""
     _names = "synera_tree_create", "synera_tree_destroy", "synera_tree_append_rope", "synera_tree_attention"
     _skips_none = True
@@ -952,7 +953,8 @@ def adjust_logits(logits, cu=None, history=None, history_len=None, n_prompt=None
     of which the first history_len[i] tokens were seen, those from n_prompt[i] on generated; repetition, presence, frequency f32 [B]; bias
     f32 [B, n] for the tokens bias_id [B, n] (of entries that name a token twice the last).  mask: bits [rows, ceil(vocab / 32)] of
     tokens that are allowed; all others become -inf.  tokens and parent [rows]: a row is a node of its request's tree, whose path
-    from the root, itself included, was generated too.  Integers are int32.  No gradients."""
+    from the root, itself included, was generated too: the history has to end before the first node, or its token counts twice.  Integers are
+    int32.  Rows of no request are not written (in a new tensor they are as the memory was).  No gradients."""
     index = _current(logits, "logits")
     rows, vocab = logits.shape
     dtype = _head_type(logits.dtype)

@@ -11,7 +11,7 @@
 // integers, so the order of the atomics does not show.
 // Then all values pass as they lie in 16-byte pieces, -infinity in the place of those that the mask hides; those that are allowed and have a word
 // are formed on the way.  (Nearly every wavefront meets some: with a branch for each value 2048 x 128256 masked took 325 us; formed behind the
-// others, from memory, 300; this way 202, as long as a plain copy of the logits.)
+// others, from memory, 300; this way 202, where torch copies these logits in 179 to 197.)
 // Paths of trees of up to LG_NODES rows: a mask of the path for each row, and a list of the nodes whose tokens are in the slice.  Rows pass those
 // tokens as they are, and behind a barrier each is formed for each row, by a lane that counts it along the list.  (198 trees of 64 nodes in a
 // vocabulary of 1096: 68 us; counted on the way, where one lane keeps its wavefront waiting, 323.)  Longer paths are added to the words before a

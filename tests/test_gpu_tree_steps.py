@@ -125,6 +125,29 @@ def test_captured_steps_whose_pool_runs_out():
     assert refused >= 2
 
 
+def test_plans_by_held_pages():
+    """A request is planned if it holds what its tokens and nodes need; where it holds what cannot be it is refused; and what the host can see."""
+    s = synera()
+    b = s.TreeBatch(2, 1, 64, 8, 20, 3)
+    ctx, n, held = [20, 20, 20, 20, 0, 20, 20, 29], [3, 3, 3, 3, 2, 0, 0, 3], [2, 1, -1, 4, 1, 2, 0, 3]
+    parent, table = i32([-1, 0, 0] * 4 + [-1, 0] + [-1, 0, 0]), i32(np.arange(24).reshape(8, 3))
+    args = i32(ctx), i32(n), parent, table, 24
+    assert b.plan(*args, held=i32(held)).tolist() == [0, s.ENOSPC, s.EINVAL, s.EINVAL, 0, 0, s.ENOSPC, 0]
+    acc = b.accept(i32(np.zeros(17)), i32(np.zeros(17)), n_given=i32([1] * 8))
+    assert acc["n_path"].tolist() == [2, 0, 0, 0, 2, 0, 0, 2]
+    assert acc["path"].tolist() == [0, 1, -1] + [-1] * 9 + [0, 1] + [0, 1, -1]
+    assert (b.plan(*args) == 0).all()
+    for bad in (i32(held)[:7], i32(held).long(), i32(held).cpu()):
+        with pytest.raises(ValueError):
+            b.plan(*args, held=bad)
+    from paper_2511_07423_amd import binding
+    at = [x.data_ptr() for x in args[:4]]
+    room = torch.zeros(16, dtype=torch.int32, device=DEV)
+    for held_at, status_at in ((room.data_ptr() + 2, room.data_ptr() + 32), (room.data_ptr(), room.data_ptr() + 28)):
+        assert binding._lib.synera_tree_plan_held(b._h, 8, at[0], at[1], at[2], 17, at[3], 3, held_at, 24, status_at,
+                                                  torch.cuda.current_stream().cuda_stream) == s.EINVAL
+
+
 # ------------------------------------------------------------------------------------------------ counts out of range
 @pytest.mark.parametrize("n,columns,counted,status", [(300, 40, 300, "EINVAL"), (200, 8, 0, "ENOSPC"), (256, 16, 256, "ENOSPC"), (257, 16, 0, "EINVAL"), (257, 17, 257, "EINVAL"),
                                                       (640, 40, 640, "EINVAL"), (641, 40, 0, "EINVAL"), (-1, 8, 0, "EINVAL"), (2 ** 31 - 1, 8, 0, "EINVAL")])
