@@ -69,7 +69,7 @@ int32_t synera_tree_destroy(synera_tree* tree);
  * Plans a step, once for all layers: d_ctx_len, d_n_nodes i32 [B], d_parent i32 [rows], d_table i32 [B][columns] (columns <= max_pages), all
  * read by this call alone.  The calls below must be on the same stream, or ordered behind it by the caller; so must a plan behind calls
  * that use the one before.  Captured calls work for any later plan of this handle (captured or not).  Calls look at what the last plan that was
- * called, or captured, says of rows and pages; once a plan was captured, they work on as many of the rows that the plan on the device has as their tensors have room for, also where the last one that was called had none. Where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
+ * called, or captured, says of rows and pages; once a plan was captured, those whose tensors say n_rows work on as many of the rows that the plan on the device has as there is room for, also where the last one that was called had none. Where a replayed plan on the device has more rows than a call's tensors (those that say n_rows),
  * the requests that do not lie in them whole are left out, as an accept or a commit leaves out requests beyond the B of the plan that it was called behind; before a captured plan's
  * first replay the handle has the requests of the plan before, or none.  That pools have room for a replayed plan's pages nothing checks.
  *   d_status  i32 [B], or NULL: 0; EINVAL: n_i outside 0 .. SYNERA_TREE_NODES, a parent outside -1 .. j - 1; ERANGE: L_i below 0, a page

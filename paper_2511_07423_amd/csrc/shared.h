@@ -106,7 +106,7 @@ struct ShTarget {
   int64_t n_tokens;            // known: of the plan; else rows that it may fill
   int32_t n_windows;
   bool known;
-  bool replays;                // the plan on the device may be another than the one that these say: served as far as the tensors go
+  bool replays;                // the plan on the device may be another than the one that these say: served as far as the tensors say that they go
   const int32_t *pos, *slot;   // device, as ShPlan's; a slot below 0: the token goes nowhere
   const ShHeader* head;
   const ShWindow* windows;     // empty ones (s1 <= s0) are passed by

@@ -376,8 +376,8 @@ int32_t sh_append(const ShTarget& b, const synera_rope* rope, int32_t dtype, con
   if (!rope || !k || !v || !d_k_layer || !d_v_layer || dtype < 0 || dtype > 2) return SYNERA_EINVAL;
   if (!(eps >= 0.f) || !std::isfinite(eps)) return SYNERA_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool captures = capturing(s), captured = captures || b.replays, graph = captured || !b.known;
-  if (b.n_tokens == 0 && !captures && (!b.replays || (k->n_rows == 0 && !k->d_in))) return SYNERA_OK;   // (an empty tensor has no address)
+  const bool captured = capturing(s) || (b.replays && (k->n_rows || v->n_rows || (q && q->n_rows))), graph = captured || !b.known;
+  if (b.n_tokens == 0 && !captured) return SYNERA_OK;                  // (an empty tensor has no address)
   if ((reinterpret_cast<uintptr_t>(d_k_layer) | reinterpret_cast<uintptr_t>(d_v_layer)) % 16) return SYNERA_EINVAL;
   const ShLimits& l = *b.lim;
   const int bytes = dtype == 0 ? 4 : 2, hd = l.hd;

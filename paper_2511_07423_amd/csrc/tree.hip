@@ -654,9 +654,8 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   const ShLimits& l = t->lim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   TreeAttnArgs a = {};
-  // A plan on the device that may be another than the last one that was called is served as far as the call's tensors go, as in a graph.
-  const bool captured = capturing(s), graph = captured || t->replays;
-  if (t->n_rows == 0 && !captured && q->n_rows == 0 && !q->d_in) return SYNERA_OK;         // (an empty tensor has no address)
+  // A plan on the device that may be another than the last one that was called is served as far as the call's tensors say that they go, as in a graph.
+  const bool captured = capturing(s), graph = captured || (t->replays && q->n_rows);
   const int32_t st = sh_attention_args(a, l, t->n_pages, t->n_rows, graph, q, d_k_layer, d_v_layer, scale, d_lse);
   if (st != SYNERA_OK) return st == SH_NOTHING ? SYNERA_OK : st;
   if (!rope_device_ok(t->device)) return SYNERA_EINVAL;
@@ -672,7 +671,7 @@ extern "C" int32_t synera_tree_attention(synera_tree* t, const synera_heads* q, 
   a.rows = q->n_rows ? q->n_rows : INT32_MAX;
   // As many blocks as there may be items, up to four for each place; the kernel loops.  Captured calls serve plans of any size.
   const int grid = std::min(t->items_room * SY_SH_DEAL, TR_GRID * l.slots) / SY_SH_DEAL * SY_SH_DEAL;
-  const bool cuts = (graph ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
+  const bool cuts = (captured || t->replays ? l.max_pages : t->columns) > 2 * TR_STEP / SY_PAGE;      // no range is shorter than two steps
   const int joins = cuts ? TR_JOIN_GRID * l.slots : 0;
   const hipError_t e = l.hd == 128 ? launch_tree<128>(a, grid, joins, s) : launch_tree<64>(a, grid, joins, s);
   if (e != hipSuccess) {

@@ -327,6 +327,16 @@ def test_eager_calls_on_no_rows_behind_a_replayed_plan():
     stream = torch.cuda.current_stream().cuda_stream
     assert binding._lib.synera_tree_append_rope(b._h, rope._h, 1, heads[0], heads[1], heads[1], 0.0, k[0].data_ptr(), v[0].data_ptr(), stream) == s.OK
     assert binding._lib.synera_tree_attention(b._h, heads[0], k[0].data_ptr(), v[0].data_ptr(), 1.0, None, stream) == s.OK
+    # one row whose steps from token to token, which one token does not need, are none: checked for the one that the last called plan has
+    b.plan(i32([3, 5]), i32([0, 1]), i32([-1]), table, 4)
+    x = torch.ones((1, hq + 2 * hkv, hd), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros((1, hq, hd), dtype=torch.bfloat16, device=DEV)
+    at = [binding._pack_heads_rows(x[:, i].data_ptr(), o, 0, h, 0, 0, hd, 0, hd) for i, h, o in ((0, hq, out.data_ptr()), (hq, hkv, 0), (hq + hkv, hkv, 0))]
+    assert binding._lib.synera_tree_append_rope(b._h, rope._h, 1, *at, 0.0, k[0].data_ptr(), v[0].data_ptr(), stream) == s.OK
+    assert (out != 0).any() and (k[0] != 0).any()
+    k.zero_(), v.zero_()
+    assert binding._lib.synera_tree_attention(b._h, binding._pack_heads_rows(x.data_ptr(), out.data_ptr(), 0, hq, 0, 0, hd, 0, hd), k[0].data_ptr(), v[0].data_ptr(), 1.0,
+                                              None, stream) == s.OK
     torch.cuda.synchronize()
     assert (k == 0).all() and (v == 0).all()
 
